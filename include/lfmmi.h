@@ -207,6 +207,103 @@ lfmmi_status lfmmi_loss(const lfmmi_graph *num, const lfmmi_graph *den, const fl
                         const int32_t *lengths, int32_t B, int32_t T, int32_t P, float leak,
                         float *objf, float *grad, int32_t *status, void *hip_stream);
 
+/* ---- log probabilities of given tokens, and gradients -------------------- */
+
+/* Types of the arrays below. */
+typedef enum { LFMMI_F32 = 0, LFMMI_BF16 = 1, LFMMI_F16 = 2 } lfmmi_dtype;
+
+/*
+ * Log probabilities of given tokens (or pdfs, of a frame alignment), with the entropy and
+ * the best alternatives of every row. For row (b, t) with logits x, m = max_i x_i,
+ * d_i = scale * (x_i - m) and s = sum_i exp(d_i):
+ *   logp[b,t]    = d_target - ln s
+ *   entropy[b,t] = ln s - (sum_i d_i exp(d_i)) / s        (a logit of -inf adds nothing)
+ *   top_id[b,t,:], top_logp[b,t,:]  the top_k largest logits' indices and log
+ *                  probabilities, largest first, equal ones by index, lowest first
+ *   stats[b,t,:] = (m, ln s), what lfmmi_token_logprobs_backward takes
+ *
+ *   logits   DEVICE, [B, T, V] of `dtype` (lfmmi_dtype): element (b, t, i) at
+ *            b * stride_b + t * stride_t + i, strides >= 0 in elements (0 repeats),
+ *            aligned to an element at least. V >= 1.
+ *   lengths  HOST int32 [B], 0 <= lengths[b] <= T, or NULL (all T).
+ *   targets  DEVICE int32 or int64 (target_bytes 4 or 8) [B, T], or NULL: no logp.
+ *            Rows t >= lengths[b] and rows with a negative target are not scored: their
+ *            logits are never read, their outputs are 0 and their top_id -1.
+ *   scale    what logits are multiplied by (an acoustic scale, the inverse of a
+ *            temperature), 1e-6 <= scale <= 1e6.
+ *   top_k    0 <= top_k <= LFMMI_MAX_TOP and <= V.
+ *   logp, entropy float32 [B, T]; stats float32 [B, T, 2]; top_id int32 and top_logp
+ *            float32 [B, T, top_k]; status int32 [B, T]: all DEVICE, any may be NULL
+ *            (logp must be if targets is).
+ *   status   0 ok; bit 0: every logit is -inf (logp and top_logp -inf, entropy 0);
+ *            bit 1: a NaN or +inf logit was read (logp, entropy, stats and top_logp NaN,
+ *            top_id -1); bit 2: the target is not below V (logp NaN).
+ *   workspace DEVICE, at least the bytes that lfmmi_token_logprobs_workspace gives for
+ *            the same dtype, B, T, V and top_k (0: may be NULL), aligned to 16; its content
+ *            before and after the call is of no account. Calls that may run at the same
+ *            time, replays of captured graphs among them, need one each.
+ * The call enqueues kernels on hip_stream and nothing else: it does not allocate or
+ * synchronise and may be captured into a HIP graph. Arrays lie on the current device.
+ * The same inputs give the same bits. B == 0 or T == 0 is valid.
+ */
+#define LFMMI_MAX_TOP 64
+lfmmi_status lfmmi_token_logprobs(const void *logits, int32_t dtype, int32_t B, int32_t T,
+                                  int32_t V, int64_t stride_b, int64_t stride_t,
+                                  const int32_t *lengths, const void *targets,
+                                  int32_t target_bytes, float scale, int32_t top_k,
+                                  float *logp, float *entropy, float *stats, int32_t *top_id,
+                                  float *top_logp, int32_t *status, void *workspace,
+                                  int64_t workspace_bytes, void *hip_stream);
+lfmmi_status lfmmi_token_logprobs_workspace(int32_t dtype, int32_t B, int32_t T, int32_t V,
+                                            int32_t top_k, int64_t *bytes);
+
+/*
+ * The gradient of a loss with respect to the logits, given its gradients with respect to
+ * logp (grad_logp) and entropy (grad_entropy), DEVICE float32 [B, T], either may be NULL
+ * (taken as 0). With l_i = d_i - ln s and p_i = exp(l_i):
+ *   grad[b,t,i] = scale * (grad_logp * (delta_{i,target} - p_i)
+ *                          - grad_entropy * p_i * (l_i + entropy))
+ * Rows that are not scored, and rows with a flag in status, become 0. stats and entropy
+ * (needed with grad_entropy) are what lfmmi_token_logprobs gave for the same logits, lengths,
+ * targets and scale. targets may be NULL (then grad_logp must be). grad: DEVICE [B, T, V]
+ * contiguous, of the logits' type; it may be the logits' own array if those are contiguous,
+ * and must not overlap them otherwise. Streams, capture, errors as above; no workspace.
+ */
+lfmmi_status lfmmi_token_logprobs_backward(const void *logits, int32_t dtype, int32_t B,
+                                           int32_t T, int32_t V, int64_t stride_b,
+                                           int64_t stride_t, const int32_t *lengths,
+                                           const void *targets, int32_t target_bytes,
+                                           float scale, const float *stats,
+                                           const float *entropy, const float *grad_logp,
+                                           const float *grad_entropy, void *grad,
+                                           void *hip_stream);
+
+/*
+ * The norm of n gradient tensors taken together, sqrt(sum of all squares), and gradients
+ * scaled so that it is at most max_norm:
+ *   norm       DEVICE float32 [1]
+ *   outs[i]    = grads[i] * min(1, max_norm / norm)
+ * grads, outs, counts, dtypes are HOST arrays [n], copied: DEVICE pointers (aligned to an
+ * element at least; NULL where the count is 0), numbers of values (0 is valid) and lfmmi_dtype codes. outs NULL, or outs[i] == grads[i],
+ * scales in place (nothing is written if norm <= max_norm); otherwise nothing written may
+ * overlap any other array of the call, nor may gradients scaled in place be listed twice
+ * (LFMMI_ERR_INVALID_ARG). Squares are summed in fp64, in a fixed order (the same inputs give the
+ * same bits): values whose squares overflow fp32 do not upset the norm. A norm
+ * that is not finite (a NaN or infinite gradient; a norm beyond fp32 counts as infinite) makes every value of
+ * outs 0, so that an update does nothing, and `norm` says so. max_norm >= 0, may be
+ * infinite.
+ * workspace: DEVICE, LFMMI_GRAD_WORKSPACE_BYTES(n) bytes, aligned to 16; otherwise as for
+ * lfmmi_token_logprobs. The calls enqueue kernels on hip_stream and nothing else.
+ */
+#define LFMMI_GRAD_WORKSPACE_BYTES(n) (16 + (((int64_t)(n) + 127) / 128 + 1) * 8192)
+lfmmi_status lfmmi_grad_norm(int32_t n, const void *const *grads, const int64_t *counts,
+                             const int32_t *dtypes, float *norm, void *workspace,
+                             int64_t workspace_bytes, void *hip_stream);
+lfmmi_status lfmmi_clip_grads(int32_t n, const void *const *grads, void *const *outs,
+                              const int64_t *counts, const int32_t *dtypes, float max_norm,
+                              float *norm, void *workspace, int64_t workspace_bytes,
+                              void *hip_stream);
+
 /* Thread-local description of the last failure on this thread ("" if none). */
 const char *lfmmi_last_error(void);
 

@@ -7,6 +7,8 @@ tensors on the GPU (PyTorch only provides device memory and the stream).
 """
 from __future__ import annotations
 
+import collections
+import contextlib
 import ctypes
 import os
 
@@ -24,6 +26,8 @@ EXPORTS = [
     "lfmmi_graph_info",
     "lfmmi_graph_ordering_info", "lfmmi_graph_ordering_copy",
     "lfmmi_profile_enable", "lfmmi_profile_read",
+    "lfmmi_token_logprobs", "lfmmi_token_logprobs_workspace", "lfmmi_token_logprobs_backward",
+    "lfmmi_grad_norm", "lfmmi_clip_grads",
 ]
 
 _lib = None
@@ -66,6 +70,13 @@ def load_library():
     lib.lfmmi_graph_ordering_copy.argtypes = [vp, i32, i32, vp, vp, vp, vp, vp, vp]
     lib.lfmmi_profile_enable.argtypes = [vp, ctypes.c_int]
     lib.lfmmi_profile_read.argtypes = [vp, vp, vp, vp]
+    lib.lfmmi_token_logprobs.argtypes = [vp, i32, i32, i32, i32, i64, i64, vp, vp, i32, f32, i32,
+                                         vp, vp, vp, vp, vp, vp, vp, i64, vp]
+    lib.lfmmi_token_logprobs_workspace.argtypes = [i32, i32, i32, i32, i32, vp]
+    lib.lfmmi_token_logprobs_backward.argtypes = [vp, i32, i32, i32, i32, i64, i64, vp, vp, i32, f32,
+                                                  vp, vp, vp, vp, vp, vp]
+    lib.lfmmi_grad_norm.argtypes = [i32, vp, vp, vp, vp, vp, i64, vp]
+    lib.lfmmi_clip_grads.argtypes = [i32, vp, vp, vp, vp, f32, vp, vp, i64, vp]
     for name in EXPORTS:
         if name not in ("lfmmi_graph_destroy", "lfmmi_last_error"):
             getattr(lib, name).restype = ctypes.c_int
@@ -314,3 +325,234 @@ def lfmmi_profile_read(graph):
     out["calls"] = int(calls[0])
     out["launches"] = int(launches[0])
     return out
+
+
+MAX_TOP = 64   # LFMMI_MAX_TOP
+
+TokenLogprobs = collections.namedtuple(
+    "TokenLogprobs", ["logp", "entropy", "stats", "top_id", "top_logp", "status"])
+
+_dtypes = None
+
+
+def _dtype_code(dtype):
+    """lfmmi_dtype of a torch dtype, None for one that the library does not take."""
+    global _dtypes
+    if _dtypes is None:
+        import torch
+        _dtypes = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+    return _dtypes.get(dtype)
+
+
+def _on_stream(dev, stream):
+    """(context, raw stream): inside the context `dev` is the current device and torch takes
+    memory that belongs to `stream` (torch's current stream if None), which may run
+    beside torch's current one."""
+    import torch
+    if stream is None:
+        if torch.cuda.current_device() == dev.index:
+            return contextlib.nullcontext(), torch.cuda.current_stream(dev).cuda_stream
+        return torch.cuda.device(dev), torch.cuda.current_stream(dev).cuda_stream
+    return torch.cuda.stream(torch.cuda.ExternalStream(stream, device=dev)), stream
+
+
+def _logit_rows(logits, targets, lengths):
+    """Checked (dtype code, B, T, V, stride_b, stride_t, lengths, target bytes) of logits
+    [B, T, V] or [B, V]."""
+    import torch
+    code = _dtype_code(logits.dtype)
+    if not logits.is_cuda or code is None or logits.dim() not in (2, 3):
+        raise ValueError("logits must be a float32, bfloat16 or float16 CUDA tensor [B, T, V] or [B, V]")
+    shape = logits.shape
+    V = shape[-1]
+    if V < 1:
+        raise ValueError("logits need at least one column")
+    if logits.dim() == 3:
+        (B, T), (stride_b, stride_t, step) = shape[:2], logits.stride()
+    else:
+        B, T = shape[0], 1
+        stride_b, step = logits.stride()
+        stride_t = V
+    if step != 1 and V > 1:
+        raise ValueError("the logits of a row must be next to each other")
+    bytes_ = 0
+    if targets is not None:
+        if targets.dtype == torch.int64:
+            bytes_ = 8
+        elif targets.dtype == torch.int32:
+            bytes_ = 4
+        else:
+            raise ValueError("targets must be int32 or int64")
+        if targets.shape != shape[:-1] or targets.device != logits.device or not targets.is_contiguous():
+            raise ValueError("targets must be contiguous, on the logits' device, one for each row")
+    lens = None
+    if lengths is not None:
+        lens = _host(lengths, np.int32)
+        if lens.shape != (B,):
+            raise ValueError("lengths must have B entries")
+    return code, B, T, V, stride_b, stride_t, lens, bytes_
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def lfmmi_token_logprobs(logits, targets=None, lengths=None, top_k=0, scale=1.0, entropy=True,
+                         out=None, stream=None):
+    """Log probabilities of given tokens, entropies and the top_k best alternatives of rows of
+    logits: a float32, bfloat16 or float16 CUDA tensor [B, T, V] or [B, V], any strides as
+    long as a row's logits are next to each other. targets: int32 or int64 CUDA tensor
+    [B, T] or [B] (negative: the row is not scored), or None; lengths: host int array
+    [B] or None. Returns a TokenLogprobs (logp, entropy, stats, top_id, top_logp, status) of
+    device tensors; logp is None without targets, entropy where it is not asked for, top_id and
+    top_logp where top_k is 0. `out`: a TokenLogprobs of an earlier call of the same shapes, to
+    write into. Enqueues on `stream` (default: torch's current stream)."""
+    import torch
+    code, B, T, V, stride_b, stride_t, lens, target_bytes = _logit_rows(logits, targets, lengths)
+    dev = logits.device
+    rows = tuple(logits.shape[:-1])
+    top_k = int(top_k)
+    context, raw = _on_stream(dev, stream)
+    lib = load_library()
+    with context:
+        if out is None:
+            f32, i32 = torch.float32, torch.int32
+            if not 0 <= top_k <= MAX_TOP:
+                raise ValueError("top_k outside [0, MAX_TOP]")
+            out = TokenLogprobs(
+                None if targets is None else torch.empty(rows, dtype=f32, device=dev),
+                torch.empty(rows, dtype=f32, device=dev) if entropy else None,
+                torch.empty(rows + (2,), dtype=f32, device=dev),
+                torch.empty(rows + (top_k,), dtype=i32, device=dev) if top_k else None,
+                torch.empty(rows + (top_k,), dtype=f32, device=dev) if top_k else None,
+                torch.empty(rows, dtype=i32, device=dev))
+        else:
+            for t, wanted, shape, dt in (
+                    (out.logp, targets is not None, rows, torch.float32),
+                    (out.entropy, entropy, rows, torch.float32),
+                    (out.stats, True, rows + (2,), torch.float32),
+                    (out.top_id, top_k > 0, rows + (top_k,), torch.int32),
+                    (out.top_logp, top_k > 0, rows + (top_k,), torch.float32),
+                    (out.status, True, rows, torch.int32)):
+                if (t is not None) != bool(wanted) or wanted and (
+                        tuple(t.shape) != shape or t.dtype != dt or not t.is_contiguous() or t.device != dev):
+                    raise ValueError("output tensor has the wrong shape, dtype, layout or device")
+        need = ctypes.c_int64(0)
+        _check(lib.lfmmi_token_logprobs_workspace(code, B, T, V, top_k, ctypes.byref(need)))
+        ws = torch.empty(need.value, dtype=torch.uint8, device=dev) if need.value else None
+        _check(lib.lfmmi_token_logprobs(
+            logits.data_ptr(), code, B, T, V, stride_b, stride_t, None if lens is None else _hp(lens),
+            _ptr(targets), target_bytes, scale, top_k, _ptr(out.logp), _ptr(out.entropy),
+            _ptr(out.stats), _ptr(out.top_id), _ptr(out.top_logp), _ptr(out.status), _ptr(ws),
+            need.value, raw))
+    return out
+
+
+def lfmmi_token_logprobs_backward(logits, targets, stats, entropy, grad_logp=None,
+                                  grad_entropy=None, lengths=None, scale=1.0, grad=None,
+                                  stream=None):
+    """Gradient with respect to `logits` of a loss whose gradients with respect to the log
+    probabilities and entropies of lfmmi_token_logprobs are grad_logp and grad_entropy
+    (float32 [B, T] or [B]; None: zero). stats and entropy: what that call returned. `grad`: a
+    contiguous tensor like logits to write into, the logits themselves if they are contiguous.
+    Returns the gradient."""
+    import torch
+    code, B, T, V, stride_b, stride_t, lens, target_bytes = _logit_rows(logits, targets, lengths)
+    dev = logits.device
+    rows = tuple(logits.shape[:-1])
+    for t, shape in ((stats, rows + (2,)), (entropy, rows), (grad_logp, rows), (grad_entropy, rows)):
+        if t is not None and (tuple(t.shape) != shape or t.dtype != torch.float32 or
+                              not t.is_contiguous() or t.device != dev):
+            raise ValueError("stats, entropy or a gradient has the wrong shape, dtype, layout or device")
+    context, raw = _on_stream(dev, stream)
+    with context:
+        if grad is None:
+            grad = torch.empty(logits.shape, dtype=logits.dtype, device=dev)
+        elif grad.shape != logits.shape or grad.dtype != logits.dtype or not grad.is_contiguous() \
+                or grad.device != dev:
+            raise ValueError("output tensor has the wrong shape, dtype, layout or device")
+        _check(load_library().lfmmi_token_logprobs_backward(
+            logits.data_ptr(), code, B, T, V, stride_b, stride_t, None if lens is None else _hp(lens),
+            _ptr(targets), target_bytes, scale, _ptr(stats), _ptr(entropy), _ptr(grad_logp),
+            _ptr(grad_entropy), grad.data_ptr(), raw))
+    return grad
+
+
+def _dense(t):
+    """Whether the values of `t` fill a stretch of memory, each once (in any order)."""
+    if t.is_contiguous():
+        return True
+    step = 1
+    for stride, size in sorted((st, n) for st, n in zip(t.stride(), t.shape) if n != 1):
+        if stride != step:
+            return False
+        step *= size
+    return True
+
+
+def _grad_list(grads):
+    """(device, host arrays of pointers, counts, dtype codes) of gradient tensors."""
+    dev = grads[0].device
+    n = len(grads)
+    pointers, counts, codes = (ctypes.c_void_p * n)(), (ctypes.c_int64 * n)(), (ctypes.c_int32 * n)()
+    for i, g in enumerate(grads):
+        code = _dtype_code(g.dtype)
+        if code is None or not g.is_cuda or g.device != dev:
+            raise ValueError("gradients must be float32, bfloat16 or float16 tensors on one CUDA device")
+        if not _dense(g):
+            raise ValueError("gradients must fill their memory: contiguous, or a permutation of that")
+        pointers[i], counts[i], codes[i] = g.data_ptr(), g.numel(), code
+    return dev, pointers, counts, codes
+
+
+def _grad_workspace(n, dev):
+    import torch
+    size = 16 + ((n + 127) // 128 + 1) * 8192   # LFMMI_GRAD_WORKSPACE_BYTES(n)
+    return torch.empty(size, dtype=torch.uint8, device=dev), size
+
+
+def lfmmi_grad_norm(grads, norm=None, stream=None):
+    """Norm of the gradient tensors `grads` (a list, of float32, bfloat16 and float16 CUDA
+    tensors of one device) taken together: a float32 device tensor of no dimensions."""
+    return _grads_call(grads, None, None, norm, stream)
+
+
+def lfmmi_clip_grads(grads, max_norm, out=None, norm=None, stream=None):
+    """Scales the gradient tensors `grads` so that their norm, taken together, is at most
+    max_norm: in place, or into the tensors `out` (of the same shapes, strides and dtypes).
+    Gradients whose norm is not finite become 0. Returns the norm they had, a float32 device
+    tensor of no dimensions."""
+    return _grads_call(grads, float(max_norm), out, norm, stream)
+
+
+def _grads_call(grads, max_norm, out, norm, stream):
+    import torch
+    grads = list(grads)
+    if not grads:
+        raise ValueError("no gradients")
+    n = len(grads)
+    dev, pointers, counts, codes = _grad_list(grads)
+    outs = None
+    if out is not None:
+        out = list(out)
+        if len(out) != n:
+            raise ValueError("out must have one tensor for each gradient")
+        outs = (ctypes.c_void_p * n)()
+        for i, (o, g) in enumerate(zip(out, grads)):
+            if o.shape != g.shape or o.dtype != g.dtype or o.stride() != g.stride() or o.device != dev:
+                raise ValueError("output tensor has the wrong shape, dtype, layout or device")
+            outs[i] = o.data_ptr()
+    if norm is not None and (norm.numel() != 1 or norm.dtype != torch.float32 or norm.device != dev):
+        raise ValueError("output tensor has the wrong shape, dtype, layout or device")
+    context, raw = _on_stream(dev, stream)
+    lib = load_library()
+    with context:
+        if norm is None:
+            norm = torch.empty((), dtype=torch.float32, device=dev)
+        ws, size = _grad_workspace(n, dev)
+        if max_norm is None:
+            _check(lib.lfmmi_grad_norm(n, pointers, counts, codes, norm.data_ptr(), ws.data_ptr(), size, raw))
+        else:
+            _check(lib.lfmmi_clip_grads(n, pointers, outs, counts, codes, max_norm, norm.data_ptr(),
+                                        ws.data_ptr(), size, raw))
+    return norm

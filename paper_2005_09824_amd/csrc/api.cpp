@@ -18,6 +18,7 @@
 
 #include "kernels.h"
 #include "pack.h"
+#include "status.h"
 
 using namespace lfmmi;
 
@@ -25,9 +26,9 @@ static_assert(LFMMI_STATIC_WORKSPACE_BYTES == kStaticWorkspaceBytes &&
                   LFMMI_STATIC_MAX_BATCH == kStaticMaxBatch,
               "the header states the limits of the static workspace");
 
-namespace {
+namespace lfmmi {
 
-thread_local std::string g_error;
+static thread_local std::string g_error;
 
 lfmmi_status fail(lfmmi_status st, const std::string& msg)
 {
@@ -39,6 +40,10 @@ lfmmi_status fail_hip(hipError_t e, const char* what)
 {
     return fail(LFMMI_ERR_HIP, std::string(what) + ": " + hipGetErrorString(e));
 }
+
+}  // namespace lfmmi
+
+namespace {
 
 constexpr size_t kLdsBytes = 160 * 1024;
 constexpr size_t kAlign = 256;

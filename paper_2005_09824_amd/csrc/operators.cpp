@@ -1,0 +1,341 @@
+// C ABI of the operators on token log probabilities and on gradients: argument checks and
+// launches. See include/lfmmi.h.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <string>
+#include <vector>
+
+#include "operators.h"
+#include "status.h"
+
+using namespace lfmmi;
+
+static_assert(LFMMI_MAX_TOP == kMaxTop, "the header states the limit");
+
+namespace {
+
+size_t dtype_size(int32_t dtype) { return dtype == LFMMI_F32 ? 4 : 2; }
+
+bool known(int32_t dtype) { return dtype == LFMMI_F32 || dtype == LFMMI_BF16 || dtype == LFMMI_F16; }
+
+bool aligned(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
+
+// What the forward and the backward call check alike.
+lfmmi_status check_rows(const void* logits, int32_t dtype, int32_t B, int32_t T, int32_t V,
+                        int64_t stride_b, int64_t stride_t, const int32_t* lengths,
+                        const void* targets, int32_t target_bytes, float scale)
+{
+    if (!known(dtype)) return fail(LFMMI_ERR_INVALID_ARG, "unknown dtype");
+    if (B < 0 || T < 0) return fail(LFMMI_ERR_INVALID_ARG, "B and T must be >= 0");
+    if (V < 1) return fail(LFMMI_ERR_INVALID_ARG, "V must be >= 1");
+    if ((int64_t)B * T > INT32_MAX) return fail(LFMMI_ERR_UNSUPPORTED, "B * T exceeds 2^31 - 1");
+    if (V > (1 << 30)) return fail(LFMMI_ERR_UNSUPPORTED, "V exceeds 2^30");
+    if (stride_b < 0 || stride_t < 0) return fail(LFMMI_ERR_INVALID_ARG, "strides must be >= 0");
+    // so that no offset passes 64 bits
+    if (stride_b > ((int64_t)1 << 60) / std::max(B, 1) || stride_t > ((int64_t)1 << 60) / std::max(T, 1))
+        return fail(LFMMI_ERR_UNSUPPORTED, "strides beyond 2^60 elements");
+    if (!(scale >= 1e-6f && scale <= 1e6f))
+        return fail(LFMMI_ERR_INVALID_ARG, "scale outside [1e-6, 1e6]");
+    if (targets && target_bytes != 4 && target_bytes != 8)
+        return fail(LFMMI_ERR_INVALID_ARG, "target_bytes must be 4 or 8");
+    if (lengths)
+        for (int32_t b = 0; b < B; ++b)
+            if (lengths[b] < 0 || lengths[b] > T)
+                return fail(LFMMI_ERR_INVALID_ARG, "lengths[" + std::to_string(b) + "] outside [0, T]");
+    if (B == 0 || T == 0) return LFMMI_OK;
+    if (!logits) return fail(LFMMI_ERR_INVALID_ARG, "logits is null");
+    if (!aligned(logits, dtype_size(dtype)) || (targets && !aligned(targets, target_bytes)))
+        return fail(LFMMI_ERR_INVALID_ARG, "an array is not aligned to its elements");
+    return LFMMI_OK;
+}
+
+// Sequences that one launch takes, and their lengths.
+int32_t fill_lengths(const int32_t* lengths, int32_t b, int32_t B, SeqLengths* out)
+{
+    if (!lengths) {
+        out->n = 0;
+        return B - b;
+    }
+    const int32_t n = std::min(B - b, kLengthsPerLaunch);
+    out->n = n;
+    std::copy(lengths + b, lengths + b + n, out->T);
+    return n;
+}
+
+template <typename U>
+U* at(U* p, int64_t i)
+{
+    return p ? p + i : nullptr;
+}
+
+const void* at_bytes(const void* p, int64_t i)
+{
+    return p ? static_cast<const char*>(p) + i : nullptr;
+}
+
+lfmmi_status check_grads(int32_t n, const void* const* grads, const int64_t* counts,
+                         const int32_t* dtypes, const float* norm, const void* workspace,
+                         int64_t workspace_bytes)
+{
+    if (n < 0) return fail(LFMMI_ERR_INVALID_ARG, "n must be >= 0");
+    if (!norm) return fail(LFMMI_ERR_INVALID_ARG, "norm is null");
+    if (n > 0 && (!grads || !counts || !dtypes))
+        return fail(LFMMI_ERR_INVALID_ARG, "grads / counts / dtypes is null");
+    if (!workspace || !aligned(workspace, 16) || workspace_bytes < LFMMI_GRAD_WORKSPACE_BYTES(n))
+        return fail(LFMMI_ERR_INVALID_ARG, "workspace is null, too small or not aligned to 16 bytes");
+    for (int32_t i = 0; i < n; ++i) {
+        if (!known(dtypes[i])) return fail(LFMMI_ERR_INVALID_ARG, "unknown dtype");
+        if (counts[i] < 0) return fail(LFMMI_ERR_INVALID_ARG, "counts must be >= 0");
+        if (counts[i] > ((int64_t)1 << 36)) return fail(LFMMI_ERR_UNSUPPORTED, "a count exceeds 2^36");
+        if (counts[i] > 0 && !grads[i])
+            return fail(LFMMI_ERR_INVALID_ARG, "grads[" + std::to_string(i) + "] is null");
+        if (!aligned(grads[i], dtype_size(dtypes[i])))
+            return fail(LFMMI_ERR_INVALID_ARG, "a gradient is not aligned to its elements");
+    }
+    return LFMMI_OK;
+}
+
+struct Span {
+    uintptr_t at, end;
+    bool written;
+};
+
+// Whether an array that is written overlaps another array.
+bool overlap(std::vector<Span>& spans)
+{
+    const auto before = [](const Span& a, const Span& b) { return a.at < b.at; };
+    if (!std::is_sorted(spans.begin(), spans.end(), before))
+        std::sort(spans.begin(), spans.end(), before);
+    uintptr_t any = 0, written = 0;  // ends of what came before
+    for (const Span& s : spans) {
+        if (s.at < written || (s.written && s.at < any)) return true;
+        any = std::max(any, s.end);
+        if (s.written) written = std::max(written, s.end);
+    }
+    return false;
+}
+
+lfmmi_status check_outs(int32_t n, const void* const* grads, void* const* outs,
+                        const int64_t* counts, const int32_t* dtypes)
+{
+    std::vector<Span> spans;
+    spans.reserve(2 * (size_t)n);
+    for (int32_t i = 0; i < n; ++i) {
+        if (counts[i] == 0) continue;
+        const size_t bytes = (size_t)counts[i] * dtype_size(dtypes[i]);
+        const uintptr_t in = reinterpret_cast<uintptr_t>(grads[i]);
+        uintptr_t out = in;
+        if (outs) {
+            if (!outs[i]) return fail(LFMMI_ERR_INVALID_ARG, "outs[" + std::to_string(i) + "] is null");
+            if (!aligned(outs[i], dtype_size(dtypes[i])))
+                return fail(LFMMI_ERR_INVALID_ARG, "an output is not aligned to its elements");
+            out = reinterpret_cast<uintptr_t>(outs[i]);
+        }
+        spans.push_back({out, out + bytes, true});
+        if (out != in) spans.push_back({in, in + bytes, false});
+    }
+    if (overlap(spans))
+        return fail(LFMMI_ERR_INVALID_ARG,
+                    "an array that is written overlaps another one, or is listed twice");
+    return LFMMI_OK;
+}
+
+// The tensors from `from` on that one launch takes.
+int32_t fill_list(int32_t from, int32_t n, const void* const* grads, void* const* outs,
+                  const int64_t* counts, const int32_t* dtypes, GradList* l)
+{
+    l->n = 0;
+    int64_t units = 0;
+    int32_t i = from;
+    static_assert(((int64_t)1 << 36) / kGradUnit * kGradTensors <= INT32_MAX, "unit numbers fit 32 bits");
+    for (; i < n && l->n < kGradTensors; ++i) {
+        if (counts[i] == 0) continue;
+        const int64_t more = (counts[i] + kGradUnit - 1) / kGradUnit;
+        l->in[l->n] = grads[i];
+        l->out[l->n] = outs ? outs[i] : const_cast<void*>(grads[i]);
+        l->count[l->n] = counts[i] << 2 | dtypes[i];
+        l->first[l->n] = (int32_t)units;
+        units += more;
+        ++l->n;
+    }
+    for (int32_t k = l->n; k <= kGradTensors; ++k) l->first[k] = (int32_t)units;
+    return i;
+}
+
+// max_norm < 0: the norm alone.
+lfmmi_status run_grads(int32_t n, const void* const* grads, void* const* outs,
+                       const int64_t* counts, const int32_t* dtypes, float max_norm, float* norm,
+                       void* workspace, hipStream_t stream)
+{
+    float* factor = static_cast<float*>(workspace);
+    double* partials = reinterpret_cast<double*>(static_cast<char*>(workspace) + 16);
+    GradList l;
+    int blocks = 0;
+    hipError_t e;
+    for (int32_t i = 0; i < n;) {
+        i = fill_list(i, n, grads, outs, counts, dtypes, &l);
+        if (l.n == 0) break;
+        if ((e = launch_grad_squares(l, partials + blocks, stream)) != hipSuccess)
+            return fail_hip(e, "kernel launch");
+        blocks += grad_blocks(l);
+    }
+    if ((e = launch_grad_norm(partials, blocks, max_norm, norm, factor, stream)) != hipSuccess)
+        return fail_hip(e, "kernel launch");
+    if (max_norm < 0.f) return LFMMI_OK;
+    for (int32_t i = 0; i < n;) {
+        i = fill_list(i, n, grads, outs, counts, dtypes, &l);
+        if (l.n == 0) break;
+        if ((e = launch_grad_scale(l, factor, stream)) != hipSuccess)
+            return fail_hip(e, "kernel launch");
+    }
+    return LFMMI_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+lfmmi_status lfmmi_token_logprobs_workspace(int32_t dtype, int32_t B, int32_t T, int32_t V,
+                                            int32_t top_k, int64_t* bytes)
+{
+    if (!bytes) return fail(LFMMI_ERR_INVALID_ARG, "bytes is null");
+    if (!known(dtype) || B < 0 || T < 0 || V < 1 || top_k < 0 || top_k > kMaxTop || top_k > V)
+        return fail(LFMMI_ERR_INVALID_ARG, "unknown dtype, or a size out of range");
+    if ((int64_t)B * T > INT32_MAX) return fail(LFMMI_ERR_UNSUPPORTED, "B * T exceeds 2^31 - 1");
+    *bytes = (int64_t)token_workspace(dtype, (int64_t)B * T, V, top_k);
+    return LFMMI_OK;
+}
+
+lfmmi_status lfmmi_token_logprobs(const void* logits, int32_t dtype, int32_t B, int32_t T,
+                                  int32_t V, int64_t stride_b, int64_t stride_t,
+                                  const int32_t* lengths, const void* targets,
+                                  int32_t target_bytes, float scale, int32_t top_k, float* logp,
+                                  float* entropy, float* stats, int32_t* top_id, float* top_logp,
+                                  int32_t* status, void* workspace, int64_t workspace_bytes,
+                                  void* hip_stream)
+try {
+    lfmmi_status st = check_rows(logits, dtype, B, T, V, stride_b, stride_t, lengths, targets,
+                                 target_bytes, scale);
+    if (st != LFMMI_OK) return st;
+    if (top_k < 0 || top_k > V) return fail(LFMMI_ERR_INVALID_ARG, "top_k outside [0, V]");
+    if (top_k > kMaxTop) return fail(LFMMI_ERR_UNSUPPORTED, "top_k exceeds LFMMI_MAX_TOP");
+    if (logp && !targets) return fail(LFMMI_ERR_INVALID_ARG, "logp without targets");
+    if (B == 0 || T == 0) return LFMMI_OK;
+    const size_t need = token_workspace(dtype, (int64_t)B * T, V, top_k);
+    if (need > 0 && (!workspace || !aligned(workspace, 16) || workspace_bytes < (int64_t)need))
+        return fail(LFMMI_ERR_INVALID_ARG, "workspace is null, too small or not aligned to 16 bytes");
+    const int64_t size = (int64_t)dtype_size(dtype);
+    for (int32_t b = 0; b < B;) {
+        SeqLengths lens;
+        const int32_t n = fill_lengths(lengths, b, B, &lens);
+        const int64_t row = (int64_t)b * T;
+        TokenParams p{};
+        p.x = at_bytes(logits, b * stride_b * size);
+        p.stride_b = stride_b;
+        p.stride_t = stride_t;
+        p.targets = at_bytes(targets, row * target_bytes);
+        p.target_bytes = target_bytes;
+        p.B = n;
+        p.T = T;
+        p.V = V;
+        p.top_k = top_id || top_logp ? top_k : 0;
+        p.scale = scale;
+        p.logp = at(logp, row);
+        p.entropy = at(entropy, row);
+        p.stats = at(stats, 2 * row);
+        p.top_id = at(top_id, row * top_k);
+        p.top_logp = at(top_logp, row * top_k);
+        p.status = at(status, row);
+        p.workspace = workspace;
+        const hipError_t e =
+            launch_token_logprobs(p, lens, dtype, static_cast<hipStream_t>(hip_stream));
+        if (e != hipSuccess) return fail_hip(e, "kernel launch");
+        b += n;
+    }
+    return LFMMI_OK;
+} catch (...) {
+    return LFMMI_ERR_OOM;
+}
+
+lfmmi_status lfmmi_token_logprobs_backward(const void* logits, int32_t dtype, int32_t B, int32_t T,
+                                           int32_t V, int64_t stride_b, int64_t stride_t,
+                                           const int32_t* lengths, const void* targets,
+                                           int32_t target_bytes, float scale, const float* stats,
+                                           const float* entropy, const float* grad_logp,
+                                           const float* grad_entropy, void* grad, void* hip_stream)
+try {
+    lfmmi_status st = check_rows(logits, dtype, B, T, V, stride_b, stride_t, lengths, targets,
+                                 target_bytes, scale);
+    if (st != LFMMI_OK) return st;
+    if (grad_logp && !targets) return fail(LFMMI_ERR_INVALID_ARG, "grad_logp without targets");
+    if (grad_entropy && !entropy) return fail(LFMMI_ERR_INVALID_ARG, "grad_entropy without entropy");
+    if (B == 0 || T == 0) return LFMMI_OK;
+    if (!stats || !grad) return fail(LFMMI_ERR_INVALID_ARG, "stats / grad is null");
+    const int64_t size = (int64_t)dtype_size(dtype);
+    if (!aligned(grad, size)) return fail(LFMMI_ERR_INVALID_ARG, "an array is not aligned to its elements");
+    // in place means the very same elements
+    const bool same = logits == grad && (T == 1 || stride_t == V) && (B == 1 || stride_b == (int64_t)T * V);
+    if (!same) {
+        const uintptr_t x = reinterpret_cast<uintptr_t>(logits), g = reinterpret_cast<uintptr_t>(grad);
+        const uintptr_t x_end = x + (uintptr_t)(((B - 1) * stride_b + (T - 1) * stride_t + V) * size);
+        if (g < x_end && x < g + (uintptr_t)((int64_t)B * T * V * size))
+            return fail(LFMMI_ERR_INVALID_ARG, "grad overlaps logits that are not contiguous");
+    }
+    for (int32_t b = 0; b < B;) {
+        SeqLengths lens;
+        const int32_t n = fill_lengths(lengths, b, B, &lens);
+        const int64_t row = (int64_t)b * T;
+        TokenGradParams p{};
+        p.x = at_bytes(logits, b * stride_b * size);
+        p.stride_b = stride_b;
+        p.stride_t = stride_t;
+        p.targets = at_bytes(targets, row * target_bytes);
+        p.target_bytes = target_bytes;
+        p.B = n;
+        p.T = T;
+        p.V = V;
+        p.scale = scale;
+        p.stats = stats + 2 * row;
+        p.entropy = at(entropy, row);
+        p.grad_logp = at(grad_logp, row);
+        p.grad_entropy = at(grad_entropy, row);
+        p.grad = static_cast<char*>(grad) + row * V * size;
+        const hipError_t e = launch_token_grad(p, lens, dtype, static_cast<hipStream_t>(hip_stream));
+        if (e != hipSuccess) return fail_hip(e, "kernel launch");
+        b += n;
+    }
+    return LFMMI_OK;
+} catch (...) {
+    return LFMMI_ERR_OOM;
+}
+
+lfmmi_status lfmmi_grad_norm(int32_t n, const void* const* grads, const int64_t* counts,
+                             const int32_t* dtypes, float* norm, void* workspace,
+                             int64_t workspace_bytes, void* hip_stream)
+try {
+    const lfmmi_status st = check_grads(n, grads, counts, dtypes, norm, workspace, workspace_bytes);
+    if (st != LFMMI_OK) return st;
+    return run_grads(n, grads, nullptr, counts, dtypes, -1.f, norm, workspace,
+                     static_cast<hipStream_t>(hip_stream));
+} catch (...) {
+    return LFMMI_ERR_OOM;
+}
+
+lfmmi_status lfmmi_clip_grads(int32_t n, const void* const* grads, void* const* outs,
+                              const int64_t* counts, const int32_t* dtypes, float max_norm,
+                              float* norm, void* workspace, int64_t workspace_bytes,
+                              void* hip_stream)
+try {
+    lfmmi_status st = check_grads(n, grads, counts, dtypes, norm, workspace, workspace_bytes);
+    if (st != LFMMI_OK) return st;
+    if (!(max_norm >= 0.f)) return fail(LFMMI_ERR_INVALID_ARG, "max_norm must be >= 0");
+    if ((st = check_outs(n, grads, outs, counts, dtypes)) != LFMMI_OK) return st;
+    return run_grads(n, grads, outs, counts, dtypes, max_norm, norm, workspace,
+                     static_cast<hipStream_t>(hip_stream));
+} catch (...) {
+    return LFMMI_ERR_OOM;
+}
+
+}  // extern "C"

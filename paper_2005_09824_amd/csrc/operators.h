@@ -1,0 +1,79 @@
+// Plain-struct interface between the C ABI (operators.cpp) and the kernels on token log
+// probabilities (tokens.hip) and on gradients (grads.hip).
+#pragma once
+#include <hip/hip_runtime.h>
+#include <cstdint>
+
+namespace lfmmi {
+
+constexpr int kMaxTop = 64;  // LFMMI_MAX_TOP
+
+// Lengths travel as a kernel argument, this many sequences a launch (a call with more of
+// them is cut into several); n == 0: every sequence has all T rows.
+constexpr int kLengthsPerLaunch = 256;
+struct SeqLengths {
+    int32_t n;
+    int32_t T[kLengthsPerLaunch];
+};
+
+struct TokenParams {
+    const void* x;        // logits of sequence 0 of this launch; element (b, t, i) at
+    int64_t stride_b;     // b * stride_b + t * stride_t + i
+    int64_t stride_t;
+    const void* targets;  // [B, T] or null
+    int32_t target_bytes; // 4 or 8
+    int32_t B, T, V;      // of this launch
+    int32_t top_k;
+    float scale;
+    float* logp;          // [B, T] or null, and so on
+    float* entropy;
+    float* stats;         // [B, T, 2]
+    int32_t* top_id;      // [B, T, top_k]
+    float* top_logp;
+    int32_t* status;
+    void* workspace;
+};
+
+struct TokenGradParams {
+    const void* x;
+    int64_t stride_b, stride_t;
+    const void* targets;
+    int32_t target_bytes;
+    int32_t B, T, V;
+    float scale;
+    const float* stats;
+    const float* entropy;
+    const float* grad_logp;     // or null
+    const float* grad_entropy;  // or null
+    void* grad;                 // [B, T, V] contiguous
+};
+
+// dtype: lfmmi_dtype
+hipError_t launch_token_logprobs(const TokenParams& p, const SeqLengths& lens, int dtype,
+                                 hipStream_t stream);
+size_t token_workspace(int dtype, int64_t rows, int V, int top_k);
+hipError_t launch_token_grad(const TokenGradParams& p, const SeqLengths& lens, int dtype,
+                             hipStream_t stream);
+
+// Gradients of one launch: values of tensor i are cut into units of kGradUnit, unit numbers
+// run through the tensors.
+constexpr int kGradTensors = 128;
+constexpr int kGradUnit = 8192;
+constexpr int kGradBlocks = 1024;  // most workgroups of a launch: one partial sum each
+struct GradList {
+    const void* in[kGradTensors];
+    void* out[kGradTensors];
+    int64_t count[kGradTensors];  // << 2 | lfmmi_dtype
+    int32_t first[kGradTensors + 1];
+    int32_t n;
+};
+
+// Sums of squares of the values of `l`: a partial sum for each of grad_blocks(l) workgroups.
+int grad_blocks(const GradList& l);
+hipError_t launch_grad_squares(const GradList& l, double* partials, hipStream_t stream);
+// norm and, for max_norm >= 0, the factor that brings it to max_norm, from all partial sums.
+hipError_t launch_grad_norm(const double* partials, int n, float max_norm, float* norm,
+                            float* factor, hipStream_t stream);
+hipError_t launch_grad_scale(const GradList& l, const float* factor, hipStream_t stream);
+
+}  // namespace lfmmi

@@ -1,0 +1,224 @@
+"""The norm of many gradients together and clipping to it, against 64 bits."""
+import numpy as np
+import pytest
+
+from paper_2005_09824_amd import binding, chain
+from tests import operators_oracle as oracle
+
+pytestmark = pytest.mark.gpu
+
+DTYPES = ["float32", "bfloat16", "float16"]
+
+
+def _torch():
+    import torch
+    return torch
+
+
+def _grads(rng, sizes, dtypes, sigma=1.0):
+    torch = _torch()
+    out = []
+    for i, n in enumerate(sizes):
+        v = torch.from_numpy(rng.normal(0, sigma, n).astype(np.float32))
+        out.append(v.to(getattr(torch, dtypes[i % len(dtypes)])).cuda())
+    return out
+
+
+def _norm64(grads):
+    return float(np.sqrt(sum(float(g.double().square().sum()) for g in grads)))
+
+
+def _name(t):
+    return str(t.dtype).replace("torch.", "")
+
+
+def _check_scaled(outs, grads, norm64, max_norm):
+    factor = min(1.0, max_norm / norm64) if norm64 > 0 else 1.0
+    for o, g in zip(outs, grads):
+        want = g.double() * factor
+        # the factor and the product are rounded to 32 bits, the result to its type
+        tol = want.abs() * (4 * oracle.U + 1.001 * oracle.HALF[_name(g)]) + oracle.TINY[_name(g)]
+        assert bool(((o.double() - want).abs() <= tol).all()), (_name(g), g.shape)
+
+
+SIZES = [[1], [7], [0, 3, 0], [64, 1, 8191, 8192, 8193], [100003], [5, 300000, 17, 65536, 0, 999],
+         list(range(1, 300)), [3] * 1000, [20000] * 129]
+
+
+@pytest.mark.parametrize("dtypes", [["float32"], ["bfloat16"], ["float16"], DTYPES])
+@pytest.mark.parametrize("sizes", SIZES, ids=lambda s: "%d_tensors_%d" % (len(s), sum(s)))
+def test_norm_and_clipping(sizes, dtypes):
+    torch = _torch()
+    rng = np.random.default_rng(sum(sizes))
+    grads = _grads(rng, sizes, dtypes)
+    before = [g.clone() for g in grads]
+    norm64 = _norm64(grads)
+    norm = binding.lfmmi_grad_norm(grads)
+    assert norm.shape == () and abs(float(norm) - norm64) <= 1.01 * oracle.U * norm64
+    for max_norm in (norm64 * 0.3, norm64 * 2, 0.0, float("inf")):
+        outs = [torch.full_like(g, 7.0) for g in grads]
+        n = binding.lfmmi_clip_grads(grads, max_norm, out=outs)
+        assert torch.equal(n, norm)
+        _check_scaled(outs, before, norm64, max_norm)
+        if max_norm >= norm64:
+            assert all(torch.equal(o, g) for o, g in zip(outs, before))
+        assert all(torch.equal(g, b) for g, b in zip(grads, before))
+    binding.lfmmi_clip_grads(grads, norm64 * 2)
+    assert all(torch.equal(g, b) for g, b in zip(grads, before))
+    outs = [torch.empty_like(g) for g in grads]
+    binding.lfmmi_clip_grads(grads, norm64 * 0.3, out=outs)
+    n = binding.lfmmi_clip_grads(grads, norm64 * 0.3)
+    assert torch.equal(n, norm)
+    assert all(torch.equal(g, o) for g, o in zip(grads, outs))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_views_at_any_alignment(dtype):
+    # gradients that are pieces of one buffer, with values between them that stay as they were
+    torch = _torch()
+    rng = np.random.default_rng(9)
+    flat = torch.from_numpy(rng.normal(0, 1, 200000).astype(np.float32)).to(getattr(torch, dtype)).cuda()
+    before = flat.clone()
+    pieces, inside, at = [], torch.zeros(200000, dtype=torch.bool, device="cuda"), 1
+    for n in (1, 2, 3, 5, 8, 13, 100, 1001, 8192, 8193, 50001, 77777):
+        pieces.append((at, at + n))
+        inside[at:at + n] = True
+        at += n + 1 + n % 3
+    norm64 = _norm64([before[a:b] for a, b in pieces])
+    norm = binding.lfmmi_clip_grads([flat[a:b] for a, b in pieces], norm64 / 4)
+    assert abs(float(norm) - norm64) <= 1.01 * oracle.U * norm64
+    _check_scaled([flat[a:b] for a, b in pieces], [before[a:b] for a, b in pieces], norm64, norm64 / 4)
+    assert torch.equal(flat[~inside], before[~inside])
+    # outputs at another alignment than their inputs
+    for shift in (0, 1, 2, 3, 5):
+        out = torch.full((200008,), 7.0, dtype=flat.dtype, device="cuda")
+        outs = [out[a + shift:b + shift] for a, b in pieces]
+        binding.lfmmi_clip_grads([before[a:b] for a, b in pieces], norm64 / 4, out=outs)
+        _check_scaled(outs, [before[a:b] for a, b in pieces], norm64, norm64 / 4)
+        rest = torch.ones(200008, dtype=torch.bool, device="cuda")
+        for a, b in pieces:
+            rest[a + shift:b + shift] = False
+        assert bool((out[rest] == 7.0).all())
+
+
+def test_layouts():
+    torch = _torch()
+    a = torch.randn((6, 50, 30), device="cuda").permute(2, 0, 1)
+    b = torch.randn((4, 8, 5, 5), device="cuda").to(memory_format=torch.channels_last)
+    c = torch.randn((), device="cuda")
+    d = torch.randn((5, 1, 7), device="cuda").transpose(0, 2)
+    before = [t.clone() for t in (a, b, c, d)]
+    norm64 = _norm64(before)
+    norm = binding.lfmmi_clip_grads([a, b, c, d], 1.0)
+    assert abs(float(norm) - norm64) <= 1.01 * oracle.U * norm64
+    _check_scaled([a, b, c, d], before, norm64, 1.0)
+    for bad in (torch.randn((4, 6), device="cuda")[:, ::2], torch.randn((4, 1), device="cuda").expand(4, 3),
+                torch.randn(8, device="cuda").as_strided((4, 3), (1, 1)), torch.zeros(3, dtype=torch.int32, device="cuda"),
+                torch.zeros(3, dtype=torch.float64, device="cuda"), torch.zeros(3)):
+        with pytest.raises(ValueError):
+            binding.lfmmi_clip_grads([a, bad], 1.0)
+
+
+def test_extreme_values_and_norms_that_are_not_finite():
+    torch = _torch()
+    # squares beyond and below the range of 32 bits
+    for value, n in ((3e30, 1000), (1e-30, 1000), (1e38, 4), (2e-45, 100)):
+        g = torch.full((n,), value, device="cuda")
+        norm64 = float(g.double().square().sum().sqrt())
+        norm = binding.lfmmi_clip_grads([g], 1.0)
+        assert abs(float(norm) - norm64) <= 1.01 * oracle.U * norm64
+        want = np.float64(np.float32(value)) * min(1.0, 1.0 / norm64)
+        # (a factor below the normal range is rounded in whole steps of 2^-149)
+        step = 2.0 ** -149 * np.float64(np.float32(value)) if norm64 > 1e37 else 0.0
+        assert float((g.double() - want).abs().max()) <= 4 * oracle.U * want + step + 1e-44
+    for bad in (float("nan"), float("inf"), -float("inf")):
+        for at in (0, 4999, 99999):
+            for dtype in DTYPES:
+                g = [torch.ones(100000, device="cuda").to(getattr(torch, dtype)), torch.ones(3, device="cuda")]
+                g[0][at] = bad
+                out = [torch.full_like(t, 5.0) for t in g]
+                norm = binding.lfmmi_clip_grads(g, 1.0, out=out)
+                assert not np.isfinite(float(norm)) and np.isnan(bad) == np.isnan(float(norm))
+                assert all(bool((t == 0).all()) for t in out)
+                assert float(g[1].sum()) == 3.0
+                binding.lfmmi_clip_grads(g, float("inf"))
+                assert all(bool((t == 0).all()) for t in g)
+    # a norm beyond 32 bits
+    g = torch.full((100,), 3e38, device="cuda")
+    assert float(binding.lfmmi_clip_grads([g], 1.0)) == float("inf") and float(g.abs().max()) == 0.0
+    g = torch.zeros(5000, device="cuda")
+    assert float(binding.lfmmi_clip_grads([g], 0.0)) == 0.0 and float(g.abs().max()) == 0.0
+
+
+def test_arrays_that_overlap_are_refused():
+    torch = _torch()
+    a = torch.ones(100, device="cuda")
+    b = torch.ones(100, device="cuda")
+    for grads, out in (([a, a], None), ([a[:60], a[50:]], None), ([a, b], [b, a]), ([a, b], [a, a]),
+                       ([a[:50], b[:50]], [a[10:60], torch.ones(50, device="cuda")])):
+        with pytest.raises(binding.LfmmiError):
+            binding.lfmmi_clip_grads(grads, 1.0, out=out)
+    assert float(binding.lfmmi_grad_norm([a, a])) == np.float32(np.sqrt(200.0))
+    assert float(binding.lfmmi_clip_grads([a, b], 1e9, out=[a, torch.empty_like(b)])) == np.float32(np.sqrt(200.0))
+
+
+def test_large_counts():
+    # one tensor of more than 2^31 values
+    torch = _torch()
+    g = torch.zeros((1 << 31) + 12345, dtype=torch.bfloat16, device="cuda")
+    g[5], g[(1 << 31) + 3], g[-1] = 3.0, 4.0, 12.0
+    norm = binding.lfmmi_clip_grads([g], 6.5)
+    assert float(norm) == 13.0
+    assert [float(g[i]) for i in (5, (1 << 31) + 3, -1)] == [1.5, 2.0, 6.0]
+    assert float(g[6:1 << 20].abs().max()) == 0.0
+
+
+def test_streams_replays_and_the_same_bits_every_time():
+    torch = _torch()
+    rng = np.random.default_rng(5)
+    grads = _grads(rng, [5000, 70001, 3] * 60, DTYPES)
+    outs = [torch.empty_like(g) for g in grads]
+    norm = binding.lfmmi_clip_grads(grads, 1.0, out=outs)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    outs2 = [torch.empty_like(g) for g in grads]
+    norm2 = binding.lfmmi_clip_grads(grads, 1.0, out=outs2, stream=side.cuda_stream)
+    more = [binding.lfmmi_grad_norm(grads) for _ in range(10)]
+    torch.cuda.synchronize()
+    assert torch.equal(norm, norm2) and all(torch.equal(a, b) for a, b in zip(outs, outs2))
+    assert all(torch.equal(norm, m) for m in more)
+    graphs = []
+    for k in range(2):
+        mine = [torch.empty_like(g) for g in grads]
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            n = binding.lfmmi_clip_grads(grads, 1.0, out=mine)
+        graphs.append((graph, n, mine))
+    for k in range(3):
+        for g in grads:
+            g.mul_(1.5)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            graphs[0][0].replay()
+        graphs[1][0].replay()
+        torch.cuda.synchronize()
+        want = [torch.empty_like(g) for g in grads]
+        norm = binding.lfmmi_clip_grads(grads, 1.0, out=want)
+        for _, n, mine in graphs:
+            assert torch.equal(n, norm) and all(torch.equal(a, b) for a, b in zip(mine, want))
+
+
+def test_parameters():
+    torch = _torch()
+    layers = torch.nn.Sequential(torch.nn.Linear(30, 50), torch.nn.ReLU(), torch.nn.Linear(50, 4)).cuda()
+    unused = torch.nn.Parameter(torch.zeros(3, device="cuda"))
+    layers(torch.randn((64, 30), device="cuda")).square().sum().backward()
+    before = [p.grad.clone() for p in layers.parameters()]
+    norm64 = _norm64(before)
+    norm = chain.clip_grad_norm(list(layers.parameters()) + [unused], 0.25)
+    assert abs(float(norm) - norm64) <= 1.01 * oracle.U * norm64
+    _check_scaled([p.grad for p in layers.parameters()], before, norm64, 0.25)
+    assert unused.grad is None
+    with pytest.raises(ValueError):
+        chain.clip_grad_norm([unused], 1.0)

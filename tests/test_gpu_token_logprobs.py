@@ -1,0 +1,482 @@
+"""Log probabilities of given tokens, entropies, alternatives and their gradient, against the
+64-bit forms of operators_oracle."""
+import numpy as np
+import pytest
+
+from paper_2005_09824_amd import binding, chain, workloads
+from tests import operators_oracle as oracle
+
+pytestmark = pytest.mark.gpu
+
+DTYPES = ["float32", "bfloat16", "float16"]
+
+
+def _torch():
+    import torch
+    return torch
+
+
+def _dtype(name):
+    return getattr(_torch(), name)
+
+
+def _logits(rng, shape, dtype, sigma=2.5):
+    """(device tensor, its values in 64 bits)"""
+    torch = _torch()
+    x = torch.from_numpy(rng.normal(0, sigma, shape).astype(np.float32)).to(_dtype(dtype)).cuda()
+    return x, x.double().cpu().numpy()
+
+
+def _live(B, T, targets, lengths):
+    live = np.ones((B, T), bool)
+    if lengths is not None:
+        live &= np.arange(T)[None] < np.asarray(lengths)[:, None]
+    if targets is not None:
+        live &= targets.reshape(B, T) >= 0
+    return live.reshape(-1)
+
+
+def _close(got, want, tol, what):
+    got = got.double().cpu().numpy().reshape(want.shape)
+    fine = np.isfinite(want)
+    assert np.array_equal(np.isnan(got), np.isnan(want)), what
+    assert np.array_equal(got[~fine & ~np.isnan(want)], want[~fine & ~np.isnan(want)]), what
+    off = np.abs(got[fine] - want[fine])
+    tol = np.broadcast_to(tol, want.shape)[fine]
+    assert np.all(off <= tol), (what, off.max(), (off / tol).max())
+
+
+def check(x, x64, targets, lengths, scale, top, r, grad_too=True, seed=3):
+    """`r`: the call's answer; then the gradient for random upstream gradients."""
+    torch = _torch()
+    V = x64.shape[-1]
+    B, T = (x64.shape[0], x64.shape[1]) if x64.ndim == 3 else (x64.shape[0], 1)
+    t64 = None if targets is None else targets.cpu().numpy().reshape(-1).astype(np.int64)
+    live = _live(B, T, t64, lengths)
+    f = float(np.float32(scale))
+    want = oracle.rows(x64.reshape(-1, V), t64, live, f, top)
+    d = np.where(np.isfinite(want["logp"]), want["logp"] + want["logs"], 0.0)
+    assert np.array_equal(r.status.cpu().numpy().reshape(-1), want["status"])
+    if t64 is not None:
+        _close(r.logp, want["logp"], oracle.bound_logp(V, want["logp"], d), "logp")
+    else:
+        assert r.logp is None
+    if r.entropy is not None:
+        _close(r.entropy, want["entropy"], oracle.bound_entropy(V), "entropy")
+    stats = r.stats.double().cpu().numpy().reshape(-1, 2)
+    assert np.array_equal(stats[:, 0], want["m"], equal_nan=True)
+    _close(r.stats[..., 1], want["logs"], oracle.bound_logs(V) + 2 * oracle.U * np.log(V + 1.0), "ln s")
+    if top:
+        assert np.array_equal(r.top_id.cpu().numpy().reshape(-1, top), want["top_id"])
+        dt = np.where(np.isfinite(want["top_logp"]), want["top_logp"] + want["logs"][:, None], 0.0)
+        _close(r.top_logp, want["top_logp"], oracle.bound_logp(V, want["top_logp"], dt), "top_logp")
+    if not grad_too:
+        return want
+    rng = np.random.default_rng(seed)
+    g = rng.normal(0, 1, len(live)).astype(np.float32) if t64 is not None else np.zeros(len(live), np.float32)
+    h = rng.normal(0, 0.3, len(live)).astype(np.float32)
+    shape = r.status.shape
+    gd = torch.from_numpy(g).cuda().reshape(shape) if t64 is not None else None
+    hd = torch.from_numpy(h).cuda().reshape(shape)
+    dtype = str(x.dtype).replace("torch.", "")
+    for gg, hh in ((gd, hd), (gd, None), (None, hd)):
+        if gg is None and hh is None:
+            continue
+        got = binding.lfmmi_token_logprobs_backward(x, targets, r.stats, r.entropy, gg, hh, lengths, scale)
+        g1 = g.astype(np.float64) if gg is not None else np.zeros(len(live))
+        h1 = h.astype(np.float64) if hh is not None else np.zeros(len(live))
+        wanted = oracle.grads(want, t64, live, f, g1, h1)
+        tol = oracle.bound_grad(want, t64, f, g1, h1, wanted, dtype)
+        tol = np.where((live & (want["status"] == 0))[:, None], tol, 0.0)  # others are exactly 0
+        _close(got, wanted, tol, "grad")
+    return want
+
+
+SIZES = [1, 2, 3, 7, 16, 63, 64, 65, 84, 127, 128, 129, 255, 257, 511, 1000, 1024, 1025, 2047, 3000,
+         4097, 8191, 16385, 32003, 50021]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("V", SIZES)
+def test_sizes(V, dtype):
+    torch = _torch()
+    rng = np.random.default_rng(V)
+    N = 37 if V < 3000 else 5
+    x, x64 = _logits(rng, (N, V), dtype)
+    targets = torch.from_numpy(rng.integers(0, V, N)).cuda()
+    targets[1] = -1
+    for top in sorted({0, 1, min(5, V), min(20, V), min(64, V)}):
+        r = binding.lfmmi_token_logprobs(x, targets, top_k=top)
+        check(x, x64, targets, None, 1.0, top, r, grad_too=top == 0)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,V", [(1, 32000), (1, 131072), (2, 100003), (16, 65537), (1, 5000), (3, 9)])
+def test_few_rows_of_many(rows, V, dtype):
+    torch = _torch()
+    rng = np.random.default_rng(V + rows)
+    x, x64 = _logits(rng, (rows, V), dtype)
+    top = min(64, V)
+    r = binding.lfmmi_token_logprobs(x, None, top_k=top, scale=1.25)
+    check(x, x64, None, None, 1.25, top, r)
+    targets = torch.from_numpy(rng.integers(0, V, rows).astype(np.int32)).cuda()
+    r = binding.lfmmi_token_logprobs(x, targets, top_k=min(8, V))
+    check(x, x64, targets, None, 1.0, min(8, V), r)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("V,pad,skip", [(84, 12, 0), (500, 3, 1), (3001, 61, 2), (9001, 7, 3)])
+def test_views_of_larger_tensors(V, pad, skip, dtype):
+    # rows that start anywhere, batches that do not follow each other; what lies around the
+    # view is NaN
+    torch = _torch()
+    rng = np.random.default_rng(V)
+    B, T = 3, 5
+    base = torch.full((B, T + 2, V + pad + skip), float("nan"), dtype=_dtype(dtype), device="cuda")
+    x = base[:, 1:T + 1, skip:skip + V]
+    x.copy_(torch.from_numpy(rng.normal(0, 2, (B, T, V)).astype(np.float32)))
+    targets = torch.from_numpy(rng.integers(0, V, (B, T))).cuda()
+    r = binding.lfmmi_token_logprobs(x, targets, top_k=7, scale=0.7)
+    check(x, x.double().cpu().numpy(), targets, None, 0.7, 7, r)
+    # one row for all frames
+    e = x[:, :1].expand(B, T, V)
+    r = binding.lfmmi_token_logprobs(e, targets, top_k=3)
+    check(e, e.double().cpu().numpy(), targets, None, 1.0, 3, r)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("B,T,V", [(7, 23, 84), (5, 11, 3000), (300, 4, 40), (513, 3, 1030), (2, 3, 20000)])
+def test_lengths_and_rows_that_are_not_scored(B, T, V, dtype):
+    torch = _torch()
+    rng = np.random.default_rng(B)
+    x, _ = _logits(rng, (B, T, V), dtype)
+    lengths = rng.integers(0, T + 1, B).astype(np.int32)
+    lengths[0], lengths[-1] = 0, T
+    targets = rng.integers(0, V, (B, T))
+    targets[rng.random((B, T)) < 0.3] = -100
+    for b in range(B):  # never read
+        x[b, int(lengths[b]):] = float("nan")
+    x[torch.from_numpy(targets < 0).cuda()] = float("nan")
+    x64 = x.double().cpu().numpy()
+    td = torch.from_numpy(targets).cuda()
+    r = binding.lfmmi_token_logprobs(x, td, lengths, top_k=4)
+    check(x, x64, td, lengths, 1.0, 4, r)
+    r = binding.lfmmi_token_logprobs(torch.nan_to_num(x), None, lengths, top_k=4)
+    check(torch.nan_to_num(x), np.nan_to_num(x64), None, lengths, 1.0, 4, r)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("V", [5, 84, 640, 3000, 40000])
+def test_masks_infinities_and_ties(V, dtype):
+    torch = _torch()
+    rng = np.random.default_rng(V)
+    lowest = float(torch.finfo(_dtype(dtype)).min)
+    inf, nan = float("inf"), float("nan")
+    x, _ = _logits(rng, (24, V), dtype)
+    targets = rng.integers(0, V, 24)
+    x[0] = -inf                      # nothing left
+    x[1] = lowest                    # a mask of the lowest value everywhere: uniform
+    x[2] = -inf
+    x[2, V - 1] = 3.0                # one token left
+    targets[2] = V - 1
+    x[3] = -inf
+    x[3, 0] = lowest                 # the one that is left is the lowest value
+    targets[3] = 0
+    x[4, ::2] = -inf                 # a target that the mask takes out
+    targets[4] = 0
+    x[5, ::2] = lowest
+    x[6, V // 2] = nan
+    x[7, V // 2] = inf
+    x[8] = 1.25                      # ties everywhere
+    x[9] = 0.0
+    x[9, ::2] = -0.0                 # the same number
+    x[10] = torch.linspace(-4, 4, V).to(x.dtype)
+    x[11] = torch.linspace(4, -4, V).to(x.dtype)
+    x[12] = -inf
+    x[13] = (torch.arange(V) % 3).to(x.dtype)
+    x[14, 0] = inf
+    x[15] = -inf
+    x[15, :2] = torch.tensor([nan, 1.0]).to(x.dtype)
+    x[16] = 60000.0                  # far from 0
+    x[16, V // 3] = 60032.0
+    x[17] = lowest
+    x[17, V // 2] = -lowest          # a difference that overflows
+    targets[18] = V                  # out of range
+    targets[19] = V + 12345678901
+    targets[20] = -1
+    x[20] = nan
+    targets[21] = V + 7
+    x[21] = -inf
+    targets[22] = V + 7
+    x[22] = nan
+    x[23, V // 2:] = -inf
+    x64 = x.double().cpu().numpy()
+    td = torch.from_numpy(targets).cuda()
+    for top in sorted({0, 1, min(V, 5), min(V, 64)}):
+        for scale in (1.0, 0.7):
+            r = binding.lfmmi_token_logprobs(x, td, top_k=top, scale=scale)
+            check(x, x64, td, None, scale, top, r, grad_too=top == 0)
+
+
+@pytest.mark.parametrize("V", [700, 20000, 100000])
+def test_many_large_values_in_few_columns(V):
+    # the best values crowd where one thread of a workgroup reads, in many ways
+    torch = _torch()
+    rng = np.random.default_rng(V)
+    x, _ = _logits(rng, (48, V), "bfloat16")
+    for n in range(48):
+        step = 1 << (n % 16)
+        width = 1 + n // 16 * 8
+        for a in range((n * 37) % step, V, step):
+            if a // step > 600:
+                break
+            x[n, a:a + width] += 20.0
+    x64 = x.double().cpu().numpy()
+    for top in (1, 20, 64):
+        check(x, x64, None, None, 1.0, top, binding.lfmmi_token_logprobs(x, None, top_k=top), grad_too=False)
+
+
+@pytest.mark.parametrize("scale", [1e-6, 0.05, 3.0, 1000.0, 1e6])
+def test_scales(scale):
+    rng = np.random.default_rng(5)
+    x, x64 = _logits(rng, (6, 777), "float32")
+    torch = _torch()
+    targets = torch.from_numpy(rng.integers(0, 777, 6)).cuda()
+    f = float(np.float32(scale))
+    r = binding.lfmmi_token_logprobs(x, targets, top_k=3, scale=scale)
+    want = oracle.rows(x64, targets.cpu().numpy(), np.ones(6, bool), f, 3)
+    d = want["logp"] + want["logs"]
+    _close(r.logp, want["logp"], oracle.bound_logp(777, want["logp"], d), "logp")
+    _close(r.entropy, want["entropy"], oracle.bound_entropy(777), "entropy")
+    assert np.array_equal(r.top_id.cpu().numpy(), want["top_id"])
+
+
+def test_gradient_against_differences():
+    # the loss in 64 bits at x + e v and x - e v; e = 1e-5: the difference is off by e^2 times
+    # the third derivative (of order 1) and 1e-16 / e by rounding, 1e-9 together
+    torch = _torch()
+    rng = np.random.default_rng(11)
+    for V in (5, 84, 1500):
+        x, x64 = _logits(rng, (9, V), "float32")
+        targets = torch.from_numpy(rng.integers(0, V, 9)).cuda()
+        t = targets.cpu().numpy()
+        g, h = rng.normal(0, 1, 9).astype(np.float32), rng.normal(0, 1, 9).astype(np.float32)
+        scale = 0.75
+        r = binding.lfmmi_token_logprobs(x, targets, scale=scale)
+        grad = binding.lfmmi_token_logprobs_backward(
+            x, targets, r.stats, r.entropy, torch.from_numpy(g).cuda(), torch.from_numpy(h).cuda(),
+            scale=scale).double().cpu().numpy()
+        want = oracle.rows(x64, t, np.ones(9, bool), scale, 0)
+        formula = oracle.grads(want, t, np.ones(9, bool), scale, g, h)
+        tol = oracle.bound_grad(want, t, scale, g.astype(np.float64), h.astype(np.float64), formula, "float32")
+        for _ in range(3):
+            v = rng.normal(0, 1, x64.shape)
+            e = 1e-5
+            diff = (oracle.loss(x64 + e * v, t, scale, g, h) - oracle.loss(x64 - e * v, t, scale, g, h)) / (2 * e)
+            assert abs((formula * v).sum() - diff) <= 1e-7 * V
+            assert abs((grad * v).sum() - diff) <= (tol * np.abs(v)).sum() + 1e-7 * V
+
+
+def test_backward_in_place():
+    torch = _torch()
+    rng = np.random.default_rng(2)
+    for V in (84, 1000, 30001):
+        x, _ = _logits(rng, (4, 3, V), "bfloat16")
+        targets = torch.from_numpy(rng.integers(0, V, (4, 3))).cuda()
+        g = torch.randn((4, 3), device="cuda")
+        r = binding.lfmmi_token_logprobs(x, targets)
+        want = binding.lfmmi_token_logprobs_backward(x, targets, r.stats, r.entropy, g, g)
+        got = binding.lfmmi_token_logprobs_backward(x, targets, r.stats, r.entropy, g, g, grad=x)
+        assert got.data_ptr() == x.data_ptr() and torch.equal(got, want)
+    with pytest.raises(binding.LfmmiError):  # over logits that are not contiguous
+        base = torch.zeros((4, 3, 100), device="cuda")
+        view = base[:, :, :90]
+        out = base.reshape(-1)[:4 * 3 * 90].reshape(4, 3, 90)
+        t = torch.zeros((4, 3), dtype=torch.int64, device="cuda")
+        r = binding.lfmmi_token_logprobs(view, t)
+        binding.lfmmi_token_logprobs_backward(view, t, r.stats, r.entropy, g, grad=out)
+
+
+def test_offsets_beyond_32_bits():
+    torch = _torch()
+    V = 60000
+    base = torch.zeros((40000, V), dtype=torch.bfloat16, device="cuda")  # 2.4e9 values
+    rng = np.random.default_rng(1)
+    at = torch.tensor([0, 1, 35791, 35792, 39999], device="cuda")
+    some, x64 = _logits(rng, (5, V), "bfloat16")
+    base[at] = some
+    targets = torch.full((40000,), -1, dtype=torch.int64, device="cuda")
+    targets[at] = torch.from_numpy(rng.integers(0, V, 5)).cuda()
+    r = binding.lfmmi_token_logprobs(base, targets, top_k=5)
+    picked = binding.TokenLogprobs(*[None if v is None else v[at] for v in r])
+    want = check(some, x64, targets[at], None, 1.0, 5, picked)
+    g = torch.ones(40000, device="cuda")
+    grad = binding.lfmmi_token_logprobs_backward(base, targets, r.stats, r.entropy, g)
+    t = targets[at].cpu().numpy()
+    wanted = oracle.grads(want, t, np.ones(5, bool), 1.0, np.ones(5), np.zeros(5))
+    _close(grad[at], wanted, oracle.bound_grad(want, t, 1.0, np.ones(5), np.zeros(5), wanted, "bfloat16"), "grad")
+    assert float(grad[2:35791].abs().max()) == 0.0
+
+
+def test_empty_calls_and_reused_outputs():
+    torch = _torch()
+    for shape in ((0, 5), (0, 3, 5), (3, 0, 5)):
+        x = torch.zeros(shape, device="cuda")
+        t = torch.zeros(shape[:-1], dtype=torch.int64, device="cuda")
+        r = binding.lfmmi_token_logprobs(x, t, top_k=2)
+        assert r.top_id.shape == shape[:-1] + (2,)
+        assert binding.lfmmi_token_logprobs_backward(x, t, r.stats, r.entropy, r.logp).shape == shape
+    rng = np.random.default_rng(0)
+    x, x64 = _logits(rng, (6, 1234), "float16")
+    t = torch.from_numpy(rng.integers(0, 1234, 6)).cuda()
+    out = binding.lfmmi_token_logprobs(torch.zeros_like(x), t, top_k=9)
+    r = binding.lfmmi_token_logprobs(x, t, top_k=9, out=out)
+    assert all(a is b for a, b in zip(r, out))
+    check(x, x64, t, None, 1.0, 9, r)
+    r = binding.lfmmi_token_logprobs(x, t, entropy=False)
+    assert r.entropy is None
+    with pytest.raises(ValueError):
+        binding.lfmmi_token_logprobs(x, t, top_k=8, out=out)
+
+
+def test_captured_replays_beside_eager_work():
+    # two graphs and eager calls, each with workspaces of its own, replayed at the same time
+    torch = _torch()
+    rng = np.random.default_rng(8)
+    xs = [_logits(rng, (2, 90001), "bfloat16")[0] for _ in range(2)]
+    ts = [torch.from_numpy(rng.integers(0, 90001, 2)).cuda() for _ in range(2)]
+    g = torch.randn(2, device="cuda")
+
+    def both(x, t):
+        r = binding.lfmmi_token_logprobs(x, t, top_k=20)
+        return r, binding.lfmmi_token_logprobs_backward(x, t, r.stats, r.entropy, g, g)
+
+    graphs, outs = [], []
+    for x, t in zip(xs, ts):
+        both(x, t)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            outs.append(both(x, t))
+        graphs.append(graph)
+    side = torch.cuda.Stream()
+    for k in range(3):
+        for x in xs:
+            x.copy_(torch.randn(x.shape, device="cuda") * (1.0 + k))
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            graphs[0].replay()
+        graphs[1].replay()
+        torch.cuda.synchronize()
+        for x, t, (r, grad) in zip(xs, ts, outs):
+            want, wanted = both(x, t)
+            for a, b in zip(r, want):
+                assert torch.equal(a, b)
+            assert torch.equal(grad, wanted)
+
+
+def test_another_stream_and_the_same_bits_every_time():
+    torch = _torch()
+    rng = np.random.default_rng(4)
+    for shape in ((3, 70000), (200, 3000), (500, 84)):
+        x, x64 = _logits(rng, shape, "bfloat16")
+        t = torch.from_numpy(rng.integers(0, shape[1], shape[0])).cuda()
+        want = binding.lfmmi_token_logprobs(x, t, top_k=20)
+        side = torch.cuda.Stream()
+        torch.cuda.synchronize()
+        r = binding.lfmmi_token_logprobs(x, t, top_k=20, stream=side.cuda_stream)
+        side.synchronize()
+        for a, b in zip(r, want):
+            assert torch.equal(a, b)
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            again = [binding.lfmmi_token_logprobs(x, t, top_k=20) for _ in range(8)]
+        here = [binding.lfmmi_token_logprobs(x, t, top_k=20) for _ in range(8)]
+        torch.cuda.synchronize()
+        for r in again + here:
+            for a, b in zip(r, want):
+                assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_autograd(dtype):
+    torch = _torch()
+    rng = np.random.default_rng(6)
+    B, T, V = 4, 9, 321
+    x, x64 = _logits(rng, (B, T, V), dtype)
+    lengths = [9, 0, 4, 7]
+    t = torch.from_numpy(rng.integers(0, V, (B, T))).cuda()
+    leaf = x.clone().requires_grad_()
+    logp, entropy, status = chain.token_logprobs(leaf, t, lengths, scale=0.5)
+    assert not status.requires_grad and int(status.abs().sum()) == 0
+    w = torch.randn((B, T), device="cuda")
+    (logp * w).sum().backward()  # the entropy is not used
+    r = binding.lfmmi_token_logprobs(x, t, lengths, scale=0.5)
+    want = binding.lfmmi_token_logprobs_backward(x, t, r.stats, r.entropy, w, None, lengths, 0.5)
+    assert torch.equal(leaf.grad, want) and torch.equal(logp.detach(), r.logp)
+    leaf.grad = None
+    logp, entropy, _ = chain.token_logprobs(leaf, t, lengths, scale=0.5)
+    (logp.sum() - 0.1 * entropy.sum()).backward()  # gradients of no strides
+    one = torch.ones((B, T), device="cuda")
+    want = binding.lfmmi_token_logprobs_backward(x, t, r.stats, r.entropy, one, -0.1 * one, lengths, 0.5)
+    assert torch.equal(leaf.grad, want)
+    # logits shared by several frames: their gradients add up
+    row = x[:1, :1].float().clone().requires_grad_()
+    logp, _, _ = chain.token_logprobs(row.expand(B, T, V), t)
+    logp.sum().backward()
+    r = oracle.rows(np.repeat(row.detach().double().cpu().numpy().reshape(1, V), B * T, 0),
+                    t.cpu().numpy().reshape(-1), np.ones(B * T, bool), 1.0, 0)
+    args = (r, t.cpu().numpy().reshape(-1), np.ones(B * T, bool), 1.0, np.ones(B * T), np.zeros(B * T))
+    each = oracle.grads(*args)
+    tol = oracle.bound_grad(r, args[1], 1.0, args[4], args[5], each, "float32").sum(0) + \
+        B * T * oracle.U * np.abs(each).sum(0)
+    _close(row.grad.reshape(-1), each.sum(0), tol, "shared")
+
+
+def test_chain_loss_with_an_alignment_and_a_clipped_step():
+    # the sequence loss, frame log probabilities beside it, and the gradients of the layer
+    # in front clipped: as a training step uses them together
+    torch = _torch()
+    wl = workloads.make_workload(1)
+    lengths, leak = wl["lengths"], wl["leak"]
+    den = binding.lfmmi_graph_create(wl["den"])
+    num = binding.lfmmi_graph_create_batch(wl["num"])
+    B, T, P = wl["logits"].shape
+    rng = np.random.default_rng(3)
+    targets = torch.from_numpy(rng.integers(-1, P, (B, T))).cuda()
+    hidden = torch.randn((B, T, 12), device="cuda")
+    weight = (torch.randn((P, 12), device="cuda") * 0.3).requires_grad_()
+    bias = torch.zeros(P, device="cuda", requires_grad=True)
+    logits = torch.nn.functional.linear(hidden, weight, bias)
+    loss = chain.chain_loss(logits, lengths, num, den, leak, targets, 0.2)
+    x = logits.detach().requires_grad_()
+    objective = chain.chain_loss(x, lengths, num, den, leak)
+    objective.backward()
+    live = _live(B, T, targets.cpu().numpy(), lengths)
+    t64 = targets.cpu().numpy().reshape(-1)
+    r = oracle.rows(x.detach().double().cpu().numpy().reshape(-1, P), t64, live, 1.0, 0)
+    frames = float(np.sum(lengths))
+    want = float(objective.detach()) - 0.2 * r["logp"].sum() / frames
+    # a sum of B T terms in 32 bits, each as far off as a log probability may be
+    tol = (0.2 * (oracle.bound_logp(P, r["logp"], r["logp"] + r["logs"]).sum() +
+                  B * T * oracle.U * np.abs(r["logp"]).sum()) / frames + 4 * oracle.U * abs(float(objective.detach())) +
+           4 * oracle.U * abs(want))
+    assert abs(float(loss.detach()) - want) <= tol
+    dlogits = x.grad.double().cpu().numpy().reshape(-1, P) + \
+        oracle.grads(r, t64, live, 1.0, np.full(B * T, -0.2 / frames), np.zeros(B * T))
+    loss.backward()
+    dw = dlogits.T @ hidden.double().cpu().numpy().reshape(-1, 12)
+    db = dlogits.sum(0)
+    # sums of B T products in 32 bits of gradients good to 1e-5
+    scale = np.abs(dlogits).sum() * float(hidden.abs().max()) + 1.0
+    assert np.abs(weight.grad.double().cpu().numpy() - dw).max() <= 1e-5 * scale
+    norm64 = float(torch.sqrt(weight.grad.double().square().sum() + bias.grad.double().square().sum()))
+    before = [p.grad.clone() for p in (weight, bias)]
+    norm = chain.clip_grad_norm([weight, bias], 0.5 * norm64)
+    assert abs(float(norm) - norm64) <= 2 * oracle.U * norm64
+    for p, b in zip((weight, bias), before):
+        off = (p.grad.double() - 0.5 * b.double()).abs()
+        assert bool((off <= 4 * oracle.U * b.double().abs() + 1e-37).all())
+    assert np.abs(before[1].double().cpu().numpy() - db).max() <= 1e-5 * scale
+    den.close()
+    num.close()
