@@ -204,7 +204,7 @@ lfmmi_status lfmmi_token_logprobs_workspace(int32_t dtype, int32_t B, int32_t T,
     if (!known(dtype) || B < 0 || T < 0 || V < 1 || top_k < 0 || top_k > kMaxTop || top_k > V)
         return fail(LFMMI_ERR_INVALID_ARG, "unknown dtype, or a size out of range");
     if ((int64_t)B * T > INT32_MAX) return fail(LFMMI_ERR_UNSUPPORTED, "B * T exceeds 2^31 - 1");
-    *bytes = (int64_t)token_workspace(dtype, (int64_t)B * T, V, top_k);
+    *bytes = B > 0 && T > 0 ? (int64_t)plan_tokens((int64_t)B * T, V, top_k).workspace : 0;
     return LFMMI_OK;
 }
 
@@ -223,8 +223,9 @@ try {
     if (top_k > kMaxTop) return fail(LFMMI_ERR_UNSUPPORTED, "top_k exceeds LFMMI_MAX_TOP");
     if (logp && !targets) return fail(LFMMI_ERR_INVALID_ARG, "logp without targets");
     if (B == 0 || T == 0) return LFMMI_OK;
-    const size_t need = token_workspace(dtype, (int64_t)B * T, V, top_k);
-    if (need > 0 && (!workspace || !aligned(workspace, 16) || workspace_bytes < (int64_t)need))
+    const TokenPlan plan = plan_tokens((int64_t)B * T, V, top_k);
+    if (plan.workspace > 0 &&
+        (!workspace || !aligned(workspace, 16) || workspace_bytes < (int64_t)plan.workspace))
         return fail(LFMMI_ERR_INVALID_ARG, "workspace is null, too small or not aligned to 16 bytes");
     const int64_t size = (int64_t)dtype_size(dtype);
     for (int32_t b = 0; b < B;) {
@@ -248,6 +249,8 @@ try {
         p.top_id = at(top_id, row * top_k);
         p.top_logp = at(top_logp, row * top_k);
         p.status = at(status, row);
+        p.parts = plan.parts;
+        p.part_size = plan.part_size;
         p.workspace = workspace;
         const hipError_t e =
             launch_token_logprobs(p, lens, dtype, static_cast<hipStream_t>(hip_stream));

@@ -31,8 +31,17 @@ struct TokenParams {
     int32_t* top_id;      // [B, T, top_k]
     float* top_logp;
     int32_t* status;
+    int32_t parts, part_size;  // a row's logits are cut into `parts` parts of part_size
     void* workspace;
 };
+
+// How a call's rows are cut, and the bytes of workspace that takes.
+constexpr int kMaxParts = 64;
+struct TokenPlan {
+    int32_t parts, part_size;
+    size_t workspace;
+};
+TokenPlan plan_tokens(int64_t rows, int V, int top_k);
 
 struct TokenGradParams {
     const void* x;
@@ -46,12 +55,12 @@ struct TokenGradParams {
     const float* grad_logp;     // or null
     const float* grad_entropy;  // or null
     void* grad;                 // [B, T, V] contiguous
+    int32_t pieces, piece;      // how a row is cut (set by the launch)
 };
 
 // dtype: lfmmi_dtype
 hipError_t launch_token_logprobs(const TokenParams& p, const SeqLengths& lens, int dtype,
                                  hipStream_t stream);
-size_t token_workspace(int dtype, int64_t rows, int V, int top_k);
 hipError_t launch_token_grad(const TokenGradParams& p, const SeqLengths& lens, int dtype,
                              hipStream_t stream);
 

@@ -480,3 +480,25 @@ def test_chain_loss_with_an_alignment_and_a_clipped_step():
     assert np.abs(before[1].double().cpu().numpy() - db).max() <= 1e-5 * scale
     den.close()
     num.close()
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+@pytest.mark.parametrize("rows,V", [(3, 3500), (600, 9000), (2, 120000)])
+def test_one_thread_holds_all_the_large_values(rows, V, dtype):
+    # twenty runs of 16 bytes in every stretch of 64 or 256 of them are large everywhere: they
+    # belong to 20 threads, all of whose values are better than any of the others'
+    rng = np.random.default_rng(V)
+    x, _ = _logits(rng, (rows, V), dtype, sigma=1.0)
+    torch = _torch()
+    per = 8 if dtype == "bfloat16" else 4
+    chunk = torch.arange(V, device="cuda") // per
+    x += torch.where(chunk % 64 < 20, 30.0, 0.0).to(x.dtype)
+    some = x[:: max(1, rows // 3)][:3]
+    r = binding.lfmmi_token_logprobs(x, None, top_k=64)
+    picked = binding.TokenLogprobs(*[None if v is None else v[:: max(1, rows // 3)][:3] for v in r])
+    check(some, some.double().cpu().numpy(), None, None, 1.0, 64, picked, grad_too=False)
+    x += torch.where((chunk % 256 < 20) | (chunk % 64 >= 20), 0.0, -30.0).to(x.dtype)
+    some = x[:: max(1, rows // 3)][:3]
+    r = binding.lfmmi_token_logprobs(x, None, top_k=64)
+    picked = binding.TokenLogprobs(*[None if v is None else v[:: max(1, rows // 3)][:3] for v in r])
+    check(some, some.double().cpu().numpy(), None, None, 1.0, 64, picked, grad_too=False)
