@@ -9,7 +9,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "liblfmmi.so")
 SOURCES = ["kernels.hip", "line.hip", "hybrid.hip", "tokens.hip", "grads.hip", "api.cpp", "operators.cpp",
            "pack.cpp"]
-HEADERS = ["kernels.h", "device.h", "operators.h", "pack.h", "status.h", "microbench.hip", os.path.join("..", "..", "include", "lfmmi.h")]
+HEADERS = ["kernels.h", "device.h", "operators.h", "pack.h", "status.h", "vec16.h", "microbench.hip",
+           os.path.join("..", "..", "include", "lfmmi.h")]
 
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
