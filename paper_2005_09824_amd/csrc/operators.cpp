@@ -16,6 +16,8 @@ static_assert(LFMMI_MAX_TOP == kMaxTop, "the header states the limit");
 
 namespace {
 
+constexpr int64_t kCacheBytes = (int64_t)256 << 20;  // behind the L2s
+
 size_t dtype_size(int32_t dtype) { return dtype == LFMMI_F32 ? 4 : 2; }
 
 bool known(int32_t dtype) { return dtype == LFMMI_F32 || dtype == LFMMI_BF16 || dtype == LFMMI_F16; }
@@ -249,6 +251,7 @@ try {
         p.top_id = at(top_id, row * top_k);
         p.top_logp = at(top_logp, row * top_k);
         p.status = at(status, row);
+        p.once = (int64_t)B * T * V * size > kCacheBytes;
         p.parts = plan.parts;
         p.part_size = plan.part_size;
         p.workspace = workspace;

@@ -31,6 +31,7 @@ struct TokenParams {
     int32_t* top_id;      // [B, T, top_k]
     float* top_logp;
     int32_t* status;
+    bool once;  // the logits are too many for the caches
     int32_t parts, part_size;  // a row's logits are cut into `parts` parts of part_size
     void* workspace;
 };

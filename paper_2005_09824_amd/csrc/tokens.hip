@@ -12,8 +12,9 @@ namespace {
 constexpr float kLog2e = 1.44269504088896341f;
 constexpr float kLn2 = 0.693147180559945309f;
 constexpr int kThreads = 256;
-constexpr int kWaves = kThreads / 64;
 constexpr int kLoads = 4;  // 16-byte loads that a lane has in flight
+
+constexpr int threads_of(int lanes) { return lanes > kThreads ? lanes : kThreads; }
 
 // 2^y as the hardware has it: results below the normal range are 0, which sums beside 1
 // do not notice.
@@ -28,6 +29,14 @@ __device__ __forceinline__ float max3(float a, float b, float c)
     return r;
 }
 
+// What is the same in every lane of a wave, held once.
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ uint64_t uniform(uint64_t v)
+{
+    return (uint64_t)uniform((uint32_t)(v >> 32)) << 32 | uniform((uint32_t)v);
+}
+__device__ __forceinline__ float uniform(float v) { return __uint_as_float(uniform(__float_as_uint(v))); }
+
 // ---- reductions over G lanes: 16 (a DPP row) or 64 (a wave); every lane has the result
 
 template <int Ror>
@@ -40,6 +49,23 @@ __device__ __forceinline__ float lane_of(float v, int lane)
 {
     return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane));
 }
+__device__ __forceinline__ uint32_t all_bits(uint32_t v)  // of a wave, and-ed
+{
+#define LFMMI_ROR(n) __builtin_amdgcn_update_dpp(v, v, 0x120 + n, 0xf, 0xf, true)
+    v &= LFMMI_ROR(8);
+    v &= LFMMI_ROR(4);
+    v &= LFMMI_ROR(2);
+    v &= LFMMI_ROR(1);
+#undef LFMMI_ROR
+    return (uint32_t)__builtin_amdgcn_readlane(v, 0) & (uint32_t)__builtin_amdgcn_readlane(v, 16) &
+           (uint32_t)__builtin_amdgcn_readlane(v, 32) & (uint32_t)__builtin_amdgcn_readlane(v, 48);
+}
+__device__ __forceinline__ uint32_t max_of_four(uint32_t v)  // lanes next to each other
+{
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(v, v, 0xb1, 0xf, 0xf, true));
+    return max(v, (uint32_t)__builtin_amdgcn_update_dpp(v, v, 0x4e, 0xf, 0xf, true));
+}
+
 template <int G>
 __device__ __forceinline__ float sum_over(float v)
 {
@@ -95,46 +121,33 @@ __device__ __forceinline__ void join_lanes(Sums& a, float scale2)
     a.u = sum_over<G>(a.u);
 }
 
-template <bool Ent>
-__device__ __forceinline__ void add(Sums& a, float x, float scale2)
-{
-    const float y = (x - a.m) * scale2, e = exp2_of(y);
-    a.s += e;
-    if (Ent) a.u += e * finite(y);
-}
-
-// Values in an order of whole numbers, equal ones (-0 and 0 are) by index, lowest first. No
-// value has key 0.
-__device__ __forceinline__ uint64_t key_of(float x, int i)
+// Values in an order of whole numbers (-0 and 0 are equal); no value is 0, and -inf is kLowest.
+constexpr uint32_t kLowest = 0x007fffffu;
+__device__ __forceinline__ uint32_t ordered(float x)
 {
     const uint32_t b = __float_as_uint(x + 0.f);
-    const uint32_t v = b >> 31 ? ~b : b | 0x80000000u;
-    return (uint64_t)v << 32 | (uint32_t)~i;
+    return b >> 31 ? ~b : b | 0x80000000u;
 }
-__device__ __forceinline__ int index_of(uint64_t key) { return (int)~(uint32_t)key; }
-__device__ __forceinline__ float value_of(uint64_t key)
-{
-    const uint32_t v = (uint32_t)(key >> 32);
-    return __uint_as_float(v >> 31 ? v & 0x7fffffffu : ~v);
-}
+__device__ __forceinline__ float value_of(uint32_t v) { return __uint_as_float(v >> 31 ? v & 0x7fffffffu : ~v); }
+
+// A value and its index as one whole number: equal values by index, lowest first.
+__device__ __forceinline__ uint64_t key_of(float x, int i) { return (uint64_t)ordered(x) << 32 | (uint32_t)~i; }
 
 struct Row {
     bool live;
-    int64_t target;  // -1: none given
+    int target;  // -1: none, V: one that is not below V
 };
 
-template <typename P>
-__device__ __forceinline__ Row row_of(const P& p, const SeqLengths& lens, int b, int t)
+// G: the lanes that take the row together.
+template <int G, typename P>
+__device__ __forceinline__ Row row_of(const P& p, const SeqLengths& lens, uint32_t row)
 {
-    Row r{true, -1};
-    if (lens.n > 0 && t >= lens.T[b]) return {false, -1};
-    if (p.targets) {
-        const int64_t at = (int64_t)b * p.T + t;
-        r.target = p.target_bytes == 8 ? static_cast<const int64_t*>(p.targets)[at]
-                                       : static_cast<const int32_t*>(p.targets)[at];
-        r.live = r.target >= 0;
-    }
-    return r;
+    if (lens.n > 0 && (int)(row % p.T) >= lens.T[row / p.T]) return {false, -1};
+    if (!p.targets) return {true, -1};
+    int64_t target = p.target_bytes == 8 ? static_cast<const int64_t*>(p.targets)[row]
+                                         : static_cast<const int32_t*>(p.targets)[row];
+    if (G >= 64) target = (int64_t)uniform((uint64_t)target);
+    return {target >= 0, target < 0 ? -1 : target < p.V ? (int)target : p.V};
 }
 
 // What a row's alternatives need to know of it. m: NaN for a row with a NaN or +inf logit,
@@ -187,117 +200,180 @@ __device__ __forceinline__ void write_top(const TokenParams& p, int64_t row, int
                                           Scores c)
 {
     const int64_t at = row * p.top_k + k;
-    if (p.top_id) p.top_id[at] = live && !(c.m != c.m) ? index_of(key) : -1;
+    if (p.top_id) p.top_id[at] = live && !(c.m != c.m) ? (int)~(uint32_t)key : -1;
     if (p.top_logp)
-        p.top_logp[at] =
-            !live ? 0.f : c.m == -INFINITY ? -INFINITY : (value_of(key) - c.m) * p.scale - c.logs;
+        p.top_logp[at] = !live ? 0.f : c.m == -INFINITY ? -INFINITY
+                                                        : (value_of((uint32_t)(key >> 32)) - c.m) * p.scale - c.logs;
 }
 
 // ---- one pass over n logits by G lanes
 
-// Chunks of 16 bytes go round the lanes; a lane takes kLoads of them at a time. `best` is the
-// largest value a lane met in whole chunks (-inf to begin with), `best_at` the first group of
-// kLoads chunks that held it.
+// Chunks of 16 bytes go round the lanes; a lane takes a group of kLoads of them at a time.
+// `first`: the largest value a lane met in whole chunks (-inf to begin with), `group` the first
+// group that held it, `second` the largest of the other groups.
 struct Best {
-    float value;
+    float first, second;
     int group;
 };
 
-template <typename D, int G>
-__device__ __forceinline__ void load_group(const typename D::Store* x, int full, int q, uint4* r)
+__device__ __forceinline__ void take(Best& best, float top, int group)
 {
-    if (__builtin_expect(q - (q & (G - 1)) + kLoads * G <= full, 1)) {
+    if (top > best.first) best.group = group;
+    best.second = __builtin_amdgcn_fmed3f(best.first, best.second, top);
+    best.first = fmaxf(best.first, top);
+}
+
+template <typename D, int G>
+__device__ __forceinline__ void load_part(const typename D::Store* x, int full, int q, uint4* r)
+{
 #pragma unroll
-        for (int k = 0; k < kLoads; ++k) r[k] = load16(x + (int64_t)(q + k * G) * D::kVec);
-    } else {
-#pragma unroll
-        for (int k = 0; k < kLoads; ++k) {
-            r[k] = make_uint4(D::kNone, D::kNone, D::kNone, D::kNone);
-            if (q + k * G < full) r[k] = load16(x + (int64_t)(q + k * G) * D::kVec);
-        }
+    for (int k = 0; k < kLoads; ++k) {
+        r[k] = make_uint4(D::kNone, D::kNone, D::kNone, D::kNone);
+        if (q + k * G < full) r[k] = load16(x + (int64_t)(q + k * G) * D::kVec);
     }
 }
 
-// Per logit of 16 bits: half an instruction for the maximum, one to unpack it, two for y, four
-// issue slots for 2^y, one for each sum and one for the clamp.
-template <typename D, int G, bool Ent, bool Top>
-__device__ __forceinline__ void scan(const typename D::Store* x, int n, int lane, float scale2, Sums& a,
-                                     Best& best)
+template <int N>
+__device__ __forceinline__ float max_of(const float (&f)[N])
 {
-    constexpr int N = D::kVec * kLoads;
-    const int full = n / D::kVec;
-    for (int q = lane, j = 0; q - lane < full; q += kLoads * G, ++j) {
+    float top = max3(f[0], f[1], f[2]);
+#pragma unroll
+    for (int i = 3; i + 1 < N; i += 2) top = max3(top, f[i], f[i + 1]);
+    return N % 2 ? top : fmaxf(top, f[N - 1]);
+}
+
+// Adds logits of any kind; a.m is their largest at least.
+template <int N>
+__device__ __forceinline__ void add_any(Sums& a, const float (&f)[N], float scale2)
+{
+    float s[4] = {a.s, 0.f, 0.f, 0.f}, u[4] = {a.u, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const float y = (f[i] - a.m) * scale2, e = exp2_of(y);
+        s[i & 3] += e;
+        u[i & 3] += e * finite(y);
+    }
+    a.s = (s[0] + s[1]) + (s[2] + s[3]);
+    a.u = (u[0] + u[1]) + (u[2] + u[3]);
+}
+
+// The same with two operations less for each: y = x scale2 - c, c = m scale2 rounded, in one, and no
+// clamp. What c is off by is taken out of the sums. Not for |m| from 1e30 on, where c overflows, and
+// false, with nothing added, where 0 * -inf has come into u.
+template <int N>
+__device__ __forceinline__ bool add_plain(Sums& a, const float (&f)[N], float scale2)
+{
+    const float c = a.m * scale2, off = fmaf(a.m, scale2, -c);
+    float s[4] = {0.f, 0.f, 0.f, 0.f}, u[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const float y = fmaf(f[i], scale2, -c), e = exp2_of(y);
+        s[i & 3] += e;
+        u[i & 3] = fmaf(e, y, u[i & 3]);
+    }
+    float sum = (s[0] + s[1]) + (s[2] + s[3]);
+    const float usum = (u[0] + u[1]) + (u[2] + u[3]);
+    asm volatile("" : "+v"(sum));  // (added up here: after the branch all 2^y would be held until then)
+    if (__builtin_amdgcn_ballot_w64(usum != usum)) return false;
+    const float back = 1.f - off * kLn2;  // 2^-off: off is below 2^-24 of c
+    a.s = fmaf(sum, back, a.s);
+    a.u = fmaf(usum - off * sum, back, a.u);
+    return true;
+}
+
+// Per logit of 16 bits: half an instruction for the maximum, one to unpack it, one for y, four
+// issue slots for 2^y, one for each sum. `once`: the loads leave nothing in the caches.
+template <typename D, int G, bool Top>
+__device__ __forceinline__ void scan(const typename D::Store* x, int n, int lane, float scale2, bool once,
+                                     Sums& a, Best& best)
+{
+    constexpr int kVec = D::kVec, N = kVec * kLoads;
+    const int full = n / kVec;
+    int q = lane, j = 0;
+    bool plain = true;  // until logits are met that add_plain does not take
+    for (; G > 16 && q - lane + kLoads * G <= full; q += kLoads * G, ++j) {
         uint4 r[kLoads];
-        load_group<D, G>(x, full, q, r);
+        if (once) {
+#pragma unroll
+            for (int k = 0; k < kLoads; ++k) r[k] = load16_once(x + (int64_t)(q + k * G) * kVec);
+        } else {
+#pragma unroll
+            for (int k = 0; k < kLoads; ++k) r[k] = load16(x + (int64_t)(q + k * G) * kVec);
+        }
         float f[N];
 #pragma unroll
-        for (int k = 0; k < kLoads; ++k) D::unpack(r[k], f + k * D::kVec);
-        float top = max3(f[0], f[1], f[2]);
-#pragma unroll
-        for (int i = 3; i + 1 < N; i += 2) top = max3(top, f[i], f[i + 1]);
-        if (N % 2 == 0) top = max3(top, f[N - 1], f[N - 1]);
-        if (Top && top > best.value) best = {top, j};
+        for (int k = 0; k < kLoads; ++k) D::unpack(r[k], f + k * kVec);
+        const float top = max_of(f);
+        if (Top) take(best, top, j);
         shift(a, fmaxf(a.m, top), scale2);
-        float s[4] = {a.s, 0.f, 0.f, 0.f}, u[4] = {a.u, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const float y = (f[i] - a.m) * scale2, e = exp2_of(y);
-            s[i & 3] += e;
-            if (Ent) u[i & 3] += e * finite(y);
-        }
-        a.s = (s[0] + s[1]) + (s[2] + s[3]);
-        a.u = (u[0] + u[1]) + (u[2] + u[3]);
+        plain = plain && !__builtin_amdgcn_ballot_w64(!(fabsf(a.m) < 1e30f));
+        if (plain) plain = add_plain(a, f, scale2);
+        if (!plain) add_any(a, f, scale2);
     }
-    for (int i = full * D::kVec + lane; i < n; i += G) {
-        const float v = D::load(x + i);
-        shift(a, fmaxf(a.m, v), scale2);
-        add<Ent>(a, v, scale2);
+    if (q - lane < full) {  // what is left of a group, chunk by chunk
+        uint4 r[kLoads];
+        load_part<D, G>(x, full, q, r);
+        float most = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < kLoads; ++k) {
+            if (q - lane + k * G >= full) break;
+            float f[kVec];
+            D::unpack(r[k], f);
+            const float top = max_of(f);
+            most = fmaxf(most, top);
+            shift(a, fmaxf(a.m, top), scale2);
+            add_any(a, f, scale2);
+        }
+        if (Top) take(best, most, j);
+    }
+    for (int i = full * kVec + lane; i < n; i += G) {
+        const float f[1] = {D::load(x + i)};
+        shift(a, fmaxf(a.m, f[0]), scale2);
+        add_any(a, f, scale2);
     }
 }
 
 // ---- the best alternatives
 //
-// The k-th largest of the lanes' own largest keys is a lower bound T of the k-th largest key
-// of the row, and every key from T on lies with one of the k lanes whose own largest is from T
-// on. So one pass finds a lane's largest value, and only k lanes' logits are looked at
-// again, from the cache, by all lanes together; rarely many more than k of them reach T. Those
-// are put in order by counting, for each, how many are larger.
+// The k-th largest, T, of the lanes' own largest values is a lower bound of the k-th largest
+// value of the row, and rarely many more than k values reach it. They lie with the lanes whose
+// largest does, in the group of chunks that the lane has noted, and anywhere with a lane whose second
+// group does too: so one pass finds T, and few chunks are looked at again. What reaches T is put in
+// order by counting, for each, how many are larger. Where more than kTies lanes over k reach T
+// (masked rows, equal logits), or more values than the list holds, T gets an index as well.
+constexpr int kTies = 32;
 
-// The key of a lane's largest value in whole chunks: the group that held it is read again for the
-// lowest index. 0 for a lane that had no chunk.
-template <typename D, int G>
-__device__ __forceinline__ uint64_t best_key(const typename D::Store* x, int n, int lane, const Best& best,
-                                             int offset)
+// Of the N values that each lane of a wave holds, how many are from `c` on.
+template <int N>
+__device__ __forceinline__ int count_from(const uint32_t (&v)[N], uint32_t c)
 {
-    const int full = n / D::kVec;
-    if (lane >= full) return 0;
-    const int q = best.group * kLoads * G + lane;
-    int at = 0;
+    int count = 0;
 #pragma unroll
-    for (int k = kLoads - 1; k >= 0; --k) {
-        if (q + k * G >= full) continue;
-        float f[D::kVec];
-        D::unpack(load16(x + (int64_t)(q + k * G) * D::kVec), f);
-#pragma unroll
-        for (int i = D::kVec - 1; i >= 0; --i)
-            if (f[i] == best.value) at = (q + k * G) * D::kVec + i;
-    }
-    return key_of(best.value, offset + at);
+    for (int i = 0; i < N; ++i) count += __builtin_popcountll(__builtin_amdgcn_ballot_w64(v[i] >= c));
+    return count;
 }
 
-// By a wave whose lanes hold N keys each: the k-th largest of the keys that are not 0 (keys are
-// different but for 0), or a lower bound of it with no key between; 0 if there are fewer.
+// The k-th largest of them, or a lower bound of it with exactly k values from there on; 0 if fewer
+// than k are not 0. Bit by bit from the highest, bits in which no two values differ left out.
 template <int N>
-__device__ __forceinline__ uint64_t kth_key(const uint64_t (&key)[N], int k)
+__device__ __forceinline__ uint32_t kth_value(const uint32_t (&v)[N], int k)
 {
-    uint64_t t = 0;
-    for (int bit = 63; bit >= 0; --bit) {
-        const uint64_t c = t | (uint64_t)1 << bit;
-        int count = 0;
+    uint32_t all = v[0], none = ~v[0];
 #pragma unroll
-        for (int i = 0; i < N; ++i) count += __popcll(__ballot(key[i] >= c));
-        if (count >= k) t = c;
-        if (count == k) break;
+    for (int i = 1; i < N; ++i) {
+        all &= v[i];
+        none &= ~v[i];
+    }
+    uint32_t t = all_bits(all), open = ~(t | all_bits(none));
+    if (t == 0 && count_from(v, 1) < k) return 0;
+    for (int count = 64 * N; open && count != k;) {
+        const uint32_t bit = 0x80000000u >> __builtin_clz(open);
+        const int above = count_from(v, t | bit);
+        open ^= bit;
+        if (above >= k) {
+            t |= bit;
+            count = above;
+        }
     }
     return t;
 }
@@ -305,11 +381,11 @@ __device__ __forceinline__ uint64_t kth_key(const uint64_t (&key)[N], int k)
 // LDS of one row's selection.
 template <int G>
 struct Selection {
-    static constexpr int kCap = G == 64 ? 512 : 1024;  // keys from T on that it holds
+    static constexpr int kCap = G == 64 ? 512 : 1024;  // keys that it holds
+    static constexpr int kBins = G == 64 ? 1 : 256;
     uint64_t list[kCap];
-    int lanes[kMaxTop];
-    int num_lanes, count;
-    uint64_t from;  // T
+    uint32_t bins[kBins];
+    int count;
 };
 
 template <int G>
@@ -324,6 +400,29 @@ __device__ __forceinline__ void row_sync()
     }
 }
 
+// A value for each lane, to be read as each wave's share of all: with more than 256 lanes the
+// largest of four.
+template <int G>
+__device__ __forceinline__ void put_bin(Selection<G>& sel, int lane, uint32_t v)
+{
+    if (G == 256) {
+        sel.bins[lane] = v;
+    } else if (G == 1024) {
+        v = max_of_four(v);
+        if (lane % 4 == 0) sel.bins[lane / 4] = v;
+    }
+}
+template <int G, int N>
+__device__ __forceinline__ void get_bins(const Selection<G>& sel, int lane, uint32_t own, uint32_t (&v)[N])
+{
+    if (G == 64) {
+        v[0] = own;
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = sel.bins[lane % 64 + 64 * i];
+    }
+}
+
 template <int G>
 __device__ __forceinline__ void push(Selection<G>& sel, uint64_t key)
 {
@@ -331,77 +430,128 @@ __device__ __forceinline__ void push(Selection<G>& sel, uint64_t key)
     if (at < Selection<G>::kCap) sel.list[at] = key;
 }
 
-// From T and the lanes that reach it to the list of all keys that do.
+// What the search for the values that reach (T, `last`) takes: larger ones, and equal ones
+// of an index up to `last`. Indices count from the first of the n logits, keys from `offset`.
+struct Bound {
+    uint32_t value;
+    int last, offset;
+};
+
 template <typename D, int G>
-__device__ __forceinline__ void gather(const typename D::Store* x, int n, int lane, int offset, Selection<G>& sel)
+__device__ __forceinline__ void push_chunk(const typename D::Store* x, int q, const Bound& to, Selection<G>& sel)
 {
-    const int full = n / D::kVec, lanes = sel.num_lanes;
-    const uint64_t from = sel.from;
-    // (T need not be a key: below that of -inf its bits are no number's)
-    const float least = (uint32_t)(from >> 32) <= 0x007fffffu ? -INFINITY : value_of(from);
-    const int deep = (full + G - 1) / G;  // chunks a lane has at most
-    for (int w = lane; w < lanes * deep; w += G) {
-        const int q = w / lanes * G + sel.lanes[w % lanes];
-        if (q >= full) continue;
-        float f[D::kVec];
-        D::unpack(load16(x + (int64_t)q * D::kVec), f);
+    // (below kLowest a bound's bits are no number's)
+    const float least = to.value <= kLowest ? -INFINITY : value_of(to.value);
+    float f[D::kVec];
+    D::unpack(load16(x + (int64_t)q * D::kVec), f);
 #pragma unroll
-        for (int i = 0; i < D::kVec; ++i)
-            if (f[i] >= least) {
-                const uint64_t key = key_of(f[i], offset + q * D::kVec + i);
-                if (key >= from) push(sel, key);
-            }
-    }
-    for (int i = full * D::kVec + lane; i < n; i += G) {
-        const uint64_t key = key_of(D::load(x + i), offset + i);
-        if (key >= from) push(sel, key);
+    for (int i = 0; i < D::kVec; ++i) {
+        const int at = q * D::kVec + i;
+        if (f[i] >= least && (ordered(f[i]) > to.value || at <= to.last))
+            push(sel, key_of(f[i], to.offset + at));
     }
 }
 
-// The k best of n logits, handed to put(rank, key) by the lane that has one. Key indices start at
-// `offset`. `mine`: this lane's best_key.
+// Each wave looks through what its own lanes have read.
+template <typename D, int G>
+__device__ __forceinline__ void gather(const typename D::Store* x, int n, int lane, const Best& best,
+                                       const Bound& to, Selection<G>& sel)
+{
+    static_assert(kLoads == 4, "four lanes look through a group");
+    constexpr int kVec = D::kVec;
+    const int full = n / kVec, in_wave = lane % 64, base = lane - in_wave;
+    const uint32_t first = ordered(best.first), second = ordered(best.second);
+    const int start = (best.group * kLoads * G + lane) * kVec;  // the lowest index it can have
+    const bool in = lane < full && (first > to.value || (first == to.value && start <= to.last) || to.value == 0);
+    // (if both are equal to T the second one's group comes later)
+    const bool later = first == to.value && (best.group + 1) * kLoads * G * kVec > to.last;
+    const bool deep = in && (second > to.value || (second == to.value && !later) || to.value == 0);
+    const uint64_t some = __builtin_amdgcn_ballot_w64(in && !deep);
+    const int count = __builtin_popcountll(some);
+    const int below = __builtin_popcountll(some & (((uint64_t)1 << in_wave) - 1));
+    // the lanes in question, and behind them the others, in a row
+    const int slot = in && !deep ? below : count + in_wave - below;
+    const int sent = __builtin_amdgcn_ds_permute(slot * 4, best.group << 6 | in_wave);
+    for (int b = 0; b < count; b += 16) {
+        const int from = b + in_wave / 4;
+        const int v = __builtin_amdgcn_ds_bpermute((from & 63) * 4, sent);
+        const int q = ((v >> 6) * kLoads + in_wave % 4) * G + base + (v & 63);
+        if (from < count && q < full) push_chunk<D, G>(x, q, to, sel);
+    }
+    for (uint64_t left = __builtin_amdgcn_ballot_w64(deep); left; left &= left - 1) {
+        const int l = base + __builtin_ctzll(left);
+        for (int q = l + in_wave * G; q < full; q += 64 * G) push_chunk<D, G>(x, q, to, sel);
+    }
+    for (int i = full * kVec + lane; i < n; i += G) {
+        const float v = D::load(x + i);
+        const uint32_t o = ordered(v);
+        if (o > to.value || (o == to.value && i <= to.last)) push(sel, key_of(v, to.offset + i));
+    }
+}
+
+// The index that goes with T: k lanes hold a larger value, or T at an index up to it.
+template <typename D, int G, int N>
+__device__ __forceinline__ int last_index(const typename D::Store* x, int n, int lane, const Best& best,
+                                          uint32_t value, int k, const uint32_t (&v)[N], Selection<G>& sel)
+{
+    const int full = n / D::kVec, larger = count_from(v, value + 1);
+    if (larger >= k) return INT32_MAX;  // (a bound that no lane's value is equal to)
+    uint32_t mine = 0;
+    if (lane < full && ordered(best.first) == value) {
+        int at = 0;
+#pragma unroll
+        for (int i = kLoads - 1; i >= 0; --i) {
+            const int q = (best.group * kLoads + i) * G + lane;
+            if (q >= full) continue;
+            float f[D::kVec];
+            D::unpack(load16(x + (int64_t)q * D::kVec), f);
+#pragma unroll
+            for (int e = D::kVec - 1; e >= 0; --e)
+                if (f[e] == best.first) at = q * D::kVec + e;
+        }
+        mine = ~(uint32_t)at;
+    }
+    uint32_t w[N];
+    row_sync<G>();
+    put_bin(sel, lane, mine);
+    row_sync<G>();
+    get_bins(sel, lane, mine, w);
+    return (int)~kth_value(w, k - larger);
+}
+
+// Before the sync that select_top is called behind.
+template <typename D, int G>
+__device__ __forceinline__ uint32_t offer(int n, int lane, const Best& best, Selection<G>& sel)
+{
+    const uint32_t own = lane < n / D::kVec ? ordered(best.first) : 0;
+    put_bin(sel, lane, own);
+    if (lane == 0) sel.count = 0;
+    return own;
+}
+
+// The k best of n logits, handed to put(rank, key) by the lane that has one. `own`: what offer gave.
 template <typename D, int G, typename Put>
 __device__ __forceinline__ void select_top(const typename D::Store* x, int n, int lane, int offset, int k,
-                                           uint64_t mine, Selection<G>& sel, Put&& put)
+                                           const Best& best, uint32_t own, Selection<G>& sel, Put&& put)
 {
-    if (G == 64) {
-        const uint64_t keys[1] = {mine};
-        const uint64_t from = kth_key(keys, k);
-        const bool in = mine != 0 && mine >= from;
-        const uint64_t mask = __ballot(in);
-        if (in) sel.lanes[__popcll(mask & (((uint64_t)1 << lane) - 1))] = lane;
-        if (lane == 0) {
-            sel.num_lanes = __popcll(mask);
-            sel.count = 0;
-            sel.from = from;
-        }
-    } else {
-        sel.list[lane] = mine;
-        __syncthreads();
-        if (lane < 64) {
-            const uint64_t keys[4] = {sel.list[lane], sel.list[lane + 64], sel.list[lane + 128],
-                                      sel.list[lane + 192]};
-            const uint64_t from = kth_key(keys, k);
-            int base = 0;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const bool in = keys[i] != 0 && keys[i] >= from;
-                const uint64_t mask = __ballot(in);
-                if (in) sel.lanes[base + __popcll(mask & (((uint64_t)1 << lane) - 1))] = lane + 64 * i;
-                base += __popcll(mask);
-            }
-            if (lane == 0) {
-                sel.num_lanes = base;
-                sel.count = 0;
-                sel.from = from;
-            }
-        }
+    constexpr int kCap = Selection<G>::kCap;
+    uint32_t v[G == 64 ? 1 : 4];
+    get_bins(sel, lane, own, v);
+    Bound to{kth_value(v, k), INT32_MAX, offset};
+    if (to.value && count_from(v, to.value) > k + kTies)
+        to.last = last_index<D, G>(x, n, lane, best, to.value, k, v, sel);
+    gather<D, G>(x, n, lane, best, to, sel);
+    row_sync<G>();
+    int count = sel.count;
+    if (__builtin_expect(count > kCap && to.value && to.last == INT32_MAX, 0)) {
+        to.last = last_index<D, G>(x, n, lane, best, to.value, k, v, sel);
+        if (lane == 0) sel.count = 0;
+        row_sync<G>();
+        gather<D, G>(x, n, lane, best, to, sel);
+        row_sync<G>();
+        count = sel.count;
     }
-    row_sync<G>();
-    gather<D, G>(x, n, lane, offset, sel);
-    row_sync<G>();
-    const int count = sel.count;
-    if (__builtin_expect(count <= Selection<G>::kCap, 1)) {
+    if (__builtin_expect(count <= kCap, 1)) {
         for (int i = lane; i < count; i += G) {
             const uint64_t key = sel.list[i];
             int rank = 0;
@@ -410,7 +560,7 @@ __device__ __forceinline__ void select_top(const typename D::Store* x, int n, in
         }
         return;
     }
-    // k or fewer lanes hold more large values than the list does: one pass for each alternative
+    // a few lanes hold more large values than the list does: one pass for each alternative
     uint64_t last = ~(uint64_t)0;
     for (int rank = 0; rank < k; ++rank) {
         uint64_t top = 0;
@@ -425,7 +575,7 @@ __device__ __forceinline__ void select_top(const typename D::Store* x, int n, in
         }
         if (G > 64) {
             row_sync<G>();
-            if ((lane & 63) == 0) sel.list[lane >> 6] = top;
+            if (lane % 64 == 0) sel.list[lane / 64] = top;
             row_sync<G>();
             for (int w = 0; w < G / 64; ++w) top = sel.list[w] > top ? sel.list[w] : top;
         }
@@ -437,46 +587,18 @@ __device__ __forceinline__ void select_top(const typename D::Store* x, int n, in
 // ---- forward kernels
 
 template <typename P>
-__device__ __forceinline__ const void* row_at(const P& p, int b, int t, size_t size)
+__device__ __forceinline__ const void* row_at(const P& p, uint32_t row, size_t size)
 {
-    return static_cast<const char*>(p.x) + (b * p.stride_b + t * p.stride_t) * (int64_t)size;
+    return static_cast<const char*>(p.x) +
+           ((int64_t)(row / p.T) * p.stride_b + (int64_t)(row % p.T) * p.stride_t) * (int64_t)size;
 }
 
-// G = 16 or 64 lanes a row, kThreads / G rows a workgroup.
-template <typename D, int G, bool Ent, bool Top>
-__global__ __launch_bounds__(kThreads) void k_token_rows(TokenParams p, SeqLengths lens)
+template <typename D, int G>
+__device__ __forceinline__ float target_logit(const typename D::Store* x, const Row& r, int V)
 {
-    static_assert(!Top || G == 64, "a selection takes a wave");
-    using Store = typename D::Store;
-    constexpr int kRows = kThreads / G;
-    __shared__ Selection<64> sels[Top ? kWaves : 1];
-    const int lane = threadIdx.x % G, sub = threadIdx.x / G;
-    const float scale2 = p.scale * kLog2e;
-    const uint32_t rows = (uint32_t)p.B * p.T;  // (below 2^31: sums with a grid fit 32 bits)
-    for (uint32_t row = blockIdx.x * kRows + sub; row < rows; row += gridDim.x * kRows) {
-        const int b = row / p.T, t = row % p.T;
-        const Row r = row_of(p, lens, b, t);
-        const Store* x = static_cast<const Store*>(row_at(p, b, t, sizeof(Store)));
-        Sums a = no_sums();
-        Best best{-INFINITY, 0};
-        float xt = 0.f;
-        if (r.live) {
-            if (r.target >= 0 && r.target < p.V) xt = D::load(x + r.target);
-            scan<D, G, Ent, Top>(x, p.V, lane, scale2, a, best);
-            join_lanes<G>(a, scale2);
-        }
-        if (lane == 0) write_row(p, row, r, a, xt);
-        if (!Top) continue;
-        const Scores c = scores_of(a);
-        if (!r.live || c.m != c.m) {
-            for (int k = lane; k < p.top_k; k += G) write_top(p, row, k, 0, r.live, c);
-        } else {
-            const uint64_t mine = best_key<D, G>(x, p.V, lane, best, 0);
-            select_top<D, 64>(x, p.V, lane, 0, p.top_k, mine, sels[sub % kWaves],
-                              [&](int k, uint64_t key) { write_top(p, row, k, key, true, c); });
-            row_sync<64>();
-        }
-    }
+    if (r.target < 0 || r.target >= V) return 0.f;
+    const float v = D::load(x + r.target);
+    return G >= 64 ? uniform(v) : v;
 }
 
 // What part j of `parts` of a row leaves for k_token_join: sums, and its k best keys.
@@ -490,74 +612,80 @@ __device__ __forceinline__ uint64_t* part_keys(const TokenParams& p, int64_t par
     return reinterpret_cast<uint64_t*>(part_sums(p, all)) + part * p.top_k;
 }
 
-// The workgroup's sums from its lanes'; every lane has them.
-__device__ __forceinline__ Sums join_waves(Sums a, float scale2, Sums* shared)
+// The sums of G lanes; every lane has them. With more than a wave behind a sync.
+template <int G>
+__device__ __forceinline__ Sums join_all(Sums a, float scale2, Sums* shared)
 {
-    join_lanes<64>(a, scale2);
-    if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = a;
-    __syncthreads();
-    a = shared[0];
-#pragma unroll
-    for (int w = 1; w < kWaves; ++w) {
-        Sums o = shared[w];
-        const float to = fmaxf(a.m, o.m);
-        shift(a, to, scale2);
-        shift(o, to, scale2);
-        a.s += o.s;
-        a.u += o.u;
+    join_lanes<(G < 64 ? G : 64)>(a, scale2);
+    if (G > 64) {
+        if (threadIdx.x % 64 == 0) shared[threadIdx.x / 64] = a;
+        __syncthreads();
+        // (each 16 lanes of a wave join what the waves have, at most 16, once more)
+        a = threadIdx.x % 16 < G / 64 ? shared[threadIdx.x % 16] : no_sums();
+        join_lanes<16>(a, scale2);
+        a = {uniform(a.m), uniform(a.s), uniform(a.u)};
     }
     return a;
 }
 
-// A workgroup a row, or for Split a workgroup for each of p.parts parts of a row.
-template <typename D, bool Ent, bool Top, bool Split>
-__global__ __launch_bounds__(kThreads) void k_token_blocks(TokenParams p, SeqLengths lens)
+// G lanes a row, or for Split G lanes for each of p.parts parts of a row.
+template <typename D, int G, bool Top, bool Split>
+__global__ __launch_bounds__(threads_of(G)) void k_token(TokenParams p, SeqLengths lens)
 {
+    static_assert(!Top || G >= 64, "a selection takes a wave");
     using Store = typename D::Store;
-    __shared__ Sums shared[kWaves];
-    __shared__ Selection<kThreads> sel;
-    const int lane = threadIdx.x;
+    constexpr int kRows = threads_of(G) / G;
+    __shared__ Sums shared[G > 64 ? G / 64 : 1];
+    __shared__ Selection<(G < 64 ? 64 : G)> sels[Top ? kRows : 1];
+    const int lane = threadIdx.x % G, sub = threadIdx.x / G;
+    auto& sel = sels[Top ? sub : 0];
     const float scale2 = p.scale * kLog2e;
-    // (rows of several parts are few)
+    // (rows are below 2^31, and those of several parts few: sums with a grid fit 32 bits)
     const uint32_t units = (uint32_t)p.B * p.T * (Split ? p.parts : 1);
-    for (uint32_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
+    for (uint32_t at = blockIdx.x * kRows + sub; at < units; at += gridDim.x * kRows) {
+        const uint32_t unit = G == 64 ? uniform(at) : at;
         const uint32_t row = Split ? unit / p.parts : unit;
         const int from = Split ? (int)(unit % p.parts) * p.part_size : 0;
         const int n = Split ? (p.V - from < p.part_size ? p.V - from : p.part_size) : p.V;
-        const int b = row / p.T, t = row % p.T;
-        const Row r = row_of(p, lens, b, t);
-        const Store* x = static_cast<const Store*>(row_at(p, b, t, sizeof(Store))) + from;
+        const Row r = row_of<G>(p, lens, row);
+        const Store* x = static_cast<const Store*>(row_at(p, row, sizeof(Store))) + from;
+        if (!r.live) {
+            if (Split) continue;
+            if (lane == 0) write_row(p, row, r, no_sums(), 0.f);
+            if (Top)
+                for (int k = lane; k < p.top_k; k += G) write_top(p, row, k, 0, false, Scores{0.f, 0.f});
+            continue;
+        }
         Sums a = no_sums();
-        Best best{-INFINITY, 0};
-        float xt = 0.f;
-        if (r.live) {
-            if (!Split && r.target >= 0 && r.target < p.V) xt = D::load(x + r.target);
-            scan<D, kThreads, Ent, Top>(x, n, lane, scale2, a, best);
-            a = join_waves(a, scale2, shared);
-        }
+        Best best{-INFINITY, -INFINITY, 0};
+        const float xt = Split ? 0.f : target_logit<D, G>(x, r, p.V);
+        scan<D, G, Top>(x, n, lane, scale2, p.once, a, best);
+        const uint32_t own = Top ? offer<D>(n, lane, best, sel) : 0;
+        a = join_all<G>(a, scale2, shared);
         if (lane == 0) {
-            if (!Split) write_row(p, row, r, a, xt);
-            else if (r.live) *part_sums(p, unit) = make_float4(a.m, a.s, a.u, 0.f);
+            if (Split) *part_sums(p, unit) = make_float4(a.m, a.s, a.u, 0.f);
+            else write_row(p, row, r, a, xt);
         }
-        if (Top && (Split ? r.live : true)) {
+        if (Top) {
             const Scores c = scores_of(a);
-            if (!r.live || c.m != c.m) {
-                for (int k = lane; k < p.top_k; k += kThreads) {
+            if (c.m != c.m) {
+                for (int k = lane; k < p.top_k; k += G) {
                     if (Split) part_keys(p, unit)[k] = 0;
-                    else write_top(p, row, k, 0, r.live, c);
+                    else write_top(p, row, k, 0, true, c);
                 }
             } else {
-                const uint64_t mine = best_key<D, kThreads>(x, n, lane, best, from);
+                row_sync<(G < 64 ? 64 : G)>();
                 const int k = p.top_k < n ? p.top_k : n;
-                select_top<D, kThreads>(x, n, lane, from, k, mine, sel, [&](int rank, uint64_t key) {
+                select_top<D>(x, n, lane, from, k, best, own, sel, [&](int rank, uint64_t key) {
                     if (Split) part_keys(p, unit)[rank] = key;
                     else write_top(p, row, rank, key, true, c);
                 });
                 if (Split)
-                    for (int rank = k + lane; rank < p.top_k; rank += kThreads) part_keys(p, unit)[rank] = 0;
+                    for (int rank = k + lane; rank < p.top_k; rank += G) part_keys(p, unit)[rank] = 0;
             }
         }
-        __syncthreads();
+        if (G > 64) __syncthreads();
+        else if (Top) row_sync<64>();
     }
 }
 
@@ -566,53 +694,45 @@ template <typename D, bool Top>
 __global__ __launch_bounds__(kThreads) void k_token_join(TokenParams p, SeqLengths lens)
 {
     using Store = typename D::Store;
-    __shared__ Sums shared[kWaves];
+    __shared__ Sums shared[kThreads / 64];
     __shared__ Selection<kThreads> sel;
     const int lane = threadIdx.x;
     const float scale2 = p.scale * kLog2e;
     const uint32_t rows = (uint32_t)p.B * p.T;
     for (uint32_t row = blockIdx.x; row < rows; row += gridDim.x) {
-        const int b = row / p.T, t = row % p.T;
-        const Row r = row_of(p, lens, b, t);
-        const Store* x = static_cast<const Store*>(row_at(p, b, t, sizeof(Store)));
+        const Row r = row_of<kThreads>(p, lens, row);
+        const Store* x = static_cast<const Store*>(row_at(p, row, sizeof(Store)));
         Sums a = no_sums();
-        float xt = 0.f;
-        uint64_t mine = 0;
         const int keys = p.parts * p.top_k;
         const uint64_t* key = part_keys(p, (int64_t)row * p.parts);
+        uint64_t mine = 0;
+        float xt = 0.f;
         if (r.live) {
-            if (r.target >= 0 && r.target < p.V) xt = D::load(x + r.target);
+            xt = target_logit<D, kThreads>(x, r, p.V);
             if (lane < p.parts) {
                 const float4 v = *part_sums(p, (int64_t)row * p.parts + lane);
                 a = {v.x, v.y, v.z};
             }
-            if (Top)
+            if (Top) {
                 for (int i = lane; i < keys; i += kThreads) mine = key[i] > mine ? key[i] : mine;
+                put_bin(sel, lane, (uint32_t)(mine >> 32));
+                if (lane == 0) sel.count = 0;
+            }
         }
-        a = join_waves(a, scale2, shared);
+        a = join_all<kThreads>(a, scale2, shared);
         if (lane == 0) write_row(p, row, r, a, xt);
         if (Top) {
             const Scores c = scores_of(a);
             if (!r.live || c.m != c.m) {
                 for (int k = lane; k < p.top_k; k += kThreads) write_top(p, row, k, 0, r.live, c);
             } else {
-                sel.list[lane] = mine;
-                __syncthreads();
-                if (lane < 64) {
-                    const uint64_t four[4] = {sel.list[lane], sel.list[lane + 64],
-                                              sel.list[lane + 128], sel.list[lane + 192]};
-                    const uint64_t from = kth_key(four, p.top_k);
-                    if (lane == 0) {
-                        sel.from = from;
-                        sel.count = 0;
-                    }
-                }
-                __syncthreads();
-                const uint64_t from = sel.from;
-                // (at most kMaxTop lanes reach it, with kMaxParts * kMaxTop / kThreads keys each)
-                if (mine >= from)
+                // (at most kMaxParts * kMaxTop keys, of which the list holds them all)
+                uint32_t v[4];
+                get_bins(sel, lane, 0, v);
+                const uint32_t from = kth_value(v, p.top_k);
+                if ((uint32_t)(mine >> 32) >= from)
                     for (int i = lane; i < keys; i += kThreads)
-                        if (key[i] != 0 && key[i] >= from) push(sel, key[i]);
+                        if (key[i] != 0 && (uint32_t)(key[i] >> 32) >= from) push(sel, key[i]);
                 __syncthreads();
                 const int count = sel.count;
                 for (int i = lane; i < count; i += kThreads) {
@@ -653,10 +773,10 @@ struct RowGrad {
     int target;
 };
 
-template <bool Ent>
+template <int G, bool Ent>
 __device__ __forceinline__ RowGrad row_grad(const TokenGradParams& p, const SeqLengths& lens, uint32_t row)
 {
-    const Row r = row_of(p, lens, row / p.T, row % p.T);
+    const Row r = row_of<G>(p, lens, row);
     RowGrad w;
     const float logs = p.stats[2 * (int64_t)row + 1];
     w.m = p.stats[2 * (int64_t)row];
@@ -667,7 +787,7 @@ __device__ __forceinline__ RowGrad row_grad(const TokenGradParams& p, const SeqL
     const float h = Ent ? p.grad_entropy[row] * p.scale : 0.f;
     w.c = Ent ? w.g + h * p.entropy[row] : w.g;
     w.h2 = h * kLn2;
-    w.target = w.zero ? -1 : (int)r.target;
+    w.target = w.zero ? -1 : r.target;
     return w;
 }
 
@@ -692,15 +812,18 @@ __global__ __launch_bounds__(kThreads) void k_token_grad(TokenGradParams p, SeqL
     using Store = typename D::Store;
     constexpr int kRows = kThreads / G;
     const int lane = threadIdx.x % G;
-    const uint64_t units = (uint64_t)p.B * p.T * p.pieces;
-    for (uint64_t unit = (uint64_t)blockIdx.x * kRows + threadIdx.x / G; unit < units;
-         unit += (uint64_t)gridDim.x * kRows) {
-        const uint32_t row = p.pieces == 1 ? (uint32_t)unit : (uint32_t)(unit / p.pieces);
-        const int from = p.pieces == 1 ? 0 : (int)(unit % p.pieces) * p.piece;
+    const uint32_t rows = (uint32_t)p.B * p.T;
+    const uint32_t at = kRows == 1 ? blockIdx.y : blockIdx.x * kRows + threadIdx.x / G;
+    const uint32_t step = kRows == 1 ? gridDim.y : gridDim.x * kRows;
+    // (with one row a workgroup its pieces are next to each other in the order of the grid: rows first
+    // took 11 % longer on 8,192 rows of 65,536)
+    for (uint32_t row = G == 64 ? uniform(at) : at; row < rows; row += step)
+    for (int piece = kRows == 1 ? blockIdx.x : 0; piece < p.pieces; piece += kRows == 1 ? gridDim.x : 1) {
+        const int from = piece * p.piece;
         const int n = p.V - from < p.piece ? p.V - from : p.piece;
         const int full = n / D::kVec;
-        const RowGrad w = row_grad<Ent>(p, lens, row);
-        const Store* x = static_cast<const Store*>(row_at(p, row / p.T, row % p.T, sizeof(Store))) + from;
+        const RowGrad w = row_grad<G, Ent>(p, lens, row);
+        const Store* x = static_cast<const Store*>(row_at(p, row, sizeof(Store))) + from;
         Store* out = static_cast<Store*>(p.grad) + (int64_t)row * p.V + from;
         if (w.zero) {
             for (int q = lane; q < full; q += G) store16(out + (int64_t)q * D::kVec, make_uint4(0, 0, 0, 0));
@@ -712,17 +835,17 @@ __global__ __launch_bounds__(kThreads) void k_token_grad(TokenGradParams p, SeqL
         const float xt = w.target >= from && target < n ? D::load(x + target) : 0.f;
         for (int q = lane; q - lane < full; q += kLoads * G) {
             uint4 r[kLoads];
-            load_group<D, G>(x, full, q, r);
+            load_part<D, G>(x, full, q, r);
 #pragma unroll
             for (int k = 0; k < kLoads; ++k) {
-                const int at = (q + k * G) * D::kVec;
+                const int first = (q + k * G) * D::kVec;
                 if (q + k * G >= full) break;
                 float f[D::kVec];
                 D::unpack(r[k], f);
 #pragma unroll
                 for (int i = 0; i < D::kVec; ++i) f[i] = grad_of<Ent>(w, f[i], false);
-                store16(out + at, D::pack(f));
-                if (__builtin_expect((uint32_t)(target - at) < (uint32_t)D::kVec, 0))
+                store16(out + first, D::pack(f));
+                if (__builtin_expect((uint32_t)(target - first) < (uint32_t)D::kVec, 0))
                     D::store(out + target, grad_of<Ent>(w, xt, true));
             }
         }
@@ -735,30 +858,30 @@ __global__ __launch_bounds__(kThreads) void k_token_grad(TokenGradParams p, SeqL
 
 namespace {
 
-template <typename D, bool Ent, bool Top>
+template <typename D, bool Top>
 void launch_rows(const TokenParams& p, const SeqLengths& lens, hipStream_t stream)
 {
     const int64_t rows = (int64_t)p.B * p.T;
     const auto blocks = [](int64_t n) { return dim3((unsigned)(n < (1 << 20) ? n : 1 << 20)); };
     if (p.parts > 1) {
-        k_token_blocks<D, Ent, Top, true><<<blocks(rows * p.parts), kThreads, 0, stream>>>(p, lens);
+        k_token<D, 256, Top, true><<<blocks(rows * p.parts), 256, 0, stream>>>(p, lens);
         k_token_join<D, Top><<<blocks(rows), kThreads, 0, stream>>>(p, lens);
+    } else if (p.V > 4096 && rows <= 512) {
+        k_token<D, 1024, Top, false><<<blocks(rows), 1024, 0, stream>>>(p, lens);
     } else if (p.V > 4096) {
-        k_token_blocks<D, Ent, Top, false><<<blocks(rows), kThreads, 0, stream>>>(p, lens);
+        k_token<D, 256, Top, false><<<blocks(rows), 256, 0, stream>>>(p, lens);
     } else if (Top || p.V > 128) {
-        k_token_rows<D, 64, Ent, Top><<<blocks((rows + 3) / 4), kThreads, 0, stream>>>(p, lens);
+        k_token<D, 64, Top, false><<<blocks((rows + 3) / 4), kThreads, 0, stream>>>(p, lens);
     } else {
-        k_token_rows<D, 16, Ent, false><<<blocks((rows + 15) / 16), kThreads, 0, stream>>>(p, lens);
+        k_token<D, 16, false, false><<<blocks((rows + 15) / 16), kThreads, 0, stream>>>(p, lens);
     }
 }
 
 template <typename D>
 hipError_t launch_type(const TokenParams& p, const SeqLengths& lens, hipStream_t stream)
 {
-    if (p.entropy && p.top_k) launch_rows<D, true, true>(p, lens, stream);
-    else if (p.entropy) launch_rows<D, true, false>(p, lens, stream);
-    else if (p.top_k) launch_rows<D, false, true>(p, lens, stream);
-    else launch_rows<D, false, false>(p, lens, stream);
+    if (p.top_k) launch_rows<D, true>(p, lens, stream);
+    else launch_rows<D, false>(p, lens, stream);
     return hipGetLastError();
 }
 
@@ -806,7 +929,11 @@ hipError_t launch_grad(TokenGradParams p, const SeqLengths& lens, hipStream_t st
     } else {
         p.piece = kThreads * kLoads * D::kVec;
         p.pieces = (p.V + p.piece - 1) / p.piece;
-        k_token_grad<D, kThreads, Ent><<<blocks(rows * p.pieces), kThreads, 0, stream>>>(p, lens);
+        // (a launch has fewer than 2^32 threads)
+        const int64_t x = p.pieces < (1 << 20) ? p.pieces : 1 << 20, most = (1 << 22) / x;
+        const int64_t y = rows < 65535 ? rows : 65535;
+        const dim3 grid((unsigned)x, (unsigned)(y < most ? y : most));
+        k_token_grad<D, kThreads, Ent><<<grid, kThreads, 0, stream>>>(p, lens);
     }
     return hipGetLastError();
 }

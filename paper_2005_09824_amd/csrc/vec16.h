@@ -14,6 +14,14 @@ __device__ __forceinline__ uint4 load16(const void* p)
     __builtin_memcpy(&v, p, 16);
     return v;
 }
+// ... of data that is not read again soon: it takes no place in the caches.
+__device__ __forceinline__ uint4 load16_once(const void* p)
+{
+    typedef uint32_t Words __attribute__((ext_vector_type(4)));
+    typedef Words Anywhere __attribute__((aligned(2)));
+    const Words v = __builtin_nontemporal_load(static_cast<const Anywhere*>(p));
+    return make_uint4(v[0], v[1], v[2], v[3]);
+}
 __device__ __forceinline__ void store16(void* p, uint4 v) { __builtin_memcpy(p, &v, 16); }
 
 typedef __bf16 Bf16x2 __attribute__((ext_vector_type(2)));
