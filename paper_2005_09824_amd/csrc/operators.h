@@ -42,7 +42,7 @@ struct TokenPlan {
     int32_t parts, part_size;
     size_t workspace;
 };
-TokenPlan plan_tokens(int64_t rows, int V, int top_k);
+TokenPlan plan_tokens(int64_t rows, int V, int size, int top_k);
 
 struct TokenGradParams {
     const void* x;

@@ -2,6 +2,8 @@
 // logits, and their gradient. See include/lfmmi.h for the formulas.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "../../include/lfmmi.h"
 #include "operators.h"
 #include "vec16.h"
@@ -59,6 +61,10 @@ __device__ __forceinline__ uint32_t all_bits(uint32_t v)  // of a wave, and-ed
 #undef LFMMI_ROR
     return (uint32_t)__builtin_amdgcn_readlane(v, 0) & (uint32_t)__builtin_amdgcn_readlane(v, 16) &
            (uint32_t)__builtin_amdgcn_readlane(v, 32) & (uint32_t)__builtin_amdgcn_readlane(v, 48);
+}
+__device__ __forceinline__ uint64_t all_bits(uint64_t v)
+{
+    return (uint64_t)all_bits((uint32_t)(v >> 32)) << 32 | all_bits((uint32_t)v);
 }
 __device__ __forceinline__ uint32_t max_of_four(uint32_t v)  // lanes next to each other
 {
@@ -121,8 +127,7 @@ __device__ __forceinline__ void join_lanes(Sums& a, float scale2)
     a.u = sum_over<G>(a.u);
 }
 
-// Values in an order of whole numbers (-0 and 0 are equal); no value is 0, and -inf is kLowest.
-constexpr uint32_t kLowest = 0x007fffffu;
+// Values in an order of whole numbers (-0 and 0 are equal); no value is 0.
 __device__ __forceinline__ uint32_t ordered(float x)
 {
     const uint32_t b = __float_as_uint(x + 0.f);
@@ -242,13 +247,15 @@ __device__ __forceinline__ float max_of(const float (&f)[N])
     return N % 2 ? top : fmaxf(top, f[N - 1]);
 }
 
-// Adds logits of any kind; a.m is their largest at least.
+// Adds the first `chunks` chunks of a lane's logits, of any kind; a.m is their largest at least.
 template <int N>
-__device__ __forceinline__ void add_any(Sums& a, const float (&f)[N], float scale2)
+__device__ __forceinline__ void add_any(Sums& a, const float (&f)[N], int chunks, float scale2)
 {
+    constexpr int kVec = N < kLoads ? N : N / kLoads;
     float s[4] = {a.s, 0.f, 0.f, 0.f}, u[4] = {a.u, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < N; ++i) {
+        if (i % kVec == 0 && i / kVec >= chunks) break;
         const float y = (f[i] - a.m) * scale2, e = exp2_of(y);
         s[i & 3] += e;
         u[i & 3] += e * finite(y);
@@ -289,16 +296,21 @@ __device__ __forceinline__ void scan(const typename D::Store* x, int n, int lane
 {
     constexpr int kVec = D::kVec, N = kVec * kLoads;
     const int full = n / kVec;
-    int q = lane, j = 0;
-    bool plain = true;  // until logits are met that add_plain does not take
-    for (; G > 16 && q - lane + kLoads * G <= full; q += kLoads * G, ++j) {
+    bool plain = G > 16;  // until logits are met that add_plain does not take
+    for (int q = lane, j = 0; q - lane < full; q += kLoads * G, ++j) {
+        const int chunks = (full - (q - lane) + G - 1) / G;  // (the last group may have fewer)
         uint4 r[kLoads];
-        if (once) {
+        if (G > 16 && q - lane + kLoads * G <= full) {
+            if (once) {
 #pragma unroll
-            for (int k = 0; k < kLoads; ++k) r[k] = load16_once(x + (int64_t)(q + k * G) * kVec);
+                for (int k = 0; k < kLoads; ++k) r[k] = load16_once(x + (int64_t)(q + k * G) * kVec);
+            } else {
+#pragma unroll
+                for (int k = 0; k < kLoads; ++k) r[k] = load16(x + (int64_t)(q + k * G) * kVec);
+            }
         } else {
-#pragma unroll
-            for (int k = 0; k < kLoads; ++k) r[k] = load16(x + (int64_t)(q + k * G) * kVec);
+            load_part<D, G>(x, full, q, r);
+            plain = false;
         }
         float f[N];
 #pragma unroll
@@ -308,28 +320,12 @@ __device__ __forceinline__ void scan(const typename D::Store* x, int n, int lane
         shift(a, fmaxf(a.m, top), scale2);
         plain = plain && !__builtin_amdgcn_ballot_w64(!(fabsf(a.m) < 1e30f));
         if (plain) plain = add_plain(a, f, scale2);
-        if (!plain) add_any(a, f, scale2);
-    }
-    if (q - lane < full) {  // what is left of a group, chunk by chunk
-        uint4 r[kLoads];
-        load_part<D, G>(x, full, q, r);
-        float most = -INFINITY;
-#pragma unroll
-        for (int k = 0; k < kLoads; ++k) {
-            if (q - lane + k * G >= full) break;
-            float f[kVec];
-            D::unpack(r[k], f);
-            const float top = max_of(f);
-            most = fmaxf(most, top);
-            shift(a, fmaxf(a.m, top), scale2);
-            add_any(a, f, scale2);
-        }
-        if (Top) take(best, most, j);
+        if (!plain) add_any(a, f, chunks, scale2);
     }
     for (int i = full * kVec + lane; i < n; i += G) {
         const float f[1] = {D::load(x + i)};
         shift(a, fmaxf(a.m, f[0]), scale2);
-        add_any(a, f, scale2);
+        add_any(a, f, 1, scale2);
     }
 }
 
@@ -342,10 +338,13 @@ __device__ __forceinline__ void scan(const typename D::Store* x, int n, int lane
 // order by counting, for each, how many are larger. Where more than kTies lanes over k reach T
 // (masked rows, equal logits), or more values than the list holds, T gets an index as well.
 constexpr int kTies = 32;
+// Where k is kFew at most, 64 lanes' worth of maxima give a T that hardly more than k values reach; and T
+// need not be the k-th exactly, the last few bits of it are left out.
+constexpr int kFew = 32, kNear = 3;
 
 // Of the N values that each lane of a wave holds, how many are from `c` on.
-template <int N>
-__device__ __forceinline__ int count_from(const uint32_t (&v)[N], uint32_t c)
+template <typename V, int N>
+__device__ __forceinline__ int count_from(const V (&v)[N], V c)
 {
     int count = 0;
 #pragma unroll
@@ -353,22 +352,22 @@ __device__ __forceinline__ int count_from(const uint32_t (&v)[N], uint32_t c)
     return count;
 }
 
-// The k-th largest of them, or a lower bound of it with exactly k values from there on; 0 if fewer
-// than k are not 0. Bit by bit from the highest, bits in which no two values differ left out.
-template <int N>
-__device__ __forceinline__ uint32_t kth_value(const uint32_t (&v)[N], int k)
+// The k-th largest of them, or a lower bound of it with at most k + more values from there on; 0 if
+// fewer than k are not 0. Bit by bit from the highest, bits in which no two values differ left out.
+template <typename V, int N>
+__device__ __forceinline__ V kth_value(const V (&v)[N], int k, int more)
 {
-    uint32_t all = v[0], none = ~v[0];
+    V all = v[0], none = ~v[0];
 #pragma unroll
     for (int i = 1; i < N; ++i) {
         all &= v[i];
         none &= ~v[i];
     }
-    uint32_t t = all_bits(all), open = ~(t | all_bits(none));
-    if (t == 0 && count_from(v, 1) < k) return 0;
-    for (int count = 64 * N; open && count != k;) {
-        const uint32_t bit = 0x80000000u >> __builtin_clz(open);
-        const int above = count_from(v, t | bit);
+    V t = all_bits(all), open = ~(t | all_bits(none));
+    if (t == 0 && count_from(v, (V)1) < k) return 0;
+    for (int count = 64 * N; open && count > k + more;) {
+        const V bit = (V)1 << (63 - __builtin_clzll(open));
+        const int above = count_from(v, (V)(t | bit));
         open ^= bit;
         if (above >= k) {
             t |= bit;
@@ -381,10 +380,9 @@ __device__ __forceinline__ uint32_t kth_value(const uint32_t (&v)[N], int k)
 // LDS of one row's selection.
 template <int G>
 struct Selection {
-    static constexpr int kCap = G == 64 ? 512 : 1024;  // keys that it holds
-    static constexpr int kBins = G == 64 ? 1 : 256;
+    static constexpr int kCap = G == 64 ? 512 : G == 256 ? 1024 : 2048;  // keys that it holds
     uint64_t list[kCap];
-    uint32_t bins[kBins];
+    uint32_t bins[G == 64 ? 1 : 256];
     int count;
 };
 
@@ -437,27 +435,18 @@ struct Bound {
     int last, offset;
 };
 
-template <typename D, int G>
-__device__ __forceinline__ void push_chunk(const typename D::Store* x, int q, const Bound& to, Selection<G>& sel)
+template <int G>
+__device__ __forceinline__ void push_if(float v, int at, const Bound& to, Selection<G>& sel)
 {
-    // (below kLowest a bound's bits are no number's)
-    const float least = to.value <= kLowest ? -INFINITY : value_of(to.value);
-    float f[D::kVec];
-    D::unpack(load16(x + (int64_t)q * D::kVec), f);
-#pragma unroll
-    for (int i = 0; i < D::kVec; ++i) {
-        const int at = q * D::kVec + i;
-        if (f[i] >= least && (ordered(f[i]) > to.value || at <= to.last))
-            push(sel, key_of(f[i], to.offset + at));
-    }
+    const uint32_t o = ordered(v);
+    if (o > to.value || (o == to.value && at <= to.last)) push(sel, (uint64_t)o << 32 | (uint32_t)~(to.offset + at));
 }
 
-// Each wave looks through what its own lanes have read.
+// Each wave looks through what its own lanes have read, a chunk a lane.
 template <typename D, int G>
 __device__ __forceinline__ void gather(const typename D::Store* x, int n, int lane, const Best& best,
                                        const Bound& to, Selection<G>& sel)
 {
-    static_assert(kLoads == 4, "four lanes look through a group");
     constexpr int kVec = D::kVec;
     const int full = n / kVec, in_wave = lane % 64, base = lane - in_wave;
     const uint32_t first = ordered(best.first), second = ordered(best.second);
@@ -466,27 +455,36 @@ __device__ __forceinline__ void gather(const typename D::Store* x, int n, int la
     // (if both are equal to T the second one's group comes later)
     const bool later = first == to.value && (best.group + 1) * kLoads * G * kVec > to.last;
     const bool deep = in && (second > to.value || (second == to.value && !later) || to.value == 0);
-    const uint64_t some = __builtin_amdgcn_ballot_w64(in && !deep);
-    const int count = __builtin_popcountll(some);
-    const int below = __builtin_popcountll(some & (((uint64_t)1 << in_wave) - 1));
-    // the lanes in question, and behind them the others, in a row
-    const int slot = in && !deep ? below : count + in_wave - below;
-    const int sent = __builtin_amdgcn_ds_permute(slot * 4, best.group << 6 | in_wave);
-    for (int b = 0; b < count; b += 16) {
-        const int from = b + in_wave / 4;
-        const int v = __builtin_amdgcn_ds_bpermute((from & 63) * 4, sent);
-        const int q = ((v >> 6) * kLoads + in_wave % 4) * G + base + (v & 63);
-        if (from < count && q < full) push_chunk<D, G>(x, q, to, sel);
+    const uint64_t ones = __builtin_amdgcn_ballot_w64(in && !deep), deeps = __builtin_amdgcn_ballot_w64(deep);
+    const int num_one = __builtin_popcountll(ones), num_deep = __builtin_popcountll(deeps);
+    if (num_one + num_deep > 0) {
+        // lanes of one group, then lanes of all groups, then the others, in a row
+        const uint64_t below = ((uint64_t)1 << in_wave) - 1;
+        const int one = __builtin_popcountll(ones & below), far = __builtin_popcountll(deeps & below);
+        const int slot = deep ? num_one + far : in ? one : num_one + num_deep + in_wave - one - far;
+        const int sent = __builtin_amdgcn_ds_permute(slot * 4, best.group << 6 | in_wave);
+        const int each = (full + G - 1) / G;  // chunks of a lane, at most
+        const int items = num_one * kLoads + num_deep * each;
+        const float least = value_of(max(to.value, ordered(-INFINITY)));  // (below that bits are no number's)
+        for (int w = in_wave; w - in_wave < items; w += 64) {
+            const int all = w - num_one * kLoads;
+            const int from = all < 0 ? w / kLoads : num_one + all / each;
+            const int v = __builtin_amdgcn_ds_bpermute((from & 63) * 4, sent);
+            const int q = (all < 0 ? (v >> 6) * kLoads + w % kLoads : all % each) * G + base + (v & 63);
+            if (w < items && q < full) {
+                float f[kVec];
+                D::unpack(load16(x + (int64_t)q * kVec), f);
+                uint32_t hits = 0;
+#pragma unroll
+                for (int i = 0; i < kVec; ++i) hits |= f[i] >= least ? 1u << i : 0u;
+                for (; hits; hits &= hits - 1) {  // (few: the value is loaded once more)
+                    const int at = q * kVec + __builtin_ctz(hits);
+                    push_if<G>(D::load(x + at), at, to, sel);
+                }
+            }
+        }
     }
-    for (uint64_t left = __builtin_amdgcn_ballot_w64(deep); left; left &= left - 1) {
-        const int l = base + __builtin_ctzll(left);
-        for (int q = l + in_wave * G; q < full; q += 64 * G) push_chunk<D, G>(x, q, to, sel);
-    }
-    for (int i = full * kVec + lane; i < n; i += G) {
-        const float v = D::load(x + i);
-        const uint32_t o = ordered(v);
-        if (o > to.value || (o == to.value && i <= to.last)) push(sel, key_of(v, to.offset + i));
-    }
+    for (int i = full * kVec + lane; i < n; i += G) push_if<G>(D::load(x + i), i, to, sel);
 }
 
 // The index that goes with T: k lanes hold a larger value, or T at an index up to it.
@@ -516,7 +514,59 @@ __device__ __forceinline__ int last_index(const typename D::Store* x, int n, int
     put_bin(sel, lane, mine);
     row_sync<G>();
     get_bins(sel, lane, mine, w);
-    return (int)~kth_value(w, k - larger);
+    return (int)~kth_value(w, k - larger, 0);
+}
+
+// Of a list of many keys those that reach the k-th largest of the lanes' own largest: the same bound once
+// more, here exact, since no two keys are the same. Returns their number.
+constexpr int kMany = 192;
+template <int G>
+__device__ __forceinline__ int thin_out(int lane, int k, int count, Selection<G>& sel)
+{
+    constexpr int kEach = Selection<G>::kCap / G;
+    uint64_t mine[kEach], most = 0;
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+        mine[j] = lane + j * G < count ? sel.list[lane + j * G] : 0;
+        most = max(most, mine[j]);
+    }
+    row_sync<G>();
+    uint64_t v[G == 64 ? 1 : 4] = {most};
+    if (G > 64) {
+        sel.list[lane] = most;
+        row_sync<G>();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v[i] = 0;
+#pragma unroll
+            for (int j = 0; j < G / 256; ++j) v[i] = max(v[i], sel.list[lane % 64 + 64 * i + 256 * j]);
+        }
+    }
+    if (lane == 0) sel.count = 0;
+    row_sync<G>();
+    const uint64_t from = kth_value(v, k, kTies);
+#pragma unroll
+    for (int j = 0; j < kEach; ++j)
+        if (mine[j] && mine[j] >= from) push(sel, mine[j]);
+    row_sync<G>();
+    return sel.count;
+}
+
+template <int G, typename Put>
+__device__ __forceinline__ void put_ranked(int lane, int k, int count, const Selection<G>& sel, Put&& put)
+{
+    for (int i = lane; i < count; i += G) {
+        const uint64_t key = sel.list[i];
+        int rank = 0;
+        for (int j = 0; j < count; j += 8) {  // (the list has a multiple of 8 places)
+            uint64_t other[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) other[e] = sel.list[j + e];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) rank += j + e < count && other[e] > key;
+        }
+        if (rank < k) put(rank, key);
+    }
 }
 
 // Before the sync that select_top is called behind.
@@ -537,7 +587,13 @@ __device__ __forceinline__ void select_top(const typename D::Store* x, int n, in
     constexpr int kCap = Selection<G>::kCap;
     uint32_t v[G == 64 ? 1 : 4];
     get_bins(sel, lane, own, v);
-    Bound to{kth_value(v, k), INT32_MAX, offset};
+    Bound to{0, INT32_MAX, offset};
+    if (G > 64 && k <= kFew) {
+        const uint32_t most[1] = {max(max(v[0], v[G > 64 ? 1 : 0]), max(v[G > 64 ? 2 : 0], v[G > 64 ? 3 : 0]))};
+        to.value = kth_value(most, k, kNear);
+    } else {
+        to.value = kth_value(v, k, kNear);
+    }
     if (to.value && count_from(v, to.value) > k + kTies)
         to.last = last_index<D, G>(x, n, lane, best, to.value, k, v, sel);
     gather<D, G>(x, n, lane, best, to, sel);
@@ -552,12 +608,8 @@ __device__ __forceinline__ void select_top(const typename D::Store* x, int n, in
         count = sel.count;
     }
     if (__builtin_expect(count <= kCap, 1)) {
-        for (int i = lane; i < count; i += G) {
-            const uint64_t key = sel.list[i];
-            int rank = 0;
-            for (int j = 0; j < count; ++j) rank += sel.list[j] > key;
-            if (rank < k) put(rank, key);
-        }
+        if (count > kMany) count = thin_out(lane, k, count, sel);
+        put_ranked(lane, k, count, sel, put);
         return;
     }
     // a few lanes hold more large values than the list does: one pass for each alternative
@@ -668,10 +720,11 @@ __global__ __launch_bounds__(threads_of(G)) void k_token(TokenParams p, SeqLengt
         }
         if (Top) {
             const Scores c = scores_of(a);
-            if (c.m != c.m) {
+            if (c.m != c.m || c.m == -INFINITY) {  // no alternatives, or the first tokens
                 for (int k = lane; k < p.top_k; k += G) {
-                    if (Split) part_keys(p, unit)[k] = 0;
-                    else write_top(p, row, k, 0, true, c);
+                    const uint64_t key = c.m != c.m || k >= n ? 0 : key_of(-INFINITY, from + k);
+                    if (Split) part_keys(p, unit)[k] = key;
+                    else write_top(p, row, k, key, true, c);
                 }
             } else {
                 row_sync<(G < 64 ? 64 : G)>();
@@ -686,6 +739,59 @@ __global__ __launch_bounds__(threads_of(G)) void k_token(TokenParams p, SeqLengt
         }
         if (G > 64) __syncthreads();
         else if (Top) row_sync<64>();
+    }
+}
+
+// Rows of up to kShort logits with alternatives, a wave a row: the logits stay in registers, and take the
+// place of the lanes' maxima in the selection.
+constexpr int kShort = 256;
+template <typename D>
+__global__ __launch_bounds__(kThreads) void k_token_short(TokenParams p, SeqLengths lens)
+{
+    using Store = typename D::Store;
+    constexpr int kRows = kThreads / 64, kEach = kShort / 64;
+    __shared__ Selection<64> sels[kRows];
+    const int lane = threadIdx.x % 64;
+    auto& sel = sels[threadIdx.x / 64];
+    const float scale2 = p.scale * kLog2e;
+    const uint32_t rows = (uint32_t)p.B * p.T;
+    for (uint32_t at = blockIdx.x * kRows + threadIdx.x / 64; at < rows; at += gridDim.x * kRows) {
+        const uint32_t row = uniform(at);
+        const Row r = row_of<64>(p, lens, row);
+        const Store* x = static_cast<const Store*>(row_at(p, row, sizeof(Store)));
+        if (!r.live) {
+            if (lane == 0) write_row(p, row, r, no_sums(), 0.f);
+            if (lane < p.top_k) write_top(p, row, lane, 0, false, Scores{0.f, 0.f});
+            continue;
+        }
+        const float xt = target_logit<D, 64>(x, r, p.V);
+        float f[kEach];
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) f[i] = lane + 64 * i < p.V ? D::load(x + lane + 64 * i) : -INFINITY;
+        if (lane == 0) sel.count = 0;
+        Sums a = no_sums();
+        a.m = max_over<64>(fmaxf(a.m, max_of(f)));
+        add_any(a, f, kLoads, scale2);
+        a.s = sum_over<64>(a.s);
+        a.u = sum_over<64>(a.u);
+        if (lane == 0) write_row(p, row, r, a, xt);
+        const Scores c = scores_of(a);
+        if (c.m != c.m) {
+            if (lane < p.top_k) write_top(p, row, lane, 0, true, c);
+            continue;
+        }
+        uint32_t v[kEach];
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) v[i] = lane + 64 * i < p.V ? ordered(f[i]) : 0;
+        const uint32_t least = kth_value(v, p.top_k, kNear);
+        row_sync<64>();
+#pragma unroll
+        for (int i = 0; i < kEach; ++i)
+            if (v[i] && v[i] >= least) push(sel, (uint64_t)v[i] << 32 | (uint32_t)~(lane + 64 * i));
+        row_sync<64>();
+        put_ranked(lane, p.top_k, sel.count, sel,
+                   [&](int rank, uint64_t key) { write_top(p, row, rank, key, true, c); });
+        row_sync<64>();
     }
 }
 
@@ -715,7 +821,7 @@ __global__ __launch_bounds__(kThreads) void k_token_join(TokenParams p, SeqLengt
             }
             if (Top) {
                 for (int i = lane; i < keys; i += kThreads) mine = key[i] > mine ? key[i] : mine;
-                put_bin(sel, lane, (uint32_t)(mine >> 32));
+                sel.list[lane] = mine;
                 if (lane == 0) sel.count = 0;
             }
         }
@@ -726,21 +832,21 @@ __global__ __launch_bounds__(kThreads) void k_token_join(TokenParams p, SeqLengt
             if (!r.live || c.m != c.m) {
                 for (int k = lane; k < p.top_k; k += kThreads) write_top(p, row, k, 0, r.live, c);
             } else {
-                // (at most kMaxParts * kMaxTop keys, of which the list holds them all)
-                uint32_t v[4];
-                get_bins(sel, lane, 0, v);
-                const uint32_t from = kth_value(v, p.top_k);
-                if ((uint32_t)(mine >> 32) >= from)
-                    for (int i = lane; i < keys; i += kThreads)
-                        if (key[i] != 0 && (uint32_t)(key[i] >> 32) >= from) push(sel, key[i]);
+                // (k lanes reach the bound, each with kMaxParts * kMaxTop / kThreads keys at most)
+                static_assert(kMaxTop * (kMaxParts * kMaxTop / kThreads) <= Selection<kThreads>::kCap, "");
+                uint64_t v[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[i] = sel.list[lane % 64 + 64 * i];
+                const uint64_t bound = kth_value(v, p.top_k, 0);
                 __syncthreads();
-                const int count = sel.count;
-                for (int i = lane; i < count; i += kThreads) {
-                    const uint64_t k = sel.list[i];
-                    int rank = 0;
-                    for (int j = 0; j < count; ++j) rank += sel.list[j] > k;
-                    if (rank < p.top_k) write_top(p, row, rank, k, true, c);
-                }
+                if (mine >= bound)
+                    for (int i = lane; i < keys; i += kThreads)
+                        if (key[i] != 0 && key[i] >= bound) push(sel, key[i]);
+                __syncthreads();
+                int count = sel.count;
+                if (count > kMany) count = thin_out(lane, p.top_k, count, sel);
+                put_ranked(lane, p.top_k, count, sel,
+                           [&](int rank, uint64_t key) { write_top(p, row, rank, key, true, c); });
             }
         }
         __syncthreads();
@@ -854,23 +960,35 @@ __global__ __launch_bounds__(kThreads) void k_token_grad(TokenGradParams p, SeqL
     }
 }
 
-}  // namespace
-
-namespace {
+constexpr int kComputeUnits = 256, kManyRows = 2048;
+constexpr int kRowOf16 = 512;                                                   // logits
+constexpr int64_t kWaveRow = 32 << 10, kLongRow = 64 << 10, kSplitRow = 192 << 10;  // bytes
 
 template <typename D, bool Top>
 void launch_rows(const TokenParams& p, const SeqLengths& lens, hipStream_t stream)
 {
     const int64_t rows = (int64_t)p.B * p.T;
     const auto blocks = [](int64_t n) { return dim3((unsigned)(n < (1 << 20) ? n : 1 << 20)); };
+    const int64_t bytes = (int64_t)p.V * sizeof(typename D::Store);
+    // Lanes a row. Microseconds a call, bf16, without / with 8 alternatives, at 64, 256, 1,024 lanes:
+    //   4,096 rows of 12,000: 18.8 / 21.6, 20.9 / 32.2; 4,096 of 16,384: 23.8 / 27.2, 23.7 / 34.1;
+    //   64 of 8,192: 4.7 / 7.7, 3.4 / 6.0; 256 of 8,192: -, 3.4 / 6.2, 4.2 / 8.2;
+    //   256 of 65,536: -, 8.8 / 11.9, 7.0 / 11.1; 512 of 65,536: -, 13.2 / 16.7, 15.8 / 23.0 (a
+    //   compute unit holds one workgroup of 1,024);
+    // in parts, at 1,024 lanes: 1 of 131,072: 5.2 / 9.7, 8.8 / 12.4; 16: 5.7 / 10.8, 9.2 / 13.2;
+    //   64: 7.1 / 14.4, 9.5 / 13.5; 1 of 65,536: 5.1 / 11.1, 5.6 / 9.6.
+    // 32,000 rows without alternatives at 16 and 64 lanes: 84 logits 5.3, 15.6; 512: 7.6, 14.9 (fp32
+    // 12.3, 14.0).
     if (p.parts > 1) {
         k_token<D, 256, Top, true><<<blocks(rows * p.parts), 256, 0, stream>>>(p, lens);
         k_token_join<D, Top><<<blocks(rows), kThreads, 0, stream>>>(p, lens);
-    } else if (p.V > 4096 && rows <= 512) {
+    } else if (bytes >= kLongRow && rows <= kComputeUnits) {
         k_token<D, 1024, Top, false><<<blocks(rows), 1024, 0, stream>>>(p, lens);
-    } else if (p.V > 4096) {
+    } else if (bytes > (rows < kManyRows ? kWaveRow / 4 : kWaveRow)) {
         k_token<D, 256, Top, false><<<blocks(rows), 256, 0, stream>>>(p, lens);
-    } else if (Top || p.V > 128) {
+    } else if (Top && p.V <= kShort) {
+        k_token_short<D><<<blocks((rows + 3) / 4), kThreads, 0, stream>>>(p, lens);
+    } else if (Top || p.V > kRowOf16) {
         k_token<D, 64, Top, false><<<blocks((rows + 3) / 4), kThreads, 0, stream>>>(p, lens);
     } else {
         k_token<D, 16, false, false><<<blocks((rows + 15) / 16), kThreads, 0, stream>>>(p, lens);
@@ -887,20 +1005,16 @@ hipError_t launch_type(const TokenParams& p, const SeqLengths& lens, hipStream_t
 
 }  // namespace
 
-TokenPlan plan_tokens(int64_t rows, int V, int top_k)
+TokenPlan plan_tokens(int64_t rows, int V, int size, int top_k)
 {
     TokenPlan plan{1, V, 0};
-    // 1,024 workgroups fill the chip, and a part of 4,096 logits is worth a workgroup
-    if (rows < 512 && V >= 8192) {
-        int64_t parts = 1024 / rows;
-        parts = parts < V / 4096 ? parts : V / 4096;
-        parts = parts < kMaxParts ? parts : kMaxParts;
-        if (parts > 1) {
-            // (a multiple of 64 logits: parts of an aligned row are aligned)
-            plan.part_size = (int)(((V + parts - 1) / parts + 63) / 64 * 64);
-            plan.parts = (V + plan.part_size - 1) / plan.part_size;
-            plan.workspace = (size_t)rows * plan.parts * (sizeof(float4) + sizeof(uint64_t) * top_k);
-        }
+    if (rows <= 32 && (int64_t)V * size >= kSplitRow) {
+        // 1,024 workgroups fill the chip, and a part of 4,096 logits is worth one
+        const int64_t parts = std::min<int64_t>({1024 / rows, V / 4096, kMaxParts});
+        // (a multiple of 64 logits: parts of an aligned row are aligned)
+        plan.part_size = (int)(((V + parts - 1) / parts + 63) / 64 * 64);
+        plan.parts = (V + plan.part_size - 1) / plan.part_size;
+        plan.workspace = (size_t)rows * plan.parts * (sizeof(float4) + sizeof(uint64_t) * top_k);
     }
     return plan;
 }
