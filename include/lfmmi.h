@@ -295,7 +295,7 @@ lfmmi_status lfmmi_token_logprobs_backward(const void *logits, int32_t dtype, in
  * workspace: DEVICE, LFMMI_GRAD_WORKSPACE_BYTES(n) bytes, aligned to 16; otherwise as for
  * lfmmi_token_logprobs. The calls enqueue kernels on hip_stream and nothing else.
  */
-#define LFMMI_GRAD_WORKSPACE_BYTES(n) (16 + (((int64_t)(n) + 127) / 128 + 1) * 8192)
+#define LFMMI_GRAD_WORKSPACE_BYTES(n) (16384 + 32 * ((int64_t)(n) + 1))
 lfmmi_status lfmmi_grad_norm(int32_t n, const void *const *grads, const int64_t *counts,
                              const int32_t *dtypes, float *norm, void *workspace,
                              int64_t workspace_bytes, void *hip_stream);

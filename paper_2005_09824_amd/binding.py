@@ -507,7 +507,7 @@ def _grad_list(grads):
 
 def _grad_workspace(n, dev):
     import torch
-    size = 16 + ((n + 127) // 128 + 1) * 8192   # LFMMI_GRAD_WORKSPACE_BYTES(n)
+    size = 16384 + 32 * (n + 1)   # LFMMI_GRAD_WORKSPACE_BYTES(n)
     return torch.empty(size, dtype=torch.uint8, device=dev), size
 
 

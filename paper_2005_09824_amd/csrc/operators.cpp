@@ -13,6 +13,8 @@
 using namespace lfmmi;
 
 static_assert(LFMMI_MAX_TOP == kMaxTop, "the header states the limit");
+// partial sums, the factor in 16 bytes, and 28 bytes a tensor and 4
+static_assert(LFMMI_GRAD_WORKSPACE_BYTES(0) >= 8 * kGradBlocks + 16 + 4, "the header states the size");
 
 namespace {
 
@@ -144,55 +146,81 @@ lfmmi_status check_outs(int32_t n, const void* const* grads, void* const* outs,
     return LFMMI_OK;
 }
 
-// The tensors from `from` on that one launch takes.
+// Units of kGradUnit values of a tensor, from the address before it that kGradAlign divides.
+int64_t units_of(const void* grad, int64_t count, int32_t dtype)
+{
+    const int64_t before = (int64_t)(reinterpret_cast<uintptr_t>(grad) % kGradAlign / dtype_size(dtype));
+    return (before + count + kGradUnit - 1) / kGradUnit;
+}
+
+// Tensors from `from` on that a list takes, and the one behind them; `units` is counted on.
 int32_t fill_list(int32_t from, int32_t n, const void* const* grads, void* const* outs,
-                  const int64_t* counts, const int32_t* dtypes, GradList* l)
+                  const int64_t* counts, const int32_t* dtypes, int64_t* units, GradList* l)
 {
     l->n = 0;
-    int64_t units = 0;
     int32_t i = from;
-    static_assert(((int64_t)1 << 36) / kGradUnit * kGradTensors <= INT32_MAX, "unit numbers fit 32 bits");
     for (; i < n && l->n < kGradTensors; ++i) {
         if (counts[i] == 0) continue;
-        const int64_t more = (counts[i] + kGradUnit - 1) / kGradUnit;
         l->in[l->n] = grads[i];
         l->out[l->n] = outs ? outs[i] : const_cast<void*>(grads[i]);
         l->count[l->n] = counts[i] << 2 | dtypes[i];
-        l->first[l->n] = (int32_t)units;
-        units += more;
+        l->first[l->n] = (int32_t)*units;
+        *units += units_of(grads[i], counts[i], dtypes[i]);
         ++l->n;
     }
-    for (int32_t k = l->n; k <= kGradTensors; ++k) l->first[k] = (int32_t)units;
+    l->first[l->n] = (int32_t)*units;
     return i;
 }
 
-// max_norm < 0: the norm alone.
+// The norm, and with `scale` outs.
 lfmmi_status run_grads(int32_t n, const void* const* grads, void* const* outs,
-                       const int64_t* counts, const int32_t* dtypes, float max_norm, float* norm,
-                       void* workspace, hipStream_t stream)
+                       const int64_t* counts, const int32_t* dtypes, bool scale, float max_norm,
+                       float* norm, void* workspace, hipStream_t stream)
 {
-    float* factor = static_cast<float*>(workspace);
-    double* partials = reinterpret_cast<double*>(static_cast<char*>(workspace) + 16);
+    int64_t units = 0, bytes = 0;
+    int32_t tensors = 0;
+    bool in_place = true;
+    for (int32_t i = 0; i < n; ++i) {
+        if (counts[i] == 0) continue;
+        ++tensors;
+        units += units_of(grads[i], counts[i], dtypes[i]);
+        bytes += counts[i] * (int64_t)dtype_size(dtypes[i]);
+        in_place = in_place && (!outs || outs[i] == grads[i]);
+    }
+    if (units > INT32_MAX) return fail(LFMMI_ERR_UNSUPPORTED, "more than 2^44 values");
+    GradCall c{};
+    c.n = tensors;
+    c.units = (int32_t)units;
+    c.blocks = std::min(c.units, kGradBlocks);
+    // what the second pass finds in the cache again; more than that goes past it
+    const int64_t kept = scale ? kCacheBytes * 3 / 4 : 0;
+    c.keep = bytes <= kCacheBytes ? 256 : (int32_t)(256 * kept / bytes);
+    c.scale = scale;
+    c.in_place = in_place;
+    c.max_norm = max_norm;
+    c.norm = norm;
+    c.partials = static_cast<double*>(workspace);
+    c.factor = reinterpret_cast<float*>(c.partials + kGradBlocks);
     GradList l;
-    int blocks = 0;
     hipError_t e;
-    for (int32_t i = 0; i < n;) {
-        i = fill_list(i, n, grads, outs, counts, dtypes, &l);
-        if (l.n == 0) break;
-        if ((e = launch_grad_squares(l, partials + blocks, stream)) != hipSuccess)
-            return fail_hip(e, "kernel launch");
-        blocks += grad_blocks(l);
+    units = 0;
+    if (tensors <= kGradTensors) {
+        fill_list(0, n, grads, outs, counts, dtypes, &units, &l);
+        e = launch_grads(l, c, stream);
+    } else {
+        GradTable t;
+        t.in = reinterpret_cast<const void**>(c.partials + kGradBlocks + 2);
+        t.out = const_cast<void**>(t.in) + tensors;
+        t.count = reinterpret_cast<int64_t*>(t.out + tensors);
+        t.first = reinterpret_cast<int32_t*>(t.count + tensors);
+        for (int32_t i = 0, at = 0; at < tensors; at += l.n) {
+            i = fill_list(i, n, grads, outs, counts, dtypes, &units, &l);
+            if ((e = launch_grad_table(l, at, t, stream)) != hipSuccess)
+                return fail_hip(e, "kernel launch");
+        }
+        e = launch_grads(t, c, stream);
     }
-    if ((e = launch_grad_norm(partials, blocks, max_norm, norm, factor, stream)) != hipSuccess)
-        return fail_hip(e, "kernel launch");
-    if (max_norm < 0.f) return LFMMI_OK;
-    for (int32_t i = 0; i < n;) {
-        i = fill_list(i, n, grads, outs, counts, dtypes, &l);
-        if (l.n == 0) break;
-        if ((e = launch_grad_scale(l, factor, stream)) != hipSuccess)
-            return fail_hip(e, "kernel launch");
-    }
-    return LFMMI_OK;
+    return e == hipSuccess ? LFMMI_OK : fail_hip(e, "kernel launch");
 }
 
 }  // namespace
@@ -323,7 +351,7 @@ lfmmi_status lfmmi_grad_norm(int32_t n, const void* const* grads, const int64_t*
 try {
     const lfmmi_status st = check_grads(n, grads, counts, dtypes, norm, workspace, workspace_bytes);
     if (st != LFMMI_OK) return st;
-    return run_grads(n, grads, nullptr, counts, dtypes, -1.f, norm, workspace,
+    return run_grads(n, grads, nullptr, counts, dtypes, false, 0.f, norm, workspace,
                      static_cast<hipStream_t>(hip_stream));
 } catch (...) {
     return LFMMI_ERR_OOM;
@@ -338,7 +366,7 @@ try {
     if (st != LFMMI_OK) return st;
     if (!(max_norm >= 0.f)) return fail(LFMMI_ERR_INVALID_ARG, "max_norm must be >= 0");
     if ((st = check_outs(n, grads, outs, counts, dtypes)) != LFMMI_OK) return st;
-    return run_grads(n, grads, outs, counts, dtypes, max_norm, norm, workspace,
+    return run_grads(n, grads, outs, counts, dtypes, true, max_norm, norm, workspace,
                      static_cast<hipStream_t>(hip_stream));
 } catch (...) {
     return LFMMI_ERR_OOM;

@@ -65,11 +65,13 @@ hipError_t launch_token_logprobs(const TokenParams& p, const SeqLengths& lens, i
 hipError_t launch_token_grad(const TokenGradParams& p, const SeqLengths& lens, int dtype,
                              hipStream_t stream);
 
-// Gradients of one launch: values of tensor i are cut into units of kGradUnit, unit numbers
-// run through the tensors.
-constexpr int kGradTensors = 128;
+// Gradient tensors: values of tensor i are cut into units of kGradUnit, counted from the address before
+// its first that kGradAlign divides; unit numbers run through the tensors and begin with first[i]; first[n]
+// is how many there are.
+constexpr int kGradTensors = 128;  // that travel as a kernel argument
 constexpr int kGradUnit = 8192;
-constexpr int kGradBlocks = 1024;  // most workgroups of a launch: one partial sum each
+constexpr int kGradAlign = 128;    // bytes
+constexpr int kGradBlocks = 2048;  // most workgroups of a launch: one partial sum each
 struct GradList {
     const void* in[kGradTensors];
     void* out[kGradTensors];
@@ -77,13 +79,27 @@ struct GradList {
     int32_t first[kGradTensors + 1];
     int32_t n;
 };
+struct GradTable {  // the same in the workspace, for any number
+    const void** in;
+    void** out;
+    int64_t* count;
+    int32_t* first;
+};
 
-// Sums of squares of the values of `l`: a partial sum for each of grad_blocks(l) workgroups.
-int grad_blocks(const GradList& l);
-hipError_t launch_grad_squares(const GradList& l, double* partials, hipStream_t stream);
-// norm and, for max_norm >= 0, the factor that brings it to max_norm, from all partial sums.
-hipError_t launch_grad_norm(const double* partials, int n, float max_norm, float* norm,
-                            float* factor, hipStream_t stream);
-hipError_t launch_grad_scale(const GradList& l, const float* factor, hipStream_t stream);
+struct GradCall {
+    int32_t n, units, blocks;
+    int32_t keep;      // 256ths of a workgroup's units, its last ones, that stay in the caches
+    bool scale;        // the norm alone otherwise
+    bool in_place;     // all tensors are
+    float max_norm;
+    float* norm;
+    float* factor;     // [1] in the workspace
+    double* partials;  // [blocks] there
+};
+
+// Writes tensors from..from + l.n - 1 of a table, and the unit behind them.
+hipError_t launch_grad_table(const GradList& l, int from, const GradTable& t, hipStream_t stream);
+hipError_t launch_grads(const GradList& l, const GradCall& c, hipStream_t stream);
+hipError_t launch_grads(const GradTable& t, const GradCall& c, hipStream_t stream);
 
 }  // namespace lfmmi

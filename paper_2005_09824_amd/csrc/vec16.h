@@ -23,6 +23,12 @@ __device__ __forceinline__ uint4 load16_once(const void* p)
     return make_uint4(v[0], v[1], v[2], v[3]);
 }
 __device__ __forceinline__ void store16(void* p, uint4 v) { __builtin_memcpy(p, &v, 16); }
+__device__ __forceinline__ void store16_once(void* p, uint4 v)
+{
+    typedef uint32_t Words __attribute__((ext_vector_type(4)));
+    typedef Words Anywhere __attribute__((aligned(2)));
+    __builtin_nontemporal_store(Words{v.x, v.y, v.z, v.w}, static_cast<Anywhere*>(p));
+}
 
 typedef __bf16 Bf16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 F16x2 __attribute__((ext_vector_type(2)));

@@ -86,7 +86,7 @@ def _clip(n=2, grads=(P, 2 * P), counts=(10, 10), dtypes=(0, 0), outs=None, max_
     lib = binding.load_library()
     arr = lambda t, v: None if v is None else (t * max(len(v), 1))(*v)
     g, c, d = arr(ctypes.c_void_p, grads), arr(ctypes.c_int64, counts), arr(ctypes.c_int32, dtypes)
-    size = 16 + 8192 * (1 + (max(n, 0) + 127) // 128) if size is None else size
+    size = 16384 + 32 * (max(n, 0) + 1) if size is None else size
     if entry == "norm":
         return lib.lfmmi_grad_norm(n, g, c, d, norm, workspace, size, None)
     return lib.lfmmi_clip_grads(n, g, arr(ctypes.c_void_p, outs), c, d, max_norm, norm, workspace, size, None)
