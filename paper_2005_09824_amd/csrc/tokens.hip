@@ -228,6 +228,11 @@ __device__ __forceinline__ void take(Best& best, float top, int group)
     best.first = fmaxf(best.first, top);
 }
 
+// A row of 16-bit logits that starts at an odd multiple of 2 is read from its second logit on (16-byte loads
+// at odd multiples of 2 take 20 % longer than at 4): `head` is 1 then, and logit -1 comes with those behind
+// the last whole chunk. The i-th of these:
+__device__ __forceinline__ int single(int i, int behind, int head) { return i < head ? -1 : behind + i - head; }
+
 template <typename D, int G>
 __device__ __forceinline__ void load_part(const typename D::Store* x, int full, int q, uint4* r)
 {
@@ -291,7 +296,7 @@ __device__ __forceinline__ bool add_plain(Sums& a, const float (&f)[N], float sc
 // Per logit of 16 bits: half an instruction for the maximum, one to unpack it, one for y, four
 // issue slots for 2^y, one for each sum. `once`: the loads leave nothing in the caches.
 template <typename D, int G, bool Top>
-__device__ __forceinline__ void scan(const typename D::Store* x, int n, int lane, float scale2, bool once,
+__device__ __forceinline__ void scan(const typename D::Store* x, int n, int head, int lane, float scale2, bool once,
                                      Sums& a, Best& best)
 {
     constexpr int kVec = D::kVec, N = kVec * kLoads;
@@ -322,8 +327,8 @@ __device__ __forceinline__ void scan(const typename D::Store* x, int n, int lane
         if (plain) plain = add_plain(a, f, scale2);
         if (!plain) add_any(a, f, chunks, scale2);
     }
-    for (int i = full * kVec + lane; i < n; i += G) {
-        const float f[1] = {D::load(x + i)};
+    for (int i = lane; i < n - full * kVec + head; i += G) {
+        const float f[1] = {D::load(x + single(i, full * kVec, head))};
         shift(a, fmaxf(a.m, f[0]), scale2);
         add_any(a, f, 1, scale2);
     }
@@ -444,7 +449,7 @@ __device__ __forceinline__ void push_if(float v, int at, const Bound& to, Select
 
 // Each wave looks through what its own lanes have read, a chunk a lane.
 template <typename D, int G>
-__device__ __forceinline__ void gather(const typename D::Store* x, int n, int lane, const Best& best,
+__device__ __forceinline__ void gather(const typename D::Store* x, int n, int head, int lane, const Best& best,
                                        const Bound& to, Selection<G>& sel)
 {
     constexpr int kVec = D::kVec;
@@ -484,7 +489,10 @@ __device__ __forceinline__ void gather(const typename D::Store* x, int n, int la
             }
         }
     }
-    for (int i = full * kVec + lane; i < n; i += G) push_if<G>(D::load(x + i), i, to, sel);
+    for (int i = lane; i < n - full * kVec + head; i += G) {
+        const int at = single(i, full * kVec, head);
+        push_if<G>(D::load(x + at), at, to, sel);
+    }
 }
 
 // The index that goes with T: k lanes hold a larger value, or T at an index up to it.
@@ -581,7 +589,7 @@ __device__ __forceinline__ uint32_t offer(int n, int lane, const Best& best, Sel
 
 // The k best of n logits, handed to put(rank, key) by the lane that has one. `own`: what offer gave.
 template <typename D, int G, typename Put>
-__device__ __forceinline__ void select_top(const typename D::Store* x, int n, int lane, int offset, int k,
+__device__ __forceinline__ void select_top(const typename D::Store* x, int n, int head, int lane, int offset, int k,
                                            const Best& best, uint32_t own, Selection<G>& sel, Put&& put)
 {
     constexpr int kCap = Selection<G>::kCap;
@@ -596,14 +604,14 @@ __device__ __forceinline__ void select_top(const typename D::Store* x, int n, in
     }
     if (to.value && count_from(v, to.value) > k + kTies)
         to.last = last_index<D, G>(x, n, lane, best, to.value, k, v, sel);
-    gather<D, G>(x, n, lane, best, to, sel);
+    gather<D, G>(x, n, head, lane, best, to, sel);
     row_sync<G>();
     int count = sel.count;
     if (__builtin_expect(count > kCap && to.value && to.last == INT32_MAX, 0)) {
         to.last = last_index<D, G>(x, n, lane, best, to.value, k, v, sel);
         if (lane == 0) sel.count = 0;
         row_sync<G>();
-        gather<D, G>(x, n, lane, best, to, sel);
+        gather<D, G>(x, n, head, lane, best, to, sel);
         row_sync<G>();
         count = sel.count;
     }
@@ -616,7 +624,7 @@ __device__ __forceinline__ void select_top(const typename D::Store* x, int n, in
     uint64_t last = ~(uint64_t)0;
     for (int rank = 0; rank < k; ++rank) {
         uint64_t top = 0;
-        for (int i = lane; i < n; i += G) {
+        for (int i = lane - head; i < n; i += G) {
             const uint64_t key = key_of(D::load(x + i), offset + i);
             if (key < last && key > top) top = key;
         }
@@ -697,10 +705,10 @@ __global__ __launch_bounds__(threads_of(G)) void k_token(TokenParams p, SeqLengt
     for (uint32_t at = blockIdx.x * kRows + sub; at < units; at += gridDim.x * kRows) {
         const uint32_t unit = G == 64 ? uniform(at) : at;
         const uint32_t row = Split ? unit / p.parts : unit;
-        const int from = Split ? (int)(unit % p.parts) * p.part_size : 0;
-        const int n = Split ? (p.V - from < p.part_size ? p.V - from : p.part_size) : p.V;
+        const int begin = Split ? (int)(unit % p.parts) * p.part_size : 0;
+        const int all = Split ? (p.V - begin < p.part_size ? p.V - begin : p.part_size) : p.V;
         const Row r = row_of<G>(p, lens, row);
-        const Store* x = static_cast<const Store*>(row_at(p, row, sizeof(Store))) + from;
+        const Store* x = static_cast<const Store*>(row_at(p, row, sizeof(Store))) + begin;
         if (!r.live) {
             if (Split) continue;
             if (lane == 0) write_row(p, row, r, no_sums(), 0.f);
@@ -711,7 +719,9 @@ __global__ __launch_bounds__(threads_of(G)) void k_token(TokenParams p, SeqLengt
         Sums a = no_sums();
         Best best{-INFINITY, -INFINITY, 0};
         const float xt = Split ? 0.f : target_logit<D, G>(x, r, p.V);
-        scan<D, G, Top>(x, n, lane, scale2, p.once, a, best);
+        const int head = (uintptr_t)x % 4 ? 1 : 0, n = all - head;
+        x += head;
+        scan<D, G, Top>(x, n, head, lane, scale2, p.once, a, best);
         const uint32_t own = Top ? offer<D>(n, lane, best, sel) : 0;
         a = join_all<G>(a, scale2, shared);
         if (lane == 0) {
@@ -722,14 +732,14 @@ __global__ __launch_bounds__(threads_of(G)) void k_token(TokenParams p, SeqLengt
             const Scores c = scores_of(a);
             if (c.m != c.m || c.m == -INFINITY) {  // no alternatives, or the first tokens
                 for (int k = lane; k < p.top_k; k += G) {
-                    const uint64_t key = c.m != c.m || k >= n ? 0 : key_of(-INFINITY, from + k);
+                    const uint64_t key = c.m != c.m || k >= all ? 0 : key_of(-INFINITY, begin + k);
                     if (Split) part_keys(p, unit)[k] = key;
                     else write_top(p, row, k, key, true, c);
                 }
             } else {
                 row_sync<(G < 64 ? 64 : G)>();
-                const int k = p.top_k < n ? p.top_k : n;
-                select_top<D>(x, n, lane, from, k, best, own, sel, [&](int rank, uint64_t key) {
+                const int k = p.top_k < all ? p.top_k : all;
+                select_top<D>(x, n, head, lane, begin + head, k, best, own, sel, [&](int rank, uint64_t key) {
                     if (Split) part_keys(p, unit)[rank] = key;
                     else write_top(p, row, rank, key, true, c);
                 });
