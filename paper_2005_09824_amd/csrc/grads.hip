@@ -211,12 +211,12 @@ __global__ __launch_bounds__(kThreads) void k_grad_norm(GradCall c)
 __device__ __forceinline__ float scaled(float x, float factor) { return factor == 0.f ? 0.f : x * factor; }
 
 template <typename D>
-__device__ __forceinline__ void scale(const Unit& u, float factor)
+__device__ __forceinline__ void scale(const Unit& u, float factor, bool once)
 {
     using Store = typename D::Store;
     Store* y = reinterpret_cast<Store*>(u.out);
     uint4 r[kUnitLoads<D>];
-    load_unit<D>(u, false, r);
+    load_unit<D>(u, once, r);
 #pragma unroll
     for (int k = 0; k < kUnitLoads<D>; ++k) {
         const int q = threadIdx.x + k * kThreads;
@@ -224,7 +224,10 @@ __device__ __forceinline__ void scale(const Unit& u, float factor)
         D::unpack(r[k], f);
 #pragma unroll
         for (int i = 0; i < D::kVec; ++i) f[i] = scaled(f[i], factor);
-        if (has<D>(u, q)) store16(y + q * D::kVec, D::pack(f));
+        if (has<D>(u, q)) {
+            if (once) store16_once(y + q * D::kVec, D::pack(f));
+            else store16(y + q * D::kVec, D::pack(f));
+        }
     }
     if (u.to - u.from < kGradUnit)
         ends_of<D>(u, [&](int i) {
@@ -243,9 +246,9 @@ __global__ __launch_bounds__(kThreads) void k_grad_scale(List list, GradCall c)
     for (int64_t at = c.units - 1 - (int64_t)blockIdx.x; at >= 0; at -= gridDim.x) {
         const Unit u = unit_of(l, (int)at);
         if (f == 1.f && u.in == u.out) continue;  // nothing to scale
-        if (u.dtype == LFMMI_F32) scale<F32>(u, f);
-        else if (u.dtype == LFMMI_BF16) scale<Bf16>(u, f);
-        else scale<F16>(u, f);
+        if (u.dtype == LFMMI_F32) scale<F32>(u, f, c.keep < 256);
+        else if (u.dtype == LFMMI_BF16) scale<Bf16>(u, f, c.keep < 256);
+        else scale<F16>(u, f, c.keep < 256);
     }
 }
 

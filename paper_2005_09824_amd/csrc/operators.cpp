@@ -336,6 +336,7 @@ try {
         p.grad_logp = at(grad_logp, row);
         p.grad_entropy = at(grad_entropy, row);
         p.grad = static_cast<char*>(grad) + row * V * size;
+        p.once = (int64_t)B * T * V * size > kCacheBytes;
         const hipError_t e = launch_token_grad(p, lens, dtype, static_cast<hipStream_t>(hip_stream));
         if (e != hipSuccess) return fail_hip(e, "kernel launch");
         b += n;

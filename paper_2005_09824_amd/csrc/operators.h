@@ -56,6 +56,7 @@ struct TokenGradParams {
     const float* grad_logp;     // or null
     const float* grad_entropy;  // or null
     void* grad;                 // [B, T, V] contiguous
+    bool once;                  // the logits are too many for the caches
     int32_t pieces, piece;      // how a row is cut (set by the launch)
 };
 

@@ -942,7 +942,10 @@ __global__ __launch_bounds__(kThreads) void k_token_grad(TokenGradParams p, SeqL
         const Store* x = static_cast<const Store*>(row_at(p, row, sizeof(Store))) + from;
         Store* out = static_cast<Store*>(p.grad) + (int64_t)row * p.V + from;
         if (w.zero) {
-            for (int q = lane; q < full; q += G) store16(out + (int64_t)q * D::kVec, make_uint4(0, 0, 0, 0));
+            for (int q = lane; q < full; q += G) {
+                if (p.once) store16_once(out + (int64_t)q * D::kVec, make_uint4(0, 0, 0, 0));
+                else store16(out + (int64_t)q * D::kVec, make_uint4(0, 0, 0, 0));
+            }
             for (int i = full * D::kVec + lane; i < n; i += G) D::store(out + i, 0.f);
             continue;
         }
@@ -951,7 +954,12 @@ __global__ __launch_bounds__(kThreads) void k_token_grad(TokenGradParams p, SeqL
         const float xt = w.target >= from && target < n ? D::load(x + target) : 0.f;
         for (int q = lane; q - lane < full; q += kLoads * G) {
             uint4 r[kLoads];
-            load_part<D, G>(x, full, q, r);
+            if (p.once && q - lane + kLoads * G <= full) {
+#pragma unroll
+                for (int k = 0; k < kLoads; ++k) r[k] = load16_once(x + (int64_t)(q + k * G) * D::kVec);
+            } else {
+                load_part<D, G>(x, full, q, r);
+            }
 #pragma unroll
             for (int k = 0; k < kLoads; ++k) {
                 const int first = (q + k * G) * D::kVec;
@@ -960,7 +968,8 @@ __global__ __launch_bounds__(kThreads) void k_token_grad(TokenGradParams p, SeqL
                 D::unpack(r[k], f);
 #pragma unroll
                 for (int i = 0; i < D::kVec; ++i) f[i] = grad_of<Ent>(w, f[i], false);
-                store16(out + first, D::pack(f));
+                if (p.once) store16_once(out + first, D::pack(f));
+                else store16(out + first, D::pack(f));
                 if (__builtin_expect((uint32_t)(target - first) < (uint32_t)D::kVec, 0))
                     D::store(out + target, grad_of<Ent>(w, xt, true));
             }
