@@ -340,8 +340,9 @@ __device__ __forceinline__ void scan(const typename D::Store* x, int n, int head
 // value of the row, and rarely many more than k values reach it. They lie with the lanes whose
 // largest does, in the group of chunks that the lane has noted, and anywhere with a lane whose second
 // group does too: so one pass finds T, and few chunks are looked at again. What reaches T is put in
-// order by counting, for each, how many are larger. Where more than kTies lanes over k reach T
-// (masked rows, equal logits), or more values than the list holds, T gets an index as well.
+// order by counting, for each, how many are larger. Where more than kTies lanes over k reach T (equal
+// logits) or T is -inf (masked rows) T gets an index as well, and where more values reach it than the list
+// holds those in the list give a higher T.
 constexpr int kTies = 32;
 // Where k is kFew at most, 64 lanes' worth of maxima give a T that hardly more than k values reach; and T
 // need not be the k-th exactly, the last few bits of it are left out.
@@ -385,7 +386,7 @@ __device__ __forceinline__ V kth_value(const V (&v)[N], int k, int more)
 // LDS of one row's selection.
 template <int G>
 struct Selection {
-    static constexpr int kCap = G == 64 ? 512 : G == 256 ? 1024 : 2048;  // keys that it holds
+    static constexpr int kCap = G == 64 ? 512 : 1024;  // keys that it holds
     uint64_t list[kCap];
     uint32_t bins[G == 64 ? 1 : 256];
     int count;
@@ -447,6 +448,12 @@ __device__ __forceinline__ void push_if(float v, int at, const Bound& to, Select
     if (o > to.value || (o == to.value && at <= to.last)) push(sel, (uint64_t)o << 32 | (uint32_t)~(to.offset + at));
 }
 
+template <int G>
+__device__ __forceinline__ bool full_list(const Selection<G>& sel)
+{
+    return (int)uniform((uint32_t)*(volatile const int*)&sel.count) > Selection<G>::kCap;
+}
+
 // Each wave looks through what its own lanes have read, a chunk a lane.
 template <typename D, int G>
 __device__ __forceinline__ void gather(const typename D::Store* x, int n, int head, int lane, const Best& best,
@@ -471,7 +478,8 @@ __device__ __forceinline__ void gather(const typename D::Store* x, int n, int he
         const int each = (full + G - 1) / G;  // chunks of a lane, at most
         const int items = num_one * kLoads + num_deep * each;
         const float least = value_of(max(to.value, ordered(-INFINITY)));  // (below that bits are no number's)
-        for (int w = in_wave; w - in_wave < items; w += 64) {
+        // (a list that is full is only there to give a better bound)
+        for (int w = in_wave; w - in_wave < items && !full_list(sel); w += 64) {
             const int all = w - num_one * kLoads;
             const int from = all < 0 ? w / kLoads : num_one + all / each;
             const int v = __builtin_amdgcn_ds_bpermute((from & 63) * 4, sent);
@@ -525,34 +533,30 @@ __device__ __forceinline__ int last_index(const typename D::Store* x, int n, int
     return (int)~kth_value(w, k - larger, 0);
 }
 
-// Of a list of many keys those that reach the k-th largest of the lanes' own largest: the same bound once
-// more, here exact, since no two keys are the same. Returns their number.
+// A bound of the list's k-th largest key, from every wave's own look at it.
+template <int G>
+__device__ __forceinline__ uint64_t bound_of_list(int lane, int k, int count, const Selection<G>& sel)
+{
+    uint64_t v[Selection<G>::kCap / 64];
+#pragma unroll
+    for (int i = 0; i < Selection<G>::kCap / 64; ++i)
+        v[i] = lane % 64 + 64 * i < count ? sel.list[lane % 64 + 64 * i] : 0;
+    return kth_value(v, k, kNear);
+}
+
+// Leaves of a list of many keys those that can be among the k largest. Returns their number.
 constexpr int kMany = 192;
 template <int G>
 __device__ __forceinline__ int thin_out(int lane, int k, int count, Selection<G>& sel)
 {
     constexpr int kEach = Selection<G>::kCap / G;
-    uint64_t mine[kEach], most = 0;
+    const uint64_t from = bound_of_list(lane, k, count, sel);
+    uint64_t mine[kEach];
 #pragma unroll
-    for (int j = 0; j < kEach; ++j) {
-        mine[j] = lane + j * G < count ? sel.list[lane + j * G] : 0;
-        most = max(most, mine[j]);
-    }
+    for (int j = 0; j < kEach; ++j) mine[j] = lane + j * G < count ? sel.list[lane + j * G] : 0;
     row_sync<G>();
-    uint64_t v[G == 64 ? 1 : 4] = {most};
-    if (G > 64) {
-        sel.list[lane] = most;
-        row_sync<G>();
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            v[i] = 0;
-#pragma unroll
-            for (int j = 0; j < G / 256; ++j) v[i] = max(v[i], sel.list[lane % 64 + 64 * i + 256 * j]);
-        }
-    }
     if (lane == 0) sel.count = 0;
     row_sync<G>();
-    const uint64_t from = kth_value(v, k, kTies);
 #pragma unroll
     for (int j = 0; j < kEach; ++j)
         if (mine[j] && mine[j] >= from) push(sel, mine[j]);
@@ -602,46 +606,25 @@ __device__ __forceinline__ void select_top(const typename D::Store* x, int n, in
     } else {
         to.value = kth_value(v, k, kNear);
     }
-    if (to.value && count_from(v, to.value) > k + kTies)
+    if (to.value && (to.value == ordered(-INFINITY) || count_from(v, to.value) > k + kTies))
         to.last = last_index<D, G>(x, n, lane, best, to.value, k, v, sel);
     gather<D, G>(x, n, head, lane, best, to, sel);
     row_sync<G>();
     int count = sel.count;
-    if (__builtin_expect(count > kCap && to.value && to.last == INT32_MAX, 0)) {
-        to.last = last_index<D, G>(x, n, lane, best, to.value, k, v, sel);
+    while (__builtin_expect(count > kCap, 0)) {
+        // What the list holds gives a higher bound, which at least kCap - k - kNear keys fewer reach.
+        const uint64_t from = bound_of_list(lane, k, kCap, sel);
+        to.value = (uint32_t)(from >> 32);
+        to.last = (int)min(~(uint32_t)from, (uint32_t)INT32_MAX) - offset;
+        row_sync<G>();
         if (lane == 0) sel.count = 0;
         row_sync<G>();
         gather<D, G>(x, n, head, lane, best, to, sel);
         row_sync<G>();
         count = sel.count;
     }
-    if (__builtin_expect(count <= kCap, 1)) {
-        if (count > kMany) count = thin_out(lane, k, count, sel);
-        put_ranked(lane, k, count, sel, put);
-        return;
-    }
-    // a few lanes hold more large values than the list does: one pass for each alternative
-    uint64_t last = ~(uint64_t)0;
-    for (int rank = 0; rank < k; ++rank) {
-        uint64_t top = 0;
-        for (int i = lane - head; i < n; i += G) {
-            const uint64_t key = key_of(D::load(x + i), offset + i);
-            if (key < last && key > top) top = key;
-        }
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) {
-            const uint64_t other = __shfl_xor(top, o, 64);
-            top = other > top ? other : top;
-        }
-        if (G > 64) {
-            row_sync<G>();
-            if (lane % 64 == 0) sel.list[lane / 64] = top;
-            row_sync<G>();
-            for (int w = 0; w < G / 64; ++w) top = sel.list[w] > top ? sel.list[w] : top;
-        }
-        if (lane == 0) put(rank, top);
-        last = top;
-    }
+    if (count > kMany) count = thin_out(lane, k, count, sel);
+    put_ranked(lane, k, count, sel, put);
 }
 
 // ---- forward kernels
@@ -752,14 +735,13 @@ __global__ __launch_bounds__(threads_of(G)) void k_token(TokenParams p, SeqLengt
     }
 }
 
-// Rows of up to kShort logits with alternatives, a wave a row: the logits stay in registers, and take the
+// Rows of up to 64 kEach logits with alternatives, a wave a row: the logits stay in registers, and take the
 // place of the lanes' maxima in the selection.
-constexpr int kShort = 256;
-template <typename D>
+template <typename D, int kEach>
 __global__ __launch_bounds__(kThreads) void k_token_short(TokenParams p, SeqLengths lens)
 {
     using Store = typename D::Store;
-    constexpr int kRows = kThreads / 64, kEach = kShort / 64;
+    constexpr int kRows = kThreads / 64;
     __shared__ Selection<64> sels[kRows];
     const int lane = threadIdx.x % 64;
     auto& sel = sels[threadIdx.x / 64];
@@ -794,10 +776,21 @@ __global__ __launch_bounds__(kThreads) void k_token_short(TokenParams p, SeqLeng
 #pragma unroll
         for (int i = 0; i < kEach; ++i) v[i] = lane + 64 * i < p.V ? ordered(f[i]) : 0;
         const uint32_t least = kth_value(v, p.top_k, kNear);
+        uint32_t least_index = 0;  // ~index that the values equal to `least` have to reach
+        if (count_from(v, least) > kMany) {  // equal logits
+            const int larger = count_from(v, least + 1);
+            uint32_t w[kEach];
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) w[i] = v[i] == least ? ~(uint32_t)(lane + 64 * i) : 0;
+            if (larger < p.top_k) least_index = kth_value(w, p.top_k - larger, kNear);
+        }
         row_sync<64>();
 #pragma unroll
-        for (int i = 0; i < kEach; ++i)
-            if (v[i] && v[i] >= least) push(sel, (uint64_t)v[i] << 32 | (uint32_t)~(lane + 64 * i));
+        for (int i = 0; i < kEach; ++i) {
+            const uint32_t index = ~(uint32_t)(lane + 64 * i);
+            if (v[i] && (v[i] > least || (v[i] == least && index >= least_index)))
+                push(sel, (uint64_t)v[i] << 32 | index);
+        }
         row_sync<64>();
         put_ranked(lane, p.top_k, sel.count, sel,
                    [&](int rank, uint64_t key) { write_top(p, row, rank, key, true, c); });
@@ -1003,10 +996,12 @@ void launch_rows(const TokenParams& p, const SeqLengths& lens, hipStream_t strea
         k_token_join<D, Top><<<blocks(rows), kThreads, 0, stream>>>(p, lens);
     } else if (bytes >= kLongRow && rows <= kComputeUnits) {
         k_token<D, 1024, Top, false><<<blocks(rows), 1024, 0, stream>>>(p, lens);
-    } else if (bytes > (rows < kManyRows ? kWaveRow / 4 : kWaveRow)) {
+    } else if (bytes > (rows < kManyRows || p.top_k > kFew ? kWaveRow / 4 : kWaveRow)) {
         k_token<D, 256, Top, false><<<blocks(rows), 256, 0, stream>>>(p, lens);
-    } else if (Top && p.V <= kShort) {
-        k_token_short<D><<<blocks((rows + 3) / 4), kThreads, 0, stream>>>(p, lens);
+    } else if (Top && p.V <= 256) {
+        k_token_short<D, 4><<<blocks((rows + 3) / 4), kThreads, 0, stream>>>(p, lens);
+    } else if (Top && p.V <= 512) {
+        k_token_short<D, 8><<<blocks((rows + 3) / 4), kThreads, 0, stream>>>(p, lens);
     } else if (Top || p.V > kRowOf16) {
         k_token<D, 64, Top, false><<<blocks((rows + 3) / 4), kThreads, 0, stream>>>(p, lens);
     } else {

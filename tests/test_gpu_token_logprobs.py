@@ -502,3 +502,28 @@ def test_one_thread_holds_all_the_large_values(rows, V, dtype):
     r = binding.lfmmi_token_logprobs(x, None, top_k=64)
     picked = binding.TokenLogprobs(*[None if v is None else v[:: max(1, rows // 3)][:3] for v in r])
     check(some, some.double().cpu().numpy(), None, None, 1.0, 64, picked, grad_too=False)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("V", [300, 900, 4000, 4096, 9001, 60000, 140000])
+def test_masks_of_all_densities(V, dtype):
+    # more and fewer tokens left than alternatives are asked for: scattered, in a block, one
+    # in a stretch, and with few different values
+    torch = _torch()
+    rng = np.random.default_rng(V)
+    keep = [1, 3, 20, 63, 64, 65, 200, V // 20, V // 3, V - 1]
+    x, _ = _logits(rng, (4 * len(keep), V), dtype)
+    for i, n in enumerate(keep):
+        n = min(n, V)
+        mask = torch.ones((4, V), dtype=torch.bool, device="cuda")
+        mask[0, torch.from_numpy(rng.permutation(V)[:n]).cuda()] = False
+        at = int(rng.integers(0, V - n + 1))
+        mask[1, at:at + n] = False
+        mask[2, (torch.arange(n, device="cuda") * 512) % V] = False
+        mask[3] = mask[0]
+        rows = x[4 * i:4 * i + 4]
+        rows[3] = torch.from_numpy(rng.integers(0, 3, V).astype(np.float32)).cuda().to(x.dtype)
+        rows.masked_fill_(mask, -float("inf"))
+    x64 = x.double().cpu().numpy()
+    for top in (1, 20, 64):
+        check(x, x64, None, None, 1.0, top, binding.lfmmi_token_logprobs(x, None, top_k=top), grad_too=False)
