@@ -354,7 +354,8 @@ def _on_stream(dev, stream):
         if torch.cuda.current_device() == dev.index:
             return contextlib.nullcontext(), torch.cuda.current_stream(dev).cuda_stream
         return torch.cuda.device(dev), torch.cuda.current_stream(dev).cuda_stream
-    return torch.cuda.stream(torch.cuda.ExternalStream(stream, device=dev)), stream
+    own = torch.cuda.ExternalStream(stream, device=dev) if stream else torch.cuda.default_stream(dev)
+    return torch.cuda.stream(own), stream
 
 
 def _logit_rows(logits, targets, lengths):

@@ -90,7 +90,7 @@ def token_logprobs(logits, targets, lengths=None, scale=1.0):
     """Log probabilities that rows of logits give to their target tokens (or pdfs, of a frame
     alignment), and the rows' entropies, both differentiable in `logits`.
 
-    logits: CUDA tensor [B, T, V] or [B, V], float32, bfloat16 or float16; targets: int32 or
+    logits: CUDA float tensor [B, T, V] or [B, V]; targets: int32 or
     int64 CUDA tensor [B, T] or [B], negative where a row is not scored; lengths: host ints [B]
     or None; scale: what logits are multiplied by. Returns (logp, entropy, status), rows that
     are not scored 0; rows flagged in `status` (nothing but -inf, a NaN or +inf
@@ -100,6 +100,10 @@ def token_logprobs(logits, targets, lengths=None, scale=1.0):
         _token_cls = _token_class()
     if lengths is not None:
         lengths = np.array(lengths, dtype=np.int32)  # (a copy: backward reads it)
+    if binding._dtype_code(logits.dtype) is None:
+        logits = logits.float()
+    if logits.dim() and logits.shape[-1] > 1 and logits.stride(-1) != 1:
+        logits = logits.contiguous()
     return _token_cls.apply(logits, targets.contiguous(), lengths, float(scale))
 
 

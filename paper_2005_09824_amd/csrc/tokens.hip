@@ -107,7 +107,7 @@ __device__ __forceinline__ Sums no_sums() { return {-3.402823466e38f, 0.f, 0.f};
 
 // (y may be -inf, from a mask or a difference that overflows: clamped where 0 * y is meant to
 // be 0; a NaN stays in 2^y)
-__device__ __forceinline__ float finite(float y) { return fmaxf(y, -1e30f); }
+__device__ __forceinline__ float finite(float y) { return fmaxf(y, -1e20f); }
 
 // Sums taken against m, as they are against `to` >= m.
 __device__ __forceinline__ void shift(Sums& a, float to, float scale2)
@@ -171,7 +171,8 @@ __device__ __forceinline__ Scores scores_of(const Sums& a)
 {
     const int flags = flags_of(a);
     const float bad = flags == 2 ? NAN : -INFINITY;
-    return flags ? Scores{bad, bad} : Scores{a.m, log2f(a.s) * kLn2};
+    // (s is 1 or more but for rounding: no log probability is above 0, no entropy below)
+    return flags ? Scores{bad, bad} : Scores{a.m, log2f(fmaxf(a.s, 1.f)) * kLn2};
 }
 
 // Everything but the alternatives, by one lane.
@@ -184,7 +185,7 @@ __device__ __forceinline__ void write_row(const TokenParams& p, int64_t row, con
     if (r.live) {
         flags = flags_of(a);
         c = scores_of(a);
-        entropy = flags == 2 ? NAN : flags == 1 ? 0.f : c.logs - kLn2 * (a.u / a.s);
+        entropy = flags == 2 ? NAN : flags == 1 ? 0.f : c.logs - kLn2 * fminf(a.u / a.s, 0.f);
         logp = flags ? c.m : (x_target - c.m) * p.scale - c.logs;
         if (r.target >= p.V) {
             flags |= 4;
@@ -270,8 +271,8 @@ __device__ __forceinline__ void add_any(Sums& a, const float (&f)[N], int chunks
 }
 
 // The same with two operations less for each: y = x scale2 - c, c = m scale2 rounded, in one, and no
-// clamp. What c is off by is taken out of the sums. Not for |m| from 1e30 on, where c overflows, and
-// false, with nothing added, where 0 * -inf has come into u.
+// clamp. What c is off by is taken out of the sums, to first order: not for |c| from 4,096 on (there
+// `off` reaches 2^-12, and its square 2^-24). False, with nothing added, where 0 * -inf has come into u.
 template <int N>
 __device__ __forceinline__ bool add_plain(Sums& a, const float (&f)[N], float scale2)
 {
@@ -287,7 +288,7 @@ __device__ __forceinline__ bool add_plain(Sums& a, const float (&f)[N], float sc
     const float usum = (u[0] + u[1]) + (u[2] + u[3]);
     asm volatile("" : "+v"(sum));  // (added up here: after the branch all 2^y would be held until then)
     if (__builtin_amdgcn_ballot_w64(usum != usum)) return false;
-    const float back = 1.f - off * kLn2;  // 2^-off: off is below 2^-24 of c
+    const float back = 1.f - off * kLn2;  // 2^-off
     a.s = fmaf(sum, back, a.s);
     a.u = fmaf(usum - off * sum, back, a.u);
     return true;
@@ -323,7 +324,7 @@ __device__ __forceinline__ void scan(const typename D::Store* x, int n, int head
         const float top = max_of(f);
         if (Top) take(best, top, j);
         shift(a, fmaxf(a.m, top), scale2);
-        plain = plain && !__builtin_amdgcn_ballot_w64(!(fabsf(a.m) < 1e30f));
+        plain = plain && !__builtin_amdgcn_ballot_w64(!(fabsf(a.m * scale2) < 4096.f));
         if (plain) plain = add_plain(a, f, scale2);
         if (!plain) add_any(a, f, chunks, scale2);
     }

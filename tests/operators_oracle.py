@@ -88,13 +88,16 @@ def bound_entropy(V):
 
 def bound_grad(r, targets, scale, g, h, grad, dtype):
     """l is off by what ln s and d are, p by as much relatively; the sum and its products round
-    8 times; the result is rounded to its type once."""
+    8 times; the result is rounded to its type once. A p below the normal range, 2^-126, may be
+    taken as 0: what is lost is at most 2^-126 times what p is multiplied by, g + h (|l| + H), where
+    |l| is about 88 and more (2^-126 is e^-87.3)."""
     N, V = r["p"].shape
     p, l = r["p"], np.where(r["p"] > 0, r["l"], 0.0)
     d = l + np.where(np.isfinite(r["logs"]), r["logs"], 0.0)[:, None]
     off = bound_logp(V, l, d)
     g, h, ent = np.abs(g)[:, None], np.abs(h)[:, None], np.where(np.isfinite(r["entropy"]), r["entropy"], 0)[:, None]
     tol = p * (g + h * (np.abs(l) + ent)) * (off + 16 * U) + p * h * (off + bound_entropy(V))
+    tol = tol + np.minimum(p, 2.0 ** -126) * (g + h * (np.abs(l) + ent))
     if targets is not None:
         at = np.clip(targets, 0, V - 1)
         tol[np.arange(N), at] += 4 * U * g[:, 0]

@@ -527,3 +527,51 @@ def test_masks_of_all_densities(V, dtype):
     x64 = x.double().cpu().numpy()
     for top in (1, 20, 64):
         check(x, x64, None, None, 1.0, top, binding.lfmmi_token_logprobs(x, None, top_k=top), grad_too=False)
+
+
+@pytest.mark.parametrize("scale", [1.0, 0.01, 30.0])
+@pytest.mark.parametrize("offset", [0.0, 90.0, -700.0, 3.0e3, -1.0e5, 1.0e7, 1.0e30])
+def test_logits_far_from_zero(offset, scale):
+    # the same differences anywhere on the scale of the type
+    torch = _torch()
+    rng = np.random.default_rng(17)
+    for V in (100, 2600, 9000):
+        x = torch.from_numpy((rng.normal(0, 3, (4, V)) + offset).astype(np.float32)).cuda()
+        x[3, V // 2:] = -float("inf")
+        targets = torch.from_numpy(rng.integers(0, V // 2, 4)).cuda()
+        r = binding.lfmmi_token_logprobs(x, targets, top_k=5, scale=scale)
+        check(x, x.double().cpu().numpy(), targets, None, scale, 5, r, grad_too=scale == 1.0)
+
+
+def test_certain_tokens():
+    # nearly all of the probability on one token: no log probability above 0, no entropy below
+    torch = _torch()
+    rng = np.random.default_rng(23)
+    for V in (40, 700, 2600, 9000, 70000):
+        x = torch.from_numpy(rng.normal(0, 3, (16, V)).astype(np.float32)).cuda()
+        at = torch.from_numpy(rng.integers(0, V, 16)).cuda()
+        x[torch.arange(16), at] = torch.from_numpy(rng.uniform(20, 200, 16).astype(np.float32)).cuda()
+        x[8:] = torch.where(x[8:] < 15.0, torch.full_like(x[8:], -float("inf")), x[8:])
+        for scale in (1.0, 0.9, 3.3):
+            r = binding.lfmmi_token_logprobs(x, at, top_k=1, scale=scale)
+            check(x, x.double().cpu().numpy(), at, None, scale, 1, r)
+            assert float(r.logp.max()) <= 0.0 and float(r.entropy.min()) >= 0.0 and float(r.top_logp.max()) <= 0.0
+            assert float(r.logp[8:].abs().max()) == 0.0 and float(r.entropy[8:].abs().max()) == 0.0
+
+
+def test_autograd_of_other_layouts_and_the_default_stream():
+    torch = _torch()
+    rng = np.random.default_rng(29)
+    x, _ = _logits(rng, (5, 3, 40), "float32")
+    t = torch.from_numpy(rng.integers(0, 40, (3, 5))).cuda().t()  # not contiguous
+    want, _, _ = chain.token_logprobs(x, t)
+    for y in (x.double(), x.transpose(1, 2).contiguous().transpose(1, 2)):
+        leaf = y.clone(memory_format=torch.preserve_format).requires_grad_()
+        logp, entropy, _ = chain.token_logprobs(leaf, t)
+        assert torch.equal(logp.detach(), want)
+        (logp.sum() + entropy.sum()).backward()
+        assert leaf.grad.shape == leaf.shape and leaf.grad.dtype == leaf.dtype
+    torch.cuda.synchronize()
+    r = binding.lfmmi_token_logprobs(x, t.contiguous(), stream=0)
+    torch.cuda.synchronize()
+    assert torch.equal(r.logp, want)
