@@ -100,6 +100,53 @@ def phase_timers(config, torch, binding, workloads):
     return 0
 
 
+def train_step(steps, warmup, torch, binding, workloads):
+    """A training step of an output layer in front of the full objective (workload 5): logits of a
+    linear layer, chain_loss with the frame log probabilities of an alignment beside it, backward,
+    gradients clipped to a norm, a step against them. Prints one JSON line."""
+    from paper_2005_09824_amd import chain
+    wl = workloads.make_workload(5)
+    lengths, leak = wl["lengths"], wl["leak"]
+    B, T, P = wl["logits"].shape
+    den, num = binding.lfmmi_graph_create(wl["den"]), binding.lfmmi_graph_create_batch(wl["num"])
+    width = 640
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    hidden = torch.randn((B, T, width), generator=gen, device="cuda")
+    alignment = torch.randint(0, P, (B, T), generator=gen, device="cuda")
+    layer = torch.nn.Linear(width, P, device="cuda")
+    parameters = list(layer.parameters())
+
+    def step():
+        for q in parameters:
+            q.grad = None
+        loss = chain.chain_loss(layer(hidden), lengths, num, den, leak, alignment, 0.1)
+        loss.backward()
+        norm = chain.clip_grad_norm(parameters, 1.0)
+        with torch.no_grad():
+            for q in parameters:
+                q.sub_(q.grad, alpha=1e-3)
+        return loss, norm
+
+    for _ in range(warmup):
+        step()
+    torch.cuda.synchronize()
+    t0 = time.perf_counter()
+    for _ in range(steps):
+        loss, norm = step()
+    torch.cuda.synchronize()
+    dt = (time.perf_counter() - t0) / steps
+    frames = int(lengths.sum())
+    print(json.dumps({"metric": "output layer training steps: LF-MMI loss, alignment term, clipping",
+                      "value": frames / dt, "unit": "frames/s", "ms_per_step": dt * 1e3, "steps": steps,
+                      "warmup": warmup, "higher_is_better": True, "dtype": "f32", "data": "synthetic",
+                      "config": {"workload": wl["name"], "batch": B, "frames": frames, "max_len": T, "pdfs": P,
+                                 "hidden": width},
+                      "loss": float(loss.detach()), "grad_norm": float(norm)}))
+    den.close()
+    num.close()
+    return 0
+
+
 def main():
     ap = argparse.ArgumentParser()
     ap.add_argument("--gpus", type=int, default=1)
@@ -112,6 +159,9 @@ def main():
     ap.add_argument("--copy-probe", type=int, default=0, metavar="BYTES",
                     help="only run plain device-to-device copies of BYTES (to calibrate the "
                          "FETCH_SIZE / WRITE_SIZE counters) and exit")
+    ap.add_argument("--train-step", action="store_true",
+                    help="time whole training steps of an output layer on workload 5 instead: loss with an "
+                         "alignment beside it, backward, clipping, update; prints one JSON line of its own")
     ap.add_argument("--phase-timers", action="store_true",
                     help="one call with the whole batch as one launch on a library built with "
                          "-DLFMMI_PHASE_TIMERS: where a frame group of the occupancy kernel "
@@ -141,6 +191,8 @@ def main():
         torch.cuda.synchronize()
         print(json.dumps({"copy_probe_bytes": n * 4, "copies": 4}))
         return 0
+    if args.train_step:
+        return train_step(min(args.steps, 200), args.warmup, torch, binding, workloads)
     if args.phase_timers:
         return phase_timers(args.config, torch, binding, workloads)
     wl = workloads.make_workload(args.config)
