@@ -333,16 +333,17 @@ MAX_TOP = 64   # LFMMI_MAX_TOP
 TokenLogprobs = collections.namedtuple(
     "TokenLogprobs", ["logp", "entropy", "stats", "top_id", "top_logp", "status"])
 
+_NO_CONTEXT = contextlib.nullcontext()
 _dtypes = None
 
 
-def _dtype_code(dtype):
-    """lfmmi_dtype of a torch dtype, None for one that the library does not take."""
+def _dtype_codes():
+    """lfmmi_dtype of each torch dtype that the library takes."""
     global _dtypes
     if _dtypes is None:
         import torch
         _dtypes = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
-    return _dtypes.get(dtype)
+    return _dtypes
 
 
 def _on_stream(dev, stream):
@@ -351,9 +352,8 @@ def _on_stream(dev, stream):
     beside torch's current one."""
     import torch
     if stream is None:
-        if torch.cuda.current_device() == dev.index:
-            return contextlib.nullcontext(), torch.cuda.current_stream(dev).cuda_stream
-        return torch.cuda.device(dev), torch.cuda.current_stream(dev).cuda_stream
+        here = torch.cuda.current_device() == dev.index
+        return (_NO_CONTEXT if here else torch.cuda.device(dev)), torch.cuda.current_stream(dev.index).cuda_stream
     own = torch.cuda.ExternalStream(stream, device=dev) if stream else torch.cuda.default_stream(dev)
     return torch.cuda.stream(own), stream
 
@@ -362,7 +362,7 @@ def _logit_rows(logits, targets, lengths):
     """Checked (dtype code, B, T, V, stride_b, stride_t, lengths, target bytes) of logits
     [B, T, V] or [B, V]."""
     import torch
-    code = _dtype_code(logits.dtype)
+    code = _dtype_codes().get(logits.dtype)
     if not logits.is_cuda or code is None or logits.dim() not in (2, 3):
         raise ValueError("logits must be a float32, bfloat16 or float16 CUDA tensor [B, T, V] or [B, V]")
     shape = logits.shape
@@ -503,7 +503,7 @@ def _grad_arrays(grads, out):
     """Checked host arrays (pointers, output pointers or None, counts, dtype codes) of gradient
     tensors of one device and tensors laid out as they are."""
     devices, dtypes, counts, plain = _described(grads)
-    codes = [_dtype_code(d) for d in dtypes]
+    codes = list(map(_dtype_codes().get, dtypes))
     if devices[0] < 0 or None in codes or devices.count(devices[0]) != len(grads):
         raise ValueError("gradients must be float32, bfloat16 or float16 tensors on one CUDA device")
     if not plain and not all([_dense(g) for g in grads]):

@@ -100,7 +100,7 @@ def token_logprobs(logits, targets, lengths=None, scale=1.0):
         _token_cls = _token_class()
     if lengths is not None:
         lengths = np.array(lengths, dtype=np.int32)  # (a copy: backward reads it)
-    if binding._dtype_code(logits.dtype) is None:
+    if logits.dtype not in binding._dtype_codes():
         logits = logits.float()
     if logits.dim() and logits.shape[-1] > 1 and logits.stride(-1) != 1:
         logits = logits.contiguous()

@@ -73,6 +73,7 @@ constexpr int kGradTensors = 128;  // that travel as a kernel argument
 constexpr int kGradUnit = 8192;
 constexpr int kGradAlign = 128;    // bytes
 constexpr int kGradBlocks = 2048;  // most workgroups of a launch: one partial sum each
+constexpr int kGradAlone = 1024;   // units up to which a call that scales does without a launch for the norm
 struct GradList {
     const void* in[kGradTensors];
     void* out[kGradTensors];
