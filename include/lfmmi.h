@@ -207,7 +207,8 @@ lfmmi_status lfmmi_loss(const lfmmi_graph *num, const lfmmi_graph *den, const fl
                         const int32_t *lengths, int32_t B, int32_t T, int32_t P, float leak,
                         float *objf, float *grad, int32_t *status, void *hip_stream);
 
-/* ---- log probabilities of given tokens, and gradients -------------------- */
+/* ---- log probabilities of given tokens, and gradients --------------------
+ * What a trainer uses beside the sequence loss. No handle: the calls keep nothing. */
 
 /* Types of the arrays below. */
 typedef enum { LFMMI_F32 = 0, LFMMI_BF16 = 1, LFMMI_F16 = 2 } lfmmi_dtype;
@@ -244,7 +245,7 @@ typedef enum { LFMMI_F32 = 0, LFMMI_BF16 = 1, LFMMI_F16 = 2 } lfmmi_dtype;
  *            time, replays of captured graphs among them, need one each.
  * The call enqueues kernels on hip_stream and nothing else: it does not allocate or
  * synchronise and may be captured into a HIP graph. Arrays lie on the current device.
- * The same inputs give the same bits. B == 0 or T == 0 is valid.
+ * The same inputs at the same alignment give the same bits. B == 0 or T == 0 is valid.
  */
 #define LFMMI_MAX_TOP 64
 lfmmi_status lfmmi_token_logprobs(const void *logits, int32_t dtype, int32_t B, int32_t T,
@@ -284,14 +285,14 @@ lfmmi_status lfmmi_token_logprobs_backward(const void *logits, int32_t dtype, in
  *   norm       DEVICE float32 [1]
  *   outs[i]    = grads[i] * min(1, max_norm / norm)
  * grads, outs, counts, dtypes are HOST arrays [n], copied: DEVICE pointers (aligned to an
- * element at least; NULL where the count is 0), numbers of values (0 is valid) and lfmmi_dtype codes. outs NULL, or outs[i] == grads[i],
- * scales in place (nothing is written if norm <= max_norm); otherwise nothing written may
- * overlap any other array of the call, nor may gradients scaled in place be listed twice
- * (LFMMI_ERR_INVALID_ARG). Squares are summed in fp64, in a fixed order (the same inputs give the
- * same bits): values whose squares overflow fp32 do not upset the norm. A norm
- * that is not finite (a NaN or infinite gradient; a norm beyond fp32 counts as infinite) makes every value of
- * outs 0, so that an update does nothing, and `norm` says so. max_norm >= 0, may be
- * infinite.
+ * element at least; NULL where the count is 0), numbers of values (0 is valid) and
+ * lfmmi_dtype codes. outs NULL, or outs[i] == grads[i], scales in place (nothing is written
+ * if norm <= max_norm); otherwise nothing written may overlap any other array of the call,
+ * nor may gradients scaled in place be listed twice (LFMMI_ERR_INVALID_ARG). Squares are
+ * summed in fp64, in a fixed order (the same inputs at the same alignment give the same
+ * bits): values whose squares overflow fp32 do not upset the norm. A norm that is not finite
+ * (a NaN or infinite gradient; a norm beyond fp32 counts as infinite) makes every value of
+ * outs 0, so that an update does nothing, and `norm` says so. max_norm >= 0, may be infinite.
  * workspace: DEVICE, LFMMI_GRAD_WORKSPACE_BYTES(n) bytes, aligned to 16; otherwise as for
  * lfmmi_token_logprobs. The calls enqueue kernels on hip_stream and nothing else.
  */

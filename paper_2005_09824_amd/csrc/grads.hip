@@ -183,6 +183,7 @@ __device__ __forceinline__ double sum_units(const L& l, const GradCall& c)
     return sum;
 }
 
+// Bound by the reads: 1.2e9 bf16 values of 420 tensors 383 us, 6.3 TB/s; 3e8 fp32 184 us, 6.5 TB/s.
 template <typename List>
 __global__ __launch_bounds__(kThreads) void k_grad_squares(List list, GradCall c)
 {
@@ -245,7 +246,7 @@ __device__ __forceinline__ void scale(const Unit& u, float factor, bool once)
 }
 
 // A unit a workgroup, from the last to the first. (2,048 workgroups that go round the units took 17 % longer
-// on 1.2e9 bf16 values.)
+// on 1.2e9 bf16 values: 830 us, 5.8 TB/s, the rate of a copy.)
 // Alone: there is no k_grad_norm before it, every workgroup adds the partial sums up for itself.
 template <typename List, bool Alone>
 __global__ __launch_bounds__(kThreads) void k_grad_scale(List list, GradCall c)
