@@ -96,6 +96,8 @@ def token_logprobs(logits, targets, lengths=None, scale=1.0):
     are not scored 0; rows flagged in `status` (nothing but -inf, a NaN or +inf
     logit, a target out of range) have a log probability that is not finite, and gradient 0."""
     global _token_cls
+    if targets is None:
+        raise ValueError("log probabilities of tokens need targets")
     if _token_cls is None:
         _token_cls = _token_class()
     if lengths is not None:

@@ -247,9 +247,9 @@ __device__ __forceinline__ void load_part(const typename D::Store* x, int full, 
 template <int N>
 __device__ __forceinline__ float max_of(const float (&f)[N])
 {
-    float top = max3(f[0], f[1], f[2]);
+    float top = f[0];
 #pragma unroll
-    for (int i = 3; i + 1 < N; i += 2) top = max3(top, f[i], f[i + 1]);
+    for (int i = 1; i + 1 < N; i += 2) top = max3(top, f[i], f[i + 1]);
     return N % 2 ? top : fmaxf(top, f[N - 1]);
 }
 
@@ -996,7 +996,8 @@ void launch_rows(const TokenParams& p, const SeqLengths& lens, hipStream_t strea
     // in parts, at 1,024 lanes: 1 of 131,072: 5.2 / 9.7, 8.8 / 12.4; 16: 5.7 / 10.8, 9.2 / 13.2;
     //   64: 7.1 / 14.4, 9.5 / 13.5; 1 of 65,536: 5.1 / 11.1, 5.6 / 9.6.
     // 32,000 rows without alternatives at 16 and 64 lanes: 84 logits 5.3, 15.6; 512: 7.6, 14.9 (fp32
-    // 12.3, 14.0).
+    // 12.3, 14.0). Alternatives from registers and from lanes' maxima: 40,000 rows of 84, 8 of them, 33, 43;
+    // 20,000 of 500, 5 of them, 35, 28, 64 of them 51, 79.
     if (p.parts > 1) {
         k_token<D, 256, Top, true><<<blocks(rows * p.parts), 256, 0, stream>>>(p, lens);
         k_token_join<D, Top><<<blocks(rows), kThreads, 0, stream>>>(p, lens);
@@ -1004,9 +1005,11 @@ void launch_rows(const TokenParams& p, const SeqLengths& lens, hipStream_t strea
         k_token<D, 1024, Top, false><<<blocks(rows), 1024, 0, stream>>>(p, lens);
     } else if (bytes > (rows < kManyRows || p.top_k > kFew ? kWaveRow / 4 : kWaveRow)) {
         k_token<D, 256, Top, false><<<blocks(rows), 256, 0, stream>>>(p, lens);
+    } else if (Top && p.V <= 128) {
+        k_token_short<D, 2><<<blocks((rows + 3) / 4), kThreads, 0, stream>>>(p, lens);
     } else if (Top && p.V <= 256) {
         k_token_short<D, 4><<<blocks((rows + 3) / 4), kThreads, 0, stream>>>(p, lens);
-    } else if (Top && p.V <= 512) {
+    } else if (p.top_k > kFew && p.V <= 512) {
         k_token_short<D, 8><<<blocks((rows + 3) / 4), kThreads, 0, stream>>>(p, lens);
     } else if (Top || p.V > kRowOf16) {
         k_token<D, 64, Top, false><<<blocks((rows + 3) / 4), kThreads, 0, stream>>>(p, lens);

@@ -575,3 +575,34 @@ def test_autograd_of_other_layouts_and_the_default_stream():
     r = binding.lfmmi_token_logprobs(x, t.contiguous(), stream=0)
     torch.cuda.synchronize()
     assert torch.equal(r.logp, want)
+
+
+def test_captured_replays_of_rows_in_parts():
+    # rows long enough to be cut: each call has a workspace, replays of two graphs one each
+    torch = _torch()
+    rng = np.random.default_rng(31)
+    V = 150001
+    xs = [_logits(rng, (3, V), "bfloat16")[0] for _ in range(2)]
+    t = torch.from_numpy(rng.integers(0, V, 3)).cuda()
+    binding.lfmmi_token_logprobs(xs[0], t, top_k=40)
+    graphs, outs = [], []
+    for x in xs:
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            outs.append(binding.lfmmi_token_logprobs(x, t, top_k=40))
+        graphs.append(graph)
+    side = torch.cuda.Stream()
+    for k in range(3):
+        for x in xs:
+            x.copy_(torch.randn(x.shape, device="cuda") * (1.0 + k))
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            graphs[0].replay()
+        graphs[1].replay()
+        here = binding.lfmmi_token_logprobs(xs[0], t, top_k=40)
+        torch.cuda.synchronize()
+        check(xs[0], xs[0].double().cpu().numpy(), t, None, 1.0, 40, here, grad_too=False)
+        for x, r in zip(xs, outs):
+            for a, b in zip(r, binding.lfmmi_token_logprobs(x, t, top_k=40)):
+                assert torch.equal(a, b)
