@@ -66,9 +66,13 @@ __device__ __forceinline__ uint64_t all_bits(uint64_t v)
 {
     return (uint64_t)all_bits((uint32_t)(v >> 32)) << 32 | all_bits((uint32_t)v);
 }
-__device__ __forceinline__ uint32_t max_of_four(uint32_t v)  // lanes next to each other
+__device__ __forceinline__ uint32_t max_of_two(uint32_t v)  // lanes next to each other
 {
-    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(v, v, 0xb1, 0xf, 0xf, true));
+    return max(v, (uint32_t)__builtin_amdgcn_update_dpp(v, v, 0xb1, 0xf, 0xf, true));
+}
+__device__ __forceinline__ uint32_t max_of_four(uint32_t v)
+{
+    v = max_of_two(v);
     return max(v, (uint32_t)__builtin_amdgcn_update_dpp(v, v, 0x4e, 0xf, 0xf, true));
 }
 
@@ -406,12 +410,15 @@ __device__ __forceinline__ void row_sync()
 }
 
 // A value for each lane, to be read as each wave's share of all: with more than 256 lanes the
-// largest of four.
+// largest of two or four.
 template <int G>
 __device__ __forceinline__ void put_bin(Selection<G>& sel, int lane, uint32_t v)
 {
     if (G == 256) {
         sel.bins[lane] = v;
+    } else if (G == 512) {
+        v = max_of_two(v);
+        if (lane % 2 == 0) sel.bins[lane / 2] = v;
     } else if (G == 1024) {
         v = max_of_four(v);
         if (lane % 4 == 0) sel.bins[lane / 4] = v;
@@ -992,7 +999,10 @@ void launch_rows(const TokenParams& p, const SeqLengths& lens, hipStream_t strea
     //   4,096 rows of 12,000: 18.8 / 21.6, 20.9 / 32.2; 4,096 of 16,384: 23.8 / 27.2, 23.7 / 34.1;
     //   64 of 8,192: 4.7 / 7.7, 3.4 / 6.0; 256 of 8,192: -, 3.4 / 6.2, 4.2 / 8.2;
     //   256 of 65,536: -, 8.8 / 11.9, 7.0 / 11.1; 512 of 65,536: -, 13.2 / 16.7, 15.8 / 23.0 (a
-    //   compute unit holds one workgroup of 1,024);
+    //   compute unit holds one workgroup of 1,024); at 256 and 512 lanes: 257 of 65,536: 11.6 / 14.4,
+    //   10.2 / 13.7, with 64 alternatives 17.3, 15.8; 257 of 50,021 fp32: 12.3 / 15.9, 10.4 / 15.1, 64:
+    //   21.0, 17.2; 512 of 65,536: 13.2 / 16.1, 13.3 / 16.9, 64: 20.4, 18.6; 768: 18.8 / 21.8, 18.8 / 24.0,
+    //   64: 26.5, 28.3 (two workgroups of 512 a compute unit);
     // in parts, at 1,024 lanes: 1 of 131,072: 5.2 / 9.7, 8.8 / 12.4; 16: 5.7 / 10.8, 9.2 / 13.2;
     //   64: 7.1 / 14.4, 9.5 / 13.5; 1 of 65,536: 5.1 / 11.1, 5.6 / 9.6.
     // 32,000 rows without alternatives at 16 and 64 lanes: 84 logits 5.3, 15.6; 512: 7.6, 14.9 (fp32
@@ -1003,6 +1013,8 @@ void launch_rows(const TokenParams& p, const SeqLengths& lens, hipStream_t strea
         k_token_join<D, Top><<<blocks(rows), kThreads, 0, stream>>>(p, lens);
     } else if (bytes >= kLongRow && rows <= kComputeUnits) {
         k_token<D, 1024, Top, false><<<blocks(rows), 1024, 0, stream>>>(p, lens);
+    } else if (bytes >= kLongRow && rows <= (p.top_k > kFew ? 2 * kComputeUnits : 3 * kComputeUnits / 2)) {
+        k_token<D, 512, Top, false><<<blocks(rows), 512, 0, stream>>>(p, lens);
     } else if (bytes > (rows < kManyRows || p.top_k > kFew ? kWaveRow / 4 : kWaveRow)) {
         k_token<D, 256, Top, false><<<blocks(rows), 256, 0, stream>>>(p, lens);
     } else if (Top && p.V <= 128) {

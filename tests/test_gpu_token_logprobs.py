@@ -606,3 +606,30 @@ def test_captured_replays_of_rows_in_parts():
         for x, r in zip(xs, outs):
             for a, b in zip(r, binding.lfmmi_token_logprobs(x, t, top_k=40)):
                 assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,V", [(200, 36001), (257, 33011), (300, 50021), (385, 40000), (500, 33003), (513, 34567)])
+def test_some_hundred_long_rows(rows, V, dtype):
+    # more rows than compute units, or a few less: random ones, masks, ties, empty ones
+    torch = _torch()
+    rng = np.random.default_rng(rows)
+    x, _ = _logits(rng, (rows, V), dtype)
+    inf = float("inf")
+    hide = torch.from_numpy(rng.random((4, V)) < np.array([[0.5], [0.99], [0.999], [0.9999]])).cuda()
+    for i in range(4):
+        x[1 + i::12] = x[1 + i::12].masked_fill(hide[i], -inf)
+    x[5::12] = -inf
+    x[6::12] = torch.from_numpy(rng.integers(0, 3, V).astype(np.float32)).cuda().to(x.dtype)
+    x[7::12] = 1.25
+    x[8::12] = torch.linspace(-4, 4, V).to(x.dtype).cuda()
+    x[9::12] = x[9::12].masked_fill((torch.arange(V, device="cuda") % 512) != 7, -inf)
+    x[10::12, V // 2] = float("nan")
+    targets = torch.from_numpy(rng.integers(0, V, rows)).cuda()
+    targets[11::24] = -1
+    some = torch.cat([torch.arange(12), torch.arange(rows - 14, rows)]).cuda()
+    x64, t = x[some].double().cpu().numpy(), targets[some]
+    for top in (0, 5, 32, 33, 64):
+        r = binding.lfmmi_token_logprobs(x, targets, top_k=top)
+        picked = binding.TokenLogprobs(*[None if v is None else v[some] for v in r])
+        check(x[some], x64, t, None, 1.0, top, picked, grad_too=top == 0)
