@@ -234,7 +234,7 @@ lfmmi_status lfmmi_token_logprobs_workspace(int32_t dtype, int32_t B, int32_t T,
     if (!known(dtype) || B < 0 || T < 0 || V < 1 || top_k < 0 || top_k > kMaxTop || top_k > V)
         return fail(LFMMI_ERR_INVALID_ARG, "unknown dtype, or a size out of range");
     if ((int64_t)B * T > INT32_MAX) return fail(LFMMI_ERR_UNSUPPORTED, "B * T exceeds 2^31 - 1");
-    *bytes = B > 0 && T > 0 ? (int64_t)plan_tokens((int64_t)B * T, V, (int)dtype_size(dtype), top_k).workspace : 0;
+    *bytes = B > 0 && T > 0 ? (int64_t)plan_tokens((int64_t)B * T, V, top_k).workspace : 0;
     return LFMMI_OK;
 }
 
@@ -253,7 +253,7 @@ try {
     if (top_k > kMaxTop) return fail(LFMMI_ERR_UNSUPPORTED, "top_k exceeds LFMMI_MAX_TOP");
     if (logp && !targets) return fail(LFMMI_ERR_INVALID_ARG, "logp without targets");
     if (B == 0 || T == 0) return LFMMI_OK;
-    const TokenPlan plan = plan_tokens((int64_t)B * T, V, (int)dtype_size(dtype), top_k);
+    const TokenPlan plan = plan_tokens((int64_t)B * T, V, top_k);
     if (plan.workspace > 0 &&
         (!workspace || !aligned(workspace, 16) || workspace_bytes < (int64_t)plan.workspace))
         return fail(LFMMI_ERR_INVALID_ARG, "workspace is null, too small or not aligned to 16 bytes");

@@ -37,12 +37,12 @@ struct TokenParams {
 };
 
 // How a call's rows are cut, and the bytes of workspace that takes.
-constexpr int kMaxParts = 64;
+constexpr int kMaxParts = 64, kMaxPartKeys = 256;  // alternatives of all parts of a row
 struct TokenPlan {
     int32_t parts, part_size;
     size_t workspace;
 };
-TokenPlan plan_tokens(int64_t rows, int V, int size, int top_k);
+TokenPlan plan_tokens(int64_t rows, int V, int top_k);
 
 struct TokenGradParams {
     const void* x;

@@ -809,11 +809,15 @@ __global__ __launch_bounds__(kThreads) void k_token_short(TokenParams p, SeqLeng
     }
 }
 
-// A workgroup a row: joins the parts' sums and alternatives.
+// A workgroup a row: joins the parts' sums and alternatives, of which a lane has one (a key of 0 stands for
+// none, and at least top_k are others). 256 ranked at once took 4 us more than behind a bound; 128 take
+// a few tenths less.
 template <typename D, bool Top>
 __global__ __launch_bounds__(kThreads) void k_token_join(TokenParams p, SeqLengths lens)
 {
     using Store = typename D::Store;
+    static_assert(kMaxPartKeys <= kThreads && kMaxParts <= kThreads, "a lane has one");
+    constexpr int kAtOnce = 128;
     __shared__ Sums shared[kThreads / 64];
     __shared__ Selection<kThreads> sel;
     const int lane = threadIdx.x;
@@ -824,7 +828,6 @@ __global__ __launch_bounds__(kThreads) void k_token_join(TokenParams p, SeqLengt
         const Store* x = static_cast<const Store*>(row_at(p, row, sizeof(Store)));
         Sums a = no_sums();
         const int keys = p.parts * p.top_k;
-        const uint64_t* key = part_keys(p, (int64_t)row * p.parts);
         uint64_t mine = 0;
         float xt = 0.f;
         if (r.live) {
@@ -834,7 +837,7 @@ __global__ __launch_bounds__(kThreads) void k_token_join(TokenParams p, SeqLengt
                 a = {v.x, v.y, v.z};
             }
             if (Top) {
-                for (int i = lane; i < keys; i += kThreads) mine = key[i] > mine ? key[i] : mine;
+                if (lane < keys) mine = part_keys(p, (int64_t)row * p.parts)[lane];
                 sel.list[lane] = mine;
                 if (lane == 0) sel.count = 0;
             }
@@ -846,19 +849,17 @@ __global__ __launch_bounds__(kThreads) void k_token_join(TokenParams p, SeqLengt
             if (!r.live || c.m != c.m) {
                 for (int k = lane; k < p.top_k; k += kThreads) write_top(p, row, k, 0, r.live, c);
             } else {
-                // (k lanes reach the bound, each with kMaxParts * kMaxTop / kThreads keys at most)
-                static_assert(kMaxTop * (kMaxParts * kMaxTop / kThreads) <= Selection<kThreads>::kCap, "");
-                uint64_t v[4];
+                int count = keys;
+                if (keys > kAtOnce) {
+                    uint64_t v[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) v[i] = sel.list[lane % 64 + 64 * i];
-                const uint64_t bound = kth_value(v, p.top_k, 0);
-                __syncthreads();
-                if (mine >= bound)
-                    for (int i = lane; i < keys; i += kThreads)
-                        if (key[i] != 0 && key[i] >= bound) push(sel, key[i]);
-                __syncthreads();
-                int count = sel.count;
-                if (count > kMany) count = thin_out(lane, p.top_k, count, sel);
+                    for (int i = 0; i < 4; ++i) v[i] = sel.list[lane % 64 + 64 * i];
+                    const uint64_t bound = kth_value(v, p.top_k, 0);
+                    __syncthreads();
+                    if (mine >= bound) push(sel, mine);
+                    __syncthreads();
+                    count = sel.count;
+                }
                 put_ranked(lane, p.top_k, count, sel,
                            [&](int rank, uint64_t key) { write_top(p, row, rank, key, true, c); });
             }
@@ -987,7 +988,7 @@ __global__ __launch_bounds__(kThreads) void k_token_grad(TokenGradParams p, SeqL
 
 constexpr int kComputeUnits = 256, kManyRows = 2048;
 constexpr int kRowOf16 = 512;                                                   // logits
-constexpr int64_t kWaveRow = 32 << 10, kLongRow = 64 << 10, kSplitRow = 192 << 10;  // bytes
+constexpr int64_t kWaveRow = 32 << 10, kLongRow = 64 << 10;                       // bytes
 
 template <typename D, bool Top>
 void launch_rows(const TokenParams& p, const SeqLengths& lens, hipStream_t stream)
@@ -1003,8 +1004,6 @@ void launch_rows(const TokenParams& p, const SeqLengths& lens, hipStream_t strea
     //   10.2 / 13.7, with 64 alternatives 17.3, 15.8; 257 of 50,021 fp32: 12.3 / 15.9, 10.4 / 15.1, 64:
     //   21.0, 17.2; 512 of 65,536: 13.2 / 16.1, 13.3 / 16.9, 64: 20.4, 18.6; 768: 18.8 / 21.8, 18.8 / 24.0,
     //   64: 26.5, 28.3 (two workgroups of 512 a compute unit);
-    // in parts, at 1,024 lanes: 1 of 131,072: 5.2 / 9.7, 8.8 / 12.4; 16: 5.7 / 10.8, 9.2 / 13.2;
-    //   64: 7.1 / 14.4, 9.5 / 13.5; 1 of 65,536: 5.1 / 11.1, 5.6 / 9.6.
     // 32,000 rows without alternatives at 16 and 64 lanes: 84 logits 5.3, 15.6; 512: 7.6, 14.9 (fp32
     // 12.3, 14.0). Alternatives from registers and from lanes' maxima: 40,000 rows of 84, 8 of them, 33, 43;
     // 20,000 of 500, 5 of them, 35, 28, 64 of them 51, 79.
@@ -1040,12 +1039,20 @@ hipError_t launch_type(const TokenParams& p, const SeqLengths& lens, hipStream_t
 
 }  // namespace
 
-TokenPlan plan_tokens(int64_t rows, int V, int size, int top_k)
+TokenPlan plan_tokens(int64_t rows, int V, int top_k)
 {
     TokenPlan plan{1, V, 0};
-    if (rows <= 32 && (int64_t)V * size >= kSplitRow) {
-        // 1,024 workgroups fill the chip, and a part of 4,096 logits is worth one
-        const int64_t parts = std::min<int64_t>({1024 / rows, V / 4096, kMaxParts});
+    // A compute unit alone takes 0.05 us for 1,000 logits; in parts there is a second launch, and a second
+    // selection that grows with the alternatives. Microseconds whole and in parts, bf16 and fp16, without / with
+    // 8 alternatives: 1 of 131,072: 8.9 / 12.4, 5.1 / 9.2; 32: 9.4 / 13.2, 6.2 / 12.0; 64 of 160,000: 12.1 / 16.1,
+    // 8.5 / 13.1; 64 of 100,000: 8.6 / 12.3, 7.2 / 13.5; with 20, 48 of 131,072: 13.7, 14.4; with 64, 16 of
+    // 131,072: 15.5, 16.5, of 200,000: 20.5, 18.7. 33 or more rows of 50,021 fp32 without: 6.0, 6.2 to 6.6.
+    const int64_t least = 65536 + (top_k ? 16384 + 768 * rows + 1024 * top_k : 512 * rows);
+    if (rows <= 64 && V >= least) {
+        // Two workgroups a compute unit, a part of 4,096 logits is worth one, and a lane of the join an
+        // alternative: 64 of them for each of 24 parts took 25 us, of 4 parts 16.5.
+        const int64_t parts = std::min<int64_t>(
+            {2 * kComputeUnits / rows, V / 4096, kMaxParts, top_k ? kMaxPartKeys / top_k : kMaxParts});
         // (a multiple of 64 logits: parts of an aligned row are aligned)
         plan.part_size = (int)(((V + parts - 1) / parts + 63) / 64 * 64);
         plan.parts = (V + plan.part_size - 1) / plan.part_size;

@@ -633,3 +633,33 @@ def test_some_hundred_long_rows(rows, V, dtype):
         r = binding.lfmmi_token_logprobs(x, targets, top_k=top)
         picked = binding.TokenLogprobs(*[None if v is None else v[some] for v in r])
         check(x[some], x64, t, None, 1.0, top, picked, grad_too=top == 0)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,V", [(1, 70001), (1, 160003), (7, 140000), (33, 120001), (64, 200003), (65, 130001)])
+def test_few_long_rows_with_any_number_of_alternatives(rows, V, dtype):
+    torch = _torch()
+    rng = np.random.default_rng(V)
+    x, _ = _logits(rng, (rows, V), dtype)
+    inf = float("inf")
+    some = torch.arange(min(rows, 9)).cuda()
+    if rows > 1:
+        x[1] = x[1].masked_fill(torch.from_numpy(rng.random(V) < 0.9998).cuda(), -inf)
+        x[2, : V - 40] = -inf                # all that is left lies in the last part
+        x[3] = -inf
+        x[4] = 1.25
+        x[5] = torch.from_numpy(rng.integers(0, 3, V).astype(np.float32)).cuda().to(x.dtype)
+        x[6, V // 2] = float("nan")
+    if rows > 7:
+        x[7, 1000:] = -inf
+        x[8] = torch.linspace(4, -4, V).to(x.dtype).cuda()
+    targets = torch.from_numpy(rng.integers(0, V, rows)).cuda()
+    if rows > 7:
+        targets[-3] = -1
+    x64, t = x[some].double().cpu().numpy(), targets[some]
+    for top in (0, 1, 2, 5, 8, 13, 20, 21, 32, 40, 64):
+        r = binding.lfmmi_token_logprobs(x, targets, top_k=top)
+        picked = binding.TokenLogprobs(*[None if v is None else v[some] for v in r])
+        check(x[some], x64, t, None, 1.0, top, picked, grad_too=False)
+        if rows > 7:
+            assert not r.logp[-3].any() and not r.entropy[-3].any() and (top == 0 or bool((r.top_id[-3] == -1).all()))
