@@ -682,7 +682,7 @@ __device__ __forceinline__ Sums join_all(Sums a, float scale2, Sums* shared)
 // G lanes a row, or for Split G lanes for each of p.parts parts of a row. Bound by the reads where rows are
 // many: 6,144 rows of 65,536 bf16 132 us, 6.1 TB/s (16-byte loads alone reach 6.9); 2,570 of 131,072 with 5
 // alternatives 122 us, 5.5 TB/s, of which the selection takes 6 us; by latency where they are few: one of 32,000
-// with 8 alternatives 8 us, 4.3 without.
+// with 8 alternatives 7.2 us, 4.4 without.
 template <typename D, int G, bool Top, bool Split>
 __global__ __launch_bounds__(threads_of(G)) void k_token(TokenParams p, SeqLengths lens)
 {
@@ -999,20 +999,24 @@ void launch_rows(const TokenParams& p, const SeqLengths& lens, hipStream_t strea
     // Lanes a row. Microseconds a call, bf16, without / with 8 alternatives, at 64, 256, 1,024 lanes:
     //   4,096 rows of 12,000: 18.8 / 21.6, 20.9 / 32.2; 4,096 of 16,384: 23.8 / 27.2, 23.7 / 34.1;
     //   64 of 8,192: 4.7 / 7.7, 3.4 / 6.0; 256 of 8,192: -, 3.4 / 6.2, 4.2 / 8.2;
-    //   256 of 65,536: -, 8.8 / 11.9, 7.0 / 11.1; 512 of 65,536: -, 13.2 / 16.7, 15.8 / 23.0 (a
-    //   compute unit holds one workgroup of 1,024); at 256 and 512 lanes: 257 of 65,536: 11.6 / 14.4,
-    //   10.2 / 13.7, with 64 alternatives 17.3, 15.8; 257 of 50,021 fp32: 12.3 / 15.9, 10.4 / 15.1, 64:
-    //   21.0, 17.2; 512 of 65,536: 13.2 / 16.1, 13.3 / 16.9, 64: 20.4, 18.6; 768: 18.8 / 21.8, 18.8 / 24.0,
-    //   64: 26.5, 28.3 (two workgroups of 512 a compute unit);
+    //   256 of 65,536: -, 8.8 / 11.9, 7.0 / 11.1 (a compute unit holds one workgroup of 1,024, two of 512);
+    // at 256, 512 and 1,024 lanes: 64 of 8,192: 3.5 / 5.8, 3.6 / 6.3, -; 64 of 16,384: 4.1 / 6.6, 3.9 / 6.5,
+    //   4.1 / 7.6; 64 of 32,000: 5.6 / 8.2, 4.9 / 7.6, 4.8 / 8.4; 64 of 65,536: -, 6.8 / 9.5, 6.2 / 9.8; 128 of
+    //   200,000, with 64 alternatives: -, 16.4 / 25.4, 16.3 / 22.9;
+    // of more rows than compute units at 256 and 512 lanes: 257 of 32,000: 6.8 / 9.4, 6.6 / 10.3; 257 of 65,536:
+    //   11.6 / 14.4, 10.2 / 13.7, with 64 alternatives 17.3, 15.8; 512 of 65,536: 13.2 / 16.1, 13.3 / 16.9,
+    //   with 64 20.4, 18.6; 768: 18.8 / 21.8, 18.8 / 24.0, with 64 26.5, 28.3.
     // 32,000 rows without alternatives at 16 and 64 lanes: 84 logits 5.3, 15.6; 512: 7.6, 14.9 (fp32
     // 12.3, 14.0). Alternatives from registers and from lanes' maxima: 40,000 rows of 84, 8 of them, 33, 43;
     // 20,000 of 500, 5 of them, 35, 28, 64 of them 51, 79.
     if (p.parts > 1) {
         k_token<D, 256, Top, true><<<blocks(rows * p.parts), 256, 0, stream>>>(p, lens);
         k_token_join<D, Top><<<blocks(rows), kThreads, 0, stream>>>(p, lens);
-    } else if (bytes >= kLongRow && rows <= kComputeUnits) {
+    } else if (bytes >= (Top ? 3 : 1) * kLongRow && rows <= kComputeUnits) {
         k_token<D, 1024, Top, false><<<blocks(rows), 1024, 0, stream>>>(p, lens);
-    } else if (bytes >= kLongRow && rows <= (p.top_k > kFew ? 2 * kComputeUnits : 3 * kComputeUnits / 2)) {
+    } else if (rows <= kComputeUnits
+                   ? bytes >= kLongRow / 2
+                   : bytes >= kLongRow && rows <= (p.top_k > kFew ? 2 * kComputeUnits : 3 * kComputeUnits / 2)) {
         k_token<D, 512, Top, false><<<blocks(rows), 512, 0, stream>>>(p, lens);
     } else if (bytes > (rows < kManyRows || p.top_k > kFew ? kWaveRow / 4 : kWaveRow)) {
         k_token<D, 256, Top, false><<<blocks(rows), 256, 0, stream>>>(p, lens);
