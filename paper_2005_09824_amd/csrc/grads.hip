@@ -32,13 +32,30 @@ __device__ __forceinline__ double block_sum(double v)
     return v;
 }
 
-// The tensors of a call: in the kernel's arguments, or for more than kGradTensors of them in the
+// The tensors of a call: in the kernel's arguments, or for more of them than those hold in the
 // workspace.
 struct Listed {
     const GradList& l;
     __device__ const void* in(int i) const { return l.in[i]; }
     __device__ void* out(int i) const { return l.out[i]; }
     __device__ int64_t count(int i) const { return l.count[i]; }
+    __device__ int first(int i) const { return l.first[i]; }
+};
+// Values between the address that kGradAlign divides and a tensor.
+__device__ __forceinline__ int values_before(const void* in, int size)
+{
+    return (int)((uintptr_t)in % kGradAlign) / size;
+}
+struct Placed {
+    const GradPlaces& l;
+    __device__ const void* in(int i) const { return l.in[i]; }
+    __device__ void* out(int i) const { return const_cast<void*>(l.in[i]); }
+    __device__ int64_t count(int i) const
+    {
+        const int dtype = l.rest[i] & 3, over = l.rest[i] >> 2;
+        const int before = values_before(l.in[i], dtype == LFMMI_F32 ? 4 : 2);
+        return ((int64_t)(l.first[i + 1] - l.first[i]) * kGradUnit - before - over) << 2 | dtype;
+    }
     __device__ int first(int i) const { return l.first[i]; }
 };
 // (no kernel that reads the table writes it: constant memory, which a wave reads once for its lanes)
@@ -60,6 +77,7 @@ struct Tensors {
     int n;
 };
 __device__ __forceinline__ Tensors<Listed> tensors(const GradList& l, int n) { return {{l}, n}; }
+__device__ __forceinline__ Tensors<Placed> tensors(const GradPlaces& l, int n) { return {{l}, n}; }
 __device__ __forceinline__ Tensors<Tabled> tensors(const GradTable& t, int n) { return {{t}, n}; }
 
 // The last tensor whose first unit is not after `unit`.
@@ -90,7 +108,7 @@ __device__ __forceinline__ Unit unit_of(const L& l, int u)
     const char* in = static_cast<const char*>(l.list.in(i));
     const int64_t packed = l.list.count(i), count = packed >> 2;
     const int dtype = (int)(packed & 3), size = dtype == LFMMI_F32 ? 4 : 2;
-    const int before = (int)((uintptr_t)in % kGradAlign) / size;
+    const int before = values_before(in, size);
     const int64_t at = (int64_t)(u - l.list.first(i)) * kGradUnit - before, left = count - at;
     return {in + at * size, static_cast<char*>(l.list.out(i)) + at * size, at < 0 ? before : 0,
             left < kGradUnit ? (int)left : kGradUnit, dtype};
@@ -266,23 +284,29 @@ __global__ __launch_bounds__(kThreads) void k_grad_scale(List list, GradCall c)
 }
 
 // Tensors from..from + l.n - 1 of a table (behind the last one, the number of units).
-__global__ __launch_bounds__(kGradTensors) void k_grad_table(GradList l, int from, GradTable t)
+template <typename List>
+__global__ __launch_bounds__(kThreads) void k_grad_table(List list, int from, GradTable t)
 {
-    const int i = threadIdx.x;
-    if (i < l.n) {
-        t.in[from + i] = l.in[i];
-        t.out[from + i] = l.out[i];
-        t.count[from + i] = l.count[i];
-        t.first[from + i] = l.first[i];
+    const auto l = tensors(list, list.n);
+    for (int i = threadIdx.x; i < l.n; i += kThreads) {
+        t.in[from + i] = l.list.in(i);
+        t.out[from + i] = l.list.out(i);
+        t.count[from + i] = l.list.count(i);
+        t.first[from + i] = l.list.first(i);
     }
-    if (i == 0) t.first[from + l.n] = l.first[l.n];
+    if (threadIdx.x == 0) t.first[from + l.n] = l.list.first(l.n);
 }
 
 }  // namespace
 
 hipError_t launch_grad_table(const GradList& l, int from, const GradTable& t, hipStream_t stream)
 {
-    k_grad_table<<<1, kGradTensors, 0, stream>>>(l, from, t);
+    k_grad_table<<<1, kThreads, 0, stream>>>(l, from, t);
+    return hipGetLastError();
+}
+hipError_t launch_grad_table(const GradPlaces& l, int from, const GradTable& t, hipStream_t stream)
+{
+    k_grad_table<<<1, kThreads, 0, stream>>>(l, from, t);
     return hipGetLastError();
 }
 
@@ -306,6 +330,7 @@ hipError_t launch(const List& list, const GradCall& c, hipStream_t stream)
 }  // namespace
 
 hipError_t launch_grads(const GradList& l, const GradCall& c, hipStream_t stream) { return launch(l, c, stream); }
+hipError_t launch_grads(const GradPlaces& l, const GradCall& c, hipStream_t stream) { return launch(l, c, stream); }
 hipError_t launch_grads(const GradTable& t, const GradCall& c, hipStream_t stream) { return launch(t, c, stream); }
 
 }  // namespace lfmmi

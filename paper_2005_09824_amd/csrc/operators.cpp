@@ -153,23 +153,66 @@ int64_t units_of(const void* grad, int64_t count, int32_t dtype)
     return (before + count + kGradUnit - 1) / kGradUnit;
 }
 
+struct Grads {
+    int32_t n;
+    const void* const* in;
+    void* const* out;  // or null: in place
+    const int64_t* counts;
+    const int32_t* dtypes;
+};
+
+void set(GradList* l, const Grads& g, int32_t i, int64_t)
+{
+    l->out[l->n] = g.out ? g.out[i] : const_cast<void*>(g.in[i]);
+    l->count[l->n] = g.counts[i] << 2 | g.dtypes[i];
+}
+
+void set(GradPlaces* l, const Grads& g, int32_t i, int64_t units)
+{
+    const int64_t before = (int64_t)(reinterpret_cast<uintptr_t>(g.in[i]) % kGradAlign / dtype_size(g.dtypes[i]));
+    l->rest[l->n] = (uint16_t)((units * kGradUnit - before - g.counts[i]) << 2 | g.dtypes[i]);
+}
+
 // Tensors from `from` on that a list takes, and the one behind them; `units` is counted on.
-int32_t fill_list(int32_t from, int32_t n, const void* const* grads, void* const* outs,
-                  const int64_t* counts, const int32_t* dtypes, int64_t* units, GradList* l)
+template <typename List>
+int32_t fill_list(const Grads& g, int32_t from, int64_t* units, List* l)
 {
     l->n = 0;
     int32_t i = from;
-    for (; i < n && l->n < kGradTensors; ++i) {
-        if (counts[i] == 0) continue;
-        l->in[l->n] = grads[i];
-        l->out[l->n] = outs ? outs[i] : const_cast<void*>(grads[i]);
-        l->count[l->n] = counts[i] << 2 | dtypes[i];
+    for (; i < g.n && l->n < List::kTensors; ++i) {
+        if (g.counts[i] == 0) continue;
+        const int64_t of_it = units_of(g.in[i], g.counts[i], g.dtypes[i]);
+        l->in[l->n] = g.in[i];
         l->first[l->n] = (int32_t)*units;
-        *units += units_of(grads[i], counts[i], dtypes[i]);
+        set(l, g, i, of_it);
+        *units += of_it;
         ++l->n;
     }
     l->first[l->n] = (int32_t)*units;
     return i;
+}
+
+// Launches for `tensors` tensors that are not empty.
+template <typename List>
+hipError_t launch_list(const Grads& g, int32_t tensors, const GradCall& c, hipStream_t stream)
+{
+    List l;
+    int64_t units = 0;
+    if (tensors <= List::kTensors) {
+        fill_list(g, 0, &units, &l);
+        return launch_grads(l, c, stream);
+    }
+    GradTable t;
+    t.in = reinterpret_cast<const void**>(c.partials + kGradBlocks + 2);
+    t.out = const_cast<void**>(t.in) + tensors;
+    t.count = reinterpret_cast<int64_t*>(t.out + tensors);
+    t.first = reinterpret_cast<int32_t*>(t.count + tensors);
+    for (int32_t i = 0, at = 0; at < tensors; at += l.n) {
+        i = fill_list(g, i, &units, &l);
+        const hipError_t e = launch_grad_table(l, at, t, stream);
+        if (e != hipSuccess) return e;
+    }
+    return launch_grads(t, c, stream);
 }
 
 // The norm, and with `scale` outs.
@@ -201,25 +244,11 @@ lfmmi_status run_grads(int32_t n, const void* const* grads, void* const* outs,
     c.norm = norm;
     c.partials = static_cast<double*>(workspace);
     c.factor = reinterpret_cast<float*>(c.partials + kGradBlocks);
-    GradList l;
-    hipError_t e;
-    units = 0;
-    if (tensors <= kGradTensors) {
-        fill_list(0, n, grads, outs, counts, dtypes, &units, &l);
-        e = launch_grads(l, c, stream);
-    } else {
-        GradTable t;
-        t.in = reinterpret_cast<const void**>(c.partials + kGradBlocks + 2);
-        t.out = const_cast<void**>(t.in) + tensors;
-        t.count = reinterpret_cast<int64_t*>(t.out + tensors);
-        t.first = reinterpret_cast<int32_t*>(t.count + tensors);
-        for (int32_t i = 0, at = 0; at < tensors; at += l.n) {
-            i = fill_list(i, n, grads, outs, counts, dtypes, &units, &l);
-            if ((e = launch_grad_table(l, at, t, stream)) != hipSuccess)
-                return fail_hip(e, "kernel launch");
-        }
-        e = launch_grads(t, c, stream);
-    }
+    const Grads g{n, grads, outs, counts, dtypes};
+    // (replays of clipping in place 150 tensors of 30,000 fp32 values: 7.4 us by one list, 10.9 by a table that two
+    // launches write; of 800,000: 80.7, 85.2)
+    const hipError_t e = in_place ? launch_list<GradPlaces>(g, tensors, c, stream)
+                                  : launch_list<GradList>(g, tensors, c, stream);
     return e == hipSuccess ? LFMMI_OK : fail_hip(e, "kernel launch");
 }
 

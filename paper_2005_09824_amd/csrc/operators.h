@@ -69,17 +69,24 @@ hipError_t launch_token_grad(const TokenGradParams& p, const SeqLengths& lens, i
 // Gradient tensors: values of tensor i are cut into units of kGradUnit, counted from the address before
 // its first that kGradAlign divides; unit numbers run through the tensors and begin with first[i]; first[n]
 // is how many there are.
-constexpr int kGradTensors = 128;  // that travel as a kernel argument
 constexpr int kGradUnit = 8192;
 constexpr int kGradAlign = 128;    // bytes
 constexpr int kGradBlocks = 2048;  // most workgroups of a launch: one partial sum each
 constexpr int kGradAlone = 1024;   // units up to which a call that scales does without a launch for the norm
-struct GradList {
-    const void* in[kGradTensors];
-    void* out[kGradTensors];
-    int64_t count[kGradTensors];  // << 2 | lfmmi_dtype
-    int32_t first[kGradTensors + 1];
+struct GradList {  // tensors that travel as a kernel argument, of 4 KB with a GradCall
+    static constexpr int kTensors = 128;
+    const void* in[kTensors];
+    void* out[kTensors];
+    int64_t count[kTensors];  // << 2 | lfmmi_dtype
+    int32_t first[kTensors + 1];
     int32_t n;
+};
+struct GradPlaces {  // more of them, that are not written, or in place
+    static constexpr int kTensors = 280;
+    const void* in[kTensors];
+    int32_t first[kTensors + 1];
+    int32_t n;
+    uint16_t rest[kTensors];  // what its last unit has behind the tensor, << 2 | lfmmi_dtype
 };
 struct GradTable {  // the same in the workspace, for any number
     const void** in;
@@ -99,9 +106,14 @@ struct GradCall {
     double* partials;  // [blocks] there
 };
 
+static_assert(sizeof(GradList) + sizeof(GradCall) <= 4096 && sizeof(GradPlaces) + sizeof(GradCall) <= 4096, "");
+static_assert(kGradUnit << 2 <= 1 << 16, "`rest` has 16 bits");
+
 // Writes tensors from..from + l.n - 1 of a table, and the unit behind them.
 hipError_t launch_grad_table(const GradList& l, int from, const GradTable& t, hipStream_t stream);
+hipError_t launch_grad_table(const GradPlaces& l, int from, const GradTable& t, hipStream_t stream);
 hipError_t launch_grads(const GradList& l, const GradCall& c, hipStream_t stream);
+hipError_t launch_grads(const GradPlaces& l, const GradCall& c, hipStream_t stream);
 hipError_t launch_grads(const GradTable& t, const GradCall& c, hipStream_t stream);
 
 }  // namespace lfmmi

@@ -222,3 +222,36 @@ def test_parameters():
     assert unused.grad is None
     with pytest.raises(ValueError):
         chain.clip_grad_norm([unused], 1.0)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n", [127, 128, 129, 279, 280, 281, 561])
+def test_any_number_of_tensors_at_any_address(n, dtype):
+    # slices of one buffer, whose values between them are NaN and stay as they were
+    torch = _torch()
+    rng = np.random.default_rng(n)
+    sizes = rng.choice([0, 1, 2, 31, 64, 1000, 8128, 8191, 8192, 8193, 16384, 20000], n)
+    gaps = rng.integers(1, 70, n)
+    at = np.cumsum(gaps + np.concatenate([[0], sizes[:-1]]))
+    total = int(at[-1] + sizes[-1] + 50)
+    base = torch.full((total,), float("nan"), dtype=getattr(torch, dtype), device="cuda")
+    for a, size in zip(at, sizes):
+        base[a:a + size] = torch.from_numpy(rng.normal(0, 2, size).astype(np.float32)).to(base.dtype)
+    whole = base.clone()
+    views = lambda b: [b[a:a + size] for a, size in zip(at.tolist(), sizes.tolist())]
+    norm64 = _norm64(views(whole))
+    norm = binding.lfmmi_grad_norm(views(base))
+    assert abs(float(norm) - norm64) <= 1.01 * oracle.U * norm64
+    out = whole.clone()
+    assert torch.equal(binding.lfmmi_clip_grads(views(base), norm64 * 0.4, out=views(out)), norm)
+    assert torch.equal(base.view(torch.uint8), whole.view(torch.uint8))
+    assert torch.equal(binding.lfmmi_clip_grads(views(base), norm64 * 0.4), norm)
+    _check_scaled(views(base), views(whole), norm64, norm64 * 0.4)
+    assert torch.equal(base.view(torch.uint8), out.view(torch.uint8))
+    between = torch.ones(total, dtype=torch.bool, device="cuda")
+    for a, size in zip(at, sizes):
+        between[a:a + size] = False
+    assert bool(torch.isnan(base[between]).all()) and not bool(torch.isnan(base[~between]).any())
+    again = binding.lfmmi_clip_grads(views(base), norm64)
+    assert abs(float(again) - 0.4 * norm64) <= 0.01 * norm64
+    assert torch.equal(base.view(torch.uint8), out.view(torch.uint8))
