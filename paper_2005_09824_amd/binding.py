@@ -377,6 +377,8 @@ def _logit_rows(logits, targets, lengths):
         stride_t = V
     if step != 1 and V > 1:
         raise ValueError("the logits of a row must be next to each other")
+    if B * T >= 1 << 31 or V > 1 << 30:   # (ctypes would pass on the lowest 32 bits)
+        raise ValueError("too many rows or columns")
     bytes_ = 0
     if targets is not None:
         if targets.dtype == torch.int64:

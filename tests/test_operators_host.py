@@ -167,3 +167,23 @@ def test_oracle_rows_by_hand():
     r = oracle.rows([[1.0, -np.inf, 1.0]], np.array([2]), [True], 1.0, 3)
     assert abs(r["logp"][0] + np.log(2)) < 1e-15 and abs(r["entropy"][0] - np.log(2)) < 1e-15
     assert r["top_id"].tolist() == [[0, 2, 1]] and r["top_logp"][0, 2] == -np.inf
+
+
+class _OnGpu:
+    """What the binding asks of a tensor of `shape` on a GPU."""
+    is_cuda = True
+
+    def __init__(self, shape):
+        import torch
+        t = torch.empty(1, dtype=torch.float32).expand(shape)
+        self.dtype, self.shape, self.device = t.dtype, t.shape, t.device
+        self.dim, self.stride = t.dim, lambda: t.stride()[:-1] + (1,)
+
+
+@pytest.mark.parametrize("shape", [((1 << 32) + 5, 4), (1 << 31, 4), (3, (1 << 32) + 7), (2, (1 << 32) + 1, 4),
+                                   ((1 << 32) + 1, 2, 4), (1 << 20, 1 << 20, 4), (2, 3, 1 << 33)])
+def test_sizes_beyond_the_libraries_types_are_refused(shape):
+    # (a size that is passed on as its lowest 32 bits scores the first rows or columns alone)
+    with pytest.raises(ValueError, match="too many rows or columns"):
+        binding._logit_rows(_OnGpu(shape), None, None)
+    assert binding._logit_rows(_OnGpu((5, 3, 4)), None, None)[:4] == (0, 5, 3, 4)
