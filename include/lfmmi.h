@@ -288,7 +288,8 @@ lfmmi_status lfmmi_token_logprobs_backward(const void *logits, int32_t dtype, in
  * element at least; NULL where the count is 0), numbers of values (0 is valid) and
  * lfmmi_dtype codes. outs NULL, or outs[i] == grads[i], scales in place (nothing is written
  * if norm <= max_norm); otherwise nothing written may overlap any other array of the call,
- * nor may gradients scaled in place be listed twice (LFMMI_ERR_INVALID_ARG). Squares are
+ * nor may gradients scaled in place be listed twice (LFMMI_ERR_INVALID_ARG); norm and
+ * workspace are written by both calls. Squares are
  * summed in fp64, in a fixed order (the same inputs at the same alignment give the same
  * bits): values whose squares overflow fp32 do not upset the norm. A norm that is not finite
  * (a NaN or infinite gradient; a norm beyond fp32 counts as infinite) makes every value of

@@ -79,6 +79,26 @@ const void* at_bytes(const void* p, int64_t i)
     return p ? static_cast<const char*>(p) + i : nullptr;
 }
 
+// What both calls write beside gradients.
+struct Written {
+    uintptr_t norm, workspace, workspace_end;
+    bool meets(uintptr_t at, uintptr_t end) const
+    {
+        return (at < norm + sizeof(float) && norm < end) || (at < workspace_end && workspace < end);
+    }
+};
+
+Written written_by(int32_t n, const float* norm, const void* workspace)
+{
+    const uintptr_t w = reinterpret_cast<uintptr_t>(workspace);
+    return {reinterpret_cast<uintptr_t>(norm), w, w + (uintptr_t)LFMMI_GRAD_WORKSPACE_BYTES(n)};
+}
+
+lfmmi_status fail_written()
+{
+    return fail(LFMMI_ERR_INVALID_ARG, "norm or workspace overlaps another array");
+}
+
 lfmmi_status check_grads(int32_t n, const void* const* grads, const int64_t* counts,
                          const int32_t* dtypes, const float* norm, const void* workspace,
                          int64_t workspace_bytes)
@@ -89,6 +109,9 @@ lfmmi_status check_grads(int32_t n, const void* const* grads, const int64_t* cou
         return fail(LFMMI_ERR_INVALID_ARG, "grads / counts / dtypes is null");
     if (!workspace || !aligned(workspace, 16) || workspace_bytes < LFMMI_GRAD_WORKSPACE_BYTES(n))
         return fail(LFMMI_ERR_INVALID_ARG, "workspace is null, too small or not aligned to 16 bytes");
+    const Written written = written_by(n, norm, workspace);
+    if (written.norm < written.workspace_end && written.workspace < written.norm + sizeof(float))
+        return fail_written();
     for (int32_t i = 0; i < n; ++i) {
         if (!known(dtypes[i])) return fail(LFMMI_ERR_INVALID_ARG, "unknown dtype");
         if (counts[i] < 0) return fail(LFMMI_ERR_INVALID_ARG, "counts must be >= 0");
@@ -97,6 +120,9 @@ lfmmi_status check_grads(int32_t n, const void* const* grads, const int64_t* cou
             return fail(LFMMI_ERR_INVALID_ARG, "grads[" + std::to_string(i) + "] is null");
         if (!aligned(grads[i], dtype_size(dtypes[i])))
             return fail(LFMMI_ERR_INVALID_ARG, "a gradient is not aligned to its elements");
+        const uintptr_t at = reinterpret_cast<uintptr_t>(grads[i]);
+        if (counts[i] > 0 && written.meets(at, at + (uintptr_t)counts[i] * dtype_size(dtypes[i])))
+            return fail_written();
     }
     return LFMMI_OK;
 }
@@ -122,7 +148,7 @@ bool overlap(std::vector<Span>& spans)
 }
 
 lfmmi_status check_outs(int32_t n, const void* const* grads, void* const* outs,
-                        const int64_t* counts, const int32_t* dtypes)
+                        const int64_t* counts, const int32_t* dtypes, const Written& written)
 {
     std::vector<Span> spans;
     spans.reserve(2 * (size_t)n);
@@ -136,6 +162,7 @@ lfmmi_status check_outs(int32_t n, const void* const* grads, void* const* outs,
             if (!aligned(outs[i], dtype_size(dtypes[i])))
                 return fail(LFMMI_ERR_INVALID_ARG, "an output is not aligned to its elements");
             out = reinterpret_cast<uintptr_t>(outs[i]);
+            if (written.meets(out, out + bytes)) return fail_written();
         }
         spans.push_back({out, out + bytes, true});
         if (out != in) spans.push_back({in, in + bytes, false});
@@ -395,7 +422,8 @@ try {
     lfmmi_status st = check_grads(n, grads, counts, dtypes, norm, workspace, workspace_bytes);
     if (st != LFMMI_OK) return st;
     if (!(max_norm >= 0.f)) return fail(LFMMI_ERR_INVALID_ARG, "max_norm must be >= 0");
-    if ((st = check_outs(n, grads, outs, counts, dtypes)) != LFMMI_OK) return st;
+    if ((st = check_outs(n, grads, outs, counts, dtypes, written_by(n, norm, workspace))) != LFMMI_OK)
+        return st;
     return run_grads(n, grads, outs, counts, dtypes, true, max_norm, norm, workspace,
                      static_cast<hipStream_t>(hip_stream));
 } catch (...) {

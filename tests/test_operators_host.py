@@ -187,3 +187,20 @@ def test_sizes_beyond_the_libraries_types_are_refused(shape):
     with pytest.raises(ValueError, match="too many rows or columns"):
         binding._logit_rows(_OnGpu(shape), None, None)
     assert binding._logit_rows(_OnGpu((5, 3, 4)), None, None)[:4] == (0, 5, 3, 4)
+
+
+@pytest.mark.parametrize("kw", [
+    dict(norm=P + 36), dict(norm=2 * P), dict(workspace=P), dict(grads=(P, 40 * P), workspace=40 * P - 16384), dict(workspace=2 * P + 32),
+    dict(norm=128 * P + 16), dict(norm=128 * P + 16384 + 32 * 3 - 4), dict(norm=128 * P),
+    dict(grads=(P, 128 * P + 16384 + 92)), dict(n=1, grads=(128 * P - 8,), counts=(3,), dtypes=(0,)),
+])
+@pytest.mark.parametrize("entry", ["clip", "norm"])
+def test_norm_and_workspace_overlap_nothing(kw, entry):
+    # (a table of addresses in the workspace, scaled like a gradient, would send writes anywhere)
+    assert _clip(entry=entry, **kw) == INVALID and "norm or workspace overlaps" in binding.lfmmi_last_error()
+
+
+@pytest.mark.parametrize("outs", [(64 * P - 36, 8 * P), (64 * P, 8 * P), (8 * P, 128 * P + 16384 + 32 * 3 - 4),
+                                  (8 * P, 128 * P - 36)])
+def test_outputs_overlap_neither_norm_nor_workspace(outs):
+    assert _clip(outs=outs) == INVALID and "norm or workspace overlaps" in binding.lfmmi_last_error()
