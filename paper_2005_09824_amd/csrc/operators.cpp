@@ -289,6 +289,7 @@ lfmmi_status lfmmi_token_logprobs_workspace(int32_t dtype, int32_t B, int32_t T,
     if (!bytes) return fail(LFMMI_ERR_INVALID_ARG, "bytes is null");
     if (!known(dtype) || B < 0 || T < 0 || V < 1 || top_k < 0 || top_k > kMaxTop || top_k > V)
         return fail(LFMMI_ERR_INVALID_ARG, "unknown dtype, or a size out of range");
+    if (V > (1 << 30)) return fail(LFMMI_ERR_UNSUPPORTED, "V exceeds 2^30");
     if ((int64_t)B * T > INT32_MAX) return fail(LFMMI_ERR_UNSUPPORTED, "B * T exceeds 2^31 - 1");
     *bytes = B > 0 && T > 0 ? (int64_t)plan_tokens((int64_t)B * T, V, top_k).workspace : 0;
     return LFMMI_OK;

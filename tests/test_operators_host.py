@@ -204,3 +204,12 @@ def test_norm_and_workspace_overlap_nothing(kw, entry):
                                   (8 * P, 128 * P - 36)])
 def test_outputs_overlap_neither_norm_nor_workspace(outs):
     assert _clip(outs=outs) == INVALID and "norm or workspace overlaps" in binding.lfmmi_last_error()
+
+
+def test_workspace_of_rows_that_the_call_refuses():
+    lib = binding.load_library()
+    n = ctypes.c_int64(-1)
+    for V in ((1 << 30) + 1, (1 << 31) - 1):
+        assert lib.lfmmi_token_logprobs_workspace(1, 1, 1, V, 0, ctypes.byref(n)) == UNSUPPORTED, n.value
+        assert "V" in binding.lfmmi_last_error()
+    assert lib.lfmmi_token_logprobs_workspace(1, 1, 1, 1 << 30, 0, ctypes.byref(n)) == 0 and n.value > 0
