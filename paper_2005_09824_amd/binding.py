@@ -358,6 +358,13 @@ def _on_stream(dev, stream):
     return torch.cuda.stream(own), stream
 
 
+def _written(tensors):
+    """Tells autograd that the caller's `tensors` have new values, as torch's own operations in
+    place do: a graph that has saved one of them then refuses its backward pass."""
+    import torch
+    torch.autograd.graph.increment_version(tensors)
+
+
 def _logit_rows(logits, targets, lengths):
     """Checked (dtype code, B, T, V, stride_b, stride_t, lengths, target bytes) of logits
     [B, T, V] or [B, V]."""
@@ -418,8 +425,9 @@ def lfmmi_token_logprobs(logits, targets=None, lengths=None, top_k=0, scale=1.0,
     top_k = int(top_k)
     context, raw = _on_stream(dev, stream)
     lib = load_library()
+    mine = out is None
     with context:
-        if out is None:
+        if mine:
             f32, i32 = torch.float32, torch.int32
             if not 0 <= top_k <= MAX_TOP:
                 raise ValueError("top_k outside [0, MAX_TOP]")
@@ -449,6 +457,8 @@ def lfmmi_token_logprobs(logits, targets=None, lengths=None, top_k=0, scale=1.0,
             _ptr(targets), target_bytes, scale, top_k, _ptr(out.logp), _ptr(out.entropy),
             _ptr(out.stats), _ptr(out.top_id), _ptr(out.top_logp), _ptr(out.status), _ptr(ws),
             need.value, raw))
+    if not mine:
+        _written([t for t in out if t is not None])
     return out
 
 
@@ -469,8 +479,9 @@ def lfmmi_token_logprobs_backward(logits, targets, stats, entropy, grad_logp=Non
                               not t.is_contiguous() or t.device != dev):
             raise ValueError("stats, entropy or a gradient has the wrong shape, dtype, layout or device")
     context, raw = _on_stream(dev, stream)
+    mine = grad is None
     with context:
-        if grad is None:
+        if mine:
             grad = torch.empty(logits.shape, dtype=logits.dtype, device=dev)
         elif grad.shape != logits.shape or grad.dtype != logits.dtype or not grad.is_contiguous() \
                 or grad.device != dev:
@@ -479,6 +490,8 @@ def lfmmi_token_logprobs_backward(logits, targets, stats, entropy, grad_logp=Non
             logits.data_ptr(), code, B, T, V, stride_b, stride_t, None if lens is None else _hp(lens),
             _ptr(targets), target_bytes, scale, _ptr(stats), _ptr(entropy), _ptr(grad_logp),
             _ptr(grad_entropy), grad.data_ptr(), raw))
+    if not mine:
+        _written(grad)
     return grad
 
 
@@ -512,7 +525,6 @@ def _grad_arrays(grads, out):
         raise ValueError("gradients must fill their memory: contiguous, or a permutation of that")
     outs = None
     if out is not None:
-        out = list(out)
         if len(out) != len(grads):
             raise ValueError("out must have one tensor for each gradient")
         out_devices, out_dtypes, out_counts, out_plain = _described(out)
@@ -555,6 +567,8 @@ def _grads_call(grads, max_norm, out, norm, stream):
     grads = list(grads)
     if not grads:
         raise ValueError("no gradients")
+    if out is not None:
+        out = list(out)
     n = len(grads)
     pointers, outs, counts, codes = _grad_arrays(grads, out)
     dev = grads[0].device
@@ -562,6 +576,7 @@ def _grads_call(grads, max_norm, out, norm, stream):
         raise ValueError("output tensor has the wrong shape, dtype, layout or device")
     context, raw = _on_stream(dev, stream)
     lib = load_library()
+    written = [] if norm is None else [norm]
     with context:
         if norm is None:
             norm = torch.empty((), dtype=torch.float32, device=dev)
@@ -572,4 +587,7 @@ def _grads_call(grads, max_norm, out, norm, stream):
         else:
             _check(lib.lfmmi_clip_grads(n, _at(pointers), None if outs is None else _at(outs), _at(counts),
                                         _at(codes), max_norm, norm.data_ptr(), ws.data_ptr(), size, raw))
+            written += grads if out is None else out
+    if written:
+        _written(written)
     return norm

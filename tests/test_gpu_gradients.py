@@ -255,3 +255,44 @@ def test_any_number_of_tensors_at_any_address(n, dtype):
     again = binding.lfmmi_clip_grads(views(base), norm64)
     assert abs(float(again) - 0.4 * norm64) <= 0.01 * norm64
     assert torch.equal(base.view(torch.uint8), out.view(torch.uint8))
+
+
+def test_autograd_sees_what_is_written():
+    # a graph that has saved a tensor which a call then writes must say so, not go on with
+    # the new values
+    torch = _torch()
+
+    def refused(loss):
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            loss.backward()
+
+    w = torch.randn(1000, device="cuda", requires_grad=True)
+    (w.grad,) = torch.autograd.grad(w.pow(3).sum(), w, create_graph=True)
+    penalty = w.grad.square().sum()            # saves w.grad
+    chain.clip_grad_norm([w], 0.5)
+    refused(penalty)
+    a = torch.ones(1000, device="cuda", requires_grad=True)
+    g, out, norm = torch.randn(1000, device="cuda"), torch.zeros(1000, device="cuda"), torch.zeros((), device="cuda")
+    for written, call in (
+            (out, lambda: binding.lfmmi_clip_grads([g], 0.5, out=iter([out]))),
+            (norm, lambda: binding.lfmmi_clip_grads([g], 0.5, out=[out], norm=norm)),
+            (norm, lambda: binding.lfmmi_grad_norm([g], norm=norm)),
+            (g, lambda: binding.lfmmi_clip_grads([g[10:20]], 0.01)),   # a view's base
+            (g, lambda: binding.lfmmi_clip_grads([g], 1e9))):          # as torch, written to or not
+        loss = (a * written).sum()
+        call()
+        refused(loss)
+    for untouched, call in (
+            (g, lambda: binding.lfmmi_grad_norm([g])), (g, lambda: binding.lfmmi_clip_grads([g], 0.5, out=[out]))):
+        loss = (a * untouched).sum()
+        call()
+        loss.backward()
+    loss = (a * g).sum()
+    with pytest.raises(binding.LfmmiError):    # nothing is written
+        binding.lfmmi_clip_grads([g, g], 0.5)
+    loss.backward()
+    with torch.inference_mode():
+        h = torch.randn(1000, device="cuda")
+        before = h.clone()
+        binding.lfmmi_clip_grads([h], 0.5)
+    _check_scaled([h], [before], _norm64([before]), 0.5)

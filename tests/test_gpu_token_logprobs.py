@@ -663,3 +663,34 @@ def test_few_long_rows_with_any_number_of_alternatives(rows, V, dtype):
         check(x[some], x64, t, None, 1.0, top, picked, grad_too=False)
         if rows > 7:
             assert not r.logp[-3].any() and not r.entropy[-3].any() and (top == 0 or bool((r.top_id[-3] == -1).all()))
+
+
+def test_autograd_sees_what_is_written():
+    # (a graph that has saved what a call then writes must not go on with the new values)
+    torch = _torch()
+    x = torch.randn((4, 300), device="cuda")
+    t = torch.randint(0, 300, (4,), device="cuda")
+    r = binding.lfmmi_token_logprobs(x, t, top_k=3)
+
+    def refused(loss):
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            loss.backward()
+
+    leaf = torch.zeros((4, 300), device="cuda", requires_grad=True)
+    logits = leaf + x
+    logp, _, _ = chain.token_logprobs(logits, t)                # saves its logits
+    binding.lfmmi_token_logprobs_backward(logits.detach(), t, r.stats, r.entropy, logp.detach(), grad=logits.detach())
+    refused(logp.sum())
+    w = torch.ones(4, device="cuda", requires_grad=True)
+    for saved in (r.logp, r.entropy, r.stats[:, 0], r.top_logp[:, 0]):
+        loss = (w * saved).sum()
+        binding.lfmmi_token_logprobs(x, t, top_k=3, out=r)
+        refused(loss)
+    loss = (w * r.logp).sum() + (w * x[:, 0]).sum()
+    binding.lfmmi_token_logprobs(x, t, top_k=3)
+    binding.lfmmi_token_logprobs_backward(x, t, r.stats, r.entropy, r.logp)
+    loss.backward()
+    with torch.inference_mode():
+        again = binding.lfmmi_token_logprobs(x.clone(), t, top_k=3)
+        binding.lfmmi_token_logprobs(x, t, top_k=3, out=again)
+        assert all(torch.equal(a, b) for a, b in zip(again, r))
