@@ -125,11 +125,12 @@ def chain_loss(logits, lengths, num_graphs, den_graph, leak=1e-5, targets=None, 
     (a scalar to minimise). Sequences flagged in `status` make it non-finite.
 
     targets: a frame alignment, an int32 or int64 CUDA tensor [B, T] of pdf-ids (negative: no
-    target), whose frame log probabilities are added to the objective with target_weight."""
+    target), whose frame log probabilities are added to the objective with target_weight; with a
+    weight of 0 they are not looked at."""
     objf, _status = chain_objective(logits, lengths, num_graphs, den_graph, leak)
     frames = max(float(np.asarray(lengths, dtype=np.int64).sum()), 1.0)
     loss = -objf.sum() / frames
-    if targets is not None:
+    if targets is not None and (not np.isscalar(target_weight) or target_weight != 0):
         logp, _entropy, _status = token_logprobs(logits, targets, lengths)
         loss = loss - logp.sum() * (target_weight / frames)
     return loss

@@ -213,3 +213,24 @@ def test_workspace_of_rows_that_the_call_refuses():
         assert lib.lfmmi_token_logprobs_workspace(1, 1, 1, V, 0, ctypes.byref(n)) == UNSUPPORTED, n.value
         assert "V" in binding.lfmmi_last_error()
     assert lib.lfmmi_token_logprobs_workspace(1, 1, 1, 1 << 30, 0, ctypes.byref(n)) == 0 and n.value > 0
+
+
+def test_an_alignment_of_no_weight_is_not_scored(monkeypatch):
+    # (0 times the log probability of a token that is masked out would be NaN)
+    import torch
+    objf = torch.tensor([-3.0, -5.0], requires_grad=True)
+    monkeypatch.setattr(chain, "chain_objective", lambda *a: (objf, None))
+    scored = []
+
+    def logprobs(logits, targets, lengths):
+        scored.append(targets)
+        return torch.tensor([[0.0, -float("inf")], [-1.0, -2.0]]), None, None
+
+    monkeypatch.setattr(chain, "token_logprobs", logprobs)
+    targets = torch.zeros((2, 2), dtype=torch.int64)
+    for weight in (0, 0.0, -0.0, np.float32(0)):
+        assert float(chain.chain_loss(None, [2, 2], None, None, 1e-5, targets, weight).detach()) == 2.0
+    assert float(chain.chain_loss(None, [2, 2], None, None, 1e-5, targets).detach()) == 2.0 and not scored
+    assert float(chain.chain_loss(None, [2, 2], None, None, 1e-5, targets, 0.5).detach()) == float("inf")
+    assert float(chain.chain_loss(None, [2, 2], None, None, 1e-5, targets, torch.tensor(0.5)).detach()) == float("inf")
+    assert len(scored) == 2
