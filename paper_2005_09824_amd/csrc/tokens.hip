@@ -870,8 +870,8 @@ __global__ __launch_bounds__(kThreads) void k_token_join(TokenParams p, SeqLengt
 
 // ---- backward kernel
 
-// 1 - e^l for l <= 0, without cancellation: its Taylor series where the ninth term is below 2^-31
-// of the first.
+// 1 - e^l for l <= 0, good to a few roundings of itself: its Taylor series where the ninth term is below
+// 2^-30 of the first.
 __device__ __forceinline__ float one_minus_exp(float l, float e)
 {
     if (l < -0.35f) return 1.f - e;
@@ -887,10 +887,10 @@ __device__ __forceinline__ float one_minus_exp(float l, float e)
 }
 
 // What the gradient of a row takes, in units of log2: l2 = (x - m) * scale2 - logs2 is a logit's log2 p,
-// and its gradient -2^l2 (c + h2 l2), the target's larger by g.
+// and its gradient -2^l2 (c + h2 l2), with c = g + hent; the target's is larger by g.
 struct RowGrad {
     bool zero;
-    float m, logs2, scale2, c, h2, g;
+    float m, logs2, scale2, c, h2, g, hent;
     int target;
 };
 
@@ -906,7 +906,8 @@ __device__ __forceinline__ RowGrad row_grad(const TokenGradParams& p, const SeqL
     w.scale2 = p.scale * kLog2e;
     w.g = p.grad_logp ? p.grad_logp[row] * p.scale : 0.f;
     const float h = Ent ? p.grad_entropy[row] * p.scale : 0.f;
-    w.c = Ent ? w.g + h * p.entropy[row] : w.g;
+    w.hent = Ent ? h * p.entropy[row] : 0.f;
+    w.c = w.g + w.hent;
     w.h2 = h * kLn2;
     w.target = w.zero ? -1 : r.target;
     return w;
@@ -918,9 +919,12 @@ __device__ __forceinline__ float grad_of(const RowGrad& w, float x, bool target)
     float l2 = (x - w.m) * w.scale2 - w.logs2;
     if (Ent) l2 = fmaxf(l2, -1e4f);  // (of a masked logit 0 * -inf would be left)
     const float pr = exp2_of(l2);
-    if (__builtin_expect(target, 0)) {  // 1 - p without cancellation where p is near 1
+    if (__builtin_expect(target, 0)) {
+        // Where p is near 1 both terms are small beside g: 1 - p comes from l, as good as ln s is (a sum of
+        // 32 bits beside 1: log p is off by some 2^-24), and g is not added to the second only to be taken off
+        // again (2 % of a gradient at p = 1 - 1e-5 were rounding then).
         l2 = fmaxf(l2, -1e4f);
-        return w.g * one_minus_exp(l2 * kLn2, pr) - pr * (w.c - w.g + w.h2 * l2);
+        return w.g * one_minus_exp(l2 * kLn2, pr) - pr * (w.hent + w.h2 * l2);
     }
     return Ent ? -pr * (w.c + w.h2 * l2) : -pr * w.c;
 }

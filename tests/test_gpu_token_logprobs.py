@@ -694,3 +694,37 @@ def test_autograd_sees_what_is_written():
         again = binding.lfmmi_token_logprobs(x.clone(), t, top_k=3)
         binding.lfmmi_token_logprobs(x, t, top_k=3, out=again)
         assert all(torch.equal(a, b) for a, b in zip(again, r))
+
+
+@pytest.mark.parametrize("with_entropy", [False, True])
+@pytest.mark.parametrize("V", [40, 700, 9000])
+def test_gradient_of_a_token_that_is_nearly_certain(V, with_entropy):
+    # Against the formula in 64 bits at the ln s and entropy that the forward pass gave: g (1 - p) and
+    # h p (l + H) are products of factors each good to a few roundings relative to itself, however near p
+    # is to 1. (l: ln s in units of log2 and back, 4; 1 - e^l from l by a series, 8; the product, 2. H: one for
+    # the product with h; l times h 6; e^l 4: 16 U for each of the two terms, whose sum rounds once.)
+    torch = _torch()
+    rng = np.random.default_rng(V)
+    rest = np.array([1e-1, 1e-2, 1e-3, 1e-4, 1e-5, 1e-6, 3e-7] * 4)
+    N = len(rest)
+    x = rng.normal(0, 1, (N, V))
+    at = rng.integers(0, V, N)
+    x[np.arange(N), at] = -np.inf
+    x -= np.log(np.exp(x).sum(1, keepdims=True)) - np.log(rest)[:, None]   # the others' weights: `rest` in all
+    x[np.arange(N), at] = 0.0
+    x = torch.from_numpy(x.astype(np.float32)).cuda()
+    targets = torch.from_numpy(at).cuda()
+    r = binding.lfmmi_token_logprobs(x, targets)
+    g = torch.from_numpy(rng.uniform(0.2, 2.0, N).astype(np.float32)).cuda()
+    h = torch.from_numpy((rng.choice([-0.1, 0.1], N) * rng.uniform(0.5, 2.0, N)).astype(np.float32)).cuda()
+    got = binding.lfmmi_token_logprobs_backward(x, targets, r.stats, r.entropy, g, h if with_entropy else None)
+    assert float(r.stats[:, 0].abs().max()) == 0.0
+    l = -r.stats[:, 1].double()
+    p = torch.exp(l)
+    first, second = g.double() * -torch.expm1(l), torch.zeros_like(l)
+    tol = 16 * oracle.U * first
+    if with_entropy:
+        second = h.double() * p * (l + r.entropy.double())
+        tol += 16 * oracle.U * h.double().abs() * p * (l.abs() + r.entropy.double())
+    off = (got[torch.arange(N), targets].double() - (first - second)).abs()
+    assert bool((off <= tol + oracle.U * (first - second).abs()).all()), (off / tol).max()
