@@ -293,7 +293,9 @@ lfmmi_status lfmmi_token_logprobs_backward(const void *logits, int32_t dtype, in
  * summed in fp64, in a fixed order (the same inputs at the same alignment give the same
  * bits): values whose squares overflow fp32 do not upset the norm. A norm that is not finite
  * (a NaN or infinite gradient; a norm beyond fp32 counts as infinite) makes every value of
- * outs 0, so that an update does nothing, and `norm` says so. max_norm >= 0, may be infinite.
+ * outs 0, so that none of it reaches the weights, and `norm` says so: plain gradient descent then
+ * does nothing, an optimiser with momentum or weight decay still moves unless the step is left
+ * out. max_norm >= 0, may be infinite.
  * workspace: DEVICE, LFMMI_GRAD_WORKSPACE_BYTES(n) bytes, aligned to 16; otherwise as for
  * lfmmi_token_logprobs. The calls enqueue kernels on hip_stream and nothing else.
  */

@@ -113,7 +113,9 @@ def clip_grad_norm(parameters, max_norm):
     """Scales the gradients of `parameters` in place so that their norm, taken together, is at
     most max_norm, and returns the norm they had (a device tensor; nothing waits for it).
     Parameters without a gradient are passed over. A norm that is not finite makes
-    all gradients 0, so that the optimiser's step does nothing with them."""
+    all gradients 0: none of it reaches the weights, but an optimiser with momentum or
+    weight decay still moves them unless its step is left out. Each gradient may be listed
+    once."""
     grads = [p.grad for p in parameters if p.grad is not None]
     if not grads:
         raise ValueError("no parameter has a gradient")
