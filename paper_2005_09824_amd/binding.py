@@ -507,6 +507,13 @@ def _dense(t):
     return True
 
 
+def _alike(a, b):
+    """Whether the values of two tensors of as many lie in the same order."""
+    if a.is_contiguous() and b.is_contiguous():
+        return True
+    return a.shape == b.shape and all(p == q for p, q, n in zip(a.stride(), b.stride(), a.shape) if n != 1)
+
+
 def _described(tensors):
     """(devices, dtypes, numbers of values, whether all are contiguous) of tensors: an attribute at a
     time, which takes half the time of a tensor at a time."""
@@ -530,8 +537,7 @@ def _grad_arrays(grads, out):
         out_devices, out_dtypes, out_counts, out_plain = _described(out)
         # (of contiguous ones the number of values says it all)
         if out_devices != devices or out_dtypes != dtypes or out_counts != counts or \
-                not (plain and out_plain) and any([o.shape != g.shape or o.stride() != g.stride()
-                                                   for o, g in zip(out, grads)]):
+                not (plain and out_plain) and not all([_alike(o, g) for o, g in zip(out, grads)]):
             raise ValueError("output tensor has the wrong shape, dtype, layout or device")
         outs = array.array("Q", [o.data_ptr() for o in out])
     return (array.array("Q", [g.data_ptr() for g in grads]), outs, array.array("q", counts),

@@ -234,3 +234,23 @@ def test_an_alignment_of_no_weight_is_not_scored(monkeypatch):
     assert float(chain.chain_loss(None, [2, 2], None, None, 1e-5, targets, 0.5).detach()) == float("inf")
     assert float(chain.chain_loss(None, [2, 2], None, None, 1e-5, targets, torch.tensor(0.5)).detach()) == float("inf")
     assert len(scored) == 2
+
+
+def test_outputs_laid_out_as_their_gradients_are(monkeypatch):
+    # strides of dimensions of one entry say nothing
+    import torch
+    described = binding._described
+    monkeypatch.setattr(binding, "_described", lambda t: ([0] * len(t),) + described(t)[1:])  # as on a GPU
+    last = dict(memory_format=torch.channels_last)
+    conv, depthwise = torch.zeros((4, 8, 5, 5)).to(**last), torch.zeros((8, 1, 3, 3)).to(**last)
+    assert depthwise.is_contiguous() and depthwise.stride() != (9, 9, 3, 1)
+    grads = [conv, depthwise, torch.zeros((5, 1, 7)).transpose(0, 2), torch.zeros((3, 4))]
+    out = [torch.zeros((4, 8, 5, 5)).to(**last), torch.zeros((8, 1, 3, 3)), torch.zeros((5, 7)).t().unsqueeze(1),
+           torch.zeros(12)]
+    assert out[2].stride() != grads[2].stride()
+    pointers, outs, counts, codes = binding._grad_arrays(grads, out)
+    assert list(outs) == [o.data_ptr() for o in out] and list(counts) == [g.numel() for g in grads]
+    for i, bad in ((0, torch.zeros((4, 8, 5, 5))), (1, torch.zeros((8, 1, 3, 3)).transpose(2, 3)), (3, torch.zeros((4, 3)).t()),
+                   (2, torch.zeros((7, 1, 5))), (3, torch.zeros(11)), (0, torch.zeros((8, 4, 5, 5)).to(**last))):
+        with pytest.raises(ValueError, match="output tensor"):
+            binding._grad_arrays(grads, [bad if j == i else o for j, o in enumerate(out)])
