@@ -296,3 +296,67 @@ def test_autograd_sees_what_is_written():
         before = h.clone()
         binding.lfmmi_clip_grads([h], 0.5)
     _check_scaled([h], [before], _norm64([before]), 0.5)
+
+
+@pytest.mark.parametrize("dtypes", [["float32"], ["bfloat16"], ["float16"], DTYPES])
+@pytest.mark.parametrize("n", [5, 129, 300])
+def test_many_units(n, dtypes):
+    # more than 1,024 units of 8,192 values: the norm by a kernel of its own before gradients are scaled
+    torch = _torch()
+    rng = np.random.default_rng(n)
+    share = rng.uniform(0.1, 2.0, n)
+    sizes = [int(v) for v in share / share.sum() * 12000000]
+    assert sum(sizes) > 1100 * 8192
+    grads = _grads(rng, sizes, dtypes)
+    before = [g.clone() for g in grads]
+    norm64 = _norm64(grads)
+    norm = binding.lfmmi_grad_norm(grads)
+    assert abs(float(norm) - norm64) <= 1.01 * oracle.U * norm64
+    for max_norm in (norm64 * 0.3, norm64 * 2):
+        outs = [torch.full_like(g, 7.0) for g in grads]
+        assert torch.equal(binding.lfmmi_clip_grads(grads, max_norm, out=outs), norm)
+        _check_scaled(outs, before, norm64, max_norm)
+        assert all(torch.equal(g, b) for g, b in zip(grads, before))
+    assert all(torch.equal(o, b) for o, b in zip(outs, before))
+    assert torch.equal(binding.lfmmi_clip_grads(grads, norm64 * 2), norm)
+    assert all(torch.equal(g, b) for g, b in zip(grads, before))
+    assert torch.equal(binding.lfmmi_clip_grads(grads, norm64 * 0.3), norm)
+    _check_scaled(grads, before, norm64, norm64 * 0.3)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n", [9, 300])
+def test_more_than_the_caches_hold(n, dtype):
+    # 320 MB of gradients, slices of one buffer with NaN between them, into a buffer of other
+    # alignments and in place: every value is its gradient times one and the same factor, rounded once
+    torch = _torch()
+    rng = np.random.default_rng(n + 1)
+    kind = getattr(torch, dtype)
+    share = rng.uniform(0.1, 2.0, n)
+    sizes = [int(v) | 1 for v in share / share.sum() * (320000000 // kind.itemsize)]
+    assert sum(sizes) * kind.itemsize > 1 << 28
+    gaps = rng.integers(1, 70, n)
+    at = np.cumsum(gaps + np.concatenate([[0], sizes[:-1]])).tolist()
+    total = at[-1] + sizes[-1] + 100
+    gen = torch.Generator(device="cuda").manual_seed(n)
+    base = torch.randn(total, generator=gen, device="cuda").to(kind)
+    inside = torch.zeros(total, dtype=torch.bool, device="cuda")
+    for a, size in zip(at, sizes):
+        inside[a:a + size] = True
+    base[~inside] = float("nan")
+    one = torch.ones(1, device="cuda")         # becomes the factor itself
+    views = lambda b, shift=0: [b[a + shift:a + shift + size] for a, size in zip(at, sizes)]
+    norm64 = float(np.sqrt(_norm64(views(base)) ** 2 + 1.0))
+    whole, factor = base.clone(), torch.empty(1, device="cuda")
+    for shift in (0, 3):
+        out = torch.full((total,), float("nan"), dtype=kind, device="cuda")
+        norm = binding.lfmmi_clip_grads(views(base) + [one], norm64 * 0.37, out=views(out, shift) + [factor])
+        assert abs(float(norm) - norm64) <= 1.01 * oracle.U * norm64
+        assert abs(float(factor) - 0.37) <= 2.01 * oracle.U * 0.37  # the limit and the factor are rounded
+        want = (whole.float() * factor).to(kind)
+        out = torch.roll(out, -shift)
+        assert torch.equal(out[inside], want[inside]) and bool(torch.isnan(out[~inside]).all())
+        assert torch.equal(base.view(torch.uint8), whole.view(torch.uint8))
+    norm = binding.lfmmi_clip_grads(views(base) + [one], norm64 * 0.37)
+    assert torch.equal(one, factor) and abs(float(norm) - norm64) <= 1.01 * oracle.U * norm64
+    assert torch.equal(base[inside], want[inside]) and bool(torch.isnan(base[~inside]).all())

@@ -728,3 +728,88 @@ def test_gradient_of_a_token_that_is_nearly_certain(V, with_entropy):
         tol += 16 * oracle.U * h.double().abs() * p * (l.abs() + r.entropy.double())
     off = (got[torch.arange(N), targets].double() - (first - second)).abs()
     assert bool((off <= tol + oracle.U * (first - second).abs()).all()), (off / tol).max()
+
+
+def _same(a, b):
+    return _torch().equal(a.view(_torch().uint8), b.view(_torch().uint8))
+
+
+# lanes a row: 16; 64, rows in registers; 64; 256
+@pytest.mark.parametrize("B,V,top", [(4098, 8, 0), (1026, 90, 5), (1026, 300, 5), (257, 4104, 33)])
+def test_more_rows_than_a_launch_has_lanes_for(B, V, top):
+    # 4,096 rows, repeated by a stride of 0: a workgroup goes on to another row, in what it used before
+    torch = _torch()
+    rng = np.random.default_rng(V)
+    x, _ = _logits(rng, (4096, V), "bfloat16")
+    x[::7, : V // 2] = -float("inf")
+    x[11::64] = float("nan")
+    x[12::64] = -float("inf")
+    targets = torch.from_numpy(rng.integers(-1, V + 1, 4096)).cuda()
+    few = binding.lfmmi_token_logprobs(x, targets, top_k=top)
+    some = torch.arange(40, device="cuda")
+    picked = binding.TokenLogprobs(*[None if v is None else v[some] for v in few])
+    check(x[some], x[some].double().cpu().numpy(), targets[some], None, 1.0, top, picked, grad_too=False)
+    many = binding.lfmmi_token_logprobs(x.expand(B, 4096, V), targets.expand(B, 4096).contiguous(), top_k=top)
+    for name, a, b in zip(few._fields, few, many):
+        if a is not None:
+            assert _same(a.expand(b.shape).contiguous(), b), name
+
+
+# lanes a row: 16, 64, 256 (a row in several stretches)
+@pytest.mark.parametrize("B,T,V", [(4098, 4096, 8), (1026, 4096, 260), (17, 4096, 8193)])
+def test_gradient_of_more_rows_than_a_launch_has_lanes_for(B, T, V):
+    torch = _torch()
+    rng = np.random.default_rng(V)
+    x, x64 = _logits(rng, (T, V), "bfloat16")
+    targets = torch.from_numpy(rng.integers(-1, V, T)).cuda()
+    r = binding.lfmmi_token_logprobs(x, targets)
+    g, h = torch.randn(T, device="cuda"), torch.randn(T, device="cuda") * 0.1
+    few = binding.lfmmi_token_logprobs_backward(x, targets, r.stats, r.entropy, g, h)
+    n = 20
+    t = targets[:n].cpu().numpy()
+    want = oracle.rows(x64[:n], t, t >= 0, 1.0, 0)
+    upstream = g[:n].double().cpu().numpy(), h[:n].double().cpu().numpy()
+    wanted = oracle.grads(want, t, t >= 0, 1.0, *upstream)
+    tol = np.where((t >= 0)[:, None], oracle.bound_grad(want, t, 1.0, *upstream, wanted, "bfloat16"), 0.0)
+    _close(few[:n], wanted, tol, "grad")
+    more = lambda v: v.expand((B,) + v.shape).contiguous()
+    many = binding.lfmmi_token_logprobs_backward(x.expand(B, T, V), more(targets), more(r.stats), more(r.entropy),
+                                                 more(g), more(h))
+    same = (many.view(torch.int16) == few.view(torch.int16)).flatten(1)
+    assert all(bool(part.all()) for part in same.split(64))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("V,rows", [(85, 1700000), (3001, 50000), (33001, 4600)])
+def test_odd_rows_of_more_than_the_caches_hold(V, rows, dtype):
+    # loads and stores past the caches, at any alignment: the bits of the same rows in batches that
+    # the caches hold, the gradient in place too
+    torch = _torch()
+    kind = _dtype(dtype)
+    gen = torch.Generator(device="cuda").manual_seed(V)
+    x = torch.empty((rows, V), dtype=kind, device="cuda")
+    x.view(-1)[:rows * V] = torch.randn(rows * V, generator=gen, device="cuda").mul_(2.5).to(kind)
+    x[5::1000] = -float("inf")
+    x[6::1000, V // 3] = float("nan")
+    x[7::50, V // 5:] = -float("inf")
+    targets = torch.randint(0, V, (rows,), generator=gen, device="cuda")
+    targets[8::30] = -1
+    g, h = (torch.randn(rows, generator=gen, device="cuda") for _ in range(2))
+    assert rows * V * kind.itemsize > 1 << 28
+    each = 300000 if V == 85 else rows // 5      # (as many lanes for a row as for all of them)
+    assert each % 2 == 0 and each * V * kind.itemsize < 1 << 28 and (V < 33001 or each > 768)
+    parts = [slice(a, min(a + each, rows)) for a in range(0, rows, each)]
+    for top in (0, 5):
+        r = binding.lfmmi_token_logprobs(x, targets, top_k=top)
+        for part in parts:
+            for a, b in zip(r, binding.lfmmi_token_logprobs(x[part], targets[part], top_k=top)):
+                assert a is None and b is None or _same(a[part], b)
+    picked = binding.TokenLogprobs(*[None if v is None else v[:20] for v in r])
+    check(x[:20], x[:20].double().cpu().numpy(), targets[:20], None, 1.0, 5, picked, grad_too=False)
+    for hh in (h, None):
+        grad = binding.lfmmi_token_logprobs_backward(x, targets, r.stats, r.entropy, g, hh)
+        for part in parts:
+            assert _same(grad[part], binding.lfmmi_token_logprobs_backward(
+                x[part], targets[part], r.stats[part], r.entropy[part], g[part], None if hh is None else hh[part]))
+    binding.lfmmi_token_logprobs_backward(x, targets, r.stats, r.entropy, g, None, grad=x)
+    assert _same(x, grad)
