@@ -681,8 +681,8 @@ __device__ __forceinline__ Sums join_all(Sums a, float scale2, Sums* shared)
 
 // G lanes a row, or for Split G lanes for each of p.parts parts of a row. Bound by the reads where rows are
 // many: 6,144 rows of 65,536 bf16 132 us, 6.1 TB/s (16-byte loads alone reach 6.9); 2,570 of 131,072 with 5
-// alternatives 122 us, 5.5 TB/s, of which the selection takes 6 us; by latency where they are few: one of 32,000
-// with 8 alternatives 7.2 us, 4.4 without.
+// alternatives 116 us, 5.8 TB/s, of which the selection takes 6 us; by latency where they are few: one of 32,000
+// with 8 alternatives 7.4 us, 4.4 without.
 template <typename D, int G, bool Top, bool Split>
 __global__ __launch_bounds__(threads_of(G)) void k_token(TokenParams p, SeqLengths lens)
 {
@@ -1000,19 +1000,22 @@ void launch_rows(const TokenParams& p, const SeqLengths& lens, hipStream_t strea
     const int64_t rows = (int64_t)p.B * p.T;
     const auto blocks = [](int64_t n) { return dim3((unsigned)(n < (1 << 20) ? n : 1 << 20)); };
     const int64_t bytes = (int64_t)p.V * sizeof(typename D::Store);
-    // Lanes a row. Microseconds a call, bf16, without / with 8 alternatives, at 64, 256, 1,024 lanes:
-    //   4,096 rows of 12,000: 18.8 / 21.6, 20.9 / 32.2; 4,096 of 16,384: 23.8 / 27.2, 23.7 / 34.1;
-    //   64 of 8,192: 4.7 / 7.7, 3.4 / 6.0; 256 of 8,192: -, 3.4 / 6.2, 4.2 / 8.2;
-    //   256 of 65,536: -, 8.8 / 11.9, 7.0 / 11.1 (a compute unit holds one workgroup of 1,024, two of 512);
-    // at 256, 512 and 1,024 lanes: 64 of 8,192: 3.5 / 5.8, 3.6 / 6.3, -; 64 of 16,384: 4.1 / 6.6, 3.9 / 6.5,
-    //   4.1 / 7.6; 64 of 32,000: 5.6 / 8.2, 4.9 / 7.6, 4.8 / 8.4; 64 of 65,536: -, 6.8 / 9.5, 6.2 / 9.8; 128 of
-    //   200,000, with 64 alternatives: -, 16.4 / 25.4, 16.3 / 22.9;
-    // of more rows than compute units at 256 and 512 lanes: 257 of 32,000: 6.8 / 9.4, 6.6 / 10.3; 257 of 65,536:
-    //   11.6 / 14.4, 10.2 / 13.7, with 64 alternatives 17.3, 15.8; 512 of 65,536: 13.2 / 16.1, 13.3 / 16.9,
-    //   with 64 20.4, 18.6; 768: 18.8 / 21.8, 18.8 / 24.0, with 64 26.5, 28.3.
-    // 32,000 rows without alternatives at 16 and 64 lanes: 84 logits 5.3, 15.6; 512: 7.6, 14.9 (fp32
-    // 12.3, 14.0). Alternatives from registers and from lanes' maxima: 40,000 rows of 84, 8 of them, 33, 43;
-    // 20,000 of 500, 5 of them, 35, 28, 64 of them 51, 79.
+    // Lanes a row. Microseconds a call in a replayed graph, the same rows each time (the caches hold them), bf16,
+    // without / with 8 alternatives, at 64, 256, 1,024 lanes:
+    //   4,096 rows of 12,000: 18.1 / 21.1, 21.1 / 31.0; 4,096 of 16,384: 23.8 / 27.5, 23.0 / 32.9;
+    //   64 of 8,192: 4.8 / 7.6, 3.5 / 5.9; 256 of 8,192: -, 3.6 / 5.9, 4.3 / 7.5;
+    //   256 of 65,536: -, 8.9 / 11.5, 7.0 / 10.3 (a compute unit holds one workgroup of 1,024, two of 512);
+    // at 256, 512 and 1,024 lanes: 64 of 8,192: 3.5 / 5.9, 3.6 / 6.3, -; 64 of 16,384: 4.1 / 6.6, 3.8 / 6.5,
+    //   4.1 / 7.6; 64 of 32,000: 5.6 / 8.2, 4.9 / 7.6, 4.7 / 8.3; 64 of 65,536: -, 6.8 / 9.5, 6.2 / 9.7; 128 of
+    //   200,000, with 64 alternatives: -, 16.8 / 23.5, 15.3 / 21.6;
+    // of more rows than compute units at 256 and 512 lanes: 257 of 32,000: 6.5 / 9.2, 6.4 / 9.9; 257 of 65,536:
+    //   11.3 / 14.1, 10.0 / 13.3, with 64 alternatives 17.5, 15.6; 512 of 65,536: 13.1 / 16.0, 13.4 / 16.7,
+    //   with 64 20.1, 18.4; 768: 18.9 / 21.8, 19.0 / 23.6, with 64 25.8, 27.9.
+    // 32,000 rows without alternatives at 16 and 64 lanes: 84 logits 5.4, 15.1; 512: 7.5, 14.8 (fp32
+    // 12.0, 13.9). Alternatives from registers and from lanes' maxima: 40,000 rows of 84, 8 of them, 33, 61;
+    // 20,000 of 500, 5 of them, 34, 28, 64 of them 50, 78.
+    // Other rows each time take 0.3 to 4 us more on both sides; the order turns only where these are less than 1 us
+    // apart (512 and 768 of 65,536 without alternatives: 16.2, 15.3 and 22.8, 22.1).
     if (p.parts > 1) {
         k_token<D, 256, Top, true><<<blocks(rows * p.parts), 256, 0, stream>>>(p, lens);
         k_token_join<D, Top><<<blocks(rows), kThreads, 0, stream>>>(p, lens);
@@ -1051,10 +1054,12 @@ TokenPlan plan_tokens(int64_t rows, int V, int top_k)
 {
     TokenPlan plan{1, V, 0};
     // A compute unit alone takes 0.05 us for 1,000 logits; in parts there is a second launch, and a second
-    // selection that grows with the alternatives. Microseconds whole and in parts, bf16 and fp16, without / with
-    // 8 alternatives: 1 of 131,072: 8.9 / 12.4, 5.1 / 9.2; 32: 9.4 / 13.2, 6.2 / 12.0; 64 of 160,000: 12.1 / 16.1,
-    // 8.5 / 13.1; 64 of 100,000: 8.6 / 12.3, 7.2 / 13.5; with 20, 48 of 131,072: 13.7, 14.4; with 64, 16 of
-    // 131,072: 15.5, 16.5, of 200,000: 20.5, 18.7. 33 or more rows of 50,021 fp32 without: 6.0, 6.2 to 6.6.
+    // selection that grows with the alternatives. Microseconds whole and in parts, without / with 8 alternatives,
+    // the same rows each time, bf16: 1 of 131,072: 8.9 / 12.4, 5.2 / 9.2; 32: 9.3 / 12.9, 6.1 / 12.1; 64 of
+    // 160,000: 11.7 / 15.4, 8.8 / 13.5; 64 of 100,000: 8.6 / 12.3, 7.2 / 11.9; with 20, 48 of 131,072: 13.6, 14.2;
+    // with 64, 16 of 131,072: 15.3, 16.4, of 200,000: 19.7, 18.7; fp32 without, 33 of 50,021: 5.9, 6.0.
+    // Other rows each time take 0.3 to 4 us more on both sides; the order turns only where these are less than 1 us
+    // apart (with 64, 16 of 200,000: 21.8, 22.5; with 20, 48 of 128,000 fp16, 14.7, 14.9 else: 16.5, 16.3).
     const int64_t least = 65536 + (top_k ? 16384 + 768 * rows + 1024 * top_k : 512 * rows);
     if (rows <= 64 && V >= least) {
         // Two workgroups a compute unit, a part of 4,096 logits is worth one, and a lane of the join an
