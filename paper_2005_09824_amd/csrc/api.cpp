@@ -41,6 +41,15 @@ lfmmi_status fail_hip(hipError_t e, const char* what)
     return fail(LFMMI_ERR_HIP, std::string(what) + ": " + hipGetErrorString(e));
 }
 
+lfmmi_status fail_memory() noexcept
+{
+    try {
+        return fail(LFMMI_ERR_OOM, "host allocation failed");
+    } catch (...) {
+        return LFMMI_ERR_OOM;
+    }
+}
+
 }  // namespace lfmmi
 
 namespace {

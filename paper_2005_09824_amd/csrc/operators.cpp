@@ -347,7 +347,7 @@ try {
     }
     return LFMMI_OK;
 } catch (...) {
-    return LFMMI_ERR_OOM;
+    return fail_memory();
 }
 
 lfmmi_status lfmmi_token_logprobs_backward(const void* logits, int32_t dtype, int32_t B, int32_t T,
@@ -400,7 +400,7 @@ try {
     }
     return LFMMI_OK;
 } catch (...) {
-    return LFMMI_ERR_OOM;
+    return fail_memory();
 }
 
 lfmmi_status lfmmi_grad_norm(int32_t n, const void* const* grads, const int64_t* counts,
@@ -412,7 +412,7 @@ try {
     return run_grads(n, grads, nullptr, counts, dtypes, false, 0.f, norm, workspace,
                      static_cast<hipStream_t>(hip_stream));
 } catch (...) {
-    return LFMMI_ERR_OOM;
+    return fail_memory();
 }
 
 lfmmi_status lfmmi_clip_grads(int32_t n, const void* const* grads, void* const* outs,
@@ -428,7 +428,7 @@ try {
     return run_grads(n, grads, outs, counts, dtypes, true, max_norm, norm, workspace,
                      static_cast<hipStream_t>(hip_stream));
 } catch (...) {
-    return LFMMI_ERR_OOM;
+    return fail_memory();
 }
 
 }  // extern "C"

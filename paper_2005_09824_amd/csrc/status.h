@@ -10,5 +10,6 @@ namespace lfmmi {
 
 lfmmi_status fail(lfmmi_status st, const std::string& msg);
 lfmmi_status fail_hip(hipError_t e, const char* what);
+lfmmi_status fail_memory() noexcept;  // host memory, where an exception must not leave
 
 }  // namespace lfmmi

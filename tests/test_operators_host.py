@@ -1,6 +1,9 @@
 """What the operators on token log probabilities and on gradients refuse before they touch a
 GPU, and the 64-bit forms that their kernels are compared with."""
 import ctypes
+import os
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -254,3 +257,27 @@ def test_outputs_laid_out_as_their_gradients_are(monkeypatch):
                    (2, torch.zeros((7, 1, 5))), (3, torch.zeros(11)), (0, torch.zeros((8, 4, 5, 5)).to(**last))):
         with pytest.raises(ValueError, match="output tensor"):
             binding._grad_arrays(grads, [bad if j == i else o for j, o in enumerate(out)])
+
+
+def test_a_call_that_runs_out_of_host_memory_says_so():
+    # in a process of its own, with 200 MB more than the lists take: the check of overlaps would
+    # need 960 MB for them
+    code = """if True:
+        import resource
+        import numpy as np
+        from paper_2005_09824_amd import binding
+        lib = binding.load_library()
+        assert lib.lfmmi_grad_norm(-1, None, None, None, None, None, 0, None) == 1   # (a text that is there before)
+        n = 20000000
+        pointers, counts, codes = np.zeros(n, np.uint64), np.zeros(n, np.int64), np.zeros(n, np.int32)
+        for a in (pointers, counts, codes):
+            a.fill(0)
+        used = int(open("/proc/self/statm").read().split()[0]) * 4096
+        resource.setrlimit(resource.RLIMIT_AS, (used + (200 << 20), resource.RLIM_INFINITY))
+        code = lib.lfmmi_clip_grads(n, pointers.ctypes.data, None, counts.ctypes.data, codes.ctypes.data, 1.0, 4096,
+                                    1 << 40, 16384 + 32 * (n + 1), None)
+        print(code, binding.lfmmi_last_error())
+    """
+    run = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=100,
+                         cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+    assert run.stdout.strip() == "3 host allocation failed", (run.stdout, run.stderr)
