@@ -308,6 +308,148 @@ lfmmi_status lfmmi_clip_grads(int32_t n, const void *const *grads, void *const *
                               float *norm, void *workspace, int64_t workspace_bytes,
                               void *hip_stream);
 
+/* ---- around an output layer ----------------------------------------------
+ * What stands in front of the layer whose logits the calls above take, and behind it: token
+ * embeddings, dropout, the end of a residual block, verification of drafted tokens. No handle:
+ * the calls keep nothing, enqueue kernels on hip_stream and nothing else, do not allocate or
+ * synchronise, and may be captured into a HIP graph. Arrays are DEVICE and lie on the current
+ * device, aligned to their elements, contiguous where no stride is given; lengths are HOST,
+ * copied. What is written may overlap no other array of a call but where that is said
+ * (LFMMI_ERR_INVALID_ARG). Workspaces as for lfmmi_token_logprobs: aligned to 16, the bytes that
+ * the call of that name gives for the same sizes, one for each call that may run at the same
+ * time, replays of captured graphs among them. The same inputs give the same bits. Sums are
+ * taken in 32 bits or more and rounded to an array's type once. */
+
+/*
+ * Rows of a table for given tokens: out[b,t,:] = scale * table[tokens[b,t],:]
+ *   table    [V, D] of `dtype`, row v at v * stride elements (stride >= 0).
+ *   tokens   int32 or int64 (token_bytes 4 or 8) [B, T]. Rows with a negative token and rows
+ *            t >= lengths[b] (lengths HOST int32 [B], or NULL: all T) are 0; the tokens of the
+ *            latter are never read. A token that is not below V makes its row NaN.
+ *   scale    1e-6 <= scale <= 1e6
+ *   out      [B, T, D]
+ *   status   int32 [B, T] or NULL: 0 ok; bit 2: the token is not below V.
+ * 1 <= D <= 2^24.
+ */
+lfmmi_status lfmmi_embed_tokens(const void *table, int32_t dtype, int32_t V, int32_t D,
+                                int64_t stride, const void *tokens, int32_t token_bytes,
+                                int32_t B, int32_t T, const int32_t *lengths, float scale,
+                                void *out, int32_t *status, void *hip_stream);
+/*
+ * The gradient of the table, given that of out:
+ *   grad[v,:] (=|+=) scale * sum of grad_out[b,t,:] over the positions whose token is v
+ * summed in fp32, in an order that the tokens alone decide; rows without a position are 0, or
+ * with accumulate != 0 left as they are. Negative tokens, tokens that are not below V and rows
+ * t >= lengths[b] add nothing, and those rows of grad_out are never read.
+ *   grad_out [B, T, D] of `dtype`, row (b, t) at b * stride_b + t * stride_t, strides >= 0
+ *   grad     [V, D] of `dtype`
+ */
+lfmmi_status lfmmi_embed_tokens_backward(const void *grad_out, int32_t dtype, int32_t V, int32_t D,
+                                         int64_t stride_b, int64_t stride_t, const void *tokens,
+                                         int32_t token_bytes, int32_t B, int32_t T,
+                                         const int32_t *lengths, float scale, int accumulate,
+                                         void *grad, void *workspace, int64_t workspace_bytes,
+                                         void *hip_stream);
+lfmmi_status lfmmi_embed_tokens_workspace(int32_t V, int32_t D, int32_t B, int32_t T,
+                                          int64_t *bytes);
+
+/*
+ * Dropout of rows: y[r,c] = kept ? x[r,c] / (1 - p') : 0, whatever x is where it is dropped.
+ * p' is p rounded to a multiple of 2^-16, 0 <= p <= 1 (1: everything is dropped). What is kept is
+ * a function of (seed, draw, r, c) alone, draw = offset + *step modulo 2^64 (step DEVICE int64
+ * [1] or NULL: 0; a captured graph draws anew when a kernel has counted it up): with the four
+ * words w of
+ * Philox4x32-10 for the counter (c / 8, r, low and high word of draw) and the key (low and high
+ * word of seed), c is kept if the 16 bits c % 8 of w (the low half of w[0] first) are at least
+ * 65536 p'. No mask is stored: the gradient is the same call on the gradient of y.
+ *   x        [R, D] of `dtype`, row r at r * stride elements (stride >= 0)
+ *   y        [R, D]; or x itself, laid out as it is (stride >= D)
+ */
+lfmmi_status lfmmi_dropout(const void *x, int32_t dtype, int32_t R, int32_t D, int64_t stride,
+                           float p, uint64_t seed, uint64_t offset, const int64_t *step, void *y,
+                           void *hip_stream);
+
+/*
+ * The end of a residual block: the residual's addition and a root-mean-square norm, with dropout
+ * on the way and the output in 8 bits if wanted. For row (b, t):
+ *   sum    = residual + dropout(x), rounded to `dtype` (row b * T + t of lfmmi_dropout)
+ *   rstd   = 1 / sqrt(mean_c sum_c^2 + eps)
+ *   y_c    = sum_c * rstd * weight_c
+ *   q_scale = max(max_c |y_c| / 448, 2^-126),  q_c = y_c / q_scale rounded to e4m3 (OCP, no infinities)
+ *
+ *   x, residual [B, T, D] of `dtype`, rows at their strides (>= 0); residual may be NULL (0).
+ *   weight   [D] of `dtype` or float32 (weight_dtype), or NULL (1)
+ *   lengths  HOST int32 [B], or NULL: rows t >= lengths[b] are never read, their outputs are 0
+ *   eps      1e-30 <= eps, finite
+ *   p, seed, offset, step  as for lfmmi_dropout
+ *   sum      [B, T, D]; may be NULL where it would be x itself (no residual, nothing dropped).
+ *            It may be x or residual, where the rows of that one follow each other.
+ *   y        [B, T, D] of `dtype`, rstd float32 [B, T]: may be NULL
+ *   q        bytes [B, T, D], q_scale float32 [B, T]: both or none. A row with a NaN has a
+ *            q_scale of NaN.
+ * 1 <= D <= 2^24. Squares are summed in fp32; where that overflows, of the values times 2^-80.
+ */
+lfmmi_status lfmmi_add_rms_norm(const void *x, int64_t stride_b, int64_t stride_t,
+                                const void *residual, int64_t residual_stride_b,
+                                int64_t residual_stride_t, int32_t dtype, int32_t B, int32_t T,
+                                int32_t D, const int32_t *lengths, const void *weight,
+                                int32_t weight_dtype, float eps, float p, uint64_t seed,
+                                uint64_t offset, const int64_t *step, void *sum, void *y,
+                                float *rstd, void *q, float *q_scale, void *hip_stream);
+/*
+ * Its gradients, given those of y (grad_y) and of sum (grad_sum), either may be NULL (0). With
+ * n = sum * rstd and g = weight * grad_y:
+ *   d             = grad_sum + rstd * (g - n * mean_c(g_c n_c))
+ *   grad_residual = d,  grad_x = dropout(d) with the forward call's p, seed, offset and step
+ *   grad_weight   = sum over the rows of grad_y * n, in fp32, in an order that the sizes decide
+ * sum (or x, where that is it; rows at their strides) and rstd: what the forward call read and
+ * gave. grad_x, grad_residual [B, T, D] of `dtype` and grad_weight [D] of weight_dtype may be
+ * NULL; either of the first two may be grad_y or grad_sum. Rows t >= lengths[b] become 0 and add
+ * nothing. workspace: needed with grad_weight.
+ */
+lfmmi_status lfmmi_add_rms_norm_backward(const void *sum, int64_t stride_b, int64_t stride_t,
+                                         int32_t dtype, int32_t B, int32_t T, int32_t D,
+                                         const int32_t *lengths, const void *weight,
+                                         int32_t weight_dtype, const float *rstd,
+                                         const void *grad_y, const void *grad_sum, float p,
+                                         uint64_t seed, uint64_t offset, const int64_t *step,
+                                         void *grad_x, void *grad_residual, void *grad_weight,
+                                         void *workspace, int64_t workspace_bytes,
+                                         void *hip_stream);
+lfmmi_status lfmmi_add_rms_norm_workspace(int32_t B, int32_t T, int32_t D, int64_t *bytes);
+
+/*
+ * Drafted tokens against the logits of the model they are drafted for. Sequence b has n =
+ * lengths[b] drafted tokens d_0 .. d_{n-1} (HOST int32 [B], 0 <= n <= K; NULL: K) and the target's
+ * logits in rows 0 .. n: row i is what follows the first i drafted tokens. With p_i the softmax of
+ * scale * logits[b,i,:], q_i that of draft_scale * draft_logits[b,i,:] (NULL: q_i is 1 at d_i, 0
+ * elsewhere) and u = uniforms[b,:], float32 [B, K + 1] in [0, 1):
+ *   d_i is taken if all before it are and u_i q_i(d_i) < p_i(d_i);
+ *   the first that is not, d_r, is replaced by a token drawn from max(0, p_r - q_r), normalised;
+ *   if all are taken (r = n), a token drawn from p_n follows.
+ * Drawn means: the first token at which the running sum of what it is drawn from, in the order of
+ * the tokens, passes u_K times the whole (a number of 1 or more: the last token of any
+ * weight). The sums are taken in fp64. The tokens that come out are distributed as p says. With K
+ * = 0 the call draws one token a sequence.
+ * uniforms NULL: greedy. d_i is taken if it is the first largest logit of row i, which replaces
+ * or follows the others too; draft_logits must be NULL.
+ *
+ *   logits   [B, K + 1, V], draft_logits [B, K, V], of `dtype`: rows at their strides (>= 0)
+ *   drafted  int32 or int64 (token_bytes 4 or 8) [B, K]
+ *   accepted int32 [B]: r.  tokens int32 [B, K + 1]: d_0 .. d_{r-1}, the token drawn, then -1
+ *   status   int32 [B] or NULL: 0 ok; otherwise row r could not be judged, tokens[b,r] is -1: bit 0:
+ *            every logit of a row is -inf; bit 1: a NaN or +inf logit; bit 2: d_r is not in
+ *            [0, V). Rows behind r do not matter.
+ */
+lfmmi_status lfmmi_verify_tokens(const void *logits, int32_t dtype, int32_t B, int32_t K, int32_t V,
+                                 int64_t stride_b, int64_t stride_t, const void *draft_logits,
+                                 int64_t draft_stride_b, int64_t draft_stride_t,
+                                 const void *drafted, int32_t token_bytes, const int32_t *lengths,
+                                 float scale, float draft_scale, const float *uniforms,
+                                 int32_t *accepted, int32_t *tokens, int32_t *status,
+                                 void *workspace, int64_t workspace_bytes, void *hip_stream);
+lfmmi_status lfmmi_verify_tokens_workspace(int32_t B, int32_t K, int32_t V, int64_t *bytes);
+
 /* Thread-local description of the last failure on this thread ("" if none). */
 const char *lfmmi_last_error(void);
 

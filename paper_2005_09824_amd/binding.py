@@ -29,6 +29,9 @@ EXPORTS = [
     "lfmmi_profile_enable", "lfmmi_profile_read",
     "lfmmi_token_logprobs", "lfmmi_token_logprobs_workspace", "lfmmi_token_logprobs_backward",
     "lfmmi_grad_norm", "lfmmi_clip_grads",
+    "lfmmi_embed_tokens", "lfmmi_embed_tokens_backward", "lfmmi_embed_tokens_workspace",
+    "lfmmi_dropout", "lfmmi_add_rms_norm", "lfmmi_add_rms_norm_backward",
+    "lfmmi_add_rms_norm_workspace", "lfmmi_verify_tokens", "lfmmi_verify_tokens_workspace",
 ]
 
 _lib = None
@@ -78,6 +81,20 @@ def load_library():
                                                   vp, vp, vp, vp, vp, vp]
     lib.lfmmi_grad_norm.argtypes = [i32, vp, vp, vp, vp, vp, i64, vp]
     lib.lfmmi_clip_grads.argtypes = [i32, vp, vp, vp, vp, f32, vp, vp, i64, vp]
+    u64 = ctypes.c_uint64
+    lib.lfmmi_embed_tokens.argtypes = [vp, i32, i32, i32, i64, vp, i32, i32, i32, vp, f32, vp, vp, vp]
+    lib.lfmmi_embed_tokens_backward.argtypes = [vp, i32, i32, i32, i64, i64, vp, i32, i32, i32, vp, f32,
+                                                ctypes.c_int, vp, vp, i64, vp]
+    lib.lfmmi_embed_tokens_workspace.argtypes = [i32, i32, i32, i32, vp]
+    lib.lfmmi_dropout.argtypes = [vp, i32, i32, i32, i64, f32, u64, u64, vp, vp, vp]
+    lib.lfmmi_add_rms_norm.argtypes = [vp, i64, i64, vp, i64, i64, i32, i32, i32, i32, vp, vp, i32, f32,
+                                       f32, u64, u64, vp, vp, vp, vp, vp, vp, vp]
+    lib.lfmmi_add_rms_norm_backward.argtypes = [vp, i64, i64, i32, i32, i32, i32, vp, vp, i32, vp, vp, vp,
+                                                f32, u64, u64, vp, vp, vp, vp, vp, i64, vp]
+    lib.lfmmi_add_rms_norm_workspace.argtypes = [i32, i32, i32, vp]
+    lib.lfmmi_verify_tokens.argtypes = [vp, i32, i32, i32, i32, i64, i64, vp, i64, i64, vp, i32, vp, f32,
+                                        f32, vp, vp, vp, vp, vp, i64, vp]
+    lib.lfmmi_verify_tokens_workspace.argtypes = [i32, i32, i32, vp]
     for name in EXPORTS:
         if name not in ("lfmmi_graph_destroy", "lfmmi_last_error"):
             getattr(lib, name).restype = ctypes.c_int
@@ -597,3 +614,386 @@ def _grads_call(grads, max_norm, out, norm, stream):
     if written:
         _written(written)
     return norm
+
+
+# ---- around an output layer
+
+AddRmsNorm = collections.namedtuple("AddRmsNorm", ["sum", "y", "rstd", "q", "q_scale"])
+AddRmsNormGrads = collections.namedtuple("AddRmsNormGrads", ["x", "residual", "weight"])
+VerifiedTokens = collections.namedtuple("VerifiedTokens", ["accepted", "tokens", "status"])
+
+_WRONG_OUT = "output tensor has the wrong shape, dtype, layout or device"
+
+
+def _batch_rows(x, what):
+    """Checked (dtype code, B, T, D, stride_b, stride_t) of rows [B, T, D] or [B, D]."""
+    code = _dtype_codes().get(x.dtype)
+    if not x.is_cuda or code is None or x.dim() not in (2, 3):
+        raise ValueError(what + " must be a float32, bfloat16 or float16 CUDA tensor [B, T, D] or [B, D]")
+    shape = x.shape
+    D = shape[-1]
+    if D < 1:
+        raise ValueError(what + " needs at least one column")
+    if x.dim() == 3:
+        (B, T), (stride_b, stride_t, step) = shape[:2], x.stride()
+    else:
+        B, T = shape[0], 1
+        stride_b, step = x.stride()
+        stride_t = D
+    if step != 1 and D > 1 and B * T > 0:
+        raise ValueError("the values of a row must be next to each other")
+    if B * T >= 1 << 31 or D > 1 << 24:   # (ctypes would pass on the lowest 32 bits)
+        raise ValueError("too many rows or columns")
+    return code, B, T, D, stride_b, stride_t
+
+
+def _host_lengths(lengths, B):
+    if lengths is None:
+        return None
+    lens = _host(lengths, np.int32)
+    if lens.shape != (B,):
+        raise ValueError("lengths must have B entries")
+    return lens
+
+
+def _token_bytes(tokens, what="tokens"):
+    import torch
+    if tokens.dtype == torch.int64:
+        return 8
+    if tokens.dtype == torch.int32:
+        return 4
+    raise ValueError(what + " must be int32 or int64")
+
+
+def _check_out(t, shape, dtype, device):
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or not t.is_contiguous() or t.device != device:
+        raise ValueError(_WRONG_OUT)
+
+
+def _token_rows(tokens, device):
+    """Checked (B, T, token bytes) of tokens [B, T] or [B]."""
+    bytes_ = _token_bytes(tokens)
+    if tokens.dim() not in (1, 2) or not tokens.is_contiguous() or tokens.device != device:
+        raise ValueError("tokens must be a contiguous tensor [B, T] or [B], on the same device")
+    B, T = tokens.shape if tokens.dim() == 2 else (tokens.shape[0], 1)
+    if B * T >= 1 << 31:
+        raise ValueError("too many tokens")
+    return B, T, bytes_
+
+
+def lfmmi_embed_tokens(table, tokens, lengths=None, scale=1.0, out=None, status=None, stream=None):
+    """scale times the rows of `table` (float32, bfloat16 or float16 CUDA tensor [V, D], its rows
+    anywhere) that `tokens` (int32 or int64 CUDA tensor [B, T] or [B]) name. Negative tokens and
+    rows behind lengths (host int array [B], or None) give rows of 0, tokens that are not below V
+    rows of NaN and a flag (4) in `status`. Returns (rows [B, T, D] or [B, D], status int32 like
+    tokens): allocated here unless passed in. Enqueues on `stream` (default: torch's current
+    stream)."""
+    import torch
+    code = _dtype_codes().get(table.dtype)
+    if not table.is_cuda or code is None or table.dim() != 2:
+        raise ValueError("table must be a float32, bfloat16 or float16 CUDA tensor [V, D]")
+    V, D = table.shape
+    if V < 1 or D < 1:
+        raise ValueError("table needs at least one row and one column")
+    if table.stride(1) != 1 and D > 1:
+        raise ValueError("the values of a row must be next to each other")
+    if V >= 1 << 31 or D > 1 << 24:
+        raise ValueError("too many rows or columns")
+    dev = table.device
+    B, T, token_bytes = _token_rows(tokens, dev)
+    lens = _host_lengths(lengths, B)
+    context, raw = _on_stream(dev, stream)
+    shape = tuple(tokens.shape)
+    written = [t for t in (out, status) if t is not None]
+    with context:
+        if out is None:
+            out = torch.empty(shape + (D,), dtype=table.dtype, device=dev)
+        else:
+            _check_out(out, shape + (D,), table.dtype, dev)
+        if status is None:
+            status = torch.empty(shape, dtype=torch.int32, device=dev)
+        else:
+            _check_out(status, shape, torch.int32, dev)
+        _check(load_library().lfmmi_embed_tokens(
+            table.data_ptr(), code, V, D, table.stride(0), tokens.data_ptr(), token_bytes, B, T,
+            None if lens is None else _hp(lens), scale, out.data_ptr(), status.data_ptr(), raw))
+    if written:
+        _written(written)
+    return out, status
+
+
+def lfmmi_embed_tokens_backward(grad_out, tokens, V, lengths=None, scale=1.0, grad=None, accumulate=False,
+                                stream=None):
+    """Gradient [V, D] of the table of lfmmi_embed_tokens for the gradient of its rows, a tensor
+    [B, T, D] or [B, D] whose rows may lie anywhere. `grad`: a contiguous tensor to write into, or
+    with `accumulate` to add to. Returns the gradient."""
+    import torch
+    code, B, T, D, stride_b, stride_t = _batch_rows(grad_out, "grad_out")
+    dev = grad_out.device
+    token_bytes = _token_bytes(tokens)
+    if tuple(tokens.shape) != tuple(grad_out.shape[:-1]) or not tokens.is_contiguous() or tokens.device != dev:
+        raise ValueError("tokens must be contiguous, on the gradient's device, one for each row")
+    V = int(V)
+    if not 1 <= V < 1 << 31:
+        raise ValueError("V outside [1, 2^31)")
+    if accumulate and grad is None:
+        raise ValueError("accumulate needs an existing grad")
+    lens = _host_lengths(lengths, B)
+    context, raw = _on_stream(dev, stream)
+    lib = load_library()
+    mine = grad is None
+    with context:
+        if mine:
+            grad = torch.empty((V, D), dtype=grad_out.dtype, device=dev)
+        else:
+            _check_out(grad, (V, D), grad_out.dtype, dev)
+        need = ctypes.c_int64(0)
+        _check(lib.lfmmi_embed_tokens_workspace(V, D, B, T, ctypes.byref(need)))
+        ws = torch.empty(need.value, dtype=torch.uint8, device=dev)
+        _check(lib.lfmmi_embed_tokens_backward(
+            grad_out.data_ptr(), code, V, D, stride_b, stride_t, tokens.data_ptr(), token_bytes, B, T,
+            None if lens is None else _hp(lens), scale, 1 if accumulate else 0, grad.data_ptr(),
+            ws.data_ptr(), need.value, raw))
+    if not mine:
+        _written(grad)
+    return grad
+
+
+def _draw_args(p, seed, offset, step, device):
+    """Checked (p, seed, offset, address of step) of what is drawn."""
+    import torch
+    p = float(p)
+    if not 0.0 <= p <= 1.0:
+        raise ValueError("p outside [0, 1]")
+    seed, offset = int(seed), int(offset)
+    if not (0 <= seed < 1 << 64 and 0 <= offset < 1 << 64):
+        raise ValueError("seed and offset are whole numbers of 64 bits")
+    if step is not None and (step.dtype != torch.int64 or step.numel() != 1 or step.device != device):
+        raise ValueError("step must be an int64 tensor of one value on the same device")
+    return p, seed, offset, _ptr(step)
+
+
+def _flat_rows(x):
+    """(R, D, stride) of a tensor [..., D] whose rows are equally far from each other."""
+    D = x.shape[-1] if x.dim() else 1
+    if 0 in x.shape:
+        return 0, D, D
+    if x.dim() and x.stride(-1) != 1 and D > 1:
+        raise ValueError("the values of a row must be next to each other")
+    R, stride = 1, None
+    for size, step in reversed(list(zip(x.shape[:-1], x.stride()[:-1]))):
+        if size == 1:
+            continue
+        if stride is not None and step != stride * R:
+            raise ValueError("the rows must be equally far from each other")
+        stride = step if stride is None else stride
+        R *= size
+    return R, D, D if stride is None else stride
+
+
+def lfmmi_dropout(x, p, seed, offset=0, step=None, out=None, stream=None):
+    """Dropout of the rows of x, a float32, bfloat16 or float16 CUDA tensor [..., D]: a share p of the
+    values becomes 0, the others are divided by 1 - p. What is kept follows from seed, offset plus
+    the value of `step` (an int64 CUDA tensor of one value, or None), the row and the column alone:
+    the same call on a gradient is the gradient. `out`: a contiguous tensor like x, or x itself.
+    Returns the result."""
+    import torch
+    code = _dtype_codes().get(x.dtype)
+    if not x.is_cuda or code is None:
+        raise ValueError("x must be a float32, bfloat16 or float16 CUDA tensor")
+    R, D, stride = _flat_rows(x)
+    if R >= 1 << 31 or D >= 1 << 31:
+        raise ValueError("too many rows or columns")
+    dev = x.device
+    p, seed, offset, at = _draw_args(p, seed, offset, step, dev)
+    context, raw = _on_stream(dev, stream)
+    mine = out is None
+    with context:
+        if mine:
+            out = torch.empty(x.shape, dtype=x.dtype, device=dev)
+        elif out is not x:
+            _check_out(out, x.shape, x.dtype, dev)
+            if out.data_ptr() == x.data_ptr() and not x.is_contiguous():
+                raise ValueError("an output in the place of x must be laid out as x is")
+        _check(load_library().lfmmi_dropout(x.data_ptr(), code, R, D, stride, p, seed, offset, at,
+                                            out.data_ptr(), raw))
+    if not mine:
+        _written(out)
+    return out
+
+
+def _check_weight(weight, D, dtype, device):
+    import torch
+    if weight is None:
+        return 0
+    if tuple(weight.shape) != (D,) or weight.dtype not in (dtype, torch.float32) or \
+            not weight.is_contiguous() or weight.device != device:
+        raise ValueError("weight must be a contiguous tensor [D] of the rows' dtype or float32, on their device")
+    return _dtype_codes()[weight.dtype]
+
+
+def lfmmi_add_rms_norm(x, residual=None, weight=None, eps=1e-6, lengths=None, p=0.0, seed=0, offset=0,
+                       step=None, y=True, quantized=False, out=None, stream=None):
+    """The end of a residual block: sum = residual + dropout(x), and its root-mean-square norm times
+    `weight`. x, residual: float32, bfloat16 or float16 CUDA tensors [B, T, D] or [B, D], their
+    rows anywhere; weight: [D] of that dtype or float32, or None; lengths: host int array [B] or
+    None, rows behind them give 0; p, seed, offset, step: as for lfmmi_dropout. Returns an
+    AddRmsNorm (sum, y, rstd, q, q_scale) of device tensors: y of x's dtype (None where y is
+    false), with `quantized` q of dtype float8_e4m3fn and its scale for each row. sum is x itself
+    where nothing is added or dropped. `out`: an AddRmsNorm to write into; its sum may be x or
+    residual, where that is contiguous (None where it would be x itself). With `quantized` alone y
+    is not computed unless y is "both"."""
+    import torch
+    code, B, T, D, stride_b, stride_t = _batch_rows(x, "x")
+    dev, dtype = x.device, x.dtype
+    r_code, r_strides = code, (0, 0)
+    if residual is not None:
+        r_code, *_sizes, r_b, r_t = _batch_rows(residual, "residual")
+        r_strides = (r_b, r_t)
+        if residual.shape != x.shape or r_code != code or residual.device != dev:
+            raise ValueError("residual must have x's shape, dtype and device")
+    w_code = _check_weight(weight, D, dtype, dev)
+    lens = _host_lengths(lengths, B)
+    p, seed, offset, at = _draw_args(p, seed, offset, step, dev)
+    wants_y = y == "both" or (bool(y) and not quantized)
+    wants_sum = residual is not None or p > 0
+    rows = tuple(x.shape[:-1])
+    context, raw = _on_stream(dev, stream)
+    mine = out is None
+    with context:
+        if mine:
+            f32 = torch.float32
+            out = AddRmsNorm(
+                torch.empty(x.shape, dtype=dtype, device=dev) if wants_sum else None,
+                torch.empty(x.shape, dtype=dtype, device=dev) if wants_y else None,
+                torch.empty(rows, dtype=f32, device=dev),
+                torch.empty(x.shape, dtype=torch.float8_e4m3fn, device=dev) if quantized else None,
+                torch.empty(rows, dtype=f32, device=dev) if quantized else None)
+        else:
+            for t, wanted, shape, dt in (
+                    (out.sum, wants_sum, x.shape, dtype), (out.y, wants_y, x.shape, dtype),
+                    (out.rstd, True, rows, torch.float32), (out.q, quantized, x.shape, torch.float8_e4m3fn),
+                    (out.q_scale, quantized, rows, torch.float32)):
+                if (t is not None) != bool(wanted):
+                    raise ValueError(_WRONG_OUT)
+                if t is not None:
+                    _check_out(t, shape, dt, dev)
+        _check(load_library().lfmmi_add_rms_norm(
+            x.data_ptr(), stride_b, stride_t, _ptr(residual), *r_strides, code, B, T, D,
+            None if lens is None else _hp(lens), _ptr(weight), w_code, eps, p, seed, offset, at,
+            _ptr(out.sum), _ptr(out.y), _ptr(out.rstd), _ptr(out.q), _ptr(out.q_scale), raw))
+    if not mine:
+        _written([t for t in out if t is not None])
+    return out if out.sum is not None else out._replace(sum=x)
+
+
+def lfmmi_add_rms_norm_backward(sum, rstd, weight, grad_y, grad_sum=None, lengths=None, p=0.0, seed=0,
+                                offset=0, step=None, residual=True, weight_grad=True, out=None, stream=None):
+    """Gradients of lfmmi_add_rms_norm for those of y and sum (contiguous tensors like sum; either
+    may be None). sum, rstd: what that call returned; lengths, p, seed, offset, step: what it was
+    given. Returns AddRmsNormGrads (x, residual, weight): residual is None where `residual` is false,
+    and x's where nothing was dropped (one tensor); weight's is None without a weight, or where
+    `weight_grad` is false. `out`: an
+    AddRmsNormGrads to write into; x and residual of it may be grad_y or grad_sum."""
+    import torch
+    code, B, T, D, stride_b, stride_t = _batch_rows(sum, "sum")
+    dev, dtype = sum.device, sum.dtype
+    rows = tuple(sum.shape[:-1])
+    if grad_y is None and grad_sum is None:
+        raise ValueError("grad_y or grad_sum must be given")
+    for t, shape, dt in ((rstd, rows, torch.float32), (grad_y, sum.shape, dtype), (grad_sum, sum.shape, dtype)):
+        if t is not None and (tuple(t.shape) != tuple(shape) or t.dtype != dt or not t.is_contiguous() or
+                              t.device != dev):
+            raise ValueError("rstd or a gradient has the wrong shape, dtype, layout or device")
+    w_code = _check_weight(weight, D, dtype, dev)
+    lens = _host_lengths(lengths, B)
+    p, seed, offset, at = _draw_args(p, seed, offset, step, dev)
+    one = p == 0
+    weight_grad = weight is not None and weight_grad
+    context, raw = _on_stream(dev, stream)
+    lib = load_library()
+    mine = out is None
+    with context:
+        if mine:
+            dx = torch.empty(sum.shape, dtype=dtype, device=dev)
+            out = AddRmsNormGrads(
+                dx, None if not residual else dx if one else torch.empty(sum.shape, dtype=dtype, device=dev),
+                torch.empty(D, dtype=weight.dtype, device=dev) if weight_grad else None)
+        else:
+            for t, wanted, shape, dt in ((out.x, True, sum.shape, dtype), (out.residual, residual, sum.shape, dtype),
+                                         (out.weight, weight_grad, (D,), weight.dtype if weight_grad else None)):
+                if (t is not None) != bool(wanted):
+                    raise ValueError(_WRONG_OUT)
+                if t is not None:
+                    _check_out(t, shape, dt, dev)
+        need = ctypes.c_int64(0)
+        ws = None
+        if weight_grad:
+            _check(lib.lfmmi_add_rms_norm_workspace(B, T, D, ctypes.byref(need)))
+            ws = torch.empty(need.value, dtype=torch.uint8, device=dev)
+        dres = None if out.residual is None or out.residual is out.x else out.residual
+        _check(lib.lfmmi_add_rms_norm_backward(
+            sum.data_ptr(), stride_b, stride_t, code, B, T, D, None if lens is None else _hp(lens), _ptr(weight),
+            w_code, _ptr(rstd), _ptr(grad_y), _ptr(grad_sum), p, seed, offset, at, _ptr(out.x), _ptr(dres),
+            _ptr(out.weight), _ptr(ws), need.value, raw))
+    if not mine:
+        _written([t for t in out if t is not None])
+    return out
+
+
+def lfmmi_verify_tokens(logits, drafted=None, uniforms=None, draft_logits=None, lengths=None, scale=1.0,
+                        draft_scale=1.0, out=None, stream=None):
+    """Drafted tokens [B, K] (int32 or int64 CUDA tensor; None: K is 0) against the logits
+    [B, K + 1, V] of the model they are drafted for, and the token that follows those that are taken.
+    uniforms: float32 CUDA tensor [B, K + 1] of random numbers in [0, 1), or None: greedy.
+    draft_logits: what they were drawn from [B, K, V], of the logits' dtype, or None: nothing but the
+    tokens is known. lengths: how many each sequence has (host int array [B]), or None: K. scale,
+    draft_scale: what the logits were multiplied by. Returns VerifiedTokens (accepted [B],
+    tokens [B, K + 1], status [B]), int32 device tensors: tokens are those taken, one that follows
+    them, then -1. `out`: a VerifiedTokens to write into."""
+    import torch
+    if logits.dim() != 3:
+        raise ValueError("logits must have the shape [B, K + 1, V]")
+    code, B, rows, V, stride_b, stride_t, lens, _bytes = _logit_rows(logits, None, lengths)
+    if rows < 1:
+        raise ValueError("logits need at least one row for each sequence")
+    K, dev = rows - 1, logits.device
+    token_bytes = 4
+    if drafted is not None:
+        token_bytes = _token_bytes(drafted, "drafted")
+    if (drafted is None and K > 0) or (drafted is not None and (
+            tuple(drafted.shape) != (B, K) or not drafted.is_contiguous() or drafted.device != dev)):
+        raise ValueError("drafted must be contiguous, on the logits' device, of the shape [B, K]")
+    draft_strides = (0, 0)
+    if draft_logits is not None:
+        if uniforms is None:
+            raise ValueError("draft_logits without uniforms")
+        if tuple(draft_logits.shape) != (B, K, V) or draft_logits.dtype != logits.dtype or draft_logits.device != dev:
+            raise ValueError("draft_logits must have the shape [B, K, V], the logits' dtype and device")
+        if draft_logits.stride(2) != 1 and V > 1 and K > 0:
+            raise ValueError("the logits of a row must be next to each other")
+        draft_strides = draft_logits.stride()[:2]
+    if uniforms is not None and (tuple(uniforms.shape) != (B, rows) or uniforms.dtype != torch.float32 or
+                                 not uniforms.is_contiguous() or uniforms.device != dev):
+        raise ValueError("uniforms must be a contiguous float32 tensor [B, K + 1] on the logits' device")
+    context, raw = _on_stream(dev, stream)
+    lib = load_library()
+    mine = out is None
+    with context:
+        if mine:
+            out = VerifiedTokens(*(torch.empty(shape, dtype=torch.int32, device=dev)
+                                   for shape in ((B,), (B, rows), (B,))))
+        else:
+            for t, shape in zip(out, ((B,), (B, rows), (B,))):
+                _check_out(t, shape, torch.int32, dev)
+        need = ctypes.c_int64(0)
+        _check(lib.lfmmi_verify_tokens_workspace(B, K, V, ctypes.byref(need)))
+        ws = torch.empty(need.value, dtype=torch.uint8, device=dev)
+        _check(lib.lfmmi_verify_tokens(
+            logits.data_ptr(), code, B, K, V, stride_b, stride_t, _ptr(draft_logits) if K > 0 else None, *draft_strides,
+            _ptr(drafted) if K > 0 else None, token_bytes, None if lens is None else _hp(lens), scale, draft_scale,
+            _ptr(uniforms), out.accepted.data_ptr(), out.tokens.data_ptr(), out.status.data_ptr(), ws.data_ptr(),
+            need.value, raw))
+    if not mine:
+        _written(list(out))
+    return out

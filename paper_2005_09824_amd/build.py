@@ -7,9 +7,10 @@ import subprocess
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "liblfmmi.so")
-SOURCES = ["kernels.hip", "line.hip", "hybrid.hip", "tokens.hip", "grads.hip", "api.cpp", "operators.cpp",
-           "pack.cpp"]
-HEADERS = ["kernels.h", "device.h", "operators.h", "pack.h", "status.h", "vec16.h", "microbench.hip",
+SOURCES = ["kernels.hip", "line.hip", "hybrid.hip", "tokens.hip", "grads.hip", "embed.hip", "norm.hip",
+           "verify.hip", "api.cpp", "operators.cpp", "layers.cpp", "pack.cpp"]
+HEADERS = ["kernels.h", "device.h", "operators.h", "layers.h", "checks.h", "lanes.h", "rows.h", "pack.h",
+           "status.h", "vec16.h", "microbench.hip",
            os.path.join("..", "..", "include", "lfmmi.h")]
 
 FLAGS = [

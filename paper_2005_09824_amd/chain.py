@@ -1,6 +1,7 @@
 """LF-MMI objective as a torch.autograd.Function on top of the C ABI (Eq. 2, Eq. 3), and
-what a training step uses beside it: log probabilities of given tokens, and clipping of
-gradients to a norm.
+what a training step uses beside it: log probabilities of given tokens, clipping of
+gradients to a norm, and in front of the output layer token embeddings, dropout and the end
+of a residual block.
 
 Argument marshalling only: both forward-backward passes, the objective and its
 gradient with respect to the logits all come out of lfmmi_loss; this
@@ -107,6 +108,144 @@ def token_logprobs(logits, targets, lengths=None, scale=1.0):
     if logits.dim() and logits.shape[-1] > 1 and logits.stride(-1) != 1:
         logits = logits.contiguous()
     return _token_cls.apply(logits, targets.contiguous(), lengths, float(scale))
+
+
+def _rows_in_order(x):
+    """x with the values of a row next to each other, in a type of the library's."""
+    if x.dtype not in binding._dtype_codes():
+        x = x.float()
+    return x.contiguous() if x.dim() and x.shape[-1] > 1 and x.stride(-1) != 1 else x
+
+
+def _embed_class():
+    import torch
+    from torch.autograd.function import once_differentiable
+
+    class _EmbedTokens(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, table, tokens, lengths, scale):
+            rows, status = binding.lfmmi_embed_tokens(table, tokens, lengths, scale)
+            ctx.save_for_backward(tokens)
+            ctx.V, ctx.lengths, ctx.scale = table.shape[0], lengths, scale
+            ctx.mark_non_differentiable(status)
+            return rows, status
+
+        @staticmethod
+        @once_differentiable
+        def backward(ctx, grad_rows, _grad_status):
+            (tokens,) = ctx.saved_tensors
+            grad = binding.lfmmi_embed_tokens_backward(_rows_in_order(grad_rows), tokens, ctx.V, ctx.lengths,
+                                                       ctx.scale)
+            return grad, None, None, None
+
+    return _EmbedTokens
+
+
+_embed_cls = None
+
+
+def embed_tokens(table, tokens, lengths=None, scale=1.0):
+    """Rows of `table` [V, D] that `tokens` (int32 or int64 CUDA tensor [B, T] or [B]) name, times
+    `scale`, differentiable in the table. Negative tokens and rows behind `lengths` (host ints [B]
+    or None) give rows of 0 and no gradient. Returns (rows, status): tokens that are not below V
+    give rows of NaN, a flag (4) in status and no gradient."""
+    global _embed_cls
+    if _embed_cls is None:
+        _embed_cls = _embed_class()
+    if lengths is not None:
+        lengths = np.array(lengths, dtype=np.int32)  # (a copy: backward reads it)
+    return _embed_cls.apply(_rows_in_order(table), tokens.contiguous(), lengths, float(scale))
+
+
+def _dropout_class():
+    import torch
+    from torch.autograd.function import once_differentiable
+
+    class _Dropout(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, p, seed, offset, step):
+            ctx.draw = (p, seed, offset)
+            ctx.save_for_backward(*([] if step is None else [step]))
+            return binding.lfmmi_dropout(x, p, seed, offset, step)
+
+        @staticmethod
+        @once_differentiable
+        def backward(ctx, grad):
+            step = ctx.saved_tensors[0] if ctx.saved_tensors else None
+            return binding.lfmmi_dropout(grad.contiguous(), *ctx.draw, step), None, None, None, None
+
+    return _Dropout
+
+
+_dropout_cls = None
+
+
+def dropout(x, p, seed, offset=0, step=None):
+    """Dropout of x [..., D], differentiable in x: a share p of the values becomes 0, the others are
+    divided by 1 - p. What is kept follows from (seed, offset + step) and a value's row and
+    column: give each call of a training run another offset. step: an int64 CUDA tensor of one
+    value or None; backward reads it again, and refuses if it has been written since by an operation
+    that torch knows of."""
+    global _dropout_cls
+    if _dropout_cls is None:
+        _dropout_cls = _dropout_class()
+    x = _rows_in_order(x)
+    try:
+        binding._flat_rows(x)
+    except ValueError:
+        x = x.contiguous()
+    return _dropout_cls.apply(x, float(p), int(seed), int(offset), step)
+
+
+def _norm_class():
+    import torch
+    from torch.autograd.function import once_differentiable
+
+    class _AddRmsNorm(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, residual, weight, eps, lengths, p, seed, offset, step):
+            ctx.set_materialize_grads(False)  # what the loss does not use costs nothing
+            r = binding.lfmmi_add_rms_norm(x, residual, weight, eps, lengths, p, seed, offset, step)
+            ctx.draw, ctx.lengths, ctx.residual = (p, seed, offset), lengths, residual is not None
+            ctx.save_for_backward(r.sum, r.rstd, weight, step)
+            return r.y, (r.sum.view_as(r.sum) if r.sum is x else r.sum)
+
+        @staticmethod
+        @once_differentiable
+        def backward(ctx, grad_y, grad_sum):
+            none = (None,) * 9
+            if grad_y is None and grad_sum is None:
+                return none
+            total, rstd, weight, step = ctx.saved_tensors
+            as_rows = lambda g: None if g is None else g.contiguous()
+            g = binding.lfmmi_add_rms_norm_backward(total, rstd, weight, as_rows(grad_y), as_rows(grad_sum),
+                                                    ctx.lengths, *ctx.draw, step, residual=ctx.residual,
+                                                    weight_grad=ctx.needs_input_grad[2])
+            return (g.x, g.residual, g.weight) + none[3:]
+
+    return _AddRmsNorm
+
+
+_norm_cls = None
+
+
+def add_rms_norm(x, residual=None, weight=None, eps=1e-6, lengths=None, p=0.0, seed=0, offset=0, step=None):
+    """The end of a residual block: sum = residual + dropout(x) and y = sum / sqrt(mean(sum^2) + eps)
+    * weight, rows [B, T, D] or [B, D], differentiable in x, residual and weight. Rows behind
+    `lengths` (host ints [B] or None) give 0 and no gradient; p, seed, offset, step: as for
+    dropout. Returns (y, sum): sum is what the next block adds to (x itself, rows behind its
+    lengths too, where nothing is added or dropped)."""
+    global _norm_cls
+    if _norm_cls is None:
+        _norm_cls = _norm_class()
+    if lengths is not None:
+        lengths = np.array(lengths, dtype=np.int32)  # (a copy: backward reads it)
+    x = _rows_in_order(x)
+    if residual is not None:
+        residual = _rows_in_order(residual.to(x.dtype))
+    if weight is not None:
+        weight = weight.contiguous()
+    return _norm_cls.apply(x, residual, weight, float(eps), lengths, float(p), int(seed), int(offset), step)
 
 
 def clip_grad_norm(parameters, max_norm):

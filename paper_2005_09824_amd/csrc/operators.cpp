@@ -7,6 +7,7 @@
 #include <string>
 #include <vector>
 
+#include "checks.h"
 #include "operators.h"
 #include "status.h"
 
@@ -18,14 +19,6 @@ static_assert(LFMMI_GRAD_WORKSPACE_BYTES(0) >= 8 * kGradBlocks + 16 + 4, "the he
 
 namespace {
 
-constexpr int64_t kCacheBytes = (int64_t)256 << 20;  // behind the L2s
-
-size_t dtype_size(int32_t dtype) { return dtype == LFMMI_F32 ? 4 : 2; }
-
-bool known(int32_t dtype) { return dtype == LFMMI_F32 || dtype == LFMMI_BF16 || dtype == LFMMI_F16; }
-
-bool aligned(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
-
 // What the forward and the backward call check alike.
 lfmmi_status check_rows(const void* logits, int32_t dtype, int32_t B, int32_t T, int32_t V,
                         int64_t stride_b, int64_t stride_t, const int32_t* lengths,
@@ -36,47 +29,18 @@ lfmmi_status check_rows(const void* logits, int32_t dtype, int32_t B, int32_t T,
     if (V < 1) return fail(LFMMI_ERR_INVALID_ARG, "V must be >= 1");
     if ((int64_t)B * T > INT32_MAX) return fail(LFMMI_ERR_UNSUPPORTED, "B * T exceeds 2^31 - 1");
     if (V > (1 << 30)) return fail(LFMMI_ERR_UNSUPPORTED, "V exceeds 2^30");
-    if (stride_b < 0 || stride_t < 0) return fail(LFMMI_ERR_INVALID_ARG, "strides must be >= 0");
-    // so that no offset passes 64 bits
-    if (stride_b > ((int64_t)1 << 60) / std::max(B, 1) || stride_t > ((int64_t)1 << 60) / std::max(T, 1))
-        return fail(LFMMI_ERR_UNSUPPORTED, "strides beyond 2^60 elements");
+    lfmmi_status st = check_strides(stride_b, stride_t, B, T);
+    if (st != LFMMI_OK) return st;
     if (!(scale >= 1e-6f && scale <= 1e6f))
         return fail(LFMMI_ERR_INVALID_ARG, "scale outside [1e-6, 1e6]");
     if (targets && target_bytes != 4 && target_bytes != 8)
         return fail(LFMMI_ERR_INVALID_ARG, "target_bytes must be 4 or 8");
-    if (lengths)
-        for (int32_t b = 0; b < B; ++b)
-            if (lengths[b] < 0 || lengths[b] > T)
-                return fail(LFMMI_ERR_INVALID_ARG, "lengths[" + std::to_string(b) + "] outside [0, T]");
+    if ((st = check_lengths(lengths, B, T)) != LFMMI_OK) return st;
     if (B == 0 || T == 0) return LFMMI_OK;
     if (!logits) return fail(LFMMI_ERR_INVALID_ARG, "logits is null");
     if (!aligned(logits, dtype_size(dtype)) || (targets && !aligned(targets, target_bytes)))
         return fail(LFMMI_ERR_INVALID_ARG, "an array is not aligned to its elements");
     return LFMMI_OK;
-}
-
-// Sequences that one launch takes, and their lengths.
-int32_t fill_lengths(const int32_t* lengths, int32_t b, int32_t B, SeqLengths* out)
-{
-    if (!lengths) {
-        out->n = 0;
-        return B - b;
-    }
-    const int32_t n = std::min(B - b, kLengthsPerLaunch);
-    out->n = n;
-    std::copy(lengths + b, lengths + b + n, out->T);
-    return n;
-}
-
-template <typename U>
-U* at(U* p, int64_t i)
-{
-    return p ? p + i : nullptr;
-}
-
-const void* at_bytes(const void* p, int64_t i)
-{
-    return p ? static_cast<const char*>(p) + i : nullptr;
 }
 
 // What both calls write beside gradients.
@@ -125,26 +89,6 @@ lfmmi_status check_grads(int32_t n, const void* const* grads, const int64_t* cou
             return fail_written();
     }
     return LFMMI_OK;
-}
-
-struct Span {
-    uintptr_t at, end;
-    bool written;
-};
-
-// Whether an array that is written overlaps another array.
-bool overlap(std::vector<Span>& spans)
-{
-    const auto before = [](const Span& a, const Span& b) { return a.at < b.at; };
-    if (!std::is_sorted(spans.begin(), spans.end(), before))
-        std::sort(spans.begin(), spans.end(), before);
-    uintptr_t any = 0, written = 0;  // ends of what came before
-    for (const Span& s : spans) {
-        if (s.at < written || (s.written && s.at < any)) return true;
-        any = std::max(any, s.end);
-        if (s.written) written = std::max(written, s.end);
-    }
-    return false;
 }
 
 lfmmi_status check_outs(int32_t n, const void* const* grads, void* const* outs,

@@ -5,6 +5,7 @@
 #include <algorithm>
 
 #include "../../include/lfmmi.h"
+#include "lanes.h"
 #include "operators.h"
 #include "vec16.h"
 
@@ -39,18 +40,8 @@ __device__ __forceinline__ uint64_t uniform(uint64_t v)
 }
 __device__ __forceinline__ float uniform(float v) { return __uint_as_float(uniform(__float_as_uint(v))); }
 
-// ---- reductions over G lanes: 16 (a DPP row) or 64 (a wave); every lane has the result
+// ---- reductions over a wave; every lane has the result
 
-template <int Ror>
-__device__ __forceinline__ float rotated(float v)
-{
-    const int i = __float_as_int(v);
-    return __int_as_float(__builtin_amdgcn_update_dpp(i, i, 0x120 + Ror, 0xf, 0xf, true));
-}
-__device__ __forceinline__ float lane_of(float v, int lane)
-{
-    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane));
-}
 __device__ __forceinline__ uint32_t all_bits(uint32_t v)  // of a wave, and-ed
 {
 #define LFMMI_ROR(n) __builtin_amdgcn_update_dpp(v, v, 0x120 + n, 0xf, 0xf, true)
@@ -74,27 +65,6 @@ __device__ __forceinline__ uint32_t max_of_four(uint32_t v)
 {
     v = max_of_two(v);
     return max(v, (uint32_t)__builtin_amdgcn_update_dpp(v, v, 0x4e, 0xf, 0xf, true));
-}
-
-template <int G>
-__device__ __forceinline__ float sum_over(float v)
-{
-    v += rotated<8>(v);
-    v += rotated<4>(v);
-    v += rotated<2>(v);
-    v += rotated<1>(v);
-    if (G == 64) v = (lane_of(v, 0) + lane_of(v, 16)) + (lane_of(v, 32) + lane_of(v, 48));
-    return v;
-}
-template <int G>
-__device__ __forceinline__ float max_over(float v)
-{
-    v = fmaxf(v, rotated<8>(v));
-    v = fmaxf(v, rotated<4>(v));
-    v = fmaxf(v, rotated<2>(v));
-    v = fmaxf(v, rotated<1>(v));
-    if (G == 64) v = fmaxf(fmaxf(lane_of(v, 0), lane_of(v, 16)), fmaxf(lane_of(v, 32), lane_of(v, 48)));
-    return v;
 }
 
 // What a lane, a wave and a workgroup know of the logits they have read: the largest of them,
