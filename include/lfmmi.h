@@ -362,7 +362,7 @@ lfmmi_status lfmmi_embed_tokens_workspace(int32_t V, int32_t D, int32_t B, int32
  * Philox4x32-10 for the counter (c / 8, r, low and high word of draw) and the key (low and high
  * word of seed), c is kept if the 16 bits c % 8 of w (the low half of w[0] first) are at least
  * 65536 p'. No mask is stored: the gradient is the same call on the gradient of y.
- *   x        [R, D] of `dtype`, row r at r * stride elements (stride >= 0)
+ *   x        [R, D] of `dtype`, D <= 2^30, row r at r * stride elements (stride >= 0)
  *   y        [R, D]; or x itself, laid out as it is (stride >= D)
  */
 lfmmi_status lfmmi_dropout(const void *x, int32_t dtype, int32_t R, int32_t D, int64_t stride,

@@ -802,7 +802,7 @@ def lfmmi_dropout(x, p, seed, offset=0, step=None, out=None, stream=None):
     if not x.is_cuda or code is None:
         raise ValueError("x must be a float32, bfloat16 or float16 CUDA tensor")
     R, D, stride = _flat_rows(x)
-    if R >= 1 << 31 or D >= 1 << 31:
+    if R >= 1 << 31 or D > 1 << 30:
         raise ValueError("too many rows or columns")
     dev = x.device
     p, seed, offset, at = _draw_args(p, seed, offset, step, dev)

@@ -48,7 +48,7 @@ int grid_of(int64_t units) { return (int)std::min<int64_t>(units, 1 << 20); }
 
 constexpr int kEmbedChunks = 2;
 
-template <typename T>
+template <typename T, bool Whole>
 __global__ __launch_bounds__(kThreads) void k_embed(EmbedParams p, SeqLengths lens, Tiles tiles)
 {
     using Store = typename T::Store;
@@ -70,7 +70,7 @@ __global__ __launch_bounds__(kThreads) void k_embed(EmbedParams p, SeqLengths le
 #pragma unroll
             for (int i = 0; i < 8; ++i) f[k][i] = bad ? NAN : 0.f;
             if (c < chunks && !bad && token >= 0)
-                load8<T>(static_cast<const Store*>(p.table) + token * p.stride + c * 8, p.D - c * 8, f[k]);
+                load_at<T, Whole>(static_cast<const Store*>(p.table) + token * p.stride, c, p.D, f[k]);
         }
 #pragma unroll
         for (int k = 0; k < kEmbedChunks; ++k) {
@@ -78,7 +78,7 @@ __global__ __launch_bounds__(kThreads) void k_embed(EmbedParams p, SeqLengths le
             if (c >= chunks) continue;
 #pragma unroll
             for (int i = 0; i < 8; ++i) f[k][i] = token < 0 ? 0.f : f[k][i] * p.scale;
-            store8<T>(static_cast<Store*>(p.out) + (int64_t)row * p.D + c * 8, p.D - c * 8, f[k]);
+            store_at<T, Whole>(static_cast<Store*>(p.out) + (int64_t)row * p.D, c, p.D, f[k]);
         }
     }
 }
@@ -232,46 +232,46 @@ __global__ __launch_bounds__(kThreads) void k_embed_starts(const uint32_t* keys,
 // ---- sums of rows
 
 // Adds the chunk of positions order[from..from + n - 1] up, in that order.
-template <typename T>
+template <typename T, bool Whole>
 __device__ __forceinline__ void add_rows(const EmbedGradParams& p, const uint32_t* order, uint32_t from, uint32_t n,
                                          int c, float* s)
 {
     using Store = typename T::Store;
     constexpr int kAtOnce = 4;
-    const Store* g = static_cast<const Store*>(p.g) + c * 8;
-    const int left = p.D - c * 8;
+    const Store* g = static_cast<const Store*>(p.g);
 #pragma unroll
     for (int i = 0; i < 8; ++i) s[i] = 0.f;
     for (uint32_t k = 0; k < n; k += kAtOnce) {
-        float f[kAtOnce][8];
+        Raw<T> v[kAtOnce];
 #pragma unroll
         for (int j = 0; j < kAtOnce; ++j) {
-            if (k + j >= n) continue;
-            const uint32_t pos = order[from + k + j], b = pos / (uint32_t)p.T;
-            load8<T>(g + (int64_t)b * p.stride_b + (int64_t)(pos - b * (uint32_t)p.T) * p.stride_t, left, f[j]);
+            const uint32_t pos = order[from + min(k + j, n - 1)], b = pos / (uint32_t)p.T;
+            v[j] = raw_at<T, Whole>(g + (int64_t)b * p.stride_b + (int64_t)(pos - b * (uint32_t)p.T) * p.stride_t, c, p.D);
         }
 #pragma unroll
         for (int j = 0; j < kAtOnce; ++j) {
             if (k + j >= n) continue;
+            float f[8];
+            unpack_at<T, Whole>(v[j], c, p.D, f);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) s[i] += f[j][i];
+            for (int i = 0; i < 8; ++i) s[i] += f[i];
         }
     }
 }
 
-template <typename T>
+template <typename T, bool Whole>
 __device__ __forceinline__ void write_grad(const EmbedGradParams& p, uint32_t v, int c, const float* s)
 {
-    typename T::Store* out = static_cast<typename T::Store*>(p.grad) + (int64_t)v * p.D + c * 8;
+    typename T::Store* out = static_cast<typename T::Store*>(p.grad) + (int64_t)v * p.D;
     float f[8];
-    if (p.accumulate) load8<T>(out, p.D - c * 8, f);
+    if (p.accumulate) load_at<T, Whole>(out, c, p.D, f);
 #pragma unroll
     for (int i = 0; i < 8; ++i) f[i] = p.accumulate ? f[i] + s[i] * p.scale : s[i] * p.scale;
-    store8<T>(out, p.D - c * 8, f);
+    store_at<T, Whole>(out, c, p.D, f);
 }
 
 // Rows of the table with at most kEmbedPiece positions, those with none among them.
-template <typename T>
+template <typename T, bool Whole>
 __global__ __launch_bounds__(kThreads) void k_embed_rows(EmbedGradParams p, Tiles tiles, const uint32_t* starts,
                                                          const uint32_t* order)
 {
@@ -284,12 +284,12 @@ __global__ __launch_bounds__(kThreads) void k_embed_rows(EmbedGradParams p, Tile
         const uint32_t from = starts[v], n = starts[v + 1] - from;
         if (n > kEmbedPiece || (n == 0 && p.accumulate)) continue;
         float s[8];
-        add_rows<T>(p, order, from, n, c, s);
-        write_grad<T>(p, (uint32_t)v, c, s);
+        add_rows<T, Whole>(p, order, from, n, c, s);
+        write_grad<T, Whole>(p, (uint32_t)v, c, s);
     }
 }
 
-template <typename T>
+template <typename T, bool Whole>
 __global__ __launch_bounds__(kThreads) void k_embed_pieces(EmbedGradParams p, Tiles tiles, const uint32_t* counts,
                                                            const uint2* piece, const uint32_t* order, float* partials)
 {
@@ -302,13 +302,13 @@ __global__ __launch_bounds__(kThreads) void k_embed_pieces(EmbedGradParams p, Ti
         if (k >= n || c >= chunks) continue;
         const uint2 q = piece[k];
         float s[8];
-        add_rows<T>(p, order, q.x, q.y, c, s);
-        store8<F32>(partials + k * p.D + c * 8, p.D - c * 8, s);
+        add_rows<T, Whole>(p, order, q.x, q.y, c, s);
+        store_at<F32, Whole>(partials + k * p.D, c, p.D, s);
     }
 }
 
 // Frequent tokens, from their pieces.
-template <typename T>
+template <typename T, bool Whole>
 __global__ __launch_bounds__(kThreads) void k_embed_join(EmbedGradParams p, Tiles tiles, const uint32_t* counts,
                                                          const uint2* first, const uint32_t* starts,
                                                          const float* partials)
@@ -321,24 +321,16 @@ __global__ __launch_bounds__(kThreads) void k_embed_join(EmbedGradParams p, Tile
         const int c = (int)(u - group * tiles.pieces) * lanes + lane;
         if (k >= heavy || c >= chunks) continue;
         const uint32_t v = first[k].x, n = (starts[v + 1] - starts[v] + kEmbedPiece - 1) / kEmbedPiece;
-        const float* part = partials + (int64_t)first[k].y * p.D + c * 8;
+        const float* part = partials + (int64_t)first[k].y * p.D;
         float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
         for (uint32_t i = 0; i < n; ++i) {
             float f[8];
-            load8<F32>(part + (int64_t)i * p.D, p.D - c * 8, f);
+            load_at<F32, Whole>(part + (int64_t)i * p.D, c, p.D, f);
 #pragma unroll
             for (int j = 0; j < 8; ++j) s[j] += f[j];
         }
-        write_grad<T>(p, v, c, s);
+        write_grad<T, Whole>(p, v, c, s);
     }
-}
-
-template <typename F>
-void by_type(int dtype, F&& f)
-{
-    if (dtype == LFMMI_F32) f(F32{});
-    else if (dtype == LFMMI_BF16) f(Bf16{});
-    else f(F16{});
 }
 
 template <typename U>
@@ -353,7 +345,9 @@ hipError_t launch_embed(const EmbedParams& p, const SeqLengths& lens, int dtype,
 {
     const Tiles t = tiles_of<kEmbedChunks>((int64_t)p.B * p.T, p.D);
     by_type(dtype, [&](auto type) {
-        k_embed<decltype(type)><<<grid_of(t.units), kThreads, 0, stream>>>(p, lens, t);
+        by_whole(p.D, [&](auto whole) {
+            k_embed<decltype(type), decltype(whole)::value><<<grid_of(t.units), kThreads, 0, stream>>>(p, lens, t);
+        });
     });
     return hipGetLastError();
 }
@@ -423,12 +417,17 @@ hipError_t launch_embed_grad(const EmbedGradParams& p, int dtype, hipStream_t st
     k_embed_starts<<<grid_of(v), kThreads, 0, stream>>>(keys[now], N, p.V, starts, counts, first, piece);
     const Tiles rows = tiles_of<1>(p.V, p.D);
     by_type(dtype, [&](auto type) {
-        using T = decltype(type);
-        k_embed_rows<T><<<grid_of(rows.units), kThreads, 0, stream>>>(p, rows, starts, order[now]);
-        if (plan.heavy == 0) return;
-        const Tiles pieces = tiles_of<1>(plan.pieces, p.D), heavy = tiles_of<1>(plan.heavy, p.D);
-        k_embed_pieces<T><<<grid_of(pieces.units), kThreads, 0, stream>>>(p, pieces, counts, piece, order[now], partials);
-        k_embed_join<T><<<grid_of(heavy.units), kThreads, 0, stream>>>(p, heavy, counts, first, starts, partials);
+        by_whole(p.D, [&](auto whole) {
+            using T = decltype(type);
+            constexpr bool kWhole = decltype(whole)::value;
+            k_embed_rows<T, kWhole><<<grid_of(rows.units), kThreads, 0, stream>>>(p, rows, starts, order[now]);
+            if (plan.heavy == 0) return;
+            const Tiles pieces = tiles_of<1>(plan.pieces, p.D), heavy = tiles_of<1>(plan.heavy, p.D);
+            k_embed_pieces<T, kWhole>
+                <<<grid_of(pieces.units), kThreads, 0, stream>>>(p, pieces, counts, piece, order[now], partials);
+            k_embed_join<T, kWhole>
+                <<<grid_of(heavy.units), kThreads, 0, stream>>>(p, heavy, counts, first, starts, partials);
+        });
     });
     return hipGetLastError();
 }

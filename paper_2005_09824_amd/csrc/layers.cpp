@@ -174,6 +174,7 @@ lfmmi_status lfmmi_dropout(const void* x, int32_t dtype, int32_t R, int32_t D, i
 try {
     if (!known(dtype)) return fail(LFMMI_ERR_INVALID_ARG, "unknown dtype");
     if (R < 0 || D < 0) return fail(LFMMI_ERR_INVALID_ARG, "R and D must be >= 0");
+    if (D > (1 << 30)) return fail(LFMMI_ERR_UNSUPPORTED, "D exceeds 2^30");
     lfmmi_status st = check_strides(stride, 0, R, 1);
     DropoutParams q{x, y, stride, y == x ? stride : (int64_t)D, R, D, {}};
     if (st == LFMMI_OK) st = make_draw(p, seed, offset, step, &q.draw);

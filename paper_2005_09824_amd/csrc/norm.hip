@@ -18,38 +18,41 @@ constexpr float kE4m3Max = 448.f;
 constexpr float kSmaller = 0x1p-80f;            // the square of the largest float times that has an exponent of 96
 constexpr float kLeastScale = 1.17549435e-38f;  // 2^-126: its inverse is finite
 
-constexpr int threads_of(int lanes) { return lanes > kThreads ? lanes : kThreads; }
+// Waves of one workgroup take a row each, or all of them one together.
+constexpr int threads_of(int lanes) { return lanes == 64 ? kThreads : lanes; }
 
 // ---- dropout alone
 
 constexpr int kDropoutChunks = 4;  // of eight values, that a lane takes of a row
 
-template <typename T>
+template <typename T, bool Whole>
 __global__ __launch_bounds__(kThreads) void k_dropout(DropoutParams p, int lanes_log2, uint32_t pieces, uint32_t units)
 {
     using Store = typename T::Store;
     const Dropping drop(p.draw);
     const int lanes = 1 << lanes_log2, lane = threadIdx.x & (lanes - 1), sub = threadIdx.x >> lanes_log2;
-    const int rows = kThreads >> lanes_log2;
+    const int rows = kThreads >> lanes_log2, chunks = (p.D + 7) / 8;
     for (uint32_t u = blockIdx.x; u < units; u += gridDim.x) {
         const uint32_t group = u / pieces;
         const int64_t row = (int64_t)group * rows + sub;
         if (row >= p.R) continue;
         const Store* x = static_cast<const Store*>(p.x) + row * p.stride_x;
         Store* y = static_cast<Store*>(p.y) + row * p.stride_y;
-        const int64_t first = (int64_t)(u - group * pieces) * kDropoutChunks * lanes + lane;
-        float f[kDropoutChunks][8];
+        const int first = (int)(u - group * pieces) * kDropoutChunks * lanes + lane;
+        Raw<T> v[kDropoutChunks];
 #pragma unroll
         for (int k = 0; k < kDropoutChunks; ++k) {
-            const int64_t c = first + k * lanes;
-            if (c * 8 < p.D) load8<T>(x + c * 8, (int)min((int64_t)8, p.D - c * 8), f[k]);
+            const int c = first + k * lanes;
+            if (c < chunks) v[k] = raw_at<T, Whole>(x, c, p.D);
         }
 #pragma unroll
         for (int k = 0; k < kDropoutChunks; ++k) {
-            const int64_t c = first + k * lanes;
-            if (c * 8 >= p.D) continue;
-            if (drop.threshold > 0) drop.apply((uint32_t)row, (uint32_t)c, f[k]);
-            store8<T>(y + c * 8, (int)min((int64_t)8, p.D - c * 8), f[k]);
+            const int c = first + k * lanes;
+            if (c >= chunks) continue;
+            float f[8];
+            unpack_at<T, Whole>(v[k], c, p.D, f);
+            if (drop.threshold > 0) drop.apply((uint32_t)row, (uint32_t)c, f);
+            store_at<T, Whole>(y, c, p.D, f);
         }
     }
 }
@@ -84,16 +87,16 @@ __device__ __forceinline__ int64_t offset_of(uint32_t row, int T, int64_t stride
     return (int64_t)(row / (uint32_t)T) * stride_b + (int64_t)(row % (uint32_t)T) * stride_t;
 }
 
-template <typename T>
-__device__ __forceinline__ void load_weight(const void* w, bool f32, int c, int left, float* f)
+template <typename T, bool Whole>
+__device__ __forceinline__ void load_weight(const void* w, bool f32, int c, int D, float* f)
 {
     if (!w) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) f[i] = 1.f;
     } else if (f32) {
-        load8<F32>(static_cast<const float*>(w) + c * 8, left, f);
+        load_at<F32, Whole>(static_cast<const float*>(w), c, D, f);
     } else {
-        load8<T>(static_cast<const typename T::Store*>(w) + c * 8, left, f);
+        load_at<T, Whole>(static_cast<const typename T::Store*>(w), c, D, f);
     }
 }
 
@@ -109,9 +112,11 @@ __device__ __forceinline__ void store_bytes(uint8_t* q, int left, const float* f
         __builtin_memcpy(q, w, 8);
         return;
     }
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if (i < left) q[i] = (uint8_t)(w[i >> 2] >> (8 * (i & 3)));
+    const uint32_t rest = left & 4 ? w[1] : w[0];
+    if (left & 4) __builtin_memcpy(q, &w[0], 4);
+    const uint16_t two = (uint16_t)rest;
+    if (left & 2) __builtin_memcpy(q + (left & 4), &two, 2);
+    if (left & 1) q[left - 1] = (uint8_t)(left & 2 ? rest >> 16 : rest);
 }
 
 // A value as it is kept in the type.
@@ -124,12 +129,19 @@ __device__ __forceinline__ float rounded(float v)
     return T::load(&s);
 }
 
+// Which of a workgroup's rows a wave has: the same in all its lanes, and held once.
+template <int G>
+__device__ __forceinline__ int row_in_group()
+{
+    return threads_of(G) == G ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / G);
+}
+
 // Bits of |y| as whole numbers: the largest of them is a NaN's, if there is one.
 __device__ __forceinline__ uint32_t magnitude(float y) { return __float_as_uint(y) & 0x7fffffffu; }
 
 // G lanes take a row, N chunks of eight values each, which stay in registers; N == 0: any number of
 // chunks, read again for each pass over the row.
-template <typename T, int G, int N>
+template <typename T, bool Whole, int G, int N>
 __global__ __launch_bounds__(threads_of(G)) void k_norm(NormParams p, SeqLengths lens)
 {
     using Store = typename T::Store;
@@ -137,9 +149,9 @@ __global__ __launch_bounds__(threads_of(G)) void k_norm(NormParams p, SeqLengths
     constexpr int kHeld = N > 0 ? N : 1;
     __shared__ float parts[2][G / 64];
     const Dropping drop(p.draw);
-    const int lane = threadIdx.x % G, chunks = (p.D + 7) / 8;
+    const int lane = threadIdx.x % G, sub = row_in_group<G>(), chunks = (p.D + 7) / 8;
     const uint32_t rows = (uint32_t)p.B * (uint32_t)p.T;
-    for (uint32_t row = blockIdx.x * kRows + threadIdx.x / G; row < rows; row += gridDim.x * kRows) {
+    for (uint32_t row = blockIdx.x * kRows + sub; row < rows; row += gridDim.x * kRows) {
         const Store* x = static_cast<const Store*>(p.x) + offset_of(row, p.T, p.x_stride_b, p.x_stride_t);
         const Store* res = p.residual
             ? static_cast<const Store*>(p.residual) + offset_of(row, p.T, p.r_stride_b, p.r_stride_t) : nullptr;
@@ -148,14 +160,13 @@ __global__ __launch_bounds__(threads_of(G)) void k_norm(NormParams p, SeqLengths
         Store* y = p.y ? static_cast<Store*>(p.y) + at : nullptr;
         uint8_t* q = p.q ? p.q + at : nullptr;
         float h[kHeld][8];
-        const auto left_of = [&](int c) { return p.D - c * 8; };
         if (!inside(lens, row, p.T)) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) h[0][i] = 0.f;
             for (int c = lane; c < chunks; c += G) {
-                if (sum) store8<T>(sum + c * 8, left_of(c), h[0]);
-                if (y) store8<T>(y + c * 8, left_of(c), h[0]);
-                if (q) store_bytes(q + c * 8, left_of(c), h[0]);
+                if (sum) store_at<T, Whole>(sum, c, p.D, h[0]);
+                if (y) store_at<T, Whole>(y, c, p.D, h[0]);
+                if (q) store_bytes(q + c * 8, p.D - c * 8, h[0]);
             }
             if (lane == 0) {
                 if (p.rstd) p.rstd[row] = 0.f;
@@ -163,33 +174,38 @@ __global__ __launch_bounds__(threads_of(G)) void k_norm(NormParams p, SeqLengths
             }
             continue;
         }
-        const auto added = [&](int c, float* f) {
+        const auto add_up = [&](int c, const Raw<T>& a, const Raw<T>& b, float* f) {
             float r[8];
-            load8<T>(x + c * 8, left_of(c), f);
-            if (res) load8<T>(res + c * 8, left_of(c), r);
+            unpack_at<T, Whole>(a, c, p.D, f);
+            if (res) unpack_at<T, Whole>(b, c, p.D, r);
             if (drop.threshold > 0) drop.apply((uint32_t)(p.row + row), (uint32_t)c, f);
 #pragma unroll
             for (int i = 0; i < 8; ++i) f[i] = rounded<T>(res ? f[i] + r[i] : f[i]);
         };
         float s = 0.f;
         if (N > 0) {
+            Raw<T> a[kHeld], b[kHeld];  // (all on their way before one is waited for)
 #pragma unroll
             for (int k = 0; k < kHeld; ++k) {
                 const int c = lane + k * G;
+                a[k] = b[k] = no_values<T>();
                 if (c < chunks) {
-                    added(c, h[k]);
-                    if (sum) store8<T>(sum + c * 8, left_of(c), h[k]);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) h[k][i] = 0.f;
+                    a[k] = raw_at<T, Whole>(x, c, p.D);
+                    if (res) b[k] = raw_at<T, Whole>(res, c, p.D);
                 }
+            }
+#pragma unroll
+            for (int k = 0; k < kHeld; ++k) {
+                const int c = lane + k * G;
+                add_up(c, a[k], b[k], h[k]);
+                if (c < chunks && sum) store_at<T, Whole>(sum, c, p.D, h[k]);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) s = fmaf(h[k][i], h[k][i], s);
             }
         } else {
             for (int c = lane; c < chunks; c += G) {
-                added(c, h[0]);
-                if (sum) store8<T>(sum + c * 8, left_of(c), h[0]);
+                add_up(c, raw_at<T, Whole>(x, c, p.D), res ? raw_at<T, Whole>(res, c, p.D) : no_values<T>(), h[0]);
+                if (sum) store_at<T, Whole>(sum, c, p.D, h[0]);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) s = fmaf(h[0][i], h[0][i], s);
             }
@@ -206,7 +222,7 @@ __global__ __launch_bounds__(threads_of(G)) void k_norm(NormParams p, SeqLengths
                     for (int i = 0; i < 8; ++i) s = fmaf(h[k][i] * kSmaller, h[k][i] * kSmaller, s);
             } else {
                 for (int c = lane; c < chunks; c += G) {
-                    load8<T>(sum ? sum + c * 8 : x + c * 8, left_of(c), h[0]);
+                    load_at<T, Whole>(sum ? sum : x, c, p.D, h[0]);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) s = fmaf(h[0][i] * kSmaller, h[0][i] * kSmaller, s);
                 }
@@ -219,8 +235,8 @@ __global__ __launch_bounds__(threads_of(G)) void k_norm(NormParams p, SeqLengths
         // (what a lane has written itself is read again: from `sum`, or from x where nothing was added)
         const auto scaled = [&](int c, int k, float* f) {
             float w[8];
-            load_weight<T>(p.weight, p.weight_f32, c, left_of(c), w);
-            if (N == 0) load8<T>(sum ? sum + c * 8 : x + c * 8, left_of(c), h[0]);
+            load_weight<T, Whole>(p.weight, p.weight_f32, c, p.D, w);
+            if (N == 0) load_at<T, Whole>(sum ? sum : x, c, p.D, h[0]);
 #pragma unroll
             for (int i = 0; i < 8; ++i) f[i] = h[N > 0 ? k : 0][i] * rstd * w[i];
         };
@@ -232,7 +248,7 @@ __global__ __launch_bounds__(threads_of(G)) void k_norm(NormParams p, SeqLengths
                 if (c >= chunks) continue;
                 float f[8];
                 scaled(c, k, f);
-                if (y) store8<T>(y + c * 8, left_of(c), f);
+                if (y) store_at<T, Whole>(y, c, p.D, f);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     top = max(top, magnitude(f[i]));
@@ -243,7 +259,7 @@ __global__ __launch_bounds__(threads_of(G)) void k_norm(NormParams p, SeqLengths
             for (int c = lane; c < chunks; c += G) {
                 float f[8];
                 scaled(c, 0, f);
-                if (y) store8<T>(y + c * 8, left_of(c), f);
+                if (y) store_at<T, Whole>(y, c, p.D, f);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) top = max(top, magnitude(f[i]));
             }
@@ -263,7 +279,7 @@ __global__ __launch_bounds__(threads_of(G)) void k_norm(NormParams p, SeqLengths
                 if (c >= chunks) continue;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) h[k][i] *= inverse;
-                store_bytes(q + c * 8, left_of(c), h[k]);
+                store_bytes(q + c * 8, p.D - c * 8, h[k]);
             }
         } else {
             for (int c = lane; c < chunks; c += G) {
@@ -271,15 +287,23 @@ __global__ __launch_bounds__(threads_of(G)) void k_norm(NormParams p, SeqLengths
                 scaled(c, 0, f);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) f[i] *= inverse;
-                store_bytes(q + c * 8, left_of(c), f);
+                store_bytes(q + c * 8, p.D - c * 8, f);
             }
         }
     }
 }
 
+// Hides from the compiler what a chunk holds: what has been unpacked from it before is not kept for the next time.
+template <typename T>
+__device__ __forceinline__ void hide(Raw<T>& v)
+{
+#pragma unroll
+    for (int k = 0; k < 8 / T::kVec; ++k) asm volatile("" : "+v"(v.r[k].x), "+v"(v.r[k].y), "+v"(v.r[k].z), "+v"(v.r[k].w));
+}
+
 // The same lanes and chunks; a workgroup adds its rows' share of the weight's gradient up, and leaves it as a
 // row of partial sums.
-template <typename T, int G, int N>
+template <typename T, bool Whole, int G, int N>
 __global__ __launch_bounds__(threads_of(G)) void k_norm_grad(NormGradParams p, SeqLengths lens)
 {
     using Store = typename T::Store;
@@ -287,7 +311,7 @@ __global__ __launch_bounds__(threads_of(G)) void k_norm_grad(NormGradParams p, S
     constexpr int kHeld = N > 0 ? N : 1;
     __shared__ float parts[G / 64];
     const Dropping drop(p.draw);
-    const int lane = threadIdx.x % G, sub = threadIdx.x / G, chunks = (p.D + 7) / 8;
+    const int lane = threadIdx.x % G, sub = row_in_group<G>(), chunks = (p.D + 7) / 8;
     const uint32_t rows = (uint32_t)p.B * (uint32_t)p.T;
     float dw[kHeld][8];
 #pragma unroll
@@ -296,92 +320,131 @@ __global__ __launch_bounds__(threads_of(G)) void k_norm_grad(NormGradParams p, S
         for (int i = 0; i < 8; ++i) dw[k][i] = 0.f;
     float* partial = p.partials ? p.partials + (int64_t)blockIdx.x * p.D : nullptr;
     if (N == 0 && partial && !p.add)
-        for (int c = lane; c < chunks; c += G) store8<F32>(partial + c * 8, p.D - c * 8, dw[0]);
-    for (uint32_t row = blockIdx.x * kRows + sub; row < rows; row += gridDim.x * kRows) {
+        for (int c = lane; c < chunks; c += G) store_at<F32, Whole>(partial, c, p.D, dw[0]);
+    const uint32_t stride = gridDim.x * kRows;
+    const auto row_of = [&](uint32_t row) {
+        return static_cast<const Store*>(p.h) + offset_of(row, p.T, p.stride_b, p.stride_t);
+    };
+    const auto dy_of = [&](uint32_t row) { return static_cast<const Store*>(p.grad_y) + (int64_t)row * p.D; };
+    // What a row begins with is asked for while the row before is dealt with, and the weight is held; two chunks a lane
+    // of 1,024 have no registers for that (16,384 columns of bf16, 8,000 rows: 448 us so, 340 without).
+    constexpr bool kAhead = N > 0 && G * N < 2048;
+    Raw<T> h_next[kHeld], y_next[kHeld];
+    float rstd_next = 0.f;
+    const auto ask = [&](uint32_t row) {
+        if (N == 0 || row >= rows || !inside(lens, row, p.T)) return;
+        rstd_next = p.rstd[row];
+        const Store* hr = row_of(row);
+#pragma unroll
+        for (int k = 0; k < kHeld; ++k) {
+            const int c = lane + k * G;
+            h_next[k] = y_next[k] = no_values<T>();
+            if (c >= chunks) continue;
+            h_next[k] = raw_at<T, Whole>(hr, c, p.D);
+            if (p.grad_y) y_next[k] = raw_at<T, Whole>(dy_of(row), c, p.D);
+        }
+    };
+    float w[kHeld][8];
+    if (kAhead) {
+#pragma unroll
+        for (int k = 0; k < kHeld; ++k)
+            load_weight<T, Whole>(p.weight, p.weight_f32, min(lane + k * G, chunks - 1), p.D, w[k]);
+        ask(blockIdx.x * kRows + sub);
+    }
+    for (uint32_t row = blockIdx.x * kRows + sub; row < rows; row += stride) {
         const int64_t at = (int64_t)row * p.D;
-        const Store* hr = static_cast<const Store*>(p.h) + offset_of(row, p.T, p.stride_b, p.stride_t);
-        const Store* dy = p.grad_y ? static_cast<const Store*>(p.grad_y) + at : nullptr;
         const Store* dsum = p.grad_sum ? static_cast<const Store*>(p.grad_sum) + at : nullptr;
         Store* dx = p.grad_x ? static_cast<Store*>(p.grad_x) + at : nullptr;
         Store* dres = p.grad_residual ? static_cast<Store*>(p.grad_residual) + at : nullptr;
-        const auto left_of = [&](int c) { return p.D - c * 8; };
         const auto write = [&](int c, float* f) {
-            if (dres) store8<T>(dres + c * 8, left_of(c), f);
+            if (dres) store_at<T, Whole>(dres, c, p.D, f);
             if (dx) {
                 if (drop.threshold > 0) drop.apply((uint32_t)(p.row + row), (uint32_t)c, f);
-                store8<T>(dx + c * 8, left_of(c), f);
+                store_at<T, Whole>(dx, c, p.D, f);
             }
         };
         if (!inside(lens, row, p.T)) {
             float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
             for (int c = lane; c < chunks; c += G) {
-                if (dres) store8<T>(dres + c * 8, left_of(c), zero);
-                if (dx) store8<T>(dx + c * 8, left_of(c), zero);
+                if (dres) store_at<T, Whole>(dres, c, p.D, zero);
+                if (dx) store_at<T, Whole>(dx, c, p.D, zero);
             }
+            if (kAhead) ask(row + stride);
             continue;
         }
-        const float rstd = p.rstd[row];
-        float h[kHeld][8], g[kHeld][8];
-        // h and w dy of a chunk; the weight's gradient on the way
-        const auto take = [&](int c, float* h, float* g, float* dw) {
-            float w[8];
-            load8<T>(hr + c * 8, left_of(c), h);
-            if (!dy) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) g[i] = 0.f;
-                return;
-            }
-            load8<T>(dy + c * 8, left_of(c), g);
-            load_weight<T>(p.weight, p.weight_f32, c, left_of(c), w);
+        if (N > 0 && !kAhead) ask(row);
+        const float rstd = N > 0 ? rstd_next : p.rstd[row];
+        // n = h rstd and w dy of a chunk
+        const auto take = [&](int c, const Raw<T>& a, const Raw<T>& b, const float* w, float* n, float* g, float* dw) {
+            unpack_at<T, Whole>(a, c, p.D, n);
+            unpack_at<T, Whole>(b, c, p.D, g);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                h[i] *= rstd;
-                if (dw) dw[i] = fmaf(g[i], h[i], dw[i]);
+                n[i] *= rstd;
+                if (dw) dw[i] = fmaf(g[i], n[i], dw[i]);
                 g[i] *= w[i];
             }
         };
-        float s = 0.f;
+        float n[8], g[8], s = 0.f;
+        // (rows stay as they lie in memory, half the registers of their values: they are unpacked twice)
+        Raw<T> a[kHeld], b[kHeld], d[kHeld];
         if (N > 0) {
 #pragma unroll
             for (int k = 0; k < kHeld; ++k) {
                 const int c = lane + k * G;
-                if (c >= chunks) continue;
-                take(c, h[k], g[k], dw[k]);
+                a[k] = h_next[k];
+                b[k] = y_next[k];
+                d[k] = no_values<T>();
+                if (c < chunks && dsum) d[k] = raw_at<T, Whole>(dsum, c, p.D);
+            }
+            if (kAhead) ask(row + stride);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) s = fmaf(g[k][i], h[k][i], s);
+            for (int k = 0; k < kHeld; ++k) {
+                if (!kAhead) load_weight<T, Whole>(p.weight, p.weight_f32, min(lane + k * G, chunks - 1), p.D, w[k]);
+                take(lane + k * G, a[k], b[k], w[k], n, g, dw[k]);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) s = fmaf(g[i], n[i], s);
             }
         } else {
             for (int c = lane; c < chunks; c += G) {
                 float add[8];
-                if (partial) load8<F32>(partial + c * 8, left_of(c), add);
-                take(c, h[0], g[0], partial ? add : nullptr);
-                if (partial) store8<F32>(partial + c * 8, left_of(c), add);
+                if (partial) load_at<F32, Whole>(partial, c, p.D, add);
+                load_weight<T, Whole>(p.weight, p.weight_f32, c, p.D, w[0]);
+                take(c, raw_at<T, Whole>(row_of(row), c, p.D),
+                     p.grad_y ? raw_at<T, Whole>(dy_of(row), c, p.D) : no_values<T>(), w[0], n, g, partial ? add : nullptr);
+                if (partial) store_at<F32, Whole>(partial, c, p.D, add);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) s = fmaf(g[0][i], h[0][i], s);
+                for (int i = 0; i < 8; ++i) s = fmaf(g[i], n[i], s);
             }
         }
         if (G > 64) __syncthreads();
         s = over_row<G, false>(s, parts) / (float)p.D;
-        const auto finish = [&](int c, const float* h, const float* g) {
+        const auto finish = [&](int c, const Raw<T>& d) {
             float f[8];
-            if (dsum) load8<T>(dsum + c * 8, left_of(c), f);
+            unpack_at<T, Whole>(d, c, p.D, f);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float d = rstd * (g[i] - h[i] * s);
-                f[i] = dsum ? f[i] + d : d;
-            }
+            for (int i = 0; i < 8; ++i) f[i] += rstd * (g[i] - n[i] * s);
             write(c, f);
         };
         if (N > 0) {
 #pragma unroll
             for (int k = 0; k < kHeld; ++k) {
                 const int c = lane + k * G;
-                if (c < chunks) finish(c, h[k], g[k]);
+                if (c >= chunks) continue;
+                if (!kAhead || !Whole) {
+                    hide(a[k]);
+                    hide(b[k]);
+                }
+                if (!kAhead) load_weight<T, Whole>(p.weight, p.weight_f32, c, p.D, w[k]);
+                take(c, a[k], b[k], w[k], n, g, nullptr);
+                finish(c, d[k]);
             }
         } else {
             for (int c = lane; c < chunks; c += G) {
-                take(c, h[0], g[0], nullptr);
-                finish(c, h[0], g[0]);
+                load_weight<T, Whole>(p.weight, p.weight_f32, c, p.D, w[0]);
+                take(c, raw_at<T, Whole>(row_of(row), c, p.D),
+                     p.grad_y ? raw_at<T, Whole>(dy_of(row), c, p.D) : no_values<T>(), w[0], n, g, nullptr);
+                finish(c, dsum ? raw_at<T, Whole>(dsum, c, p.D) : no_values<T>());
             }
         }
     }
@@ -402,17 +465,17 @@ __global__ __launch_bounds__(threads_of(G)) void k_norm_grad(NormGradParams p, S
         if (c >= chunks) continue;
         if (p.add) {
             float old[8];
-            load8<F32>(partial + c * 8, p.D - c * 8, old);
+            load_at<F32, Whole>(partial, c, p.D, old);
 #pragma unroll
             for (int i = 0; i < 8; ++i) dw[k][i] += old[i];
         }
-        store8<F32>(partial + c * 8, p.D - c * 8, dw[k]);
+        store_at<F32, Whole>(partial, c, p.D, dw[k]);
     }
 }
 
 // Columns of the partial sums, added up in the order of the workgroups: 32 columns and 32 stretches of rows a
 // workgroup.
-constexpr int kColumns = 32, kStretches = 32;
+constexpr int kColumns = 32, kStretches = 32, kAtOnce = 16;
 template <typename T>
 __global__ __launch_bounds__(kColumns * kStretches) void k_norm_weight(const float* partials, int blocks, int D,
                                                                        typename T::Store* out)
@@ -421,9 +484,16 @@ __global__ __launch_bounds__(kColumns * kStretches) void k_norm_weight(const flo
     const int column = threadIdx.x % kColumns, stretch = threadIdx.x / kColumns;
     const int at = blockIdx.x * kColumns + column;
     const int each = (blocks + kStretches - 1) / kStretches;
+    const int to = min(blocks, (stretch + 1) * each);
     float s = 0.f;
     if (at < D)
-        for (int b = stretch * each; b < min(blocks, (stretch + 1) * each); ++b) s += partials[(int64_t)b * D + at];
+        for (int b = stretch * each; b < to; b += kAtOnce) {
+            float f[kAtOnce];
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k) f[k] = b + k < to ? partials[(int64_t)(b + k) * D + at] : 0.f;
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k) s += f[k];
+        }
     sums[stretch][column] = s;
     __syncthreads();
     if (stretch > 0 || at >= D) return;
@@ -431,31 +501,48 @@ __global__ __launch_bounds__(kColumns * kStretches) void k_norm_weight(const flo
     T::store(out + at, s);
 }
 
-template <typename F>
-void by_type(int dtype, F&& f)
-{
-    if (dtype == LFMMI_F32) f(F32{});
-    else if (dtype == LFMMI_BF16) f(Bf16{});
-    else f(F16{});
-}
-
 template <int G_, int N_>
 struct Shape {
     static constexpr int G = G_, N = N_;
 };
 
-// Lanes and chunks of a row.
+// Lanes and chunks of a row, forward (us of fp32 / bf16, dropout 0.1, replayed; 32,000 rows of 640 and 1,024, 16,000 of the
+// others): 640: 64 x 2 67 / 33, 128 x 1 67 / 38. 1,500: 128 x 2 80 / 46, 64 x 4 85 / 45, 256 x 1 78 / 55. 2,496: 192 x 2
+// 118 / 71, 256 x 2 118 / 81, 128 x 4 121 / 77. 4,096: 256 x 2 194 / 101, 128 x 4 196 / 103. 8,192: 256 x 4 380 / 192,
+// 512 x 2 376 / 198, 1024 x 1 394 / 245.
 template <typename F>
 void by_shape(int D, F&& f)
 {
     const int chunks = (D + 7) / 8;
     if (chunks <= 64) f(Shape<64, 1>{});
     else if (chunks <= 128) f(Shape<64, 2>{});
-    else if (chunks <= 256) f(Shape<64, 4>{});
+    else if (chunks <= 256) f(Shape<128, 2>{});
+    else if (chunks <= 384) f(Shape<192, 2>{});
     else if (chunks <= 512) f(Shape<256, 2>{});
     else if (chunks <= 1024) f(Shape<256, 4>{});
     else if (chunks <= 2048) f(Shape<1024, 2>{});
     else f(Shape<1024, 0>{});
+}
+
+// ... and backward, with the workgroups that go round the rows, as many as the registers leave place for (the same rows): 640:
+// 64 x 2 768 84 / 37, 1,024 90 / 45, 128 x 1 2,048 86 / 54. 2,048: 256 x 1 1,024 128 / 64, 128 x 2 1,024 128 / 69. 4,096:
+// 512 x 1 512 240 / 125, 256 x 2 512 239 / 131. 8,192: 512 x 2 256 505 / 238, 512 496 / 246, 1024 x 1 496 / 244. 16,384 (8,000
+// rows): 1024 x 2 698 / 399, chunks read again 731 / 468.
+template <int G_, int N_, int Blocks_>
+struct Rounds : Shape<G_, N_> {
+    static constexpr int kBlocks = Blocks_;
+};
+template <typename F>
+void by_rounds(int D, F&& f)
+{
+    const int chunks = (D + 7) / 8;
+    if (chunks <= 64) f(Rounds<64, 1, 1024>{});
+    else if (chunks <= 128) f(Rounds<64, 2, 768>{});
+    else if (chunks <= 256) f(Rounds<256, 1, 1024>{});
+    else if (chunks <= 512) f(Rounds<512, 1, 512>{});
+    else if (chunks <= 1024) f(Rounds<512, 2, 256>{});
+    else if (chunks <= 2048) f(Rounds<1024, 2, 256>{});
+    else f(Rounds<1024, 0, 256>{});
 }
 
 }  // namespace
@@ -471,7 +558,10 @@ hipError_t launch_dropout(const DropoutParams& p, int dtype, hipStream_t stream)
     if (units > UINT32_MAX - (1 << 20)) return hipErrorInvalidValue;
     const int grid = (int)std::min<int64_t>(units, 1 << 20);
     by_type(dtype, [&](auto t) {
-        k_dropout<decltype(t)><<<grid, kThreads, 0, stream>>>(p, lanes_log2, (uint32_t)pieces, (uint32_t)units);
+        by_whole(p.D, [&](auto whole) {
+            k_dropout<decltype(t), decltype(whole)::value>
+                <<<grid, kThreads, 0, stream>>>(p, lanes_log2, (uint32_t)pieces, (uint32_t)units);
+        });
     });
     return hipGetLastError();
 }
@@ -483,7 +573,9 @@ hipError_t launch_norm(const NormParams& p, const SeqLengths& lens, int dtype, h
         by_shape(p.D, [&](auto s) {
             constexpr int G = decltype(s)::G, N = decltype(s)::N, kRows = threads_of(G) / G;
             const int grid = (int)std::min<int64_t>((rows + kRows - 1) / kRows, 1 << 20);
-            k_norm<decltype(t), G, N><<<grid, threads_of(G), 0, stream>>>(p, lens);
+            by_whole(p.D, [&](auto whole) {
+                k_norm<decltype(t), decltype(whole)::value, G, N><<<grid, threads_of(G), 0, stream>>>(p, lens);
+            });
         });
     });
     return hipGetLastError();
@@ -492,9 +584,9 @@ hipError_t launch_norm(const NormParams& p, const SeqLengths& lens, int dtype, h
 int norm_blocks(int64_t rows, int D)
 {
     int blocks = 0;
-    by_shape(D, [&](auto s) {
+    by_rounds(D, [&](auto s) {
         constexpr int G = decltype(s)::G, kRows = threads_of(G) / G;
-        blocks = (int)std::min<int64_t>((rows + kRows - 1) / kRows, G == 1024 ? 512 : kNormBlocks);
+        blocks = (int)std::min<int64_t>((rows + kRows - 1) / kRows, decltype(s)::kBlocks);
     });
     return blocks;
 }
@@ -502,9 +594,11 @@ int norm_blocks(int64_t rows, int D)
 hipError_t launch_norm_grad(const NormGradParams& p, const SeqLengths& lens, int dtype, hipStream_t stream)
 {
     by_type(dtype, [&](auto t) {
-        by_shape(p.D, [&](auto s) {
+        by_rounds(p.D, [&](auto s) {
             constexpr int G = decltype(s)::G, N = decltype(s)::N;
-            k_norm_grad<decltype(t), G, N><<<p.blocks, threads_of(G), 0, stream>>>(p, lens);
+            by_whole(p.D, [&](auto whole) {
+                k_norm_grad<decltype(t), decltype(whole)::value, G, N><<<p.blocks, threads_of(G), 0, stream>>>(p, lens);
+            });
         });
     });
     return hipGetLastError();

@@ -118,7 +118,7 @@ __global__ __launch_bounds__(kThreads) void k_verify_rows(VerifyParams p, SeqLen
             const int c = first + (k * kThreads + threadIdx.x) * 8;
 #pragma unroll
             for (int j = 0; j < 8; ++j) f[k][j] = -INFINITY;
-            if (c + 8 <= p.V) load8<T>(x + c, 8, f[k]);
+            if (c + 8 <= p.V) load_at<T, true>(x, c / 8, p.V, f[k]);
             else
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
@@ -477,14 +477,6 @@ __global__ __launch_bounds__(kPickThreads) void k_verify_pick(VerifyParams p)
         write_tokens(p, b, c, found != INT32_MAX ? found : last);
         __syncthreads();
     }
-}
-
-template <typename F>
-void by_type(int dtype, F&& f)
-{
-    if (dtype == LFMMI_F32) f(F32{});
-    else if (dtype == LFMMI_BF16) f(Bf16{});
-    else f(F16{});
 }
 
 }  // namespace
