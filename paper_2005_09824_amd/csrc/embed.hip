@@ -13,7 +13,6 @@ namespace lfmmi {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kWaves = kThreads / 64;
 
 __device__ __forceinline__ int64_t token_at(const void* tokens, int bytes, uint32_t i)
 {
@@ -25,232 +24,248 @@ __device__ __forceinline__ bool inside(const SeqLengths& lens, uint32_t row, int
     return lens.n == 0 || (int)(row % (uint32_t)T) < lens.T[row / (uint32_t)T];
 }
 
-// Workgroups take pieces of rows: 2^lanes_log2 lanes a row, `chunks` of eight values each.
+// Workgroups take pieces of groups of rows: 2^lanes_log2 lanes a row, one chunk of eight values each, and `rows` rows that
+// follow each other by the same lanes.
 struct Tiles {
     int lanes_log2;
     uint32_t pieces;
     int64_t units;
 };
-template <int Chunks>
-Tiles tiles_of(int64_t rows, int D)
+Tiles tiles_of(int64_t groups, int D)
 {
     const int chunks = (D + 7) / 8;
     Tiles t{0, 0, 0};
     while ((1 << t.lanes_log2) < kThreads && (1 << t.lanes_log2) < chunks) ++t.lanes_log2;
-    const int piece = Chunks << t.lanes_log2, at_once = kThreads >> t.lanes_log2;
-    t.pieces = (uint32_t)((chunks + piece - 1) / piece);
-    t.units = (rows + at_once - 1) / at_once * t.pieces;
+    const int at_once = kThreads >> t.lanes_log2;
+    t.pieces = (uint32_t)((chunks + (1 << t.lanes_log2) - 1) >> t.lanes_log2);
+    t.units = (groups + at_once - 1) / at_once * t.pieces;
     return t;
 }
+struct Place {
+    int64_t group;
+    int c;
+};
+__device__ __forceinline__ Place place_of(const Tiles& t, int64_t unit)
+{
+    const int64_t g = unit / t.pieces;
+    return {(g << (8 - t.lanes_log2)) + (threadIdx.x >> t.lanes_log2),
+            ((int)(unit - g * t.pieces) << t.lanes_log2) + ((int)threadIdx.x & ((1 << t.lanes_log2) - 1))};
+}
+static_assert(kThreads == 1 << 8, "place_of");
 int grid_of(int64_t units) { return (int)std::min<int64_t>(units, 1 << 20); }
 
 // ---- forward
 
-constexpr int kEmbedChunks = 2;
+// Rows that a lane has on their way: a token, then its row, are two waits. (32,768 rows of 2,048 bf16, a table of 65,536:
+// 55 us with one row a lane.)
+constexpr int kEmbedRows = 4;
 
-template <typename T, bool Whole>
+template <typename T, bool Whole, int Rows>
 __global__ __launch_bounds__(kThreads) void k_embed(EmbedParams p, SeqLengths lens, Tiles tiles)
 {
     using Store = typename T::Store;
-    const int lanes = 1 << tiles.lanes_log2, lane = threadIdx.x & (lanes - 1), sub = threadIdx.x >> tiles.lanes_log2;
     const uint32_t rows = (uint32_t)p.B * (uint32_t)p.T;
-    const int at_once = kThreads >> tiles.lanes_log2, chunks = (p.D + 7) / 8;
+    const int chunks = (p.D + 7) / 8;
     for (int64_t u = blockIdx.x; u < tiles.units; u += gridDim.x) {
-        const uint32_t group = (uint32_t)(u / tiles.pieces), piece = (uint32_t)(u - (int64_t)group * tiles.pieces);
-        const uint32_t row = group * (uint32_t)at_once + sub;
-        if (row >= rows) continue;
-        int64_t token = inside(lens, row, p.T) ? token_at(p.tokens, p.token_bytes, row) : -1;
-        const bool bad = token >= p.V;
-        const int first = (int)piece * kEmbedChunks * lanes + lane;
-        if (p.status && first == 0) p.status[row] = bad ? 4 : 0;
-        float f[kEmbedChunks][8];
+        const Place at = place_of(tiles, u);
+        if (at.c >= chunks) continue;
+        const int64_t first = at.group * Rows;
+        int64_t token[Rows];
+        Raw<T> v[Rows];
 #pragma unroll
-        for (int k = 0; k < kEmbedChunks; ++k) {
-            const int c = first + k * lanes;
+        for (int k = 0; k < Rows; ++k)
+            token[k] = first + k < rows && inside(lens, (uint32_t)(first + k), p.T)
+                ? token_at(p.tokens, p.token_bytes, (uint32_t)(first + k)) : -1;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) f[k][i] = bad ? NAN : 0.f;
-            if (c < chunks && !bad && token >= 0)
-                load_at<T, Whole>(static_cast<const Store*>(p.table) + token * p.stride, c, p.D, f[k]);
-        }
+        for (int k = 0; k < Rows; ++k)
+            if (token[k] >= 0 && token[k] < p.V)
+                v[k] = raw_at<T, Whole>(static_cast<const Store*>(p.table) + token[k] * p.stride, at.c, p.D);
 #pragma unroll
-        for (int k = 0; k < kEmbedChunks; ++k) {
-            const int c = first + k * lanes;
-            if (c >= chunks) continue;
+        for (int k = 0; k < Rows; ++k) {
+            if (first + k >= rows) continue;
+            const bool bad = token[k] >= p.V;
+            float f[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) f[k][i] = token < 0 ? 0.f : f[k][i] * p.scale;
-            store_at<T, Whole>(static_cast<Store*>(p.out) + (int64_t)row * p.D, c, p.D, f[k]);
+            for (int i = 0; i < 8; ++i) f[i] = bad ? NAN : 0.f;
+            if (token[k] >= 0 && !bad) {
+                unpack_at<T, Whole>(v[k], at.c, p.D, f);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) f[i] *= p.scale;
+            }
+            store_at<T, Whole>(static_cast<Store*>(p.out) + (first + k) * p.D, at.c, p.D, f, p.once);
+            if (p.status && at.c == 0) p.status[first + k] = bad ? 4 : 0;
         }
     }
 }
 
-// ---- sorting positions by token: digits of p.plan.bits bits, the lowest first, every pass keeps the order of
-// equal digits. Keys are tokens; V where there is none, or none of the table.
+// ---- sorting positions by token: digits of plan.bits bits, the lowest first, every pass keeps the order of equal
+// digits. Keys are tokens; V where there is none, or none of the table. A workgroup takes a tile of positions, a wave a
+// stretch of it, 64 at a time in order.
 
-// (the counters of frequent tokens and pieces are cleared on the way)
-__global__ __launch_bounds__(kThreads) void k_embed_keys(EmbedGradParams p, SeqLengths lens, uint32_t from, uint32_t n,
-                                                         uint32_t* keys, uint32_t* counts)
+constexpr int kSort = 1024;
+constexpr int kSortWaves = kSort / 64;
+
+__device__ __forceinline__ uint32_t key_of(const EmbedGradParams& p, const SeqLengths& lens, uint32_t i, uint32_t from)
 {
-    if (from == 0 && blockIdx.x == 0 && threadIdx.x < 2) counts[threadIdx.x] = 0;
-    for (uint32_t i = blockIdx.x * kThreads + threadIdx.x; i < n; i += gridDim.x * kThreads) {
-        const int64_t token = inside(lens, i, p.T) ? token_at(p.tokens, p.token_bytes, from + i) : -1;
-        keys[from + i] = token < 0 || token >= p.V ? (uint32_t)p.V : (uint32_t)token;
-    }
+    const int64_t token = inside(lens, i, p.T) ? token_at(p.tokens, p.token_bytes, from + i) : -1;
+    return token < 0 || token >= p.V ? (uint32_t)p.V : (uint32_t)token;
 }
 
-// How many keys of every tile have a digit: hist[digit][tile].
-__global__ __launch_bounds__(kThreads) void k_embed_count(const uint32_t* keys, uint32_t N, int shift, int bits,
-                                                          uint32_t tiles, uint32_t* hist)
+// Keys of some sequences of a call of many.
+__global__ __launch_bounds__(kThreads) void k_embed_keys(EmbedGradParams p, SeqLengths lens, uint32_t from, uint32_t n,
+                                                         uint32_t* keys)
+{
+    for (uint32_t i = blockIdx.x * kThreads + threadIdx.x; i < n; i += gridDim.x * kThreads)
+        keys[from + i] = key_of(p, lens, i, from);
+}
+
+// How many keys of a tile have a digit: hist[tile][digit]. Tokens: the keys are made here, of all sequences.
+template <bool Tokens>
+__global__ __launch_bounds__(kSort) void k_embed_count(EmbedGradParams p, SeqLengths lens, uint32_t* keys, uint32_t N,
+                                                       int shift, uint32_t* hist)
 {
     extern __shared__ uint32_t bins[];
-    const int n = 1 << bits;
-    for (uint32_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-        for (int i = threadIdx.x; i < n; i += kThreads) bins[i] = 0;
-        __syncthreads();
-        for (int k = 0; k < kEmbedTile / kThreads; ++k) {
-            const uint32_t i = tile * kEmbedTile + k * kThreads + threadIdx.x;
-            if (i < N) atomicAdd(&bins[keys[i] >> shift & (n - 1)], 1u);
-        }
-        __syncthreads();
-        for (int i = threadIdx.x; i < n; i += kThreads) hist[(int64_t)i * tiles + tile] = bins[i];
-        __syncthreads();
-    }
-}
-
-// Sums of all entries before each, by one workgroup.
-constexpr int kScanThreads = 1024;
-__global__ __launch_bounds__(kScanThreads) void k_embed_scan(uint32_t* hist, int64_t n)
-{
-    __shared__ uint32_t sums[2][kScanThreads];
-    const int64_t each = (n + kScanThreads - 1) / kScanThreads;
-    const int64_t from = min(n, each * threadIdx.x), to = min(n, from + each);
-    uint32_t s = 0;
-    for (int64_t i = from; i < to; ++i) s += hist[i];
-    int now = 0;
-    sums[0][threadIdx.x] = s;
+    const int n = 1 << p.plan.bits;
+    for (int i = threadIdx.x; i < n; i += kSort) bins[i] = 0;
     __syncthreads();
-    for (int o = 1; o < kScanThreads; o <<= 1) {
-        uint32_t v = sums[now][threadIdx.x];
-        if ((int)threadIdx.x >= o) v += sums[now][threadIdx.x - o];
-        sums[now ^ 1][threadIdx.x] = v;
-        now ^= 1;
-        __syncthreads();
+    const int64_t first = (int64_t)blockIdx.x * p.plan.tile, end = min((int64_t)N, first + p.plan.tile);
+    for (int64_t i = first + threadIdx.x; i < end; i += kSort) {
+        const uint32_t key = Tokens ? key_of(p, lens, (uint32_t)i, 0) : keys[i];
+        if (Tokens) keys[i] = key;
+        atomicAdd(&bins[key >> shift & (n - 1)], 1u);
     }
-    uint32_t before = threadIdx.x > 0 ? sums[now][threadIdx.x - 1] : 0;
-    for (int64_t i = from; i < to; ++i) {
-        const uint32_t v = hist[i];
-        hist[i] = before;
-        before += v;
-    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += kSort) hist[(int64_t)blockIdx.x * n + i] = bins[i];
 }
 
-// Keys of a tile to their places. A wave takes a quarter of the tile, 64 keys at a time in order; lanes with equal
-// digits find each other by a ballot on each bit.
-__global__ __launch_bounds__(kThreads) void k_embed_place(const uint32_t* keys, const uint32_t* order, uint32_t N,
-                                                          int shift, int bits, uint32_t tiles, const uint32_t* hist,
-                                                          uint32_t* keys_out, uint32_t* order_out)
+// Keys of a tile to their places. Every workgroup adds up for itself how many keys have a smaller digit, or the same in an
+// earlier tile; lanes with equal digits find each other by a ballot on each bit.
+__global__ __launch_bounds__(kSort) void k_embed_place(EmbedGradParams p, const uint32_t* keys, const uint32_t* order,
+                                                       uint32_t N, int shift, const uint32_t* hist, uint32_t* keys_out,
+                                                       uint32_t* order_out)
 {
     extern __shared__ uint32_t places[];  // [wave][digit]
-    const int n = 1 << bits, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    constexpr int kStrips = kEmbedTile / kThreads;
-    for (uint32_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-        for (int i = threadIdx.x; i < n * kWaves; i += kThreads) places[i] = 0;
-        __syncthreads();
-        const uint32_t first = tile * kEmbedTile + wave * (kEmbedTile / kWaves) + lane;
-        uint32_t key[kStrips], from[kStrips];
+    __shared__ uint32_t sums[kSortWaves];
+    const int bits = p.plan.bits, n = 1 << bits, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    uint32_t* mine = places + wave * n;
+    const int64_t stretch = p.plan.tile / kSortWaves, first = (int64_t)blockIdx.x * p.plan.tile + wave * stretch;
+    const int64_t end = min((int64_t)N, first + stretch);
+    // (a tile's first strip stays in registers: of most calls it is the only one)
+    const bool here = first + lane < end;
+    const uint32_t key0 = here ? keys[first + lane] : 0, whence0 = here ? (order ? order[first + lane] : (uint32_t)(first + lane)) : 0;
+    // a digit a thread: how many keys there are in all, and in the tiles before
+    const int d = threadIdx.x;
+    uint32_t all = 0, before = 0;
+    if (d < n)
+        for (int t = 0; t < p.plan.tiles; t += 16) {
+            uint32_t h[16];
 #pragma unroll
-        for (int k = 0; k < kStrips; ++k) {
-            const uint32_t i = first + k * 64;
-            key[k] = i < N ? keys[i] : 0;
-            from[k] = i < N ? (order ? order[i] : i) : 0;
-            if (i < N) atomicAdd(&places[wave * n + (key[k] >> shift & (n - 1))], 1u);
-        }
-        __syncthreads();
-        for (int i = threadIdx.x; i < n; i += kThreads) {
-            uint32_t at = hist[(int64_t)i * tiles + tile];
-            for (int w = 0; w < kWaves; ++w) {
-                const uint32_t count = places[w * n + i];
-                places[w * n + i] = at;
-                at += count;
-            }
-        }
-        __syncthreads();
+            for (int k = 0; k < 16; ++k) h[k] = t + k < p.plan.tiles ? hist[(int64_t)(t + k) * n + d] : 0;
 #pragma unroll
-        for (int k = 0; k < kStrips; ++k) {
-            const bool here = first + k * 64 < N;
-            const uint32_t digit = key[k] >> shift & (n - 1);
-            uint64_t same = __ballot(here);
-            for (int b = 0; b < bits; ++b) {
-                const bool bit = digit >> b & 1;
-                const uint64_t set = __ballot(bit);
-                same &= bit ? set : ~set;
-            }
-            volatile uint32_t* place = &places[wave * n + digit];
-            uint32_t at = 0;
-            if (here) at = *place + __popcll(same & ((1ull << lane) - 1));
-            __builtin_amdgcn_wave_barrier();
-            if (here && (same >> lane) == 1) *place = at + 1;  // the last of them
-            __builtin_amdgcn_wave_barrier();
-            if (here) {
-                keys_out[at] = key[k];
-                order_out[at] = from[k];
+            for (int k = 0; k < 16; ++k) {
+                all += h[k];
+                if (t + k < (int)blockIdx.x) before += h[k];
             }
         }
-        __syncthreads();
+    for (int i = threadIdx.x; i < n * kSortWaves; i += kSort) places[i] = 0;
+    __syncthreads();
+    if (here) atomicAdd(&mine[key0 >> shift & (n - 1)], 1u);
+    for (int64_t i = first + 64 + lane; i < end; i += 64) atomicAdd(&mine[keys[i] >> shift & (n - 1)], 1u);
+    uint32_t upto = all;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const uint32_t v = __shfl_up(upto, o, 64);
+        if (lane >= o) upto += v;
+    }
+    if (lane == 63) sums[wave] = upto;
+    __syncthreads();
+    if (d < n) {
+        uint32_t at = upto - all + before;
+        for (int w = 0; w < wave; ++w) at += sums[w];
+        for (int w = 0; w < kSortWaves; ++w) {
+            const uint32_t count = places[w * n + d];
+            places[w * n + d] = at;
+            at += count;
+        }
+    }
+    __syncthreads();
+    for (int64_t strip = first; strip < end; strip += 64) {
+        const int64_t i = strip + lane;
+        const bool in = i < end;
+        uint32_t key = key0, whence = whence0;
+        if (strip > first && in) {
+            key = keys[i];
+            whence = order ? order[i] : (uint32_t)i;
+        }
+        const uint32_t digit = key >> shift & (n - 1);
+        uint64_t same = __ballot(in);
+        for (int b = 0; b < bits; ++b) {
+            const bool bit = digit >> b & 1;
+            const uint64_t set = __ballot(bit);
+            same &= bit ? set : ~set;
+        }
+        volatile uint32_t* place = &mine[digit];
+        uint32_t to = 0;
+        if (in) to = *place + __popcll(same & ((1ull << lane) - 1));
+        __builtin_amdgcn_wave_barrier();
+        if (in && (same >> lane) == 1) *place = to + 1;  // the last of them
+        __builtin_amdgcn_wave_barrier();
+        if (in) {
+            keys_out[to] = key;
+            order_out[to] = whence;
+        }
     }
 }
 
-__device__ __forceinline__ uint32_t lower_bound(const uint32_t* keys, uint32_t n, uint32_t key)
+// Where the positions of every token begin: by halves, first among one key in `step` that lie in LDS.
+constexpr int kSamples = 1024;
+__global__ __launch_bounds__(kThreads) void k_embed_starts(const uint32_t* keys, uint32_t N, int V, uint32_t* starts)
 {
-    uint32_t lo = 0, hi = n;
-    while (lo < hi) {
-        const uint32_t mid = lo + (hi - lo) / 2;
-        if (keys[mid] < key) lo = mid + 1;
-        else hi = mid;
-    }
-    return lo;
-}
-
-// Where the positions of every token begin, and pieces of those of frequent ones. Which numbers a token's pieces get is
-// left to chance; they go by those numbers alone.
-__global__ __launch_bounds__(kThreads) void k_embed_starts(const uint32_t* keys, uint32_t N, int V, uint32_t* starts,
-                                                           uint32_t* counts, uint2* first, uint2* piece)
-{
+    __shared__ uint32_t samples[kSamples];
+    const uint32_t step = (N + kSamples - 1) / kSamples, have = step ? (N + step - 1) / step : 0;
+    for (uint32_t i = threadIdx.x; i < have; i += kThreads) samples[i] = keys[i * step];
+    __syncthreads();
     for (int64_t v = (int64_t)blockIdx.x * kThreads + threadIdx.x; v <= V; v += (int64_t)gridDim.x * kThreads) {
-        const uint32_t at = lower_bound(keys, N, (uint32_t)v);
-        starts[v] = at;
-        if (v == V) continue;
-        const uint32_t count = lower_bound(keys, N, (uint32_t)v + 1) - at;
-        if (count <= kEmbedPiece) continue;
-        const uint32_t n = (count + kEmbedPiece - 1) / kEmbedPiece;
-        const uint32_t k = atomicAdd(&counts[0], 1u), to = atomicAdd(&counts[1], n);
-        first[k] = make_uint2((uint32_t)v, to);
-        for (uint32_t i = 0; i < n; ++i)
-            piece[to + i] = make_uint2(at + i * kEmbedPiece, min((uint32_t)kEmbedPiece, count - i * kEmbedPiece));
+        uint32_t lo = 0, hi = have;
+        while (lo < hi) {
+            const uint32_t mid = (lo + hi) / 2;
+            if (samples[mid] < (uint32_t)v) lo = mid + 1;
+            else hi = mid;
+        }
+        // the first sample that is not below v, and so behind the one before
+        hi = (uint32_t)min((uint64_t)N, (uint64_t)lo * step);
+        lo = lo > 0 ? (lo - 1) * step + 1 : 0;
+        while (lo < hi) {
+            const uint32_t mid = lo + (hi - lo) / 2;
+            if (keys[mid] < (uint32_t)v) lo = mid + 1;
+            else hi = mid;
+        }
+        starts[v] = lo;
     }
 }
 
 // ---- sums of rows
 
-// Adds the chunk of positions order[from..from + n - 1] up, in that order.
 template <typename T, bool Whole>
-__device__ __forceinline__ void add_rows(const EmbedGradParams& p, const uint32_t* order, uint32_t from, uint32_t n,
+__device__ __forceinline__ Raw<T> row_of(const EmbedGradParams& p, uint32_t pos, int c)
+{
+    const uint32_t b = pos / (uint32_t)p.T;
+    return raw_at<T, Whole>(static_cast<const typename T::Store*>(p.g) + (int64_t)b * p.stride_b +
+                                (int64_t)(pos - b * (uint32_t)p.T) * p.stride_t, c, p.D);
+}
+
+// Adds the chunk of positions order[from..to - 1], in that order.
+template <typename T, bool Whole, int AtOnce>
+__device__ __forceinline__ void add_rows(const EmbedGradParams& p, const uint32_t* order, uint32_t from, uint32_t to,
                                          int c, float* s)
 {
-    using Store = typename T::Store;
-    constexpr int kAtOnce = 4;
-    const Store* g = static_cast<const Store*>(p.g);
+    for (uint32_t k = from; k < to; k += AtOnce) {
+        Raw<T> v[AtOnce];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) s[i] = 0.f;
-    for (uint32_t k = 0; k < n; k += kAtOnce) {
-        Raw<T> v[kAtOnce];
+        for (int j = 0; j < AtOnce; ++j) v[j] = row_of<T, Whole>(p, order[min(k + j, to - 1)], c);
 #pragma unroll
-        for (int j = 0; j < kAtOnce; ++j) {
-            const uint32_t pos = order[from + min(k + j, n - 1)], b = pos / (uint32_t)p.T;
-            v[j] = raw_at<T, Whole>(g + (int64_t)b * p.stride_b + (int64_t)(pos - b * (uint32_t)p.T) * p.stride_t, c, p.D);
-        }
-#pragma unroll
-        for (int j = 0; j < kAtOnce; ++j) {
-            if (k + j >= n) continue;
+        for (int j = 0; j < AtOnce; ++j) {
+            if (k + j >= to) continue;
             float f[8];
             unpack_at<T, Whole>(v[j], c, p.D, f);
 #pragma unroll
@@ -260,76 +275,130 @@ __device__ __forceinline__ void add_rows(const EmbedGradParams& p, const uint32_
 }
 
 template <typename T, bool Whole>
-__device__ __forceinline__ void write_grad(const EmbedGradParams& p, uint32_t v, int c, const float* s)
+__device__ __forceinline__ void write_grad(const EmbedGradParams& p, int64_t v, int c, const float* s)
 {
-    typename T::Store* out = static_cast<typename T::Store*>(p.grad) + (int64_t)v * p.D;
+    typename T::Store* out = static_cast<typename T::Store*>(p.grad) + v * p.D;
     float f[8];
     if (p.accumulate) load_at<T, Whole>(out, c, p.D, f);
 #pragma unroll
     for (int i = 0; i < 8; ++i) f[i] = p.accumulate ? f[i] + s[i] * p.scale : s[i] * p.scale;
-    store_at<T, Whole>(out, c, p.D, f);
+    store_at<T, Whole>(out, c, p.D, f, p.once);
 }
 
-// Rows of the table with at most kEmbedPiece positions, those with none among them.
-template <typename T, bool Whole>
-__global__ __launch_bounds__(kThreads) void k_embed_rows(EmbedGradParams p, Tiles tiles, const uint32_t* starts,
-                                                         const uint32_t* order)
+// The sorted positions in pieces of kEmbedPiece: one that a token has as a whole is added up by itself. A token's row is the
+// sum of its positions before its first such piece, its pieces, and the positions behind the last.
+struct Segment {
+    uint32_t from, to, first, last;  // positions; pieces first..last - 1 are the token's
+};
+__device__ __forceinline__ Segment segment_of(uint32_t from, uint32_t to)
 {
-    const int lanes = 1 << tiles.lanes_log2, lane = threadIdx.x & (lanes - 1), sub = threadIdx.x >> tiles.lanes_log2;
-    const int at_once = kThreads >> tiles.lanes_log2, chunks = (p.D + 7) / 8;
-    for (int64_t u = blockIdx.x; u < tiles.units; u += gridDim.x) {
-        const int64_t group = u / tiles.pieces, v = group * at_once + sub;
-        const int c = (int)(u - group * tiles.pieces) * lanes + lane;
-        if (v >= p.V || c >= chunks) continue;
-        const uint32_t from = starts[v], n = starts[v + 1] - from;
-        if (n > kEmbedPiece || (n == 0 && p.accumulate)) continue;
-        float s[8];
-        add_rows<T, Whole>(p, order, from, n, c, s);
-        write_grad<T, Whole>(p, (uint32_t)v, c, s);
-    }
+    const uint32_t first = (uint32_t)(((uint64_t)from + kEmbedPiece - 1) / kEmbedPiece), last = to / kEmbedPiece;
+    return {from, to, first, last};
 }
 
+// Such pieces, and the rows of the table that have none, those without a position among them. A lane has kGradRows rows of
+// the table, and asks for the first position's row of each before it waits for one.
+constexpr int kGradRows = 4;
 template <typename T, bool Whole>
-__global__ __launch_bounds__(kThreads) void k_embed_pieces(EmbedGradParams p, Tiles tiles, const uint32_t* counts,
-                                                           const uint2* piece, const uint32_t* order, float* partials)
+__global__ __launch_bounds__(kThreads) void k_embed_rows(EmbedGradParams p, Tiles rows, Tiles pieces, const uint32_t* starts,
+                                                         const uint32_t* keys, const uint32_t* order, float* partials)
 {
-    const int lanes = 1 << tiles.lanes_log2, lane = threadIdx.x & (lanes - 1), sub = threadIdx.x >> tiles.lanes_log2;
-    const int at_once = kThreads >> tiles.lanes_log2, chunks = (p.D + 7) / 8;
-    const uint32_t n = counts[1];
-    for (int64_t u = blockIdx.x; u < tiles.units; u += gridDim.x) {
-        const int64_t group = u / tiles.pieces, k = group * at_once + sub;
-        const int c = (int)(u - group * tiles.pieces) * lanes + lane;
-        if (k >= n || c >= chunks) continue;
-        const uint2 q = piece[k];
-        float s[8];
-        add_rows<T, Whole>(p, order, q.x, q.y, c, s);
-        store_at<F32, Whole>(partials + k * p.D, c, p.D, s);
-    }
-}
-
-// Frequent tokens, from their pieces.
-template <typename T, bool Whole>
-__global__ __launch_bounds__(kThreads) void k_embed_join(EmbedGradParams p, Tiles tiles, const uint32_t* counts,
-                                                         const uint2* first, const uint32_t* starts,
-                                                         const float* partials)
-{
-    const int lanes = 1 << tiles.lanes_log2, lane = threadIdx.x & (lanes - 1), sub = threadIdx.x >> tiles.lanes_log2;
-    const int at_once = kThreads >> tiles.lanes_log2, chunks = (p.D + 7) / 8;
-    const uint32_t heavy = counts[0];
-    for (int64_t u = blockIdx.x; u < tiles.units; u += gridDim.x) {
-        const int64_t group = u / tiles.pieces, k = group * at_once + sub;
-        const int c = (int)(u - group * tiles.pieces) * lanes + lane;
-        if (k >= heavy || c >= chunks) continue;
-        const uint32_t v = first[k].x, n = (starts[v + 1] - starts[v] + kEmbedPiece - 1) / kEmbedPiece;
-        const float* part = partials + (int64_t)first[k].y * p.D;
-        float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        for (uint32_t i = 0; i < n; ++i) {
-            float f[8];
-            load_at<F32, Whole>(part + (int64_t)i * p.D, c, p.D, f);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) s[j] += f[j];
+    const int chunks = (p.D + 7) / 8;
+    const uint32_t whole = (uint32_t)p.plan.pieces;
+    for (int64_t u = blockIdx.x; u < pieces.units + rows.units; u += gridDim.x) {
+        if (u < pieces.units) {
+            const Place at = place_of(pieces, u);
+            if (at.c >= chunks || at.group >= whole) continue;
+            const uint32_t from = (uint32_t)at.group * kEmbedPiece, key = keys[from];
+            if (key != keys[from + kEmbedPiece - 1] || key == (uint32_t)p.V) continue;
+            float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            add_rows<T, Whole, 8>(p, order, from, from + kEmbedPiece, at.c, s);
+            store_at<F32, Whole>(partials + at.group * p.D, at.c, p.D, s);
+            continue;
         }
-        write_grad<T, Whole>(p, v, c, s);
+        const Place at = place_of(rows, u - pieces.units);
+        const int64_t v = at.group * kGradRows;
+        if (at.c >= chunks || v >= p.V) continue;
+        uint32_t begin[kGradRows + 1];
+        Raw<T> first[kGradRows];
+#pragma unroll
+        for (int k = 0; k <= kGradRows; ++k) begin[k] = starts[min(v + k, (int64_t)p.V)];
+#pragma unroll
+        for (int k = 0; k < kGradRows; ++k) {
+            const Segment g = segment_of(begin[k], begin[k + 1]);
+            first[k] = no_values<T>();
+            if (g.from < g.to && g.first >= g.last) first[k] = row_of<T, Whole>(p, order[g.from], at.c);
+        }
+#pragma unroll
+        for (int k = 0; k < kGradRows; ++k) {
+            const Segment g = segment_of(begin[k], begin[k + 1]);
+            if (g.first < g.last || v + k >= p.V || (g.from == g.to && p.accumulate)) continue;
+            float s[8];
+            unpack_at<T, Whole>(first[k], at.c, p.D, s);
+            if (g.from + 1 < g.to) add_rows<T, Whole, 4>(p, order, g.from + 1, g.to, at.c, s);
+            write_grad<T, Whole>(p, v + k, at.c, s);
+        }
+    }
+}
+
+// Tokens with pieces: a workgroup has 64 chunks of a row, every wave a stretch of the pieces and of the positions before and
+// behind them. It does so for the tokens whose first piece is one of kJoinPieces (a workgroup for each piece, most of which
+// are no token's first: 24 us instead of 9 for 32,768 positions of 2,048 bf16).
+constexpr int kJoinWaves = 8, kJoinPieces = 8;
+template <typename T, bool Whole>
+__global__ __launch_bounds__(kJoinWaves * 64) void k_embed_join(EmbedGradParams p, int parts, int64_t units,
+                                                                const uint32_t* starts, const uint32_t* keys,
+                                                                const uint32_t* order, const float* partials)
+{
+    __shared__ float sums[kJoinWaves][64 * 8];
+    constexpr int kEnds = kEmbedPiece / kJoinWaves;  // positions of a wave before the pieces, and behind
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, chunks = (p.D + 7) / 8;
+    for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
+        const uint32_t group = (uint32_t)(u / parts);
+        const int c = (int)(u - (int64_t)group * parts) * 64 + lane;
+        const uint32_t mine = group * kJoinPieces + lane;
+        uint32_t v = (uint32_t)p.V;
+        if (lane < kJoinPieces && mine < (uint32_t)p.plan.pieces) {
+            const uint32_t at = mine * kEmbedPiece;
+            v = keys[at];
+            if (v != keys[at + kEmbedPiece - 1] || (mine > 0 && v == keys[at - kEmbedPiece])) v = (uint32_t)p.V;
+        }
+        for (uint64_t some = __ballot(v < (uint32_t)p.V); some; some &= some - 1) {
+            const uint32_t token = __shfl(v, __ffsll((unsigned long long)some) - 1, 64);
+            const Segment g = segment_of(starts[token], starts[token + 1]);
+            const uint32_t n = g.last - g.first, each = (n + kJoinWaves - 1) / kJoinWaves, to = min(n, (wave + 1) * each);
+            const float* part = partials + (int64_t)g.first * p.D;
+            float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            if (c < chunks) {
+                const uint32_t head = g.from + wave * kEnds, tail = g.last * kEmbedPiece + wave * kEnds;
+                add_rows<T, Whole, kEnds>(p, order, head, min(head + kEnds, g.first * kEmbedPiece), c, s);
+                for (uint32_t i = wave * each; i < to; i += 8) {
+                    Raw<F32> f[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        f[j] = raw_at<F32, Whole>(part + (int64_t)min(i + j, to - 1) * p.D, c, p.D);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        if (i + j >= to) continue;
+                        float e[8];
+                        unpack_at<F32, Whole>(f[j], c, p.D, e);
+#pragma unroll
+                        for (int x = 0; x < 8; ++x) s[x] += e[x];
+                    }
+                }
+                add_rows<T, Whole, kEnds>(p, order, tail, min(tail + kEnds, g.to), c, s);
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sums[wave][e * 64 + lane] = s[e];
+            __syncthreads();
+            if (wave == 0 && c < chunks) {
+                for (int w = 1; w < kJoinWaves; ++w)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) s[e] += sums[w][e * 64 + lane];
+                write_grad<T, Whole>(p, token, c, s);
+            }
+            __syncthreads();
+        }
     }
 }
 
@@ -343,10 +412,16 @@ U* place(const EmbedGradParams& p, size_t at)
 
 hipError_t launch_embed(const EmbedParams& p, const SeqLengths& lens, int dtype, hipStream_t stream)
 {
-    const Tiles t = tiles_of<kEmbedChunks>((int64_t)p.B * p.T, p.D);
+    const int64_t rows = (int64_t)p.B * p.T;
+    // (few rows: all at once)
+    const bool few = rows * ((p.D + 2047) / 2048) < 4096;
+    const Tiles t = tiles_of(few ? rows : (rows + kEmbedRows - 1) / kEmbedRows, p.D);
     by_type(dtype, [&](auto type) {
         by_whole(p.D, [&](auto whole) {
-            k_embed<decltype(type), decltype(whole)::value><<<grid_of(t.units), kThreads, 0, stream>>>(p, lens, t);
+            using Type = decltype(type);
+            constexpr bool kWhole = decltype(whole)::value;
+            if (few) k_embed<Type, kWhole, 1><<<grid_of(t.units), kThreads, 0, stream>>>(p, lens, t);
+            else k_embed<Type, kWhole, kEmbedRows><<<grid_of(t.units), kThreads, 0, stream>>>(p, lens, t);
         });
     });
     return hipGetLastError();
@@ -357,12 +432,13 @@ EmbedPlan plan_embed(int64_t N, int V, int D)
     EmbedPlan p{};
     int bits = 1;  // of a key: V is one
     while (bits < 31 && (int64_t)V >> bits > 0) ++bits;
-    p.passes = (bits + 9) / 10;
+    p.passes = (bits + 8) / 9;  // (512 digits of 16 waves: 32 KB of LDS)
     p.bits = (bits + p.passes - 1) / p.passes;
-    p.tiles = (int32_t)((N + kEmbedTile - 1) / kEmbedTile);
-    // a frequent token has kEmbedPiece + 1 positions or more, all its pieces but the last are full
-    p.heavy = (int32_t)(N / (kEmbedPiece + 1));
-    p.pieces = (int32_t)(N / kEmbedPiece + p.heavy);
+    // tiles of 1,024 positions, or more, so that there are 128 at most: every workgroup looks at all tiles' counts
+    const int64_t tile = std::max<int64_t>(kSort, (N + 127) / 128);
+    p.tile = (int32_t)((tile + kSort - 1) / kSort * kSort);
+    p.tiles = (int32_t)((N + p.tile - 1) / p.tile);
+    p.pieces = (int32_t)(N / kEmbedPiece);
     size_t at = 0;
     const auto take = [&](size_t bytes) {
         const size_t from = at;
@@ -373,9 +449,6 @@ EmbedPlan plan_embed(int64_t N, int V, int D)
     p.order = take((size_t)N * 4 * 2);
     p.hist = take(((size_t)p.tiles << p.bits) * 4);
     p.starts = take(((size_t)V + 1) * 4);
-    p.counts = take(8);
-    p.first = take((size_t)p.heavy * 8);
-    p.piece = take((size_t)p.pieces * 8);
     p.partials = take((size_t)p.pieces * D * 4);
     p.bytes = at;
     return p;
@@ -386,11 +459,11 @@ hipError_t launch_embed_keys(const EmbedGradParams& p, const SeqLengths& lens, i
     const uint32_t count = (uint32_t)n * (uint32_t)p.T;
     const int grid = (int)std::min<int64_t>(((int64_t)count + kThreads - 1) / kThreads, 4096);
     k_embed_keys<<<grid, kThreads, 0, stream>>>(p, lens, (uint32_t)b * (uint32_t)p.T, count,
-                                                place<uint32_t>(p, p.plan.keys), place<uint32_t>(p, p.plan.counts));
+                                                place<uint32_t>(p, p.plan.keys));
     return hipGetLastError();
 }
 
-hipError_t launch_embed_grad(const EmbedGradParams& p, int dtype, hipStream_t stream)
+hipError_t launch_embed_grad(const EmbedGradParams& p, const SeqLengths* lens, int dtype, hipStream_t stream)
 {
     const EmbedPlan& plan = p.plan;
     const uint32_t N = (uint32_t)p.B * (uint32_t)p.T;
@@ -398,35 +471,32 @@ hipError_t launch_embed_grad(const EmbedGradParams& p, int dtype, hipStream_t st
     uint32_t* order[2] = {place<uint32_t>(p, plan.order), place<uint32_t>(p, plan.order) + N};
     uint32_t* hist = place<uint32_t>(p, plan.hist);
     uint32_t* starts = place<uint32_t>(p, plan.starts);
-    uint32_t* counts = place<uint32_t>(p, plan.counts);
-    uint2* first = place<uint2>(p, plan.first);
-    uint2* piece = place<uint2>(p, plan.piece);
     float* partials = place<float>(p, plan.partials);
     int now = 0;
-    const int grid = std::min(plan.tiles, 1 << 16);
     const int bins = 4 << plan.bits;
     for (int pass = 0; N > 0 && pass < plan.passes; ++pass, now ^= 1) {
         const int shift = pass * plan.bits;
-        k_embed_count<<<grid, kThreads, bins, stream>>>(keys[now], N, shift, plan.bits, plan.tiles, hist);
-        k_embed_scan<<<1, kScanThreads, 0, stream>>>(hist, (int64_t)plan.tiles << plan.bits);
-        k_embed_place<<<grid, kThreads, bins * kWaves, stream>>>(keys[now], pass ? order[now] : nullptr, N, shift,
-                                                                 plan.bits, plan.tiles, hist, keys[now ^ 1],
-                                                                 order[now ^ 1]);
+        if (pass == 0 && lens)
+            k_embed_count<true><<<plan.tiles, kSort, bins, stream>>>(p, *lens, keys[0], N, shift, hist);
+        else
+            k_embed_count<false><<<plan.tiles, kSort, bins, stream>>>(p, SeqLengths{}, keys[now], N, shift, hist);
+        k_embed_place<<<plan.tiles, kSort, bins * kSortWaves, stream>>>(p, keys[now], pass ? order[now] : nullptr, N, shift,
+                                                                        hist, keys[now ^ 1], order[now ^ 1]);
     }
-    const int64_t v = ((int64_t)p.V + 1 + kThreads - 1) / kThreads;
-    k_embed_starts<<<grid_of(v), kThreads, 0, stream>>>(keys[now], N, p.V, starts, counts, first, piece);
-    const Tiles rows = tiles_of<1>(p.V, p.D);
+    const int64_t v = ((int64_t)p.V + kThreads) / kThreads;
+    k_embed_starts<<<(int)std::min<int64_t>(v, 2048), kThreads, 0, stream>>>(keys[now], N, p.V, starts);
+    const Tiles rows = tiles_of(((int64_t)p.V + kGradRows - 1) / kGradRows, p.D), pieces = tiles_of(plan.pieces, p.D);
     by_type(dtype, [&](auto type) {
         by_whole(p.D, [&](auto whole) {
             using T = decltype(type);
             constexpr bool kWhole = decltype(whole)::value;
-            k_embed_rows<T, kWhole><<<grid_of(rows.units), kThreads, 0, stream>>>(p, rows, starts, order[now]);
-            if (plan.heavy == 0) return;
-            const Tiles pieces = tiles_of<1>(plan.pieces, p.D), heavy = tiles_of<1>(plan.heavy, p.D);
-            k_embed_pieces<T, kWhole>
-                <<<grid_of(pieces.units), kThreads, 0, stream>>>(p, pieces, counts, piece, order[now], partials);
-            k_embed_join<T, kWhole>
-                <<<grid_of(heavy.units), kThreads, 0, stream>>>(p, heavy, counts, first, starts, partials);
+            k_embed_rows<T, kWhole><<<grid_of(rows.units + pieces.units), kThreads, 0, stream>>>(
+                p, rows, pieces, starts, keys[now], order[now], partials);
+            if (plan.pieces == 0) return;
+            const int parts = (p.D + 511) / 512;
+            const int64_t units = ((int64_t)plan.pieces + kJoinPieces - 1) / kJoinPieces * parts;
+            k_embed_join<T, kWhole><<<(int)std::min<int64_t>(units, 1 << 16), kJoinWaves * 64, 0, stream>>>(
+                p, parts, units, starts, keys[now], order[now], partials);
         });
     });
     return hipGetLastError();

@@ -22,6 +22,7 @@ struct DropoutParams {
     int64_t stride_x, stride_y;
     int32_t R, D;
     Draw draw;
+    bool once;  // what is written is too much for the caches
 };
 hipError_t launch_dropout(const DropoutParams& p, int dtype, hipStream_t stream);
 
@@ -40,6 +41,7 @@ struct NormParams {
     float* rstd;           // [B, T]
     uint8_t* q;
     float* q_scale;
+    bool once;             // an output is too much for the caches
 };
 hipError_t launch_norm(const NormParams& p, const SeqLengths& lens, int dtype, hipStream_t stream);
 
@@ -60,6 +62,7 @@ struct NormGradParams {
     float* partials;       // [blocks, D] or null
     int32_t blocks;
     bool add;              // to the partial sums of an earlier launch
+    bool once;
 };
 hipError_t launch_norm_grad(const NormGradParams& p, const SeqLengths& lens, int dtype, hipStream_t stream);
 hipError_t launch_norm_weight(const float* partials, int blocks, int D, void* grad_weight, int dtype,
@@ -74,18 +77,18 @@ struct EmbedParams {
     float scale;
     void* out;
     int32_t* status;  // or null
+    bool once;
 };
 hipError_t launch_embed(const EmbedParams& p, const SeqLengths& lens, int dtype, hipStream_t stream);
 
 // The gradient of a table: positions sorted by token, then every row of the table the sum of its positions' rows.
 struct EmbedPlan {
     int32_t bits, passes;   // of a digit, and how many there are
-    int32_t tiles;          // of kEmbedTile positions
-    int32_t pieces, heavy;  // most pieces of frequent tokens, and most such tokens
-    size_t keys, order, hist, starts, counts, piece, first, partials, bytes;  // offsets in the workspace
+    int32_t tile, tiles;    // positions that a workgroup sorts, and how many tiles there are
+    int32_t pieces;         // whole pieces of the sorted positions
+    size_t keys, order, hist, starts, partials, bytes;  // offsets in the workspace
 };
-constexpr int kEmbedTile = 2048;  // positions that a workgroup sorts
-constexpr int kEmbedPiece = 32;   // positions above which a token's rows are cut into pieces of as many
+constexpr int kEmbedPiece = 16;  // positions
 EmbedPlan plan_embed(int64_t N, int V, int D);
 
 struct EmbedGradParams {
@@ -99,10 +102,11 @@ struct EmbedGradParams {
     void* grad;  // [V, D]
     void* workspace;
     EmbedPlan plan;
+    bool once;
 };
-// The keys of a launch's sequences, from position `from` of the call on; then all of the rest.
+// The keys of sequences b..b + n - 1, where the lengths of all do not fit a launch (`lens` null then); all of the rest.
 hipError_t launch_embed_keys(const EmbedGradParams& p, const SeqLengths& lens, int b, int n, hipStream_t stream);
-hipError_t launch_embed_grad(const EmbedGradParams& p, int dtype, hipStream_t stream);
+hipError_t launch_embed_grad(const EmbedGradParams& p, const SeqLengths* lens, int dtype, hipStream_t stream);
 
 struct VerifyParams {
     const void* x;  // [B, K + 1, V]

@@ -52,7 +52,7 @@ __global__ __launch_bounds__(kThreads) void k_dropout(DropoutParams p, int lanes
             float f[8];
             unpack_at<T, Whole>(v[k], c, p.D, f);
             if (drop.threshold > 0) drop.apply((uint32_t)row, (uint32_t)c, f);
-            store_at<T, Whole>(y, c, p.D, f);
+            store_at<T, Whole>(y, c, p.D, f, p.once);
         }
     }
 }
@@ -164,8 +164,8 @@ __global__ __launch_bounds__(threads_of(G)) void k_norm(NormParams p, SeqLengths
 #pragma unroll
             for (int i = 0; i < 8; ++i) h[0][i] = 0.f;
             for (int c = lane; c < chunks; c += G) {
-                if (sum) store_at<T, Whole>(sum, c, p.D, h[0]);
-                if (y) store_at<T, Whole>(y, c, p.D, h[0]);
+                if (sum) store_at<T, Whole>(sum, c, p.D, h[0], p.once);
+                if (y) store_at<T, Whole>(y, c, p.D, h[0], p.once);
                 if (q) store_bytes(q + c * 8, p.D - c * 8, h[0]);
             }
             if (lane == 0) {
@@ -198,14 +198,14 @@ __global__ __launch_bounds__(threads_of(G)) void k_norm(NormParams p, SeqLengths
             for (int k = 0; k < kHeld; ++k) {
                 const int c = lane + k * G;
                 add_up(c, a[k], b[k], h[k]);
-                if (c < chunks && sum) store_at<T, Whole>(sum, c, p.D, h[k]);
+                if (c < chunks && sum) store_at<T, Whole>(sum, c, p.D, h[k], p.once);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) s = fmaf(h[k][i], h[k][i], s);
             }
         } else {
             for (int c = lane; c < chunks; c += G) {
                 add_up(c, raw_at<T, Whole>(x, c, p.D), res ? raw_at<T, Whole>(res, c, p.D) : no_values<T>(), h[0]);
-                if (sum) store_at<T, Whole>(sum, c, p.D, h[0]);
+                if (sum) store_at<T, Whole>(sum, c, p.D, h[0], p.once);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) s = fmaf(h[0][i], h[0][i], s);
             }
@@ -248,7 +248,7 @@ __global__ __launch_bounds__(threads_of(G)) void k_norm(NormParams p, SeqLengths
                 if (c >= chunks) continue;
                 float f[8];
                 scaled(c, k, f);
-                if (y) store_at<T, Whole>(y, c, p.D, f);
+                if (y) store_at<T, Whole>(y, c, p.D, f, p.once);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     top = max(top, magnitude(f[i]));
@@ -259,7 +259,7 @@ __global__ __launch_bounds__(threads_of(G)) void k_norm(NormParams p, SeqLengths
             for (int c = lane; c < chunks; c += G) {
                 float f[8];
                 scaled(c, 0, f);
-                if (y) store_at<T, Whole>(y, c, p.D, f);
+                if (y) store_at<T, Whole>(y, c, p.D, f, p.once);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) top = max(top, magnitude(f[i]));
             }
@@ -357,17 +357,17 @@ __global__ __launch_bounds__(threads_of(G)) void k_norm_grad(NormGradParams p, S
         Store* dx = p.grad_x ? static_cast<Store*>(p.grad_x) + at : nullptr;
         Store* dres = p.grad_residual ? static_cast<Store*>(p.grad_residual) + at : nullptr;
         const auto write = [&](int c, float* f) {
-            if (dres) store_at<T, Whole>(dres, c, p.D, f);
+            if (dres) store_at<T, Whole>(dres, c, p.D, f, p.once);
             if (dx) {
                 if (drop.threshold > 0) drop.apply((uint32_t)(p.row + row), (uint32_t)c, f);
-                store_at<T, Whole>(dx, c, p.D, f);
+                store_at<T, Whole>(dx, c, p.D, f, p.once);
             }
         };
         if (!inside(lens, row, p.T)) {
             float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
             for (int c = lane; c < chunks; c += G) {
-                if (dres) store_at<T, Whole>(dres, c, p.D, zero);
-                if (dx) store_at<T, Whole>(dx, c, p.D, zero);
+                if (dres) store_at<T, Whole>(dres, c, p.D, zero, p.once);
+                if (dx) store_at<T, Whole>(dx, c, p.D, zero, p.once);
             }
             if (kAhead) ask(row + stride);
             continue;

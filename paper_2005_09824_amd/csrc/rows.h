@@ -77,9 +77,9 @@ __device__ __forceinline__ void load_at(const typename T::Store* row, int c, int
 {
     unpack_at<T, Whole>(raw_at<T, Whole>(row, c, D), c, D, f);
 }
-// (the values of a last chunk four, two and one at a time)
+// (the values of a last chunk four, two and one at a time; once: past the caches, the same for all lanes)
 template <typename T, bool Whole>
-__device__ __forceinline__ void store_at(typename T::Store* row, int c, int D, const float* f)
+__device__ __forceinline__ void store_at(typename T::Store* row, int c, int D, const float* f, bool once = false)
 {
     typename T::Store* p = row + c * 8;
     const int left = D - c * 8;
@@ -88,7 +88,15 @@ __device__ __forceinline__ void store_at(typename T::Store* row, int c, int D, c
     for (int k = 0; k < 8 / T::kVec; ++k) r[k] = T::pack(f + k * T::kVec);
     if (Whole || left >= 8) {
 #pragma unroll
-        for (int k = 0; k < 8 / T::kVec; ++k) store16(p + k * T::kVec, r[k]);
+        for (int k = 0; k < 8 / T::kVec; ++k) {
+            if (once) {
+                asm volatile("");  // (two stores that differ by a hint alone are made one without it)
+                store16_once(p + k * T::kVec, r[k]);
+                asm volatile("");
+            } else {
+                store16(p + k * T::kVec, r[k]);
+            }
+        }
         return;
     }
     if constexpr (T::kVec == 4) {

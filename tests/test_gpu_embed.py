@@ -102,7 +102,7 @@ def test_frequent_tokens(V, dtype):
         assert torch.equal(binding.lfmmi_embed_tokens_backward(g, tokens, V), grad)
 
 
-@pytest.mark.parametrize("count", [31, 32, 33, 63, 64, 65, 95, 96, 97, 2047, 2048, 2049, 4097])
+@pytest.mark.parametrize("count", [15, 16, 17, 31, 32, 33, 63, 64, 65, 95, 96, 97, 2047, 2048, 2049, 4097])
 def test_counts_next_to_a_piece(count):
     torch = _torch()
     rng = np.random.default_rng(count)
