@@ -12,46 +12,45 @@
 namespace lfmmi {
 namespace {
 
-constexpr float kLog2e = 1.44269504088896341f;
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 constexpr int kChunks = kVerifyPart / 8 / kThreads;  // of eight logits, that a lane takes of a part
-constexpr int kPickThreads = kVerifyPart / 8;
+constexpr int kPickThreads = 512;
+constexpr int kPickTokens = kVerifyPart / kPickThreads;  // that follow each other, of a lane
+constexpr int kRestThreads = 512;
+constexpr int kRestChunks = kVerifyPart / 8 / kRestThreads;
 
-// What a part of a row comes to: its largest logit m, the sum of 2^((x - m) scale log2 e) (NaN where a logit is NaN or
-// +inf), the first index of the largest.
+// What a part of a row comes to: its largest logit m, the sum s of exp(scale (x - m)) (0 of nothing but -inf, NaN where a logit
+// is NaN or +inf), the first index of the largest.
 struct Part {
-    float m, s;
+    double s;
+    float m;
     int first;
 };
 
 enum Kind { kLost, kAll, kDrafted, kGiven };  // what the last token is drawn from: nothing, p, p - q, p without the drafted one
-struct Choice {
+struct Choice {  // the row that ends a sequence, its flags, a token (greedy: the best; kGiven: the drafted one)
     int row, flags, kind, token;
-    float m, mq;
+    float m, mq;      // largest logits of the target's row and the draft's
+    double per, per_q;  // 1 / sums of those rows
 };
 
 struct Space {  // of the workspace
     Part* parts;      // [B, 2 K + 1, parts]: K + 1 rows of the target, K of the draft
     Choice* choice;   // [B]
-    double* sums;     // [B, parts]: sums of exponentials of the row that is drawn from
-    double* draft;    // [B, parts]: the same of the draft's row
-    double* rest;     // [B, parts]: sums of what is drawn from
+    double* rest;     // [B, parts]: sums of what is left of p - q
 };
 __host__ __device__ size_t up(size_t bytes) { return (bytes + 15) / 16 * 16; }
 __host__ __device__ size_t space_of(void* workspace, int64_t B, int K, int parts, Space* s)
 {
     char* at = static_cast<char*>(workspace);
-    const size_t rows = up((size_t)B * (2 * (size_t)K + 1) * parts * sizeof(Part)), choices = up((size_t)B * sizeof(Choice)),
-                 sums = up((size_t)B * parts * sizeof(double));
+    const size_t rows = up((size_t)B * (2 * (size_t)K + 1) * parts * sizeof(Part)), choices = up((size_t)B * sizeof(Choice));
     if (s) {
         s->parts = reinterpret_cast<Part*>(at);
         s->choice = reinterpret_cast<Choice*>(at + rows);
-        s->sums = reinterpret_cast<double*>(at + rows + choices);
-        s->draft = reinterpret_cast<double*>(at + rows + choices + sums);
-        s->rest = reinterpret_cast<double*>(at + rows + choices + 2 * sums);
+        s->rest = reinterpret_cast<double*>(at + rows + choices);
     }
-    return rows + choices + 3 * sums;
+    return rows + choices + up((size_t)B * parts * sizeof(double));
 }
 
 __device__ __forceinline__ int drafts_of(const VerifyParams& p, const SeqLengths& lens, int b)
@@ -85,21 +84,103 @@ __device__ __forceinline__ uint64_t wave_best(uint64_t k)
     for (int o = 32; o > 0; o >>= 1) k = max(k, (uint64_t)__shfl_xor((unsigned long long)k, o, 64));
     return k;
 }
+// A double of another lane of 16 (DPP); 0 where there is none, or the lane's row is masked out.
+template <int Control, int Rows>
+__device__ __forceinline__ double from_lane(double v)
+{
+    const int lo = __builtin_amdgcn_update_dpp(0, __double2loint(v), Control, Rows, 0xf, Rows == 0xf);
+    const int hi = __builtin_amdgcn_update_dpp(0, __double2hiint(v), Control, Rows, 0xf, Rows == 0xf);
+    return __hiloint2double(hi, lo);
+}
+__device__ __forceinline__ double lane_of(double v, int lane)
+{
+    return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(v), lane), __builtin_amdgcn_readlane(__double2loint(v), lane));
+}
+// The sum over a wave, in every lane.
 __device__ __forceinline__ double wave_sum(double v)
 {
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+    v += from_lane<0x128, 0xf>(v);  // rotated by 8, 4, 2, 1
+    v += from_lane<0x124, 0xf>(v);
+    v += from_lane<0x122, 0xf>(v);
+    v += from_lane<0x121, 0xf>(v);
+    return (lane_of(v, 0) + lane_of(v, 16)) + (lane_of(v, 32) + lane_of(v, 48));
+}
+// The sums of the lanes up to each.
+__device__ __forceinline__ double wave_scan(double v)
+{
+    v += from_lane<0x111, 0xf>(v);  // moved up by 1, 2, 4, 8 within 16 lanes
+    v += from_lane<0x112, 0xf>(v);
+    v += from_lane<0x114, 0xf>(v);
+    v += from_lane<0x118, 0xf>(v);
+    v += from_lane<0x142, 0xa>(v);  // a row's last lane to the row behind it: rows 1 and 3
+    v += from_lane<0x143, 0xc>(v);  // lane 31 to rows 2 and 3
     return v;
 }
 
-// exp(scale (x - m)), to 64 bits: the place where a running sum passes a random number shows errors of 32.
-__device__ __forceinline__ double weight(float x, float m, float scale) { return exp(((double)x - (double)m) * (double)scale); }
+// exp(scale (x - m)) for x <= m, in 64 bits: the place where a running sum passes a random number shows errors of 32. With t
+// its logarithm of base 2, n the whole number next to t and f = t - n, 2^f is the polynomial of degree 8 that meets it at the
+// nine Chebyshev points of [-1/2, 1/2] (1.1e-12 off at most); n is added to the exponent. 0 for t <= -1,000, -inf among it.
+struct Weights {
+    double m, scale2;
+    double c[8];  // of the polynomial, in scalar registers (otherwise the compiler moves a constant for every product)
+    __device__ __forceinline__ Weights(float top, float scale) : m(top), scale2((double)scale * 1.44269504088896340736)
+    {
+        const double of[8] = {6.931471805459335e-01,  2.402265069581299e-01,  5.550410941205933e-02,  9.618129159402558e-03,
+                              1.3333450568000645e-03, 1.5403455852453838e-04, 1.5310079402249296e-05, 1.3255224878668817e-06};
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            c[k] = of[k];
+            asm("" : "+s"(c[k]));
+        }
+    }
+    __device__ __forceinline__ double log2_of(float x) const { return ((double)x - m) * scale2; }
+    __device__ __forceinline__ double exp2_of(double t) const
+    {
+        const double shifted = t + 6755399441055744.;  // 1.5 * 2^52: whole numbers in the last bits
+        const double f = t - (shifted - 6755399441055744.);
+        double e = fma(f, c[7], c[6]);
+#pragma unroll
+        for (int k = 5; k >= 0; --k) e = fma(e, f, c[k]);
+        e = fma(e, f, 1.);
+        return __hiloint2double(__double2hiint(e) + (__double2loint(shifted) << 20), __double2loint(e));
+    }
+    // 2^-1000 where it is to be 0, which adds nothing beside the 1 of the largest
+    __device__ __forceinline__ double at_least(float x) const { return exp2_of(fmax(log2_of(x), -1000.)); }
+    __device__ __forceinline__ double operator()(float x) const
+    {
+        const double t = log2_of(x);
+        return t > -1000. ? exp2_of(t) : 0.;
+    }
+};
 
-// ---- every row of a sequence's, a part at a time
+// A lane's logits of a part: chunks first, first + Threads and on of the row, -inf behind its end.
+template <typename T, int Threads, int Chunks>
+__device__ __forceinline__ void load_part(const typename T::Store* x, int first, int V, float (*f)[8])
+{
+    const int last = (V - 1) / 8;
+    Raw<T> v[Chunks];
+#pragma unroll
+    for (int k = 0; k < Chunks; ++k) v[k] = raw_at<T, false>(x, min(first + k * Threads, last), V);
+#pragma unroll
+    for (int k = 0; k < Chunks; ++k) {
+        const int c = first + k * Threads;
+        unpack_at<T, false>(v[k], min(c, last), V, f[k]);
+        if (c < last) continue;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (c * 8 + j >= V) f[k][j] = -INFINITY;
+    }
+}
+
+// ---- every row of a sequence's, a part at a time. (All sums in 64 bits. Sums of 32 bits decide nearly as well whether a
+// token is taken, and 64 bits of the one row that is drawn from could follow in a kernel of its own: 71 us so for 48 x 7 rows
+// of 128,000, 33 for 9 rows of 32,000.)
 
 template <typename T, bool Greedy>
 __global__ __launch_bounds__(kThreads) void k_verify_rows(VerifyParams p, SeqLengths lens, int64_t units)
 {
-    __shared__ float parts[2][kWaves];
+    __shared__ float tops[kWaves];
+    __shared__ double sums[kWaves];
     __shared__ uint64_t keys[kWaves];
     Space space;
     space_of(p.workspace, p.B, p.K, p.parts, &space);
@@ -109,59 +190,54 @@ __global__ __launch_bounds__(kThreads) void k_verify_rows(VerifyParams p, SeqLen
         const bool of_draft = row > p.K;
         const int i = of_draft ? row - p.K - 1 : row, n = drafts_of(p, lens, b);
         if (of_draft ? i >= n : i > n) continue;
-        const typename T::Store* x = of_draft ? draft_row<T>(p, b, i) : target_row<T>(p, b, i);
-        const float scale2 = (of_draft ? p.draft_scale : p.scale) * kLog2e;
-        const int first = part * kVerifyPart;
+        const int first = part * (kVerifyPart / 8) + (int)threadIdx.x;
         float f[kChunks][8];
-#pragma unroll
-        for (int k = 0; k < kChunks; ++k) {
-            const int c = first + (k * kThreads + threadIdx.x) * 8;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) f[k][j] = -INFINITY;
-            if (c + 8 <= p.V) load_at<T, true>(x, c / 8, p.V, f[k]);
-            else
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (c + j < p.V) f[k][j] = T::load(x + c + j);
-        }
+        load_part<T, kThreads, kChunks>(of_draft ? draft_row<T>(p, b, i) : target_row<T>(p, b, i), first, p.V, f);
         float m = -INFINITY;
+        bool bad = false;
 #pragma unroll
         for (int k = 0; k < kChunks; ++k)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) m = fmaxf(m, f[k][j]);
+            for (int j = 0; j < 8; ++j) {
+                m = fmaxf(m, f[k][j]);
+                bad |= !(f[k][j] < INFINITY);
+            }
         m = max_over<64>(m);
-        if ((threadIdx.x & 63) == 0) parts[0][wave] = m;
+        if ((threadIdx.x & 63) == 0) tops[wave] = m;
         __syncthreads();
-        for (int w = 0; w < kWaves; ++w) m = fmaxf(m, parts[0][w]);
-        const float against = m == -INFINITY ? 0.f : m;  // (a part of nothing but -inf sums to 0)
-        float s = 0.f;
-#pragma unroll
-        for (int k = 0; k < kChunks; ++k)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) s += __builtin_amdgcn_exp2f((f[k][j] - against) * scale2);
-        s = sum_over<64>(s);
-        if ((threadIdx.x & 63) == 0) parts[1][wave] = s;
+        for (int w = 0; w < kWaves; ++w) m = fmaxf(m, tops[w]);
+        double s = 0.;
+        uint64_t best = 0;
         if (Greedy) {
-            uint64_t best = 0;
+            s = m > -INFINITY ? 1. : 0.;
 #pragma unroll
             for (int k = 0; k < kChunks; ++k)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const int c = first + (k * kThreads + threadIdx.x) * 8 + j;
-                    if (c < p.V) best = max(best, key_of(f[k][j], c));
+                    const int at = (first + k * kThreads) * 8 + j;
+                    if (at < p.V) best = max(best, key_of(f[k][j], at));
                 }
             best = wave_best(best);
             if ((threadIdx.x & 63) == 0) keys[wave] = best;
+        } else if (m > -INFINITY) {
+            const Weights weight(m, of_draft ? p.draft_scale : p.scale);
+#pragma unroll
+            for (int k = 0; k < kChunks; ++k) {
+                if ((first + k * kThreads) * 8 >= p.V) break;  // (nothing but padding, of a wave for the most part)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) s += weight.at_least(f[k][j]);
+            }
         }
+        s = wave_sum(bad ? (double)NAN : s);
+        if ((threadIdx.x & 63) == 0) sums[wave] = s;
         __syncthreads();
         if (threadIdx.x == 0) {
-            s = 0.f;
-            uint64_t best = 0;
+            s = 0.;
             for (int w = 0; w < kWaves; ++w) {
-                s += parts[1][w];
+                s += sums[w];
                 if (Greedy) best = max(best, keys[w]);
             }
-            space.parts[((int64_t)b * (2 * p.K + 1) + row) * p.parts + part] = {m, s, Greedy ? (int)~(uint32_t)best : 0};
+            space.parts[((int64_t)b * (2 * p.K + 1) + row) * p.parts + part] = {s, m, Greedy ? (int)~(uint32_t)best : 0};
         }
     }
 }
@@ -180,85 +256,61 @@ __device__ __forceinline__ RowSum join(const VerifyParams& p, const Space& space
 {
     const Part* part = space.parts + ((int64_t)b * (2 * p.K + 1) + row) * p.parts;
     const int lane = threadIdx.x & 63;
-    float m = -INFINITY;
-    for (int k = lane; k < p.parts; k += 64) m = fmaxf(m, part[k].m);
+    const Part own = lane < p.parts ? part[lane] : Part{0., -INFINITY, 0};
+    float m = own.m;
+    for (int k = lane + 64; k < p.parts; k += 64) m = fmaxf(m, part[k].m);
     m = max_over<64>(m);
-    const float against = m == -INFINITY ? 0.f : m;
+    const Weights weight(m == -INFINITY ? 0.f : m, scale);
     double s = 0.;
     uint64_t best = 0;
-    for (int k = lane; k < p.parts; k += 64) {
-        const Part q = part[k];
-        s += (double)q.s * (double)__builtin_amdgcn_exp2f((q.m - against) * scale * kLog2e);
+    const auto add = [&](const Part& q) {
+        s += q.s * weight(q.m);
         if (Greedy) best = max(best, key_of(q.m, q.first));
-    }
+    };
+    if (lane < p.parts) add(own);
+    for (int k = lane + 64; k < p.parts; k += 64) add(part[k]);
     s = wave_sum(s);
     if (Greedy) best = wave_best(best);
     return {m, s, Greedy ? (int)~(uint32_t)best : 0, !(s < INFINITY) ? 2 : m == -INFINITY ? 1 : 0};
 }
 
-// The sum of a whole row in 64 bits, by a wave.
-template <typename T>
-__device__ __noinline__ double sum_again(const typename T::Store* x, int V, float m, float scale)
-{
-    double s = 0.;
-    for (int i = threadIdx.x & 63; i < V; i += 64) s += weight(T::load(x + i), m, scale);
-    return wave_sum(s);
-}
-
-// Sums of 32 bits are off by at most 2^-24 times some 130: a term exp(d) by 4 |d| + 2, where the mean of |d| is at most ln V,
-// and 42 additions. Where u q and p are no further apart than kNear the sums are taken again.
-constexpr double kNear = 0x1p-14;
-
-// The first row that ends sequence b, by a whole workgroup: the first drafted token that is not taken, or the row behind
-// the last. `token`: the greedy one.
+// The first row that ends sequence b, by a whole workgroup, a wave a row: the first drafted token that is not taken, or the
+// row behind the last.
 template <typename T, bool Greedy>
-__device__ __forceinline__ Choice choose(const VerifyParams& p, const Space& space, int b, int n, int* ends)
+__device__ __forceinline__ Choice choose(const VerifyParams& p, const Space& space, int b, int n, int* ends, Choice* shared)
 {
     if (threadIdx.x == 0) *ends = n;
     __syncthreads();
     const int waves = blockDim.x >> 6;
-    for (int i = threadIdx.x >> 6; i < n; i += waves) {
+    Choice c{-1, 0, kAll, -1, 0.f, 0.f, 0., 0.};
+    for (int i = threadIdx.x >> 6; i <= n; i += waves) {
+        const int64_t d = i < n ? drafted(p, b, i) : 0;
+        const bool known = d >= 0 && d < p.V, two = !Greedy && p.draft && i < n;
+        // (all that the row takes is on its way before any of it is waited for)
+        const float u = !Greedy && i < n ? p.uniforms[(int64_t)b * (p.K + 1) + i] : 0.f;
+        const float xd = !Greedy && known ? T::load(target_row<T>(p, b, i) + d) : 0.f;
+        const float yd = two && known ? T::load(draft_row<T>(p, b, i) + d) : 0.f;
         const RowSum r = join<Greedy>(p, space, b, i, p.scale);
-        const int64_t d = drafted(p, b, i);
-        bool ok = r.flags == 0 && d >= 0 && d < p.V;
+        RowSum q{0.f, 1., 0, 0};
+        if (two) q = join<false>(p, space, b, p.K + 1 + i, p.draft_scale);
+        const int flags = r.flags | q.flags | (known ? 0 : 4);
+        bool ok = i < n && flags == 0;
+        const double per = 1. / r.s, per_q = 1. / q.s;
         if (ok && Greedy) ok = d == r.first;
         if (ok && !Greedy) {
-            const typename T::Store *x = target_row<T>(p, b, i), *y = p.draft ? draft_row<T>(p, b, i) : x;
-            const double u = (double)p.uniforms[(int64_t)b * (p.K + 1) + i], e = weight(T::load(x + d), r.m, p.scale);
-            RowSum q{0.f, 1., 0, 0};
-            double eq = 1.;
-            if (p.draft) {
-                q = join<false>(p, space, b, p.K + 1 + i, p.draft_scale);
-                eq = weight(T::load(y + d), q.m, p.draft_scale);
-            }
-            double here = e / r.s, there = u * (eq / q.s);
-            if (fabs(here - there) <= kNear * here) {
-                here = e / sum_again<T>(x, p.V, r.m, p.scale);
-                if (p.draft) there = u * (eq / sum_again<T>(y, p.V, q.m, p.draft_scale));
-            }
-            ok = q.flags == 0 && there < here;
+            const double e = Weights(r.m, p.scale)(xd), eq = two ? Weights(q.m, p.draft_scale)(yd) : 1.;
+            const double here = e / r.s, there = u * (eq / q.s);
+            ok = there < here;
         }
-        if (!ok && (threadIdx.x & 63) == 0) atomicMin(ends, i);
+        if (ok) continue;
+        c = {i, flags, flags ? kLost : i == n ? kAll : two ? kDrafted : kGiven, Greedy ? r.first : (int)d, r.m, q.m, per, per_q};
+        if ((threadIdx.x & 63) == 0) atomicMin(ends, i);
+        break;
     }
     __syncthreads();
-    Choice c{*ends, 0, kAll, -1, 0.f, 0.f};
-    const RowSum r = join<Greedy>(p, space, b, c.row, p.scale);
-    c.m = r.m;
-    c.flags = r.flags;
-    c.token = r.first;
-    if (c.row < n) {
-        const int64_t d = drafted(p, b, c.row);
-        if (d < 0 || d >= p.V) c.flags |= 4;
-        c.kind = kGiven;
-        if (!Greedy && p.draft) {
-            const RowSum q = join<false>(p, space, b, p.K + 1 + c.row, p.draft_scale);
-            c.flags |= q.flags;
-            c.mq = q.m;
-            c.kind = kDrafted;
-        }
-    }
-    if (c.flags) c.kind = kLost;
-    return c;
+    if (c.row == *ends && (threadIdx.x & 63) == 0) *shared = c;
+    __syncthreads();
+    return *shared;
 }
 
 __device__ __forceinline__ void write_tokens(const VerifyParams& p, int b, const Choice& c, int token)
@@ -271,200 +323,172 @@ __device__ __forceinline__ void write_tokens(const VerifyParams& p, int b, const
 }
 
 template <typename T>
-__global__ __launch_bounds__(kThreads) void k_verify_greedy(VerifyParams p, SeqLengths lens)
+__global__ __launch_bounds__(kRestThreads) void k_verify_greedy(VerifyParams p, SeqLengths lens)
 {
     __shared__ int ends;
+    __shared__ Choice shared;
     Space space;
     space_of(p.workspace, p.B, p.K, p.parts, &space);
     for (int b = blockIdx.x; b < p.B; b += gridDim.x) {
-        const Choice c = choose<T, true>(p, space, b, drafts_of(p, lens, b), &ends);
+        const Choice c = choose<T, true>(p, space, b, drafts_of(p, lens, b), &ends, &shared);
         write_tokens(p, b, c, c.kind == kLost ? -1 : c.token);
         __syncthreads();
     }
 }
 
-// Sum over a workgroup of kThreads, in thread 0.
+// What is left of p - q. (Equal products have to leave nothing: no product goes unrounded into the difference.)
+__device__ __forceinline__ double left_over(double p, double per, double q, double per_q)
+{
+#pragma clang fp contract(off)
+    const double a = p * per, b = q * per_q;
+    return fmax(0., a - b);
+}
+
+// The sum over a workgroup, the same bits in every thread. `parts`: a place for each wave.
 __device__ __forceinline__ double block_sum(double v, double* parts)
 {
     v = wave_sum(v);
-    __syncthreads();
     if ((threadIdx.x & 63) == 0) parts[threadIdx.x >> 6] = v;
     __syncthreads();
     v = 0.;
-    for (int w = 0; w < kWaves; ++w) v += parts[w];
+    for (int w = 0; w < (int)(blockDim.x >> 6); ++w) v += parts[w];
     return v;
 }
 
-// Calls each(i, x_i) for a lane's logits of a part.
-template <typename T, typename F>
-__device__ __forceinline__ void of_part(const VerifyParams& p, int part, F&& each)
-{
-    for (int k = 0; k < kChunks; ++k) {
-        const int c = part * kVerifyPart + (k * kThreads + (int)threadIdx.x) * 8;
-        for (int j = 0; j < 8; ++j)
-            if (c + j < p.V) each(c + j);
-    }
-}
-
-// The row that ends every sequence, and a part's sums of it.
+// Where a draft's logits are given: the row that ends every sequence, and if a drafted token is replaced there a part's sum of
+// max(0, p - q).
 template <typename T>
-__global__ __launch_bounds__(kThreads) void k_verify_sums(VerifyParams p, SeqLengths lens, int64_t units)
+__global__ __launch_bounds__(kRestThreads) void k_verify_rest(VerifyParams p, SeqLengths lens, int64_t units)
 {
     __shared__ int ends;
-    __shared__ double parts[kWaves];
+    __shared__ Choice shared;
+    __shared__ double sums[kRestThreads / 64];
     Space space;
     space_of(p.workspace, p.B, p.K, p.parts, &space);
     for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
         const int part = (int)(u % p.parts), b = (int)(u / p.parts);
-        const Choice c = choose<T, false>(p, space, b, drafts_of(p, lens, b), &ends);
+        const Choice c = choose<T, false>(p, space, b, drafts_of(p, lens, b), &ends, &shared);
         if (part == 0 && threadIdx.x == 0) space.choice[b] = c;
-        if (c.kind != kLost) {
-            const typename T::Store* x = target_row<T>(p, b, c.row);
-            const int64_t d = c.kind == kGiven ? drafted(p, b, c.row) : -1;
-            double s = 0., without = 0., q = 0.;
-            of_part<T>(p, part, [&](int i) {
-                const double e = weight(T::load(x + i), c.m, p.scale);
-                s += e;
-                if (i != d) without += e;
-            });
-            if (c.kind == kDrafted) {
-                const typename T::Store* y = draft_row<T>(p, b, c.row);
-                of_part<T>(p, part, [&](int i) { q += weight(T::load(y + i), c.mq, p.draft_scale); });
+        if (c.kind == kDrafted) {
+            const int first = part * (kVerifyPart / 8) + (int)threadIdx.x;
+            float f[kRestChunks][8], g[kRestChunks][8];
+            load_part<T, kRestThreads, kRestChunks>(target_row<T>(p, b, c.row), first, p.V, f);
+            load_part<T, kRestThreads, kRestChunks>(draft_row<T>(p, b, c.row), first, p.V, g);
+            const Weights weight(c.m, p.scale), weight_q(c.mq, p.draft_scale);
+            double s = 0.;
+#pragma unroll
+            for (int k = 0; k < kRestChunks; ++k) {
+                if ((first + k * kRestThreads) * 8 >= p.V) break;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) s += left_over(weight(f[k][j]), c.per, weight_q(g[k][j]), c.per_q);
             }
-            s = block_sum(s, parts);
-            without = block_sum(without, parts);
-            q = block_sum(q, parts);
-            if (threadIdx.x == 0) {
-                space.sums[u] = s;
-                space.rest[u] = without;
-                space.draft[u] = q;
-            }
+            s = block_sum(s, sums);
+            if (threadIdx.x == 0) space.rest[u] = s;
         }
         __syncthreads();
     }
 }
 
-// Sum of a sequence's parts, the same bits in every wave.
-__device__ __forceinline__ double total(const double* sums, int parts)
-{
-    double s = 0.;
-    for (int k = threadIdx.x & 63; k < parts; k += 64) s += sums[k];
-    return wave_sum(s);
-}
-
-__device__ __forceinline__ double left_over(float x, float m, double s, float scale, float y, float mq, double sq, float scale_q)
-{
-    return fmax(0., weight(x, m, scale) / s - weight(y, mq, scale_q) / sq);
-}
-
-// Where a draft's logits are given: a part's sum of max(0, p - q).
-template <typename T>
-__global__ __launch_bounds__(kThreads) void k_verify_rest(VerifyParams p, int64_t units)
-{
-    __shared__ double parts[kWaves];
-    Space space;
-    space_of(p.workspace, p.B, p.K, p.parts, &space);
-    for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
-        const int part = (int)(u % p.parts), b = (int)(u / p.parts);
-        const Choice c = space.choice[b];
-        if (c.kind != kDrafted) continue;
-        const double s = total(space.sums + (int64_t)b * p.parts, p.parts), q = total(space.draft + (int64_t)b * p.parts, p.parts);
-        const typename T::Store *x = target_row<T>(p, b, c.row), *y = draft_row<T>(p, b, c.row);
-        double r = 0.;
-        of_part<T>(p, part, [&](int i) {
-            r += left_over(T::load(x + i), c.m, s, p.scale, T::load(y + i), c.mq, q, p.draft_scale);
-        });
-        r = block_sum(r, parts);
-        if (threadIdx.x == 0) space.rest[u] = r;
-    }
-}
-
-// Sums of the lanes up to each.
-__device__ __forceinline__ double wave_scan(double v)
-{
-    const int lane = threadIdx.x & 63;
-    for (int o = 1; o < 64; o <<= 1) {
-        const double w = __shfl_up(v, o, 64);
-        if (lane >= o) v += w;
-    }
-    return v;
-}
-
-// The last token of every sequence: the first whose running sum passes the random number times the whole.
-template <typename T>
-__global__ __launch_bounds__(kPickThreads) void k_verify_pick(VerifyParams p)
+// The last token of every sequence: the first whose running sum passes the random number times the whole. Chosen: k_verify_rest
+// has said which row ends the sequence.
+template <typename T, bool Chosen>
+__global__ __launch_bounds__(kPickThreads) void k_verify_pick(VerifyParams p, SeqLengths lens)
 {
     __shared__ double scan[kPickThreads / 64];
-    __shared__ int found, last;
+    __shared__ int ends, found, last;
+    __shared__ Choice shared;
     Space space;
     space_of(p.workspace, p.B, p.K, p.parts, &space);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     for (int b = blockIdx.x; b < p.B; b += gridDim.x) {
-        Choice c = space.choice[b];
-        if (c.kind == kLost) {
-            write_tokens(p, b, c, -1);
-            continue;
-        }
-        const double *sums = space.sums + (int64_t)b * p.parts, *rest = space.rest + (int64_t)b * p.parts;
-        const double s = total(sums, p.parts);
-        const double q = c.kind == kDrafted ? total(space.draft + (int64_t)b * p.parts, p.parts) : 1.;
-        // (nothing is left where p and q are the same but for rounding)
-        if (!(total(rest, p.parts) > 0.)) {
-            c.kind = kAll;
-            rest = sums;
-        }
-        // every wave: running sums of the parts, 64 at a time, and the part that passes
-        double whole = 0.;
-        for (int k = 0; k < p.parts; k += 64) whole += __shfl(wave_scan(k + lane < p.parts ? rest[k + lane] : 0.), 63, 64);
-        const double mark = (double)p.uniforms[(int64_t)b * (p.K + 1) + p.K] * whole;
-        double before = 0., run = 0.;
-        int part = -1;
-        for (int k = 0; k < p.parts && part < 0; k += 64) {
-            const double here = k + lane < p.parts ? rest[k + lane] : 0., upto = run + wave_scan(here);
-            const uint64_t passed = __ballot(here > 0. && upto > mark);
-            if (passed) {
-                const int at = __ffsll((unsigned long long)passed) - 1;
-                part = k + at;
-                const double earlier = __shfl(upto, at > 0 ? at - 1 : 0, 64);
-                before = at > 0 ? earlier : run;
-            }
-            run = __shfl(upto, 63, 64);
-        }
-        if (part < 0) {  // a number of 1 or more: the last token of any weight
-            for (int k = 0; k < p.parts; k += 64) {
-                const uint64_t some = __ballot(k + lane < p.parts && rest[k + lane] > 0.);
-                if (some) part = k + 63 - __clzll((long long)some);
-            }
-            before = -INFINITY;
-        }
-        const typename T::Store* x = target_row<T>(p, b, c.row);
-        const typename T::Store* y = c.kind == kDrafted ? draft_row<T>(p, b, c.row) : x;
-        const int64_t d = c.kind == kGiven ? drafted(p, b, c.row) : -1;
-        const int first = part * kVerifyPart + (int)threadIdx.x * 8;
-        double w[8], sum = 0.;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int i = first + j;
-            w[j] = 0.;
-            if (i < p.V && i != d)
-                w[j] = c.kind == kDrafted
-                    ? left_over(T::load(x + i), c.m, s, p.scale, T::load(y + i), c.mq, q, p.draft_scale)
-                    : weight(T::load(x + i), c.m, p.scale);
-            sum += w[j];
-        }
-        const double upto = wave_scan(sum);
+        const float u = p.uniforms[(int64_t)b * (p.K + 1) + p.K];
+        Choice c = Chosen ? space.choice[b] : choose<T, false>(p, space, b, drafts_of(p, lens, b), &ends, &shared);
         if (threadIdx.x == 0) {
             found = INT32_MAX;
             last = -1;
         }
+        if (c.kind == kLost) {
+            write_tokens(p, b, c, -1);
+            continue;
+        }
+        const Weights weight(c.m, p.scale), weight_q(c.mq, p.draft_scale);
+        const Part* parts = space.parts + ((int64_t)b * (2 * p.K + 1) + c.row) * p.parts;
+        const double* rest = space.rest + (int64_t)b * p.parts;
+        // a lane's weights of tokens of a part that follow each other
+        const auto weights_of = [&](int part, double* w) {
+            const int chunk = (part * kPickThreads + (int)threadIdx.x) * (kPickTokens / 8);
+            float f[kPickTokens / 8][8], g[kPickTokens / 8][8];
+            load_part<T, 1, kPickTokens / 8>(target_row<T>(p, b, c.row), chunk, p.V, f);
+            if (c.kind == kDrafted) load_part<T, 1, kPickTokens / 8>(draft_row<T>(p, b, c.row), chunk, p.V, g);
+            double s = 0.;
+#pragma unroll
+            for (int j = 0; j < kPickTokens; ++j) {
+                w[j] = weight(f[j / 8][j % 8]);
+                if (c.kind == kDrafted) w[j] = left_over(w[j], c.per, weight_q(g[j / 8][j % 8]), c.per_q);
+                if (c.kind == kGiven && chunk * 8 + j == c.token) w[j] = 0.;
+                s += w[j];
+            }
+            return s;
+        };
+        // the part that a token is taken out of is added up again without it: of a sum minus nearly all of it little is right
+        double w[kPickTokens], without = 0.;
+        const int given = c.kind == kGiven ? c.token / kVerifyPart : -1;
+        if (given >= 0) {
+            without = block_sum(weights_of(given, w), scan);
+            __syncthreads();
+        }
+        const auto weight_of = [&](int k) {
+            return k >= p.parts ? 0. : c.kind == kDrafted ? rest[k] : k == given ? without : parts[k].s * weight(parts[k].m);
+        };
+        // every wave: running sums of the parts, 64 at a time, and the part that passes
+        double whole = 0.;
+        for (int k = 0; k < p.parts; k += 64) whole += lane_of(wave_scan(weight_of(k + lane)), 63);
+        int out = given;
+        if (!(whole > 0.)) {  // nothing is left where p and q are the same but for rounding: p is drawn from
+            c.kind = kAll;
+            out = -1;
+            whole = 0.;
+            for (int k = 0; k < p.parts; k += 64)
+                whole += lane_of(wave_scan(k + lane < p.parts ? parts[k + lane].s * weight(parts[k + lane].m) : 0.), 63);
+        }
+        const auto drawn_of = [&](int k) {
+            return c.kind != kAll ? weight_of(k) : k >= p.parts ? 0. : parts[k].s * weight(parts[k].m);
+        };
+        const double mark = (double)u * whole;
+        double before = 0., run = 0.;
+        int part = -1;
+        for (int k = 0; k < p.parts && part < 0; k += 64) {
+            const double here = drawn_of(k + lane), upto = run + wave_scan(here);
+            const uint64_t passed = __ballot(here > 0. && upto > mark);
+            if (passed) {
+                const int at = __ffsll((unsigned long long)passed) - 1;
+                part = k + at;
+                before = at > 0 ? lane_of(upto, at > 0 ? at - 1 : 0) : run;
+            }
+            run = lane_of(upto, 63);
+        }
+        if (part < 0) {  // a number of 1 or more: the last token of any weight
+            for (int k = 0; k < p.parts; k += 64) {
+                const uint64_t some = __ballot(drawn_of(k + lane) > 0.);
+                if (some) part = k + 63 - __clzll((long long)some);
+            }
+            before = -INFINITY;
+        }
+        double sum = 0.;
+        if (part == out)
+            for (int j = 0; j < kPickTokens; ++j) sum += w[j];
+        else
+            sum = weights_of(part, w);
+        const double upto = wave_scan(sum);
         if (lane == 63) scan[wave] = upto;
         __syncthreads();
         double cum = before;
         for (int k = 0; k < wave; ++k) cum += scan[k];
         cum += upto - sum;
+        const int first = part * kVerifyPart + (int)threadIdx.x * kPickTokens;
         int mine = INT32_MAX, some = -1;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
+        for (int j = 0; j < kPickTokens; ++j) {
             cum += w[j];
             if (w[j] > 0.) {
                 some = first + j;
@@ -495,13 +519,16 @@ hipError_t launch_verify(const VerifyParams& p, const SeqLengths& lens, int dtyp
         using T = decltype(type);
         if (!p.uniforms) {
             k_verify_rows<T, true><<<grid_of(all), kThreads, 0, stream>>>(p, lens, all);
-            k_verify_greedy<T><<<grid_of(p.B), kThreads, 0, stream>>>(p, lens);
+            k_verify_greedy<T><<<grid_of(p.B), kRestThreads, 0, stream>>>(p, lens);
             return;
         }
         k_verify_rows<T, false><<<grid_of(all), kThreads, 0, stream>>>(p, lens, all);
-        k_verify_sums<T><<<grid_of(units), kThreads, 0, stream>>>(p, lens, units);
-        if (p.draft && p.K > 0) k_verify_rest<T><<<grid_of(units), kThreads, 0, stream>>>(p, units);
-        k_verify_pick<T><<<grid_of(p.B), kPickThreads, 0, stream>>>(p);
+        if (p.draft) {
+            k_verify_rest<T><<<grid_of(units), kRestThreads, 0, stream>>>(p, lens, units);
+            k_verify_pick<T, true><<<grid_of(p.B), kPickThreads, 0, stream>>>(p, lens);
+        } else {
+            k_verify_pick<T, false><<<grid_of(p.B), kPickThreads, 0, stream>>>(p, lens);
+        }
     });
     return hipGetLastError();
 }
