@@ -509,12 +509,18 @@ struct Shape {
 // Lanes and chunks of a row, forward (us of fp32 / bf16, dropout 0.1, replayed; 32,000 rows of 640 and 1,024, 16,000 of the
 // others): 640: 64 x 2 67 / 33, 128 x 1 67 / 38. 1,500: 128 x 2 80 / 46, 64 x 4 85 / 45, 256 x 1 78 / 55. 2,496: 192 x 2
 // 118 / 71, 256 x 2 118 / 81, 128 x 4 121 / 77. 4,096: 256 x 2 194 / 101, 128 x 4 196 / 103. 8,192: 256 x 4 380 / 192,
-// 512 x 2 376 / 198, 1024 x 1 394 / 245.
+// 512 x 2 376 / 198, 1024 x 1 394 / 245. Few rows leave most of the chip idle, and each is spread over more lanes (256 rows of
+// bf16): 640: 256 x 1 3.1, 64 x 2 3.5. 2,048: 256 x 1 3.2, 128 x 2 3.8. 4,096: 512 x 1 3.9, 256 x 2 4.2. 8,192: 512 x 2 5.2,
+// 256 x 4 6.0; 1,024 rows of 640: 4.3 and 4.0, of 4,096: 7.5 and 7.3.
+constexpr int kFewRows = 512;
 template <typename F>
-void by_shape(int D, F&& f)
+void by_shape(int64_t rows, int D, F&& f)
 {
     const int chunks = (D + 7) / 8;
     if (chunks <= 64) f(Shape<64, 1>{});
+    else if (rows <= kFewRows && chunks <= 256) f(Shape<256, 1>{});
+    else if (rows <= kFewRows && chunks <= 512) f(Shape<512, 1>{});
+    else if (rows <= kFewRows && chunks <= 1024) f(Shape<512, 2>{});
     else if (chunks <= 128) f(Shape<64, 2>{});
     else if (chunks <= 256) f(Shape<128, 2>{});
     else if (chunks <= 384) f(Shape<192, 2>{});
@@ -570,7 +576,7 @@ hipError_t launch_norm(const NormParams& p, const SeqLengths& lens, int dtype, h
 {
     const int64_t rows = (int64_t)p.B * p.T;
     by_type(dtype, [&](auto t) {
-        by_shape(p.D, [&](auto s) {
+        by_shape(rows, p.D, [&](auto s) {
             constexpr int G = decltype(s)::G, N = decltype(s)::N, kRows = threads_of(G) / G;
             const int grid = (int)std::min<int64_t>((rows + kRows - 1) / kRows, 1 << 20);
             by_whole(p.D, [&](auto whole) {
