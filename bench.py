@@ -100,10 +100,12 @@ def phase_timers(config, torch, binding, workloads):
     return 0
 
 
-def train_step(steps, warmup, torch, binding, workloads):
+def train_step(steps, warmup, block, torch, binding, workloads):
     """A training step of an output layer in front of the full objective (workload 5): logits of a
     linear layer, chain_loss with the frame log probabilities of an alignment beside it, backward,
-    gradients clipped to a norm, a step against them. Prints one JSON line."""
+    gradients clipped to a norm, a step against them. block: in front of the layer the end of a residual
+    block, dropout of the features, which are added to an embedding of the frame before's pdf, and a norm, both
+    trained. Prints one JSON line."""
     from paper_2005_09824_amd import chain
     wl = workloads.make_workload(5)
     lengths, leak = wl["lengths"], wl["leak"]
@@ -115,11 +117,24 @@ def train_step(steps, warmup, torch, binding, workloads):
     alignment = torch.randint(0, P, (B, T), generator=gen, device="cuda")
     layer = torch.nn.Linear(width, P, device="cuda")
     parameters = list(layer.parameters())
+    if block:
+        before = torch.nn.functional.pad(alignment[:, :-1], (1, 0), value=-1)
+        table = torch.randn((P, width), generator=gen, device="cuda").requires_grad_()
+        scale = torch.ones(width, device="cuda", requires_grad=True)
+        parameters += [table, scale]
+    taken = [0]
+
+    def features():
+        if not block:
+            return hidden
+        taken[0] += 1   # another mask for each step
+        rows, _status = chain.embed_tokens(table, before, lengths)
+        return chain.add_rms_norm(hidden, rows, scale, lengths=lengths, p=0.1, seed=5, offset=taken[0])[0]
 
     def step():
         for q in parameters:
             q.grad = None
-        loss = chain.chain_loss(layer(hidden), lengths, num, den, leak, alignment, 0.1)
+        loss = chain.chain_loss(layer(features()), lengths, num, den, leak, alignment, 0.1)
         loss.backward()
         norm = chain.clip_grad_norm(parameters, 1.0)
         with torch.no_grad():
@@ -140,7 +155,7 @@ def train_step(steps, warmup, torch, binding, workloads):
                       "value": frames / dt, "unit": "frames/s", "ms_per_step": dt * 1e3, "steps": steps,
                       "warmup": warmup, "higher_is_better": True, "dtype": "f32", "data": "synthetic",
                       "config": {"workload": wl["name"], "batch": B, "frames": frames, "max_len": T, "pdfs": P,
-                                 "hidden": width},
+                                 "hidden": width, **({"block": "embedding, dropout, norm"} if block else {})},
                       "loss": float(loss.detach()), "grad_norm": float(norm)}))
     den.close()
     num.close()
@@ -162,6 +177,9 @@ def main():
     ap.add_argument("--train-step", action="store_true",
                     help="time whole training steps of an output layer on workload 5 instead: loss with an "
                          "alignment beside it, backward, clipping, update; prints one JSON line of its own")
+    ap.add_argument("--block", action="store_true",
+                    help="with --train-step: in front of the layer the end of a residual block, an embedding of the "
+                         "frame before's pdf, dropout and a norm")
     ap.add_argument("--phase-timers", action="store_true",
                     help="one call with the whole batch as one launch on a library built with "
                          "-DLFMMI_PHASE_TIMERS: where a frame group of the occupancy kernel "
@@ -192,7 +210,7 @@ def main():
         print(json.dumps({"copy_probe_bytes": n * 4, "copies": 4}))
         return 0
     if args.train_step:
-        return train_step(min(args.steps, 200), args.warmup, torch, binding, workloads)
+        return train_step(min(args.steps, 200), args.warmup, args.block, torch, binding, workloads)
     if args.phase_timers:
         return phase_timers(args.config, torch, binding, workloads)
     wl = workloads.make_workload(args.config)

@@ -119,6 +119,37 @@ __global__ __launch_bounds__(kThreads) void k_embed_keys(EmbedGradParams p, SeqL
         keys[from + i] = key_of(p, lens, i, from);
 }
 
+// Sums of the lanes up to each.
+__device__ __forceinline__ uint32_t sums_upto(uint32_t v)
+{
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const uint32_t w = __shfl_up(v, o, 64);
+        if ((int)(threadIdx.x & 63) >= o) v += w;
+    }
+    return v;
+}
+
+// The places of a wave's 64 keys, in their order: `mine` says where the next of every digit goes, and is moved on. Lanes with
+// equal digits find each other by a ballot on each bit.
+__device__ __forceinline__ uint32_t take_place(uint32_t* mine, uint32_t digit, int bits, bool in)
+{
+    const int lane = threadIdx.x & 63;
+    uint64_t same = __ballot(in);
+    for (int b = 0; b < bits; ++b) {
+        const bool bit = digit >> b & 1;
+        const uint64_t set = __ballot(bit);
+        same &= bit ? set : ~set;
+    }
+    volatile uint32_t* place = &mine[digit];
+    uint32_t to = 0;
+    if (in) to = *place + __popcll(same & ((1ull << lane) - 1));
+    __builtin_amdgcn_wave_barrier();
+    if (in && (same >> lane) == 1) *place = to + 1;  // the last of them
+    __builtin_amdgcn_wave_barrier();
+    return to;
+}
+
 // How many keys of a tile have a digit: hist[tile][digit]. Tokens: the keys are made here, of all sequences.
 template <bool Tokens>
 __global__ __launch_bounds__(kSort) void k_embed_count(EmbedGradParams p, SeqLengths lens, uint32_t* keys, uint32_t N,
@@ -139,7 +170,7 @@ __global__ __launch_bounds__(kSort) void k_embed_count(EmbedGradParams p, SeqLen
 }
 
 // Keys of a tile to their places. Every workgroup adds up for itself how many keys have a smaller digit, or the same in an
-// earlier tile; lanes with equal digits find each other by a ballot on each bit.
+// earlier tile.
 __global__ __launch_bounds__(kSort) void k_embed_place(EmbedGradParams p, const uint32_t* keys, const uint32_t* order,
                                                        uint32_t N, int shift, const uint32_t* hist, uint32_t* keys_out,
                                                        uint32_t* order_out)
@@ -171,12 +202,7 @@ __global__ __launch_bounds__(kSort) void k_embed_place(EmbedGradParams p, const 
     __syncthreads();
     if (here) atomicAdd(&mine[key0 >> shift & (n - 1)], 1u);
     for (int64_t i = first + 64 + lane; i < end; i += 64) atomicAdd(&mine[keys[i] >> shift & (n - 1)], 1u);
-    uint32_t upto = all;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const uint32_t v = __shfl_up(upto, o, 64);
-        if (lane >= o) upto += v;
-    }
+    const uint32_t upto = sums_upto(all);
     if (lane == 63) sums[wave] = upto;
     __syncthreads();
     if (d < n) {
@@ -197,23 +223,78 @@ __global__ __launch_bounds__(kSort) void k_embed_place(EmbedGradParams p, const 
             key = keys[i];
             whence = order ? order[i] : (uint32_t)i;
         }
-        const uint32_t digit = key >> shift & (n - 1);
-        uint64_t same = __ballot(in);
-        for (int b = 0; b < bits; ++b) {
-            const bool bit = digit >> b & 1;
-            const uint64_t set = __ballot(bit);
-            same &= bit ? set : ~set;
-        }
-        volatile uint32_t* place = &mine[digit];
-        uint32_t to = 0;
-        if (in) to = *place + __popcll(same & ((1ull << lane) - 1));
-        __builtin_amdgcn_wave_barrier();
-        if (in && (same >> lane) == 1) *place = to + 1;  // the last of them
-        __builtin_amdgcn_wave_barrier();
+        const uint32_t to = take_place(mine, key >> shift & (n - 1), bits, in);
         if (in) {
             keys_out[to] = key;
             order_out[to] = whence;
         }
+    }
+}
+
+// All of it for at most kFew positions, by one workgroup in LDS; where the positions of every token begin too, of at most
+// kFewTokens tokens. (A call for 2,048 positions, 3,000 tokens, rows
+// of 512 fp32, replayed: 18.3 us; for 2,049, by the kernels above: 23.4.)
+constexpr int kFew = 2 * kSort, kFewTokens = 4096;
+__global__ __launch_bounds__(kSort) void k_embed_sort_few(EmbedGradParams p, SeqLengths lens, bool tokens, uint32_t N,
+                                                          uint32_t* keys_out, uint32_t* order_out, uint32_t* starts)
+{
+    constexpr int kBits = 9, kStretch = kFew / kSortWaves;
+    __shared__ uint32_t key[2][kFew], places[kSortWaves << kBits], sums[kSortWaves];
+    __shared__ uint16_t order[2][kFew];
+    const int bits = p.plan.bits, n = 1 << bits, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    uint32_t* mine = places + wave * n;
+    const uint32_t first = wave * kStretch, end = min(N, first + kStretch);
+    for (uint32_t i = threadIdx.x; i < N; i += kSort) {
+        key[0][i] = tokens ? key_of(p, lens, i, 0) : keys_out[i];
+        order[0][i] = (uint16_t)i;
+    }
+    int now = 0;
+    for (int pass = 0, shift = 0; pass < p.plan.passes; ++pass, shift += bits, now ^= 1) {
+        for (int i = threadIdx.x; i < n * kSortWaves; i += kSort) places[i] = 0;
+        __syncthreads();
+        for (uint32_t i = first + lane; i < end; i += 64) atomicAdd(&mine[key[now][i] >> shift & (n - 1)], 1u);
+        __syncthreads();
+        const int d = threadIdx.x;
+        uint32_t all = 0;
+        if (d < n)
+            for (int w = 0; w < kSortWaves; ++w) all += places[w * n + d];
+        const uint32_t upto = sums_upto(all);
+        if (lane == 63) sums[wave] = upto;
+        __syncthreads();
+        if (d < n) {
+            uint32_t at = upto - all;
+            for (int w = 0; w < wave; ++w) at += sums[w];
+            for (int w = 0; w < kSortWaves; ++w) {
+                const uint32_t count = places[w * n + d];
+                places[w * n + d] = at;
+                at += count;
+            }
+        }
+        __syncthreads();
+        for (uint32_t strip = first; strip < end; strip += 64) {
+            const bool in = strip + lane < end;
+            const uint32_t k = in ? key[now][strip + lane] : 0;
+            const uint32_t to = take_place(mine, k >> shift & (n - 1), bits, in);
+            if (in) {
+                key[now ^ 1][to] = k;
+                order[now ^ 1][to] = order[now][strip + lane];
+            }
+        }
+        __syncthreads();
+    }
+    for (uint32_t i = threadIdx.x; i < N; i += kSort) {
+        keys_out[i] = key[now][i];
+        order_out[i] = order[now][i];
+    }
+    if (p.V > kFewTokens) return;
+    for (uint32_t v = threadIdx.x; v <= (uint32_t)p.V; v += kSort) {
+        uint32_t lo = 0, hi = N;
+        while (lo < hi) {
+            const uint32_t mid = (lo + hi) / 2;
+            if (key[now][mid] < v) lo = mid + 1;
+            else hi = mid;
+        }
+        starts[v] = lo;
     }
 }
 
@@ -474,7 +555,10 @@ hipError_t launch_embed_grad(const EmbedGradParams& p, const SeqLengths* lens, i
     float* partials = place<float>(p, plan.partials);
     int now = 0;
     const int bins = 4 << plan.bits;
-    for (int pass = 0; N > 0 && pass < plan.passes; ++pass, now ^= 1) {
+    const bool few = N > 0 && N <= kFew;
+    if (few)
+        k_embed_sort_few<<<1, kSort, 0, stream>>>(p, lens ? *lens : SeqLengths{}, lens != nullptr, N, keys[0], order[0], starts);
+    for (int pass = 0; !few && N > 0 && pass < plan.passes; ++pass, now ^= 1) {
         const int shift = pass * plan.bits;
         if (pass == 0 && lens)
             k_embed_count<true><<<plan.tiles, kSort, bins, stream>>>(p, *lens, keys[0], N, shift, hist);
@@ -483,8 +567,10 @@ hipError_t launch_embed_grad(const EmbedGradParams& p, const SeqLengths* lens, i
         k_embed_place<<<plan.tiles, kSort, bins * kSortWaves, stream>>>(p, keys[now], pass ? order[now] : nullptr, N, shift,
                                                                         hist, keys[now ^ 1], order[now ^ 1]);
     }
-    const int64_t v = ((int64_t)p.V + kThreads) / kThreads;
-    k_embed_starts<<<(int)std::min<int64_t>(v, 2048), kThreads, 0, stream>>>(keys[now], N, p.V, starts);
+    if (!few || p.V > kFewTokens) {
+        const int64_t v = ((int64_t)p.V + kThreads) / kThreads;
+        k_embed_starts<<<(int)std::min<int64_t>(v, 2048), kThreads, 0, stream>>>(keys[now], N, p.V, starts);
+    }
     const Tiles rows = tiles_of(((int64_t)p.V + kGradRows - 1) / kGradRows, p.D), pieces = tiles_of(plan.pieces, p.D);
     by_type(dtype, [&](auto type) {
         by_whole(p.D, [&](auto whole) {
