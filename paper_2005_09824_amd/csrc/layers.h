@@ -123,7 +123,7 @@ struct VerifyParams {
     int32_t parts;
     void* workspace;
 };
-constexpr int kVerifyPart = 8192;  // logits of a row that a workgroup takes
+constexpr int kVerifyPart = 2048;  // logits of a row that a wave takes
 size_t verify_workspace(int64_t B, int K, int V);
 hipError_t launch_verify(const VerifyParams& p, const SeqLengths& lens, int dtype, hipStream_t stream);
 

@@ -14,11 +14,10 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
-constexpr int kChunks = kVerifyPart / 8 / kThreads;  // of eight logits, that a lane takes of a part
+constexpr int kChunks = kVerifyPart / 8 / 64;  // of eight logits, that a lane takes of a part: a part is a wave's
+constexpr int kRestThreads = 256;
+constexpr int kRestParts = kRestThreads / 128;  // two waves a part
 constexpr int kPickThreads = 512;
-constexpr int kPickTokens = kVerifyPart / kPickThreads;  // that follow each other, of a lane
-constexpr int kRestThreads = 512;
-constexpr int kRestChunks = kVerifyPart / 8 / kRestThreads;
 
 // What a part of a row comes to: its largest logit m, the sum s of exp(scale (x - m)) (0 of nothing but -inf, NaN where a logit
 // is NaN or +inf), the first index of the largest.
@@ -144,8 +143,13 @@ struct Weights {
         e = fma(e, f, 1.);
         return __hiloint2double(__double2hiint(e) + (__double2loint(shifted) << 20), __double2loint(e));
     }
-    // 2^-1000 where it is to be 0, which adds nothing beside the 1 of the largest
-    __device__ __forceinline__ double at_least(float x) const { return exp2_of(fmax(log2_of(x), -1000.)); }
+    // 2^-1000 where it is to be 0, which adds nothing beside the 1 of the largest (t's high word is at most that of -1,000,
+    // as a whole number without a sign: a comparison of 32 bits)
+    __device__ __forceinline__ double at_least(float x) const
+    {
+        const double t = log2_of(x);
+        return exp2_of(__hiloint2double((int)min((uint32_t)__double2hiint(t), 0xc08f4000u), __double2loint(t)));
+    }
     __device__ __forceinline__ double operator()(float x) const
     {
         const double t = log2_of(x);
@@ -172,27 +176,26 @@ __device__ __forceinline__ void load_part(const typename T::Store* x, int first,
     }
 }
 
-// ---- every row of a sequence's, a part at a time. (All sums in 64 bits. Sums of 32 bits decide nearly as well whether a
-// token is taken, and 64 bits of the one row that is drawn from could follow in a kernel of its own: 71 us so for 48 x 7 rows
-// of 128,000, 33 for 9 rows of 32,000.)
+// ---- every row of a sequence's, a part at a time, a wave each. (All sums in 64 bits. Sums of 32 bits decide nearly as well
+// whether a token is taken, and 64 bits of the one row that is drawn from could follow in a kernel of its own: 71 us so for
+// 48 x 7 rows of 128,000, 33 for 9 rows of 32,000.)
 
 template <typename T, bool Greedy>
 __global__ __launch_bounds__(kThreads) void k_verify_rows(VerifyParams p, SeqLengths lens, int64_t units)
 {
-    __shared__ float tops[kWaves];
-    __shared__ double sums[kWaves];
-    __shared__ uint64_t keys[kWaves];
     Space space;
     space_of(p.workspace, p.B, p.K, p.parts, &space);
-    const int rows = p.draft ? 2 * p.K + 1 : p.K + 1, wave = threadIdx.x >> 6;
-    for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
-        const int part = (int)(u % p.parts), row = (int)(u / p.parts % rows), b = (int)(u / p.parts / rows);
+    const int rows = p.draft ? 2 * p.K + 1 : p.K + 1, lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    for (int64_t u = (int64_t)blockIdx.x * kWaves + wave; u < units; u += (int64_t)gridDim.x * kWaves) {
+        const int64_t of = u / p.parts;
+        const int part = (int)(u - of * p.parts), b = (int)(of / rows), row = (int)(of - (int64_t)b * rows);
         const bool of_draft = row > p.K;
         const int i = of_draft ? row - p.K - 1 : row, n = drafts_of(p, lens, b);
         if (of_draft ? i >= n : i > n) continue;
-        const int first = part * (kVerifyPart / 8) + (int)threadIdx.x;
+        const int first = part * (kVerifyPart / 8) + lane;
         float f[kChunks][8];
-        load_part<T, kThreads, kChunks>(of_draft ? draft_row<T>(p, b, i) : target_row<T>(p, b, i), first, p.V, f);
+        load_part<T, 64, kChunks>(of_draft ? draft_row<T>(p, b, i) : target_row<T>(p, b, i), first, p.V, f);
         float m = -INFINITY;
         bool bad = false;
 #pragma unroll
@@ -203,9 +206,6 @@ __global__ __launch_bounds__(kThreads) void k_verify_rows(VerifyParams p, SeqLen
                 bad |= !(f[k][j] < INFINITY);
             }
         m = max_over<64>(m);
-        if ((threadIdx.x & 63) == 0) tops[wave] = m;
-        __syncthreads();
-        for (int w = 0; w < kWaves; ++w) m = fmaxf(m, tops[w]);
         double s = 0.;
         uint64_t best = 0;
         if (Greedy) {
@@ -214,31 +214,22 @@ __global__ __launch_bounds__(kThreads) void k_verify_rows(VerifyParams p, SeqLen
             for (int k = 0; k < kChunks; ++k)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const int at = (first + k * kThreads) * 8 + j;
+                    const int at = (first + k * 64) * 8 + j;
                     if (at < p.V) best = max(best, key_of(f[k][j], at));
                 }
             best = wave_best(best);
-            if ((threadIdx.x & 63) == 0) keys[wave] = best;
         } else if (m > -INFINITY) {
             const Weights weight(m, of_draft ? p.draft_scale : p.scale);
 #pragma unroll
             for (int k = 0; k < kChunks; ++k) {
-                if ((first + k * kThreads) * 8 >= p.V) break;  // (nothing but padding, of a wave for the most part)
+                if ((first - lane + k * 64) * 8 >= p.V) break;  // (nothing but padding)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) s += weight.at_least(f[k][j]);
             }
         }
         s = wave_sum(bad ? (double)NAN : s);
-        if ((threadIdx.x & 63) == 0) sums[wave] = s;
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            s = 0.;
-            for (int w = 0; w < kWaves; ++w) {
-                s += sums[w];
-                if (Greedy) best = max(best, keys[w]);
-            }
+        if (lane == 0)
             space.parts[((int64_t)b * (2 * p.K + 1) + row) * p.parts + part] = {s, m, Greedy ? (int)~(uint32_t)best : 0};
-        }
     }
 }
 
@@ -323,7 +314,7 @@ __device__ __forceinline__ void write_tokens(const VerifyParams& p, int b, const
 }
 
 template <typename T>
-__global__ __launch_bounds__(kRestThreads) void k_verify_greedy(VerifyParams p, SeqLengths lens)
+__global__ __launch_bounds__(kPickThreads) void k_verify_greedy(VerifyParams p, SeqLengths lens)
 {
     __shared__ int ends;
     __shared__ Choice shared;
@@ -355,41 +346,58 @@ __device__ __forceinline__ double block_sum(double v, double* parts)
     return v;
 }
 
-// Where a draft's logits are given: the row that ends every sequence, and if a drafted token is replaced there a part's sum of
-// max(0, p - q).
+// The row that ends every sequence, where a draft's logits are given. (In every workgroup of k_verify_rest by itself it took 12
+// us of 48 x 7 rows of 128,000, and 4 here.)
 template <typename T>
-__global__ __launch_bounds__(kRestThreads) void k_verify_rest(VerifyParams p, SeqLengths lens, int64_t units)
+__global__ __launch_bounds__(kPickThreads) void k_verify_choose(VerifyParams p, SeqLengths lens)
 {
     __shared__ int ends;
     __shared__ Choice shared;
-    __shared__ double sums[kRestThreads / 64];
     Space space;
     space_of(p.workspace, p.B, p.K, p.parts, &space);
-    for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
-        const int part = (int)(u % p.parts), b = (int)(u / p.parts);
+    for (int b = blockIdx.x; b < p.B; b += gridDim.x) {
         const Choice c = choose<T, false>(p, space, b, drafts_of(p, lens, b), &ends, &shared);
-        if (part == 0 && threadIdx.x == 0) space.choice[b] = c;
-        if (c.kind == kDrafted) {
-            const int first = part * (kVerifyPart / 8) + (int)threadIdx.x;
-            float f[kRestChunks][8], g[kRestChunks][8];
-            load_part<T, kRestThreads, kRestChunks>(target_row<T>(p, b, c.row), first, p.V, f);
-            load_part<T, kRestThreads, kRestChunks>(draft_row<T>(p, b, c.row), first, p.V, g);
+        if (threadIdx.x == 0) space.choice[b] = c;
+    }
+}
+
+// If a drafted token is replaced: the sums of max(0, p - q) of kRestParts parts, two waves each.
+template <typename T>
+__global__ __launch_bounds__(kRestThreads) void k_verify_rest(VerifyParams p, int64_t units)
+{
+    __shared__ double halves[kRestThreads / 64];
+    Space space;
+    space_of(p.workspace, p.B, p.K, p.parts, &space);
+    const int groups = (p.parts + kRestParts - 1) / kRestParts, lane = threadIdx.x & 63, wave = (int)(threadIdx.x >> 6);
+    for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
+        const int b = (int)(u / groups), part = (int)(u - (int64_t)b * groups) * kRestParts + wave / 2;
+        const Choice c = space.choice[b];
+        if (c.kind != kDrafted) continue;
+        if (part < p.parts) {
+            constexpr int kHalf = kChunks / 2;
+            const int first = part * (kVerifyPart / 8) + (wave & 1) * kHalf * 64 + lane;
+            float f[kHalf][8], g[kHalf][8];
+            load_part<T, 64, kHalf>(target_row<T>(p, b, c.row), first, p.V, f);
+            load_part<T, 64, kHalf>(draft_row<T>(p, b, c.row), first, p.V, g);
             const Weights weight(c.m, p.scale), weight_q(c.mq, p.draft_scale);
             double s = 0.;
 #pragma unroll
-            for (int k = 0; k < kRestChunks; ++k) {
-                if ((first + k * kRestThreads) * 8 >= p.V) break;
+            for (int k = 0; k < kHalf; ++k) {
+                if ((first - lane + k * 64) * 8 >= p.V) break;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) s += left_over(weight(f[k][j]), c.per, weight_q(g[k][j]), c.per_q);
             }
-            s = block_sum(s, sums);
-            if (threadIdx.x == 0) space.rest[u] = s;
+            s = wave_sum(s);
+            if (lane == 0) halves[wave] = s;
         }
+        __syncthreads();
+        if (part < p.parts && (threadIdx.x & 127) == 0)
+            space.rest[(int64_t)b * p.parts + part] = halves[wave] + halves[wave + 1];
         __syncthreads();
     }
 }
 
-// The last token of every sequence: the first whose running sum passes the random number times the whole. Chosen: k_verify_rest
+// The last token of every sequence: the first whose running sum passes the random number times the whole. Chosen: k_verify_choose
 // has said which row ends the sequence.
 template <typename T, bool Chosen>
 __global__ __launch_bounds__(kPickThreads) void k_verify_pick(VerifyParams p, SeqLengths lens)
@@ -414,24 +422,27 @@ __global__ __launch_bounds__(kPickThreads) void k_verify_pick(VerifyParams p, Se
         const Weights weight(c.m, p.scale), weight_q(c.mq, p.draft_scale);
         const Part* parts = space.parts + ((int64_t)b * (2 * p.K + 1) + c.row) * p.parts;
         const double* rest = space.rest + (int64_t)b * p.parts;
-        // a lane's weights of tokens of a part that follow each other
+        // a lane's weights of eight tokens of a part
         const auto weights_of = [&](int part, double* w) {
-            const int chunk = (part * kPickThreads + (int)threadIdx.x) * (kPickTokens / 8);
-            float f[kPickTokens / 8][8], g[kPickTokens / 8][8];
-            load_part<T, 1, kPickTokens / 8>(target_row<T>(p, b, c.row), chunk, p.V, f);
-            if (c.kind == kDrafted) load_part<T, 1, kPickTokens / 8>(draft_row<T>(p, b, c.row), chunk, p.V, g);
             double s = 0.;
 #pragma unroll
-            for (int j = 0; j < kPickTokens; ++j) {
-                w[j] = weight(f[j / 8][j % 8]);
-                if (c.kind == kDrafted) w[j] = left_over(w[j], c.per, weight_q(g[j / 8][j % 8]), c.per_q);
+            for (int j = 0; j < 8; ++j) w[j] = 0.;
+            if (threadIdx.x >= kVerifyPart / 8) return s;
+            const int chunk = part * (kVerifyPart / 8) + (int)threadIdx.x;
+            float f[1][8], g[1][8];
+            load_part<T, 1, 1>(target_row<T>(p, b, c.row), chunk, p.V, f);
+            if (c.kind == kDrafted) load_part<T, 1, 1>(draft_row<T>(p, b, c.row), chunk, p.V, g);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                w[j] = weight(f[0][j]);
+                if (c.kind == kDrafted) w[j] = left_over(w[j], c.per, weight_q(g[0][j]), c.per_q);
                 if (c.kind == kGiven && chunk * 8 + j == c.token) w[j] = 0.;
                 s += w[j];
             }
             return s;
         };
         // the part that a token is taken out of is added up again without it: of a sum minus nearly all of it little is right
-        double w[kPickTokens], without = 0.;
+        double w[8], without = 0.;
         const int given = c.kind == kGiven ? c.token / kVerifyPart : -1;
         if (given >= 0) {
             without = block_sum(weights_of(given, w), scan);
@@ -476,7 +487,7 @@ __global__ __launch_bounds__(kPickThreads) void k_verify_pick(VerifyParams p, Se
         }
         double sum = 0.;
         if (part == out)
-            for (int j = 0; j < kPickTokens; ++j) sum += w[j];
+            for (int j = 0; j < 8; ++j) sum += w[j];
         else
             sum = weights_of(part, w);
         const double upto = wave_scan(sum);
@@ -485,10 +496,10 @@ __global__ __launch_bounds__(kPickThreads) void k_verify_pick(VerifyParams p, Se
         double cum = before;
         for (int k = 0; k < wave; ++k) cum += scan[k];
         cum += upto - sum;
-        const int first = part * kVerifyPart + (int)threadIdx.x * kPickTokens;
+        const int first = part * kVerifyPart + (int)threadIdx.x * 8;
         int mine = INT32_MAX, some = -1;
 #pragma unroll
-        for (int j = 0; j < kPickTokens; ++j) {
+        for (int j = 0; j < 8; ++j) {
             cum += w[j];
             if (w[j] > 0.) {
                 some = first + j;
@@ -513,18 +524,20 @@ size_t verify_workspace(int64_t B, int K, int V)
 hipError_t launch_verify(const VerifyParams& p, const SeqLengths& lens, int dtype, hipStream_t stream)
 {
     const int rows = p.draft ? 2 * p.K + 1 : p.K + 1;
-    const int64_t units = (int64_t)p.B * p.parts, all = units * rows;
+    const int64_t all = ((int64_t)p.B * rows * p.parts + kWaves - 1) / kWaves, units = (int64_t)p.B * rows * p.parts;
+    const int64_t groups = (int64_t)p.B * ((p.parts + kRestParts - 1) / kRestParts);
     const auto grid_of = [](int64_t n) { return (int)std::min<int64_t>(n, 1 << 20); };
     by_type(dtype, [&](auto type) {
         using T = decltype(type);
         if (!p.uniforms) {
-            k_verify_rows<T, true><<<grid_of(all), kThreads, 0, stream>>>(p, lens, all);
-            k_verify_greedy<T><<<grid_of(p.B), kRestThreads, 0, stream>>>(p, lens);
+            k_verify_rows<T, true><<<grid_of(all), kThreads, 0, stream>>>(p, lens, units);
+            k_verify_greedy<T><<<grid_of(p.B), kPickThreads, 0, stream>>>(p, lens);
             return;
         }
-        k_verify_rows<T, false><<<grid_of(all), kThreads, 0, stream>>>(p, lens, all);
+        k_verify_rows<T, false><<<grid_of(all), kThreads, 0, stream>>>(p, lens, units);
         if (p.draft) {
-            k_verify_rest<T><<<grid_of(units), kRestThreads, 0, stream>>>(p, lens, units);
+            k_verify_choose<T><<<grid_of(p.B), kPickThreads, 0, stream>>>(p, lens);
+            k_verify_rest<T><<<grid_of(groups), kRestThreads, 0, stream>>>(p, groups);
             k_verify_pick<T, true><<<grid_of(p.B), kPickThreads, 0, stream>>>(p, lens);
         } else {
             k_verify_pick<T, false><<<grid_of(p.B), kPickThreads, 0, stream>>>(p, lens);

@@ -253,6 +253,23 @@ def test_norm(D, dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("D", [513, 1024, 1100, 2048, 2100, 3001, 4096, 5003, 8192])
+def test_norm_of_many_rows(D, dtype):
+    # (few rows are spread over more lanes each)
+    torch = _torch()
+    rng = np.random.default_rng(D)
+    N = 523
+    x, x64 = _values(rng, (N, D), dtype)
+    res, r64 = _values(rng, (N, D), dtype, 3.0)
+    weight = torch.from_numpy(rng.normal(1, 0.3, D).astype(np.float32)).cuda()
+    for p, quantized in ((0.0, True), (0.2, False)):
+        r = binding.lfmmi_add_rms_norm(x, res, weight, p=p, seed=3, offset=4, quantized=quantized, y="both" if quantized else True)
+        check_norm(x64, r64, weight, 1e-6, None, p, 3, 4, r, dtype, (N, D))
+    few = binding.lfmmi_add_rms_norm(x[:300], res[:300], weight, p=0.2, seed=3, offset=4)
+    assert torch.equal(few.sum, r.sum[:300])
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("B,T,D", [(1, 1, 16), (5, 7, 40), (300, 3, 24), (600, 1, 640), (4, 700, 72), (3, 40, 2100), (2, 9, 16400),
                                    (1, 3000, 16), (280, 2, 20000)])
 def test_sequences(B, T, D, dtype):
