@@ -425,7 +425,7 @@ __global__ __launch_bounds__(kThreads) void k_embed_rows(EmbedGradParams p, Tile
 // Tokens with pieces: a workgroup has 64 chunks of a row, every wave a stretch of the pieces and of the positions before and
 // behind them. It does so for the tokens whose first piece is one of kJoinPieces (a workgroup for each piece, most of which
 // are no token's first: 24 us instead of 9 for 32,768 positions of 2,048 bf16).
-constexpr int kJoinWaves = 8, kJoinPieces = 8;
+constexpr int kJoinWaves = 4, kJoinPieces = 2;
 template <typename T, bool Whole>
 __global__ __launch_bounds__(kJoinWaves * 64) void k_embed_join(EmbedGradParams p, int parts, int64_t units,
                                                                 const uint32_t* starts, const uint32_t* keys,
