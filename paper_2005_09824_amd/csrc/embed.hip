@@ -56,8 +56,8 @@ int grid_of(int64_t units) { return (int)std::min<int64_t>(units, 1 << 20); }
 
 // ---- forward
 
-// Rows that a lane has on their way: a token, then its row, are two waits. (32,768 rows of 2,048 bf16, a table of 65,536:
-// 55 us with one row a lane.)
+// Rows that a lane has on their way: a token, then its row, are two waits. Bound by HBM: 32,768 rows of 2,048 bf16 of a table of
+// 65,536, a third of them padding, 39 us (134 MB written, 65 MB of the table read; 55 us with one row a lane).
 constexpr int kEmbedRows = 4;
 
 template <typename T, bool Whole, int Rows>
@@ -234,7 +234,7 @@ __global__ __launch_bounds__(kSort) void k_embed_place(EmbedGradParams p, const 
 // All of it for at most kFew positions, by one workgroup in LDS; where the positions of every token begin too, of at most
 // kFewTokens tokens. (A call for 2,048 positions, 3,000 tokens, rows
 // of 512 fp32, replayed: 18.3 us; for 2,049, by the kernels above: 23.4.)
-constexpr int kFew = 2 * kSort, kFewTokens = 4096;
+constexpr int kFew = 2 * kSort, kFewTokens = 2048;
 __global__ __launch_bounds__(kSort) void k_embed_sort_few(EmbedGradParams p, SeqLengths lens, bool tokens, uint32_t N,
                                                           uint32_t* keys_out, uint32_t* order_out, uint32_t* starts)
 {
@@ -378,7 +378,9 @@ __device__ __forceinline__ Segment segment_of(uint32_t from, uint32_t to)
 }
 
 // Such pieces, and the rows of the table that have none, those without a position among them. A lane has kGradRows rows of
-// the table, and asks for the first position's row of each before it waits for one.
+// the table, and asks for the first position's row of each before it waits for one. Bound by HBM and by three waits in a row (a
+// token's positions, a position, its row): 65,536 rows of 2,048 bf16 for 21,000 positions 82 us (268 MB written, 85 read), of which
+// the writes alone take 42; eight rows a lane 5 us more, two 5 us more.
 constexpr int kGradRows = 4;
 template <typename T, bool Whole>
 __global__ __launch_bounds__(kThreads) void k_embed_rows(EmbedGradParams p, Tiles rows, Tiles pieces, const uint32_t* starts,
@@ -423,8 +425,8 @@ __global__ __launch_bounds__(kThreads) void k_embed_rows(EmbedGradParams p, Tile
 }
 
 // Tokens with pieces: a workgroup has 64 chunks of a row, every wave a stretch of the pieces and of the positions before and
-// behind them. It does so for the tokens whose first piece is one of kJoinPieces (a workgroup for each piece, most of which
-// are no token's first: 24 us instead of 9 for 32,768 positions of 2,048 bf16).
+// behind them. It does so for the tokens whose first piece is one of kJoinPieces. (32,768 positions of 2,048 bf16: 11 us; 24 with a
+// workgroup of eight waves for each piece, most of which are no token's first, and 15 for eight pieces.)
 constexpr int kJoinWaves = 4, kJoinPieces = 2;
 template <typename T, bool Whole>
 __global__ __launch_bounds__(kJoinWaves * 64) void k_embed_join(EmbedGradParams p, int parts, int64_t units,

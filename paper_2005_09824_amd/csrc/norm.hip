@@ -21,7 +21,8 @@ constexpr float kLeastScale = 1.17549435e-38f;  // 2^-126: its inverse is finite
 // Waves of one workgroup take a row each, or all of them one together.
 constexpr int threads_of(int lanes) { return lanes == 64 ? kThreads : lanes; }
 
-// ---- dropout alone
+// ---- dropout alone. Bound by HBM (16,384 rows of 8,189 bf16, a view: 101 us, 5.3 TB/s; 32,000 of 640 fp32: 28 us, 5.9 TB/s); the
+// random bits, ten rounds of two products of 32 bits for eight values, fit beside it.
 
 constexpr int kDropoutChunks = 4;  // of eight values, that a lane takes of a row
 
@@ -140,7 +141,8 @@ __device__ __forceinline__ int row_in_group()
 __device__ __forceinline__ uint32_t magnitude(float y) { return __float_as_uint(y) & 0x7fffffffu; }
 
 // G lanes take a row, N chunks of eight values each, which stay in registers; N == 0: any number of
-// chunks, read again for each pass over the row.
+// chunks, read again for each pass over the row. Bound by HBM: 16,384 rows of 8,192 bf16, two arrays read and two written, 187
+// us, 5.7 TB/s, what a copy takes.
 template <typename T, bool Whole, int G, int N>
 __global__ __launch_bounds__(threads_of(G)) void k_norm(NormParams p, SeqLengths lens)
 {
@@ -302,7 +304,8 @@ __device__ __forceinline__ void hide(Raw<T>& v)
 }
 
 // The same lanes and chunks; a workgroup adds its rows' share of the weight's gradient up, and leaves it as a
-// row of partial sums.
+// row of partial sums. Bound by HBM: 16,384 rows of 8,192 bf16, three arrays read and two written, 242 to 269 us, 5.0 to 5.5 TB/s
+// (435 without the rows asked for ahead).
 template <typename T, bool Whole, int G, int N>
 __global__ __launch_bounds__(threads_of(G)) void k_norm_grad(NormGradParams p, SeqLengths lens)
 {
@@ -474,7 +477,7 @@ __global__ __launch_bounds__(threads_of(G)) void k_norm_grad(NormGradParams p, S
 }
 
 // Columns of the partial sums, added up in the order of the workgroups: 32 columns and 32 stretches of rows a
-// workgroup.
+// workgroup, 16 loads at once (5 us for 768 x 640; 11 one at a time).
 constexpr int kColumns = 32, kStretches = 32, kAtOnce = 16;
 template <typename T>
 __global__ __launch_bounds__(kColumns * kStretches) void k_norm_weight(const float* partials, int blocks, int D,

@@ -168,7 +168,9 @@ def softmax(x, scale):
         return None, 2
     if np.isneginf(x).all():
         return None, 1
-    e = np.exp((x - x.max()) * float(np.float32(scale)))
+    with np.errstate(over="ignore"):
+        d = (x - x.max()) * float(np.float32(scale))
+    e = np.where(d > -1000.0 * np.log(2.0), np.exp(np.maximum(d, -700.0)), 0.0)
     return e / e.sum(), 0
 
 

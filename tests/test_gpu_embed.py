@@ -64,7 +64,7 @@ def _check_backward(g64, dtype, tokens, lengths, scale, grad, old=None, accumula
 SHAPES = [(1, 1, 1, 1), (3, 2, 5, 7), (1, 1, 4096, 64), (17, 9, 10, 63), (2, 700, 84, 64), (5, 333, 3, 65), (300, 3, 50, 40),
           (1, 5000, 1000, 17), (64, 33, 1025, 128), (4, 1000, 40000, 24), (1, 3, 200000, 8), (2, 90, 7, 2049), (1, 40, 3, 8200),
           (1, 70, 2, 4097), (2, 2049, 1, 8),
-          (1, 2047, 600, 8), (2, 1024, 4096, 9), (1, 500, 4097, 16), (1, 1030, 90, 24), (1, 2048, 300000, 8), (1, 140000, 70, 8),
+          (1, 2047, 600, 8), (2, 1024, 2048, 9), (1, 500, 2049, 16), (1, 1030, 90, 24), (1, 2048, 300000, 8), (1, 140000, 70, 8),
           (600, 4, 33, 16)]
 
 

@@ -166,6 +166,62 @@ def test_flags():
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+def test_values_that_are_none(dtype):
+    # NaN of either sign and +inf, at the beginning, in the middle and at the very end of a row, and in one of -inf
+    torch = _torch()
+    V = 5000
+    base = torch.randn((9, 2, V), device="cuda").to(getattr(torch, dtype))
+    minus = (torch.tensor(-4194304, dtype=torch.int32) if dtype == "float32" else torch.tensor(-64, dtype=torch.int16)).view(base.dtype).cuda()
+    assert torch.isnan(minus) and torch.signbit(minus)
+    for row in (0, 1):
+        x = base.clone()
+        for b, (at, value) in enumerate(((0, float("nan")), (2500, minus), (V - 1, minus), (0, float("inf")), (V - 1, float("inf")),
+                                         (4999, float("nan")), (17, minus))):
+            if b == 6:
+                x[b, row] = -np.inf
+            x[b, row, at] = value
+            assert torch.isnan(x[b, row, at]) == np.isnan(float(value))
+        x[7, row] = -np.inf
+        t = torch.zeros((9, 1), dtype=torch.int64, device="cuda")
+        t[:, 0] = x[:, 0].float().nan_to_num(0).argmax(-1)
+        u = torch.full((9, 2), 1e-30, device="cuda")
+        d = base[:, :1].clone()
+        for draft, uniforms in ((d, u), (None, u), (None, None)):
+            r = binding.lfmmi_verify_tokens(x, t, uniforms, draft)
+            check(x.double().cpu().numpy(), t.cpu().numpy(), None, 1.0, None if uniforms is None else u.cpu().numpy(),
+                  None if draft is None else d.double().cpu().numpy(), 1.0, r)
+            assert r.status[8] == 0 and (row == 1 or r.status[:8].tolist() == [2] * 7 + [1])
+        if row == 0:   # the same in the draft's row
+            r = binding.lfmmi_verify_tokens(base, t, u, x[:, :1].contiguous())
+            assert r.status.tolist() == [2] * 7 + [1, 0] and not r.accepted[:8].any()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("scale", [1e-6, 0.37, 1e6])
+def test_large_and_small_logits(scale, dtype):
+    # rows whose largest logit is far from 0, where the next smaller value of the type is far below it
+    torch = _torch()
+    rng = np.random.default_rng(int(scale * 100) + 1)
+    top = 3e4 if dtype == "float16" else 1e30
+    x = torch.from_numpy(rng.normal(0, 1, (6, 3, 3000)).astype(np.float32)).to(getattr(torch, dtype)).cuda()
+    x[0] += top
+    x[1] -= top
+    x[2] *= 1e-6
+    x[3, :, 2047:] = top
+    x[4] *= 1e4
+    x[5, :, 1:] = torch.finfo(x.dtype).min
+    x[5, :, 0] = -np.inf
+    u = rng.random((6, 3)).astype(np.float32)
+    t = rng.integers(0, 3000, (6, 2))
+    t[:3, 0] = x[:3, 0].double().cpu().numpy().argmax(-1)
+    x64 = x.double().cpu().numpy()
+    check(x64, t, None, scale, u, x64[:, 1:], scale,
+          binding.lfmmi_verify_tokens(x, torch.from_numpy(t).cuda(), torch.from_numpy(u).cuda(), x[:, 1:], scale=scale, draft_scale=scale))
+    check(x64, t, None, scale, u, None, 1.0,
+          binding.lfmmi_verify_tokens(x, torch.from_numpy(t).cuda(), torch.from_numpy(u).cuda(), scale=scale))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 def test_views(dtype):
     torch = _torch()
     rng = np.random.default_rng(5)
