@@ -60,7 +60,7 @@ int grid_of(int64_t units) { return (int)std::min<int64_t>(units, 1 << 20); }
 // 65,536, a third of them padding, 39 us (134 MB written, 65 MB of the table read; 55 us with one row a lane).
 constexpr int kEmbedRows = 4;
 
-template <typename T, bool Whole, int Rows>
+template <typename T, Width W, int Rows>
 __global__ __launch_bounds__(kThreads) void k_embed(EmbedParams p, SeqLengths lens, Tiles tiles)
 {
     using Store = typename T::Store;
@@ -79,7 +79,7 @@ __global__ __launch_bounds__(kThreads) void k_embed(EmbedParams p, SeqLengths le
 #pragma unroll
         for (int k = 0; k < Rows; ++k)
             if (token[k] >= 0 && token[k] < p.V)
-                v[k] = raw_at<T, Whole>(static_cast<const Store*>(p.table) + token[k] * p.stride, at.c, p.D);
+                v[k] = raw_at<T, W>(static_cast<const Store*>(p.table) + token[k] * p.stride, at.c, p.D);
 #pragma unroll
         for (int k = 0; k < Rows; ++k) {
             if (first + k >= rows) continue;
@@ -88,11 +88,11 @@ __global__ __launch_bounds__(kThreads) void k_embed(EmbedParams p, SeqLengths le
 #pragma unroll
             for (int i = 0; i < 8; ++i) f[i] = bad ? NAN : 0.f;
             if (token[k] >= 0 && !bad) {
-                unpack_at<T, Whole>(v[k], at.c, p.D, f);
+                unpack_at<T, W>(v[k], at.c, p.D, f);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) f[i] *= p.scale;
             }
-            store_at<T, Whole>(static_cast<Store*>(p.out) + (first + k) * p.D, at.c, p.D, f, p.once);
+            store_at<T, W>(static_cast<Store*>(p.out) + (first + k) * p.D, at.c, p.D, f, p.once);
             if (p.status && at.c == 0) p.status[first + k] = bad ? 4 : 0;
         }
     }
@@ -232,8 +232,9 @@ __global__ __launch_bounds__(kSort) void k_embed_place(EmbedGradParams p, const 
 }
 
 // All of it for at most kFew positions, by one workgroup in LDS; where the positions of every token begin too, of at most
-// kFewTokens tokens. (A call for 2,048 positions, 3,000 tokens, rows
-// of 512 fp32, replayed: 18.3 us; for 2,049, by the kernels above: 23.4.)
+// kFewTokens tokens. (A call, replayed: 2,000 positions of 512 fp32, a table of 2,000: 17 us, sorted by the kernels above 24,
+// the beginnings by a kernel of their own 19. A table of 5,000: 20, 24 and 20; 2,048 positions of 256, a table of 30,000: 44, 30
+// and 25.)
 constexpr int kFew = 2 * kSort, kFewTokens = 2048;
 __global__ __launch_bounds__(kSort) void k_embed_sort_few(EmbedGradParams p, SeqLengths lens, bool tokens, uint32_t N,
                                                           uint32_t* keys_out, uint32_t* order_out, uint32_t* starts)
@@ -327,43 +328,43 @@ __global__ __launch_bounds__(kThreads) void k_embed_starts(const uint32_t* keys,
 
 // ---- sums of rows
 
-template <typename T, bool Whole>
+template <typename T, Width W>
 __device__ __forceinline__ Raw<T> row_of(const EmbedGradParams& p, uint32_t pos, int c)
 {
     const uint32_t b = pos / (uint32_t)p.T;
-    return raw_at<T, Whole>(static_cast<const typename T::Store*>(p.g) + (int64_t)b * p.stride_b +
+    return raw_at<T, W>(static_cast<const typename T::Store*>(p.g) + (int64_t)b * p.stride_b +
                                 (int64_t)(pos - b * (uint32_t)p.T) * p.stride_t, c, p.D);
 }
 
 // Adds the chunk of positions order[from..to - 1], in that order.
-template <typename T, bool Whole, int AtOnce>
+template <typename T, Width W, int AtOnce>
 __device__ __forceinline__ void add_rows(const EmbedGradParams& p, const uint32_t* order, uint32_t from, uint32_t to,
                                          int c, float* s)
 {
     for (uint32_t k = from; k < to; k += AtOnce) {
         Raw<T> v[AtOnce];
 #pragma unroll
-        for (int j = 0; j < AtOnce; ++j) v[j] = row_of<T, Whole>(p, order[min(k + j, to - 1)], c);
+        for (int j = 0; j < AtOnce; ++j) v[j] = row_of<T, W>(p, order[min(k + j, to - 1)], c);
 #pragma unroll
         for (int j = 0; j < AtOnce; ++j) {
             if (k + j >= to) continue;
             float f[8];
-            unpack_at<T, Whole>(v[j], c, p.D, f);
+            unpack_at<T, W>(v[j], c, p.D, f);
 #pragma unroll
             for (int i = 0; i < 8; ++i) s[i] += f[i];
         }
     }
 }
 
-template <typename T, bool Whole>
+template <typename T, Width W>
 __device__ __forceinline__ void write_grad(const EmbedGradParams& p, int64_t v, int c, const float* s)
 {
     typename T::Store* out = static_cast<typename T::Store*>(p.grad) + v * p.D;
     float f[8];
-    if (p.accumulate) load_at<T, Whole>(out, c, p.D, f);
+    if (p.accumulate) load_at<T, W>(out, c, p.D, f);
 #pragma unroll
     for (int i = 0; i < 8; ++i) f[i] = p.accumulate ? f[i] + s[i] * p.scale : s[i] * p.scale;
-    store_at<T, Whole>(out, c, p.D, f, p.once);
+    store_at<T, W>(out, c, p.D, f, p.once);
 }
 
 // The sorted positions in pieces of kEmbedPiece: one that a token has as a whole is added up by itself. A token's row is the
@@ -382,7 +383,7 @@ __device__ __forceinline__ Segment segment_of(uint32_t from, uint32_t to)
 // token's positions, a position, its row): 65,536 rows of 2,048 bf16 for 21,000 positions 82 us (268 MB written, 85 read), of which
 // the writes alone take 42; eight rows a lane 5 us more, two 5 us more.
 constexpr int kGradRows = 4;
-template <typename T, bool Whole>
+template <typename T, Width W>
 __global__ __launch_bounds__(kThreads) void k_embed_rows(EmbedGradParams p, Tiles rows, Tiles pieces, const uint32_t* starts,
                                                          const uint32_t* keys, const uint32_t* order, float* partials)
 {
@@ -395,8 +396,8 @@ __global__ __launch_bounds__(kThreads) void k_embed_rows(EmbedGradParams p, Tile
             const uint32_t from = (uint32_t)at.group * kEmbedPiece, key = keys[from];
             if (key != keys[from + kEmbedPiece - 1] || key == (uint32_t)p.V) continue;
             float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-            add_rows<T, Whole, 8>(p, order, from, from + kEmbedPiece, at.c, s);
-            store_at<F32, Whole>(partials + at.group * p.D, at.c, p.D, s);
+            add_rows<T, W, 8>(p, order, from, from + kEmbedPiece, at.c, s);
+            store_at<F32, W>(partials + at.group * p.D, at.c, p.D, s);
             continue;
         }
         const Place at = place_of(rows, u - pieces.units);
@@ -410,16 +411,16 @@ __global__ __launch_bounds__(kThreads) void k_embed_rows(EmbedGradParams p, Tile
         for (int k = 0; k < kGradRows; ++k) {
             const Segment g = segment_of(begin[k], begin[k + 1]);
             first[k] = no_values<T>();
-            if (g.from < g.to && g.first >= g.last) first[k] = row_of<T, Whole>(p, order[g.from], at.c);
+            if (g.from < g.to && g.first >= g.last) first[k] = row_of<T, W>(p, order[g.from], at.c);
         }
 #pragma unroll
         for (int k = 0; k < kGradRows; ++k) {
             const Segment g = segment_of(begin[k], begin[k + 1]);
             if (g.first < g.last || v + k >= p.V || (g.from == g.to && p.accumulate)) continue;
             float s[8];
-            unpack_at<T, Whole>(first[k], at.c, p.D, s);
-            if (g.from + 1 < g.to) add_rows<T, Whole, 4>(p, order, g.from + 1, g.to, at.c, s);
-            write_grad<T, Whole>(p, v + k, at.c, s);
+            unpack_at<T, W>(first[k], at.c, p.D, s);
+            if (g.from + 1 < g.to) add_rows<T, W, 4>(p, order, g.from + 1, g.to, at.c, s);
+            write_grad<T, W>(p, v + k, at.c, s);
         }
     }
 }
@@ -428,7 +429,7 @@ __global__ __launch_bounds__(kThreads) void k_embed_rows(EmbedGradParams p, Tile
 // behind them. It does so for the tokens whose first piece is one of kJoinPieces. (32,768 positions of 2,048 bf16: 11 us; 24 with a
 // workgroup of eight waves for each piece, most of which are no token's first, and 15 for eight pieces.)
 constexpr int kJoinWaves = 4, kJoinPieces = 2;
-template <typename T, bool Whole>
+template <typename T, Width W>
 __global__ __launch_bounds__(kJoinWaves * 64) void k_embed_join(EmbedGradParams p, int parts, int64_t units,
                                                                 const uint32_t* starts, const uint32_t* keys,
                                                                 const uint32_t* order, const float* partials)
@@ -454,22 +455,22 @@ __global__ __launch_bounds__(kJoinWaves * 64) void k_embed_join(EmbedGradParams 
             float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
             if (c < chunks) {
                 const uint32_t head = g.from + wave * kEnds, tail = g.last * kEmbedPiece + wave * kEnds;
-                add_rows<T, Whole, kEnds>(p, order, head, min(head + kEnds, g.first * kEmbedPiece), c, s);
+                add_rows<T, W, kEnds>(p, order, head, min(head + kEnds, g.first * kEmbedPiece), c, s);
                 for (uint32_t i = wave * each; i < to; i += 8) {
                     Raw<F32> f[8];
 #pragma unroll
                     for (int j = 0; j < 8; ++j)
-                        f[j] = raw_at<F32, Whole>(part + (int64_t)min(i + j, to - 1) * p.D, c, p.D);
+                        f[j] = raw_at<F32, W>(part + (int64_t)min(i + j, to - 1) * p.D, c, p.D);
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
                         if (i + j >= to) continue;
                         float e[8];
-                        unpack_at<F32, Whole>(f[j], c, p.D, e);
+                        unpack_at<F32, W>(f[j], c, p.D, e);
 #pragma unroll
                         for (int x = 0; x < 8; ++x) s[x] += e[x];
                     }
                 }
-                add_rows<T, Whole, kEnds>(p, order, tail, min(tail + kEnds, g.to), c, s);
+                add_rows<T, W, kEnds>(p, order, tail, min(tail + kEnds, g.to), c, s);
             }
 #pragma unroll
             for (int e = 0; e < 8; ++e) sums[wave][e * 64 + lane] = s[e];
@@ -478,7 +479,7 @@ __global__ __launch_bounds__(kJoinWaves * 64) void k_embed_join(EmbedGradParams 
                 for (int w = 1; w < kJoinWaves; ++w)
 #pragma unroll
                     for (int e = 0; e < 8; ++e) s[e] += sums[w][e * 64 + lane];
-                write_grad<T, Whole>(p, token, c, s);
+                write_grad<T, W>(p, token, c, s);
             }
             __syncthreads();
         }
@@ -496,15 +497,16 @@ U* place(const EmbedGradParams& p, size_t at)
 hipError_t launch_embed(const EmbedParams& p, const SeqLengths& lens, int dtype, hipStream_t stream)
 {
     const int64_t rows = (int64_t)p.B * p.T;
-    // (few rows: all at once)
+    // Few rows: one a lane, all at once (us, replayed, its own rows in the caches: 1,000 of 1,024 bf16 3.6, four a lane 4.0; 2,000 of
+    // 2,048 5.0 and 5.1; 8,000 of 1,024 7.4 and 7.2; 30,000 of 2,048, which the caches do not hold, 50 and 44).
     const bool few = rows * ((p.D + 2047) / 2048) < 4096;
     const Tiles t = tiles_of(few ? rows : (rows + kEmbedRows - 1) / kEmbedRows, p.D);
     by_type(dtype, [&](auto type) {
-        by_whole(p.D, [&](auto whole) {
+        by_width<true>(p.D, [&](auto whole) {
             using Type = decltype(type);
-            constexpr bool kWhole = decltype(whole)::value;
-            if (few) k_embed<Type, kWhole, 1><<<grid_of(t.units), kThreads, 0, stream>>>(p, lens, t);
-            else k_embed<Type, kWhole, kEmbedRows><<<grid_of(t.units), kThreads, 0, stream>>>(p, lens, t);
+            constexpr Width kWidth = decltype(whole)::value;
+            if (few) k_embed<Type, kWidth, 1><<<grid_of(t.units), kThreads, 0, stream>>>(p, lens, t);
+            else k_embed<Type, kWidth, kEmbedRows><<<grid_of(t.units), kThreads, 0, stream>>>(p, lens, t);
         });
     });
     return hipGetLastError();
@@ -575,15 +577,15 @@ hipError_t launch_embed_grad(const EmbedGradParams& p, const SeqLengths* lens, i
     }
     const Tiles rows = tiles_of(((int64_t)p.V + kGradRows - 1) / kGradRows, p.D), pieces = tiles_of(plan.pieces, p.D);
     by_type(dtype, [&](auto type) {
-        by_whole(p.D, [&](auto whole) {
+        by_width<true>(p.D, [&](auto whole) {
             using T = decltype(type);
-            constexpr bool kWhole = decltype(whole)::value;
-            k_embed_rows<T, kWhole><<<grid_of(rows.units + pieces.units), kThreads, 0, stream>>>(
+            constexpr Width kWidth = decltype(whole)::value;
+            k_embed_rows<T, kWidth><<<grid_of(rows.units + pieces.units), kThreads, 0, stream>>>(
                 p, rows, pieces, starts, keys[now], order[now], partials);
             if (plan.pieces == 0) return;
             const int parts = (p.D + 511) / 512;
             const int64_t units = ((int64_t)plan.pieces + kJoinPieces - 1) / kJoinPieces * parts;
-            k_embed_join<T, kWhole><<<(int)std::min<int64_t>(units, 1 << 16), kJoinWaves * 64, 0, stream>>>(
+            k_embed_join<T, kWidth><<<(int)std::min<int64_t>(units, 1 << 16), kJoinWaves * 64, 0, stream>>>(
                 p, parts, units, starts, keys[now], order[now], partials);
         });
     });

@@ -26,7 +26,7 @@ constexpr int threads_of(int lanes) { return lanes == 64 ? kThreads : lanes; }
 
 constexpr int kDropoutChunks = 4;  // of eight values, that a lane takes of a row
 
-template <typename T, bool Whole>
+template <typename T, Width W>
 __global__ __launch_bounds__(kThreads) void k_dropout(DropoutParams p, int lanes_log2, uint32_t pieces, uint32_t units)
 {
     using Store = typename T::Store;
@@ -44,16 +44,16 @@ __global__ __launch_bounds__(kThreads) void k_dropout(DropoutParams p, int lanes
 #pragma unroll
         for (int k = 0; k < kDropoutChunks; ++k) {
             const int c = first + k * lanes;
-            if (c < chunks) v[k] = raw_at<T, Whole>(x, c, p.D);
+            if (c < chunks) v[k] = raw_at<T, W>(x, c, p.D);
         }
 #pragma unroll
         for (int k = 0; k < kDropoutChunks; ++k) {
             const int c = first + k * lanes;
             if (c >= chunks) continue;
             float f[8];
-            unpack_at<T, Whole>(v[k], c, p.D, f);
+            unpack_at<T, W>(v[k], c, p.D, f);
             if (drop.threshold > 0) drop.apply((uint32_t)row, (uint32_t)c, f);
-            store_at<T, Whole>(y, c, p.D, f, p.once);
+            store_at<T, W>(y, c, p.D, f, p.once);
         }
     }
 }
@@ -88,16 +88,16 @@ __device__ __forceinline__ int64_t offset_of(uint32_t row, int T, int64_t stride
     return (int64_t)(row / (uint32_t)T) * stride_b + (int64_t)(row % (uint32_t)T) * stride_t;
 }
 
-template <typename T, bool Whole>
+template <typename T, Width W>
 __device__ __forceinline__ void load_weight(const void* w, bool f32, int c, int D, float* f)
 {
     if (!w) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) f[i] = 1.f;
     } else if (f32) {
-        load_at<F32, Whole>(static_cast<const float*>(w), c, D, f);
+        load_at<F32, W>(static_cast<const float*>(w), c, D, f);
     } else {
-        load_at<T, Whole>(static_cast<const typename T::Store*>(w), c, D, f);
+        load_at<T, W>(static_cast<const typename T::Store*>(w), c, D, f);
     }
 }
 
@@ -143,7 +143,7 @@ __device__ __forceinline__ uint32_t magnitude(float y) { return __float_as_uint(
 // G lanes take a row, N chunks of eight values each, which stay in registers; N == 0: any number of
 // chunks, read again for each pass over the row. Bound by HBM: 16,384 rows of 8,192 bf16, two arrays read and two written, 187
 // us, 5.7 TB/s, what a copy takes.
-template <typename T, bool Whole, int G, int N>
+template <typename T, Width W, int G, int N>
 __global__ __launch_bounds__(threads_of(G)) void k_norm(NormParams p, SeqLengths lens)
 {
     using Store = typename T::Store;
@@ -166,8 +166,8 @@ __global__ __launch_bounds__(threads_of(G)) void k_norm(NormParams p, SeqLengths
 #pragma unroll
             for (int i = 0; i < 8; ++i) h[0][i] = 0.f;
             for (int c = lane; c < chunks; c += G) {
-                if (sum) store_at<T, Whole>(sum, c, p.D, h[0], p.once);
-                if (y) store_at<T, Whole>(y, c, p.D, h[0], p.once);
+                if (sum) store_at<T, W>(sum, c, p.D, h[0], p.once);
+                if (y) store_at<T, W>(y, c, p.D, h[0], p.once);
                 if (q) store_bytes(q + c * 8, p.D - c * 8, h[0]);
             }
             if (lane == 0) {
@@ -178,8 +178,8 @@ __global__ __launch_bounds__(threads_of(G)) void k_norm(NormParams p, SeqLengths
         }
         const auto add_up = [&](int c, const Raw<T>& a, const Raw<T>& b, float* f) {
             float r[8];
-            unpack_at<T, Whole>(a, c, p.D, f);
-            if (res) unpack_at<T, Whole>(b, c, p.D, r);
+            unpack_at<T, W>(a, c, p.D, f);
+            if (res) unpack_at<T, W>(b, c, p.D, r);
             if (drop.threshold > 0) drop.apply((uint32_t)(p.row + row), (uint32_t)c, f);
 #pragma unroll
             for (int i = 0; i < 8; ++i) f[i] = rounded<T>(res ? f[i] + r[i] : f[i]);
@@ -192,22 +192,22 @@ __global__ __launch_bounds__(threads_of(G)) void k_norm(NormParams p, SeqLengths
                 const int c = lane + k * G;
                 a[k] = b[k] = no_values<T>();
                 if (c < chunks) {
-                    a[k] = raw_at<T, Whole>(x, c, p.D);
-                    if (res) b[k] = raw_at<T, Whole>(res, c, p.D);
+                    a[k] = raw_at<T, W>(x, c, p.D);
+                    if (res) b[k] = raw_at<T, W>(res, c, p.D);
                 }
             }
 #pragma unroll
             for (int k = 0; k < kHeld; ++k) {
                 const int c = lane + k * G;
                 add_up(c, a[k], b[k], h[k]);
-                if (c < chunks && sum) store_at<T, Whole>(sum, c, p.D, h[k], p.once);
+                if (c < chunks && sum) store_at<T, W>(sum, c, p.D, h[k], p.once);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) s = fmaf(h[k][i], h[k][i], s);
             }
         } else {
             for (int c = lane; c < chunks; c += G) {
-                add_up(c, raw_at<T, Whole>(x, c, p.D), res ? raw_at<T, Whole>(res, c, p.D) : no_values<T>(), h[0]);
-                if (sum) store_at<T, Whole>(sum, c, p.D, h[0], p.once);
+                add_up(c, raw_at<T, W>(x, c, p.D), res ? raw_at<T, W>(res, c, p.D) : no_values<T>(), h[0]);
+                if (sum) store_at<T, W>(sum, c, p.D, h[0], p.once);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) s = fmaf(h[0][i], h[0][i], s);
             }
@@ -215,7 +215,8 @@ __global__ __launch_bounds__(threads_of(G)) void k_norm(NormParams p, SeqLengths
         if (G > 64) __syncthreads();  // (the row before has read `parts`)
         s = over_row<G, false>(s, parts[0]);
         float rstd = 1.f / sqrtf(s / (float)p.D + p.eps);
-        if (__builtin_expect(!(s < INFINITY), 0)) {  // squares beyond fp32, unless there is an infinity or a NaN: taken again of smaller values
+        // squares beyond fp32, unless there is an infinity or a NaN: taken again of smaller values
+        if (__builtin_expect(!(s < INFINITY), 0)) {
             s = 0.f;
             if (N > 0) {
 #pragma unroll
@@ -224,7 +225,7 @@ __global__ __launch_bounds__(threads_of(G)) void k_norm(NormParams p, SeqLengths
                     for (int i = 0; i < 8; ++i) s = fmaf(h[k][i] * kSmaller, h[k][i] * kSmaller, s);
             } else {
                 for (int c = lane; c < chunks; c += G) {
-                    load_at<T, Whole>(sum ? sum : x, c, p.D, h[0]);
+                    load_at<T, W>(sum ? sum : x, c, p.D, h[0]);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) s = fmaf(h[0][i] * kSmaller, h[0][i] * kSmaller, s);
                 }
@@ -237,8 +238,8 @@ __global__ __launch_bounds__(threads_of(G)) void k_norm(NormParams p, SeqLengths
         // (what a lane has written itself is read again: from `sum`, or from x where nothing was added)
         const auto scaled = [&](int c, int k, float* f) {
             float w[8];
-            load_weight<T, Whole>(p.weight, p.weight_f32, c, p.D, w);
-            if (N == 0) load_at<T, Whole>(sum ? sum : x, c, p.D, h[0]);
+            load_weight<T, W>(p.weight, p.weight_f32, c, p.D, w);
+            if (N == 0) load_at<T, W>(sum ? sum : x, c, p.D, h[0]);
 #pragma unroll
             for (int i = 0; i < 8; ++i) f[i] = h[N > 0 ? k : 0][i] * rstd * w[i];
         };
@@ -250,7 +251,7 @@ __global__ __launch_bounds__(threads_of(G)) void k_norm(NormParams p, SeqLengths
                 if (c >= chunks) continue;
                 float f[8];
                 scaled(c, k, f);
-                if (y) store_at<T, Whole>(y, c, p.D, f, p.once);
+                if (y) store_at<T, W>(y, c, p.D, f, p.once);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     top = max(top, magnitude(f[i]));
@@ -261,7 +262,7 @@ __global__ __launch_bounds__(threads_of(G)) void k_norm(NormParams p, SeqLengths
             for (int c = lane; c < chunks; c += G) {
                 float f[8];
                 scaled(c, 0, f);
-                if (y) store_at<T, Whole>(y, c, p.D, f, p.once);
+                if (y) store_at<T, W>(y, c, p.D, f, p.once);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) top = max(top, magnitude(f[i]));
             }
@@ -306,7 +307,7 @@ __device__ __forceinline__ void hide(Raw<T>& v)
 // The same lanes and chunks; a workgroup adds its rows' share of the weight's gradient up, and leaves it as a
 // row of partial sums. Bound by HBM: 16,384 rows of 8,192 bf16, three arrays read and two written, 242 to 269 us, 5.0 to 5.5 TB/s
 // (435 without the rows asked for ahead).
-template <typename T, bool Whole, int G, int N>
+template <typename T, Width W, int G, int N>
 __global__ __launch_bounds__(threads_of(G)) void k_norm_grad(NormGradParams p, SeqLengths lens)
 {
     using Store = typename T::Store;
@@ -323,7 +324,7 @@ __global__ __launch_bounds__(threads_of(G)) void k_norm_grad(NormGradParams p, S
         for (int i = 0; i < 8; ++i) dw[k][i] = 0.f;
     float* partial = p.partials ? p.partials + (int64_t)blockIdx.x * p.D : nullptr;
     if (N == 0 && partial && !p.add)
-        for (int c = lane; c < chunks; c += G) store_at<F32, Whole>(partial, c, p.D, dw[0]);
+        for (int c = lane; c < chunks; c += G) store_at<F32, W>(partial, c, p.D, dw[0]);
     const uint32_t stride = gridDim.x * kRows;
     const auto row_of = [&](uint32_t row) {
         return static_cast<const Store*>(p.h) + offset_of(row, p.T, p.stride_b, p.stride_t);
@@ -343,15 +344,15 @@ __global__ __launch_bounds__(threads_of(G)) void k_norm_grad(NormGradParams p, S
             const int c = lane + k * G;
             h_next[k] = y_next[k] = no_values<T>();
             if (c >= chunks) continue;
-            h_next[k] = raw_at<T, Whole>(hr, c, p.D);
-            if (p.grad_y) y_next[k] = raw_at<T, Whole>(dy_of(row), c, p.D);
+            h_next[k] = raw_at<T, W>(hr, c, p.D);
+            if (p.grad_y) y_next[k] = raw_at<T, W>(dy_of(row), c, p.D);
         }
     };
     float w[kHeld][8];
     if (kAhead) {
 #pragma unroll
         for (int k = 0; k < kHeld; ++k)
-            load_weight<T, Whole>(p.weight, p.weight_f32, min(lane + k * G, chunks - 1), p.D, w[k]);
+            load_weight<T, W>(p.weight, p.weight_f32, min(lane + k * G, chunks - 1), p.D, w[k]);
         ask(blockIdx.x * kRows + sub);
     }
     for (uint32_t row = blockIdx.x * kRows + sub; row < rows; row += stride) {
@@ -360,17 +361,17 @@ __global__ __launch_bounds__(threads_of(G)) void k_norm_grad(NormGradParams p, S
         Store* dx = p.grad_x ? static_cast<Store*>(p.grad_x) + at : nullptr;
         Store* dres = p.grad_residual ? static_cast<Store*>(p.grad_residual) + at : nullptr;
         const auto write = [&](int c, float* f) {
-            if (dres) store_at<T, Whole>(dres, c, p.D, f, p.once);
+            if (dres) store_at<T, W>(dres, c, p.D, f, p.once);
             if (dx) {
                 if (drop.threshold > 0) drop.apply((uint32_t)(p.row + row), (uint32_t)c, f);
-                store_at<T, Whole>(dx, c, p.D, f, p.once);
+                store_at<T, W>(dx, c, p.D, f, p.once);
             }
         };
         if (!inside(lens, row, p.T)) {
             float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
             for (int c = lane; c < chunks; c += G) {
-                if (dres) store_at<T, Whole>(dres, c, p.D, zero, p.once);
-                if (dx) store_at<T, Whole>(dx, c, p.D, zero, p.once);
+                if (dres) store_at<T, W>(dres, c, p.D, zero, p.once);
+                if (dx) store_at<T, W>(dx, c, p.D, zero, p.once);
             }
             if (kAhead) ask(row + stride);
             continue;
@@ -379,8 +380,8 @@ __global__ __launch_bounds__(threads_of(G)) void k_norm_grad(NormGradParams p, S
         const float rstd = N > 0 ? rstd_next : p.rstd[row];
         // n = h rstd and w dy of a chunk
         const auto take = [&](int c, const Raw<T>& a, const Raw<T>& b, const float* w, float* n, float* g, float* dw) {
-            unpack_at<T, Whole>(a, c, p.D, n);
-            unpack_at<T, Whole>(b, c, p.D, g);
+            unpack_at<T, W>(a, c, p.D, n);
+            unpack_at<T, W>(b, c, p.D, g);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 n[i] *= rstd;
@@ -398,12 +399,12 @@ __global__ __launch_bounds__(threads_of(G)) void k_norm_grad(NormGradParams p, S
                 a[k] = h_next[k];
                 b[k] = y_next[k];
                 d[k] = no_values<T>();
-                if (c < chunks && dsum) d[k] = raw_at<T, Whole>(dsum, c, p.D);
+                if (c < chunks && dsum) d[k] = raw_at<T, W>(dsum, c, p.D);
             }
             if (kAhead) ask(row + stride);
 #pragma unroll
             for (int k = 0; k < kHeld; ++k) {
-                if (!kAhead) load_weight<T, Whole>(p.weight, p.weight_f32, min(lane + k * G, chunks - 1), p.D, w[k]);
+                if (!kAhead) load_weight<T, W>(p.weight, p.weight_f32, min(lane + k * G, chunks - 1), p.D, w[k]);
                 take(lane + k * G, a[k], b[k], w[k], n, g, dw[k]);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) s = fmaf(g[i], n[i], s);
@@ -411,11 +412,11 @@ __global__ __launch_bounds__(threads_of(G)) void k_norm_grad(NormGradParams p, S
         } else {
             for (int c = lane; c < chunks; c += G) {
                 float add[8];
-                if (partial) load_at<F32, Whole>(partial, c, p.D, add);
-                load_weight<T, Whole>(p.weight, p.weight_f32, c, p.D, w[0]);
-                take(c, raw_at<T, Whole>(row_of(row), c, p.D),
-                     p.grad_y ? raw_at<T, Whole>(dy_of(row), c, p.D) : no_values<T>(), w[0], n, g, partial ? add : nullptr);
-                if (partial) store_at<F32, Whole>(partial, c, p.D, add);
+                if (partial) load_at<F32, W>(partial, c, p.D, add);
+                load_weight<T, W>(p.weight, p.weight_f32, c, p.D, w[0]);
+                take(c, raw_at<T, W>(row_of(row), c, p.D),
+                     p.grad_y ? raw_at<T, W>(dy_of(row), c, p.D) : no_values<T>(), w[0], n, g, partial ? add : nullptr);
+                if (partial) store_at<F32, W>(partial, c, p.D, add);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) s = fmaf(g[i], n[i], s);
             }
@@ -424,7 +425,7 @@ __global__ __launch_bounds__(threads_of(G)) void k_norm_grad(NormGradParams p, S
         s = over_row<G, false>(s, parts) / (float)p.D;
         const auto finish = [&](int c, const Raw<T>& d) {
             float f[8];
-            unpack_at<T, Whole>(d, c, p.D, f);
+            unpack_at<T, W>(d, c, p.D, f);
 #pragma unroll
             for (int i = 0; i < 8; ++i) f[i] += rstd * (g[i] - n[i] * s);
             write(c, f);
@@ -434,20 +435,20 @@ __global__ __launch_bounds__(threads_of(G)) void k_norm_grad(NormGradParams p, S
             for (int k = 0; k < kHeld; ++k) {
                 const int c = lane + k * G;
                 if (c >= chunks) continue;
-                if (!kAhead || !Whole) {
+                if (!kAhead || W != kWhole) {
                     hide(a[k]);
                     hide(b[k]);
                 }
-                if (!kAhead) load_weight<T, Whole>(p.weight, p.weight_f32, c, p.D, w[k]);
+                if (!kAhead) load_weight<T, W>(p.weight, p.weight_f32, c, p.D, w[k]);
                 take(c, a[k], b[k], w[k], n, g, nullptr);
                 finish(c, d[k]);
             }
         } else {
             for (int c = lane; c < chunks; c += G) {
-                load_weight<T, Whole>(p.weight, p.weight_f32, c, p.D, w[0]);
-                take(c, raw_at<T, Whole>(row_of(row), c, p.D),
-                     p.grad_y ? raw_at<T, Whole>(dy_of(row), c, p.D) : no_values<T>(), w[0], n, g, nullptr);
-                finish(c, dsum ? raw_at<T, Whole>(dsum, c, p.D) : no_values<T>());
+                load_weight<T, W>(p.weight, p.weight_f32, c, p.D, w[0]);
+                take(c, raw_at<T, W>(row_of(row), c, p.D),
+                     p.grad_y ? raw_at<T, W>(dy_of(row), c, p.D) : no_values<T>(), w[0], n, g, nullptr);
+                finish(c, dsum ? raw_at<T, W>(dsum, c, p.D) : no_values<T>());
             }
         }
     }
@@ -468,11 +469,11 @@ __global__ __launch_bounds__(threads_of(G)) void k_norm_grad(NormGradParams p, S
         if (c >= chunks) continue;
         if (p.add) {
             float old[8];
-            load_at<F32, Whole>(partial, c, p.D, old);
+            load_at<F32, W>(partial, c, p.D, old);
 #pragma unroll
             for (int i = 0; i < 8; ++i) dw[k][i] += old[i];
         }
-        store_at<F32, Whole>(partial, c, p.D, dw[k]);
+        store_at<F32, W>(partial, c, p.D, dw[k]);
     }
 }
 
@@ -509,12 +510,13 @@ struct Shape {
     static constexpr int G = G_, N = N_;
 };
 
-// Lanes and chunks of a row, forward (us of fp32 / bf16, dropout 0.1, replayed; 32,000 rows of 640 and 1,024, 16,000 of the
-// others): 640: 64 x 2 67 / 33, 128 x 1 67 / 38. 1,500: 128 x 2 80 / 46, 64 x 4 85 / 45, 256 x 1 78 / 55. 2,496: 192 x 2
-// 118 / 71, 256 x 2 118 / 81, 128 x 4 121 / 77. 4,096: 256 x 2 194 / 101, 128 x 4 196 / 103. 8,192: 256 x 4 380 / 192,
-// 512 x 2 376 / 198, 1024 x 1 394 / 245. Few rows leave most of the chip idle, and each is spread over more lanes (256 rows of
-// bf16): 640: 256 x 1 3.1, 64 x 2 3.5. 2,048: 256 x 1 3.2, 128 x 2 3.8. 4,096: 512 x 1 3.9, 256 x 2 4.2. 8,192: 512 x 2 5.2,
-// 256 x 4 6.0; 1,024 rows of 640: 4.3 and 4.0, of 4,096: 7.5 and 7.3.
+// Lanes and chunks of a row, forward (us of fp32 / bf16, dropout 0.1, replayed; 32,000 rows of 640, 20,000 of 1,500, 8,000 of
+// 8,192, 6,000 of 16,384, 16,000 of the others): 640: 64 x 2 65 / 32, 128 x 1 69 / 42. 1,500: 128 x 2 100 / 53, 256 x 1 95 / 58.
+// 2,048: 128 x 2 102 / 43, 256 x 1 99 / 45. 2,500: 192 x 2 129 / 68, 256 x 2 130 / 94. 4,096: 256 x 2 192 / 103, 512 x 1 185 /
+// 105. 5,003: 256 x 4 242 / 170, 512 x 2 263 / 201. 8,192: 256 x 4 193 / 106, 512 x 2 190 / 104, 1024 x 1 192 / 126. 16,384: 1024
+// x 2 290 / 155, chunks read again 319 / 202. Few rows leave most of the chip idle, and each is spread over more lanes (256 rows
+// of bf16): 640: 256 x 1 3.8, 64 x 2 4.5. 2,048: 256 x 1 4.0, 128 x 2 4.6. 4,096: 512 x 1 4.6, 256 x 2 5.0. 8,192: 512 x 2 6.3,
+// 256 x 4 7.1; 1,024 rows of 640: 5.4 and 4.7, of 4,096: 8.9 and 8.7.
 constexpr int kFewRows = 512;
 template <typename F>
 void by_shape(int64_t rows, int D, F&& f)
@@ -533,10 +535,11 @@ void by_shape(int64_t rows, int D, F&& f)
     else f(Shape<1024, 0>{});
 }
 
-// ... and backward, with the workgroups that go round the rows, as many as the registers leave place for (the same rows): 640:
-// 64 x 2 768 84 / 37, 1,024 90 / 45, 128 x 1 2,048 86 / 54. 2,048: 256 x 1 1,024 128 / 64, 128 x 2 1,024 128 / 69. 4,096:
-// 512 x 1 512 240 / 125, 256 x 2 512 239 / 131. 8,192: 512 x 2 256 505 / 238, 512 496 / 246, 1024 x 1 496 / 244. 16,384 (8,000
-// rows): 1024 x 2 698 / 399, chunks read again 731 / 468.
+// ... and backward, with the workgroups that go round the rows, as many as the registers leave place for (the same rows, 60,000 of
+// 500): 500: 64 x 1 1,024 127 / 63, 2,048 130 / 74. 640: 64 x 2 768 84 / 38, 1,024 88 / 44, 128 x 1 2,048 87 / 41. 2,048: 256 x 1
+// 1,024 128 / 65, 128 x 2 1,024 128 / 67. 2,500: 512 x 1 512 156 / 109, 256 x 2 512 157 / 129, 192 x 2 768 188 / 100. 4,096: 512 x
+// 1 512 243 / 128, 256 x 2 512 240 / 124. 4,100: 640 x 1 256 248 / 198, 512 x 2 256 261 / 224; 5,003: 298 / 230 and 295 / 240.
+// 8,192: 512 x 2 256 256 / 126, 512 254 / 134, 1024 x 1 250 / 126. 16,384: 1024 x 2 420 / 282, chunks read again 536 / 344.
 template <int G_, int N_, int Blocks_>
 struct Rounds : Shape<G_, N_> {
     static constexpr int kBlocks = Blocks_;
@@ -549,6 +552,7 @@ void by_rounds(int D, F&& f)
     else if (chunks <= 128) f(Rounds<64, 2, 768>{});
     else if (chunks <= 256) f(Rounds<256, 1, 1024>{});
     else if (chunks <= 512) f(Rounds<512, 1, 512>{});
+    else if (chunks <= 640) f(Rounds<640, 1, 256>{});
     else if (chunks <= 1024) f(Rounds<512, 2, 256>{});
     else if (chunks <= 2048) f(Rounds<1024, 2, 256>{});
     else f(Rounds<1024, 0, 256>{});
@@ -567,7 +571,7 @@ hipError_t launch_dropout(const DropoutParams& p, int dtype, hipStream_t stream)
     if (units > UINT32_MAX - (1 << 20)) return hipErrorInvalidValue;
     const int grid = (int)std::min<int64_t>(units, 1 << 20);
     by_type(dtype, [&](auto t) {
-        by_whole(p.D, [&](auto whole) {
+        by_width<true>(p.D, [&](auto whole) {
             k_dropout<decltype(t), decltype(whole)::value>
                 <<<grid, kThreads, 0, stream>>>(p, lanes_log2, (uint32_t)pieces, (uint32_t)units);
         });
@@ -582,7 +586,7 @@ hipError_t launch_norm(const NormParams& p, const SeqLengths& lens, int dtype, h
         by_shape(rows, p.D, [&](auto s) {
             constexpr int G = decltype(s)::G, N = decltype(s)::N, kRows = threads_of(G) / G;
             const int grid = (int)std::min<int64_t>((rows + kRows - 1) / kRows, 1 << 20);
-            by_whole(p.D, [&](auto whole) {
+            by_width<G == 64 && N == 1>(p.D, [&](auto whole) {
                 k_norm<decltype(t), decltype(whole)::value, G, N><<<grid, threads_of(G), 0, stream>>>(p, lens);
             });
         });
@@ -605,7 +609,7 @@ hipError_t launch_norm_grad(const NormGradParams& p, const SeqLengths& lens, int
     by_type(dtype, [&](auto t) {
         by_rounds(p.D, [&](auto s) {
             constexpr int G = decltype(s)::G, N = decltype(s)::N;
-            by_whole(p.D, [&](auto whole) {
+            by_width<G == 64 && N == 1>(p.D, [&](auto whole) {
                 k_norm_grad<decltype(t), decltype(whole)::value, G, N><<<p.blocks, threads_of(G), 0, stream>>>(p, lens);
             });
         });

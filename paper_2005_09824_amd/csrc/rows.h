@@ -43,14 +43,16 @@ __device__ __forceinline__ Raw<T> raw_short(const typename T::Store* p, int D)
     return v;
 }
 
-// Chunk c of a row of D values: columns 8 c and on. Whole: eight divides D. Otherwise the last chunk is read as the
-// row's last eight values, and moved to its place when it is unpacked: a path of its own for it would be waited for
-// where it ends (2,500 columns of bf16, 16,000 rows, forward: 101 us that way, 83 this way; 78 for 2,504).
-template <typename T, bool Whole>
+// Chunk c of a row of D values: columns 8 c and on. kWhole: eight divides D. kAny: otherwise, the last chunk is read as the
+// row's last eight values, and moved to its place when it is unpacked. kShort: fewer than eight values. A branch around a load
+// is waited for where it ends: a path of its own for the last chunk made 101 us of 83 (2,500 columns of bf16, 16,000 rows,
+// forward), a look at D for short rows 152 of 146 (8,190 columns, 8,000 rows, backward).
+enum Width { kAny, kWhole, kShort };
+template <typename T, Width W>
 __device__ __forceinline__ Raw<T> raw_at(const typename T::Store* row, int c, int D)
 {
-    if (!Whole && D < 8) return raw_short<T>(row, D);
-    const typename T::Store* p = row + (Whole ? c * 8 : min(c * 8, D - 8));
+    if (W == kShort) return raw_short<T>(row, D);
+    const typename T::Store* p = row + (W == kWhole ? c * 8 : min(c * 8, D - 8));
     Raw<T> v;
 #pragma unroll
     for (int k = 0; k < 8 / T::kVec; ++k) v.r[k] = load16(p + k * T::kVec);
@@ -62,24 +64,24 @@ __device__ __forceinline__ void move_down(float* f)
 #pragma unroll
     for (int i = 0; i < 8; ++i) f[i] = i + By < 8 ? f[i + By < 8 ? i + By : 0] : 0.f;
 }
-template <typename T, bool Whole>
+template <typename T, Width W>
 __device__ __forceinline__ void unpack_at(const Raw<T>& v, int c, int D, float* f)
 {
     v.unpack(f);
-    if (Whole || c * 8 + 8 <= D || D < 8) return;
+    if (W != kAny || c * 8 + 8 <= D) return;
     const int by = 8 - (D & 7);
     if (by & 4) move_down<4>(f);
     if (by & 2) move_down<2>(f);
     if (by & 1) move_down<1>(f);
 }
-template <typename T, bool Whole>
+template <typename T, Width W>
 __device__ __forceinline__ void load_at(const typename T::Store* row, int c, int D, float* f)
 {
-    unpack_at<T, Whole>(raw_at<T, Whole>(row, c, D), c, D, f);
+    unpack_at<T, W>(raw_at<T, W>(row, c, D), c, D, f);
 }
 // (the values of a last chunk four, two and one at a time; once: past the caches, the same for all lanes. Eight values of 32 bits
 // are two stores that each fill halves of lines, which the caches have to put together: 16,000 rows of 4,096 so 258 us, 194.)
-template <typename T, bool Whole>
+template <typename T, Width W>
 __device__ __forceinline__ void store_at(typename T::Store* row, int c, int D, const float* f, bool once = false)
 {
     typename T::Store* p = row + c * 8;
@@ -87,7 +89,7 @@ __device__ __forceinline__ void store_at(typename T::Store* row, int c, int D, c
     uint4 r[8 / T::kVec];
 #pragma unroll
     for (int k = 0; k < 8 / T::kVec; ++k) r[k] = T::pack(f + k * T::kVec);
-    if (Whole || left >= 8) {
+    if (W == kWhole || left >= 8) {
 #pragma unroll
         for (int k = 0; k < 8 / T::kVec; ++k) {
             if (once && T::kVec == 8) {
@@ -115,12 +117,13 @@ __device__ __forceinline__ void store_at(typename T::Store* row, int c, int D, c
     }
 }
 
-// Calls f(std::true_type or std::false_type): whether eight divides D.
-template <typename F>
-void by_whole(int D, F&& f)
+// Calls f with the kind of a width, as a type; kShort where rows of fewer than eight values come here at all.
+template <bool Short, typename F>
+void by_width(int D, F&& f)
 {
-    if (D % 8 == 0) f(std::true_type{});
-    else f(std::false_type{});
+    if (D % 8 == 0) f(std::integral_constant<Width, kWhole>{});
+    else if (Short && D < 8) f(std::integral_constant<Width, Short ? kShort : kAny>{});
+    else f(std::integral_constant<Width, kAny>{});
 }
 template <typename F>
 void by_type(int dtype, F&& f)

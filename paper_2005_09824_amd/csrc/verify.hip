@@ -163,15 +163,23 @@ struct Weights {
 template <typename T, int Threads, int Chunks>
 __device__ __forceinline__ void load_part(const typename T::Store* x, int first, int V, float (*f)[8])
 {
+    if (V < 8) {
+#pragma unroll
+        for (int k = 0; k < Chunks; ++k)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f[k][j] = k == 0 && first == 0 && j < V ? T::load(x + j) : -INFINITY;
+        return;
+    }
     const int last = (V - 1) / 8;
     Raw<T> v[Chunks];
 #pragma unroll
-    for (int k = 0; k < Chunks; ++k) v[k] = raw_at<T, false>(x, min(first + k * Threads, last), V);
+    for (int k = 0; k < Chunks; ++k) v[k] = raw_at<T, kAny>(x, min(first + k * Threads, last), V);
 #pragma unroll
     for (int k = 0; k < Chunks; ++k) {
         const int c = first + k * Threads;
-        unpack_at<T, false>(v[k], min(c, last), V, f[k]);
+        v[k].unpack(f[k]);
         if (c < last) continue;
+        if (V % 8) unpack_at<T, kAny>(v[k], last, V, f[k]);
 #pragma unroll
         for (int j = 0; j < 8; ++j)
             if (c * 8 + j >= V) f[k][j] = -INFINITY;
