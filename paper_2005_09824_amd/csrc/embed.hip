@@ -24,6 +24,14 @@ __device__ __forceinline__ bool inside(const SeqLengths& lens, uint32_t row, int
     return lens.n == 0 || (int)(row % (uint32_t)T) < lens.T[row / (uint32_t)T];
 }
 
+template <bool Wave>
+__device__ __forceinline__ uint32_t of_wave(uint32_t v) { return Wave ? (uint32_t)__builtin_amdgcn_readfirstlane((int)v) : v; }
+template <bool Wave>
+__device__ __forceinline__ int64_t of_wave(int64_t v)
+{
+    return (int64_t)((uint64_t)of_wave<Wave>((uint32_t)((uint64_t)v >> 32)) << 32 | of_wave<Wave>((uint32_t)v));
+}
+
 // Workgroups take pieces of groups of rows: 2^lanes_log2 lanes a row, one chunk of eight values each, and `rows` rows that
 // follow each other by the same lanes.
 struct Tiles {
@@ -45,29 +53,38 @@ struct Place {
     int64_t group;
     int c;
 };
+template <bool Wave>
 __device__ __forceinline__ Place place_of(const Tiles& t, int64_t unit)
 {
-    const int64_t g = unit / t.pieces;
-    return {(g << (8 - t.lanes_log2)) + (threadIdx.x >> t.lanes_log2),
+    const int64_t g = t.pieces == 1 ? unit : unit / t.pieces;
+    return {(g << (8 - t.lanes_log2)) + of_wave<Wave>(threadIdx.x >> t.lanes_log2),
             ((int)(unit - g * t.pieces) << t.lanes_log2) + ((int)threadIdx.x & ((1 << t.lanes_log2) - 1))};
 }
 static_assert(kThreads == 1 << 8, "place_of");
+// Wave: a row has 64 lanes or more, so that what belongs to it is the same in all lanes of a wave, and is held and computed
+// once: a division for every row's sequence, the products of its place.
+template <typename F>
+void by_wave(const Tiles& t, F&& f)
+{
+    if (t.lanes_log2 >= 6) f(std::true_type{});
+    else f(std::false_type{});
+}
 int grid_of(int64_t units) { return (int)std::min<int64_t>(units, 1 << 20); }
 
 // ---- forward
 
 // Rows that a lane has on their way: a token, then its row, are two waits. Bound by HBM: 32,768 rows of 2,048 bf16 of a table of
-// 65,536, a third of them padding, 39 us (134 MB written, 65 MB of the table read; 55 us with one row a lane).
+// 65,536, a third of them padding, 32 us (134 MB written, 65 MB of the table read; 55 us with one row a lane, 39 with rows in vector registers).
 constexpr int kEmbedRows = 4;
 
-template <typename T, Width W, int Rows>
+template <typename T, Width W, int Rows, bool Wave>
 __global__ __launch_bounds__(kThreads) void k_embed(EmbedParams p, SeqLengths lens, Tiles tiles)
 {
     using Store = typename T::Store;
     const uint32_t rows = (uint32_t)p.B * (uint32_t)p.T;
     const int chunks = (p.D + 7) / 8;
     for (int64_t u = blockIdx.x; u < tiles.units; u += gridDim.x) {
-        const Place at = place_of(tiles, u);
+        const Place at = place_of<Wave>(tiles, u);
         if (at.c >= chunks) continue;
         const int64_t first = at.group * Rows;
         int64_t token[Rows];
@@ -76,6 +93,8 @@ __global__ __launch_bounds__(kThreads) void k_embed(EmbedParams p, SeqLengths le
         for (int k = 0; k < Rows; ++k)
             token[k] = first + k < rows && inside(lens, (uint32_t)(first + k), p.T)
                 ? token_at(p.tokens, p.token_bytes, (uint32_t)(first + k)) : -1;
+#pragma unroll
+        for (int k = 0; k < Rows; ++k) token[k] = of_wave<Wave>(token[k]);
 #pragma unroll
         for (int k = 0; k < Rows; ++k)
             if (token[k] >= 0 && token[k] < p.V)
@@ -170,10 +189,10 @@ __global__ __launch_bounds__(kSort) void k_embed_count(EmbedGradParams p, SeqLen
 }
 
 // Keys of a tile to their places. Every workgroup adds up for itself how many keys have a smaller digit, or the same in an
-// earlier tile.
+// earlier tile. starts: of the only pass, whose digits are the tokens, or null.
 __global__ __launch_bounds__(kSort) void k_embed_place(EmbedGradParams p, const uint32_t* keys, const uint32_t* order,
                                                        uint32_t N, int shift, const uint32_t* hist, uint32_t* keys_out,
-                                                       uint32_t* order_out)
+                                                       uint32_t* order_out, uint32_t* starts)
 {
     extern __shared__ uint32_t places[];  // [wave][digit]
     __shared__ uint32_t sums[kSortWaves];
@@ -208,6 +227,7 @@ __global__ __launch_bounds__(kSort) void k_embed_place(EmbedGradParams p, const 
     if (d < n) {
         uint32_t at = upto - all + before;
         for (int w = 0; w < wave; ++w) at += sums[w];
+        if (starts && d <= p.V && blockIdx.x == 0) starts[d] = at;  // (nothing lies before the first tile)
         for (int w = 0; w < kSortWaves; ++w) {
             const uint32_t count = places[w * n + d];
             places[w * n + d] = at;
@@ -337,14 +357,14 @@ __device__ __forceinline__ Raw<T> row_of(const EmbedGradParams& p, uint32_t pos,
 }
 
 // Adds the chunk of positions order[from..to - 1], in that order.
-template <typename T, Width W, int AtOnce>
+template <typename T, Width W, int AtOnce, bool Wave>
 __device__ __forceinline__ void add_rows(const EmbedGradParams& p, const uint32_t* order, uint32_t from, uint32_t to,
                                          int c, float* s)
 {
     for (uint32_t k = from; k < to; k += AtOnce) {
         Raw<T> v[AtOnce];
 #pragma unroll
-        for (int j = 0; j < AtOnce; ++j) v[j] = row_of<T, W>(p, order[min(k + j, to - 1)], c);
+        for (int j = 0; j < AtOnce; ++j) v[j] = row_of<T, W>(p, of_wave<Wave>(order[min(k + j, to - 1)]), c);
 #pragma unroll
         for (int j = 0; j < AtOnce; ++j) {
             if (k + j >= to) continue;
@@ -380,7 +400,7 @@ __device__ __forceinline__ Segment segment_of(uint32_t from, uint32_t to)
 
 // Such pieces, and the rows of the table that have none, those without a position among them. A lane has kGradRows rows of
 // the table, and asks for the first position's row of each before it waits for one. Bound by HBM and by three waits in a row (a
-// token's positions, a position, its row): 65,536 rows of 2,048 bf16 for 21,000 positions 82 us (268 MB written, 85 read), of which
+// token's positions, a position, its row): 65,536 rows of 2,048 bf16 for 21,000 positions 78 us (268 MB written, 85 read), of which
 // the writes alone take 42; eight rows a lane 5 us more, two 5 us more.
 constexpr int kGradRows = 4;
 template <typename T, Width W>
@@ -391,16 +411,16 @@ __global__ __launch_bounds__(kThreads) void k_embed_rows(EmbedGradParams p, Tile
     const uint32_t whole = (uint32_t)p.plan.pieces;
     for (int64_t u = blockIdx.x; u < pieces.units + rows.units; u += gridDim.x) {
         if (u < pieces.units) {
-            const Place at = place_of(pieces, u);
+            const Place at = place_of<false>(pieces, u);
             if (at.c >= chunks || at.group >= whole) continue;
             const uint32_t from = (uint32_t)at.group * kEmbedPiece, key = keys[from];
             if (key != keys[from + kEmbedPiece - 1] || key == (uint32_t)p.V) continue;
             float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-            add_rows<T, W, 8>(p, order, from, from + kEmbedPiece, at.c, s);
+            add_rows<T, W, 8, false>(p, order, from, from + kEmbedPiece, at.c, s);
             store_at<F32, W>(partials + at.group * p.D, at.c, p.D, s);
             continue;
         }
-        const Place at = place_of(rows, u - pieces.units);
+        const Place at = place_of<false>(rows, u - pieces.units);
         const int64_t v = at.group * kGradRows;
         if (at.c >= chunks || v >= p.V) continue;
         uint32_t begin[kGradRows + 1];
@@ -419,7 +439,7 @@ __global__ __launch_bounds__(kThreads) void k_embed_rows(EmbedGradParams p, Tile
             if (g.first < g.last || v + k >= p.V || (g.from == g.to && p.accumulate)) continue;
             float s[8];
             unpack_at<T, W>(first[k], at.c, p.D, s);
-            if (g.from + 1 < g.to) add_rows<T, W, 4>(p, order, g.from + 1, g.to, at.c, s);
+            if (g.from + 1 < g.to) add_rows<T, W, 4, false>(p, order, g.from + 1, g.to, at.c, s);
             write_grad<T, W>(p, v + k, at.c, s);
         }
     }
@@ -436,7 +456,7 @@ __global__ __launch_bounds__(kJoinWaves * 64) void k_embed_join(EmbedGradParams 
 {
     __shared__ float sums[kJoinWaves][64 * 8];
     constexpr int kEnds = kEmbedPiece / kJoinWaves;  // positions of a wave before the pieces, and behind
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, chunks = (p.D + 7) / 8;
+    const int lane = threadIdx.x & 63, wave = (int)of_wave<true>(threadIdx.x >> 6), chunks = (p.D + 7) / 8;
     for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
         const uint32_t group = (uint32_t)(u / parts);
         const int c = (int)(u - (int64_t)group * parts) * 64 + lane;
@@ -448,14 +468,14 @@ __global__ __launch_bounds__(kJoinWaves * 64) void k_embed_join(EmbedGradParams 
             if (v != keys[at + kEmbedPiece - 1] || (mine > 0 && v == keys[at - kEmbedPiece])) v = (uint32_t)p.V;
         }
         for (uint64_t some = __ballot(v < (uint32_t)p.V); some; some &= some - 1) {
-            const uint32_t token = __shfl(v, __ffsll((unsigned long long)some) - 1, 64);
-            const Segment g = segment_of(starts[token], starts[token + 1]);
+            const uint32_t token = (uint32_t)__builtin_amdgcn_readlane((int)v, __ffsll((unsigned long long)some) - 1);
+            const Segment g = segment_of(of_wave<true>(starts[token]), of_wave<true>(starts[token + 1]));
             const uint32_t n = g.last - g.first, each = (n + kJoinWaves - 1) / kJoinWaves, to = min(n, (wave + 1) * each);
             const float* part = partials + (int64_t)g.first * p.D;
             float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
             if (c < chunks) {
                 const uint32_t head = g.from + wave * kEnds, tail = g.last * kEmbedPiece + wave * kEnds;
-                add_rows<T, W, kEnds>(p, order, head, min(head + kEnds, g.first * kEmbedPiece), c, s);
+                add_rows<T, W, kEnds, true>(p, order, head, min(head + kEnds, g.first * kEmbedPiece), c, s);
                 for (uint32_t i = wave * each; i < to; i += 8) {
                     Raw<F32> f[8];
 #pragma unroll
@@ -470,7 +490,7 @@ __global__ __launch_bounds__(kJoinWaves * 64) void k_embed_join(EmbedGradParams 
                         for (int x = 0; x < 8; ++x) s[x] += e[x];
                     }
                 }
-                add_rows<T, W, kEnds>(p, order, tail, min(tail + kEnds, g.to), c, s);
+                add_rows<T, W, kEnds, true>(p, order, tail, min(tail + kEnds, g.to), c, s);
             }
 #pragma unroll
             for (int e = 0; e < 8; ++e) sums[wave][e * 64 + lane] = s[e];
@@ -505,8 +525,11 @@ hipError_t launch_embed(const EmbedParams& p, const SeqLengths& lens, int dtype,
         by_width<true>(p.D, [&](auto whole) {
             using Type = decltype(type);
             constexpr Width kWidth = decltype(whole)::value;
-            if (few) k_embed<Type, kWidth, 1><<<grid_of(t.units), kThreads, 0, stream>>>(p, lens, t);
-            else k_embed<Type, kWidth, kEmbedRows><<<grid_of(t.units), kThreads, 0, stream>>>(p, lens, t);
+            by_wave(t, [&](auto wave) {
+                constexpr bool kWave = decltype(wave)::value;
+                if (few) k_embed<Type, kWidth, 1, kWave><<<grid_of(t.units), kThreads, 0, stream>>>(p, lens, t);
+                else k_embed<Type, kWidth, kEmbedRows, kWave><<<grid_of(t.units), kThreads, 0, stream>>>(p, lens, t);
+            });
         });
     });
     return hipGetLastError();
@@ -569,9 +592,10 @@ hipError_t launch_embed_grad(const EmbedGradParams& p, const SeqLengths* lens, i
         else
             k_embed_count<false><<<plan.tiles, kSort, bins, stream>>>(p, SeqLengths{}, keys[now], N, shift, hist);
         k_embed_place<<<plan.tiles, kSort, bins * kSortWaves, stream>>>(p, keys[now], pass ? order[now] : nullptr, N, shift,
-                                                                        hist, keys[now ^ 1], order[now ^ 1]);
+                                                                        hist, keys[now ^ 1], order[now ^ 1],
+                                                                        plan.passes == 1 ? starts : nullptr);
     }
-    if (!few || p.V > kFewTokens) {
+    if (few ? p.V > kFewTokens : N == 0 || plan.passes > 1) {
         const int64_t v = ((int64_t)p.V + kThreads) / kThreads;
         k_embed_starts<<<(int)std::min<int64_t>(v, 2048), kThreads, 0, stream>>>(keys[now], N, p.V, starts);
     }
