@@ -231,7 +231,7 @@ __global__ __launch_bounds__(threads_of(G)) void k_norm(NormParams p, SeqLengths
                 }
             }
             s = over_row<G, false>(s, parts[1]);
-            rstd = kSmaller / sqrtf(s / (float)p.D);
+            rstd = kSmaller / sqrtf(s / (float)p.D + p.eps * kSmaller * kSmaller);
             if (G > 64) __syncthreads();
         }
         if (p.rstd && lane == 0) p.rstd[row] = rstd;

@@ -133,6 +133,11 @@ def test_refused_norms(kw, code, text):
     _refused(_norm(**kw), code, text)
 
 
+@pytest.mark.parametrize("eps", [0.9e-30, 1.1e30, 3e38])
+def test_eps_beyond_what_sums_of_squares_leave_room_for_is_refused(eps):
+    _refused(_norm(eps=eps), INVALID, "eps")
+
+
 def _norm_backward(lengths=None, **kw):
     a = dict(sum=P, stride_b=12, stride_t=4, dtype=0, B=2, T=3, D=4, weight=2 * P, wd=0, rstd=3 * P, dy=4 * P, ds=5 * P,
              p=0.1, seed=0, offset=0, step=None, dx=6 * P, dr=7 * P, dw=8 * P, ws=FAR, size=1 << 20)
