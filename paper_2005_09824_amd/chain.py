@@ -3,6 +3,11 @@ what a training step uses beside it: log probabilities of given tokens, clipping
 gradients to a norm, and in front of the output layer token embeddings, dropout and the end
 of a residual block.
 
+All of them may be captured into a HIP graph, backward passes too (torch.autograd.grad, or leaves whose
+gradients were never accumulated outside). Before a capture let every eager autograd graph of the same
+leaves go: torch ties a leaf's accumulation of gradients to the stream that it first ran on, and a captured
+backward pass that meets such a node can end the process.
+
 Argument marshalling only: both forward-backward passes, the objective and its
 gradient with respect to the logits all come out of lfmmi_loss; this
 file stores that gradient for backward() and scales it by the incoming gradient.

@@ -382,6 +382,78 @@ def test_a_training_step():
     assert abs(float(chain.clip_grad_norm(ours, 0.1)) - total) < 1e-4 * total
 
 
+def test_a_captured_training_step():
+    # forward and backward through autograd in one graph, a step on the device that moves the masks; every replay against
+    # the eager step of the same number. The warm-up's graphs are gone before the capture begins
+    torch = _torch()
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    V, D, B, T = 90, 72, 3, 20
+    lengths = [20, 0, 11]
+    leaves = [torch.randn((V, D), generator=gen, device="cuda").mul_(0.3).requires_grad_(),
+              torch.ones(D, device="cuda").requires_grad_()]
+    tokens = torch.randint(-1, V, (B, T), generator=gen, device="cuda")
+    targets = torch.randint(0, V, (B, T), generator=gen, device="cuda")
+    grad = torch.randn((B, T), generator=gen, device="cuda")
+    number = torch.zeros(1, dtype=torch.int64, device="cuda")
+
+    def step(at):
+        table, weight = leaves
+        h, _status = chain.embed_tokens(table, tokens, lengths, 2.0)
+        y, h = chain.add_rms_norm(chain.dropout(h, 0.2, 5, 1 << 40, at), h, weight, 1e-5, lengths, 0.3, 5, 0, at)
+        logp, _entropy, _status = chain.token_logprobs((y + h) @ table.t(), targets, lengths)
+        return [logp.detach()] + list(torch.autograd.grad(logp, leaves, grad))
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for _ in range(2):
+            step(number)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step(number)
+    seen = []
+    for k in (0, 3, 1 << 33, 3, -1):
+        number.fill_(k)
+        graph.replay()
+        torch.cuda.synchronize()
+        want = step(torch.full((1,), k, dtype=torch.int64, device="cuda"))
+        for a, b in zip(out, want):
+            assert float((a - b).abs().max()) <= 1e-5 * float(b.abs().max())   # (products may be cut otherwise: 90 terms, 2^-24 each, twice)
+        seen.append(out[0].clone())
+    assert torch.equal(seen[1], seen[3]) and not torch.equal(seen[0], seen[1]) and not torch.equal(seen[2], seen[4])
+
+
+def test_gradients_of_two_streams_at_once():
+    torch = _torch()
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    B, T, D, V = 8, 400, 512, 700
+    made = []
+    for k in range(2):
+        made.append({"g": torch.randn((B, T, D), generator=gen, device="cuda"),
+                     "x": torch.randn((B, T, D), generator=gen, device="cuda"),
+                     "tokens": torch.randint(0, V, (B, T), generator=gen, device="cuda")})
+    weight = torch.ones(D, device="cuda")
+
+    def call(m, seed):
+        r = binding.lfmmi_add_rms_norm(m["x"], m["g"], weight, p=0.1, seed=seed)
+        d = binding.lfmmi_add_rms_norm_backward(r.sum, r.rstd, weight, m["g"], m["x"], p=0.1, seed=seed)
+        return list(d) + [binding.lfmmi_embed_tokens_backward(d.x, m["tokens"], V)]
+
+    want = [call(m, k) for k, m in enumerate(made)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in made]
+    got = [[], []]
+    for _ in range(5):
+        for k, (m, s) in enumerate(zip(made, streams)):
+            with torch.cuda.stream(s):
+                got[k].append(call(m, k))
+    torch.cuda.synchronize()
+    for k in range(2):
+        for tensors in got[k]:
+            assert all(torch.equal(a, b) for a, b in zip(tensors, want[k]))
+
+
 def test_a_serving_step():
     # embeddings of what was drafted, a norm into 8 bits, a layer, verification, scores of what was taken
     torch = _torch()
