@@ -144,18 +144,96 @@ struct Weights {
         e = fma(e, f, 1.);
         return __hiloint2double(__double2hiint(e) + (__double2loint(shifted) << 20), __double2loint(e));
     }
-    // 2^-1000 where it is to be 0, which adds nothing beside the 1 of the largest: t's high word is made at most that of
-    // -1,000, as a whole number without a sign, where a NaN's is smaller. A NaN, and a +inf, which is the m then, come out as a
-    // NaN. (A comparison of every logit for that: 6 us more for 43 million.)
-    __device__ __forceinline__ double at_least(float x) const
-    {
-        const double t = log2_of(x);
-        return exp2_of(__hiloint2double((int)min((uint32_t)__double2hiint(t), 0xc08f4000u), __double2loint(t)));
-    }
     __device__ __forceinline__ double operator()(float x) const
     {
         const double t = log2_of(x);
         return t > -1000. ? exp2_of(t) : 0.;
+    }
+};
+
+// 2^(j / 64)
+struct Roots {
+    double of[64];
+};
+constexpr Roots make_roots()
+{
+    const double root[6] = {1.0108892860517005, 1.0218971486541166, 1.0442737824274138,
+                            1.0905077326652577, 1.189207115002721,  1.4142135623730951};  // of 2: the 64th, 32nd and so on
+    Roots r{};
+    for (int j = 0; j < 64; ++j) {
+        r.of[j] = 1.;
+        for (int b = 0; b < 6; ++b)
+            if (j >> b & 1) r.of[j] *= root[b];
+    }
+    return r;
+}
+__device__ const Roots kRoots = make_roots();
+
+// The same exponential for code that all 64 lanes of a wave go through: 64 t is rounded to a whole number 64 n + j, lane j holds
+// 2^(j / 64), and 2^f for |f| <= 1/128 is 1 and a polynomial of degree 3 (6.2e-12 off at most). 13 operations of the vector pipe
+// and two passes through the crossbar for a logit, where degree 8 has 17. Lanes ask for two logits' roots before they use one (33 us
+// for the rows below; one 34, four 33 with registers for a wave less).
+constexpr int kAtOnce = 2;
+struct WaveWeights {
+    double m, scale2, c[3];
+    int hi, lo;  // of the lane's root, less j in the place to which j is shifted
+    __device__ __forceinline__ explicit WaveWeights(double root)
+    {
+        const double of[3] = {0.6931471805578869, 0.24022699328385197, 0.05550422379655395};
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+            c[k] = of[k];
+            asm("" : "+s"(c[k]));
+        }
+        hi = __double2hiint(root) - (int)((threadIdx.x & 63) << 14);
+        lo = __double2loint(root);
+    }
+    __device__ __forceinline__ void against(float top, float scale)
+    {
+        m = top;
+        scale2 = (double)scale * 1.44269504088896340736;
+    }
+    static __device__ __forceinline__ double root() { return kRoots.of[threadIdx.x & 63]; }
+    // t = log2 of the weight, at least -1,000: its parts on their way, then s + 2^t
+    struct Asked {
+        double f;
+        int j, high, low;
+    };
+    __device__ __forceinline__ Asked ask(double t) const
+    {
+        const double shifted = t + 105553116266496.;  // 1.5 * 2^46: 64ths in the last bits
+        const int j = __double2loint(shifted);
+        return {t - (shifted - 105553116266496.), j, __builtin_amdgcn_ds_bpermute(j << 2, hi), __builtin_amdgcn_ds_bpermute(j << 2, lo)};
+    }
+    __device__ __forceinline__ double add(const Asked& a, double s) const
+    {
+        double e = fma(a.f, c[2], c[1]);
+        e = fma(e, a.f, c[0]);
+        e = fma(e, a.f, 1.);
+        return fma(__hiloint2double(a.high + (a.j << 14), a.low), e, s);
+    }
+    __device__ __forceinline__ double log2_of(float x) const { return fabs((double)x - m) * -scale2; }
+    // 2^-1000 where it is to be 0, which adds nothing beside the 1 of the largest: t's high word is made at most that of
+    // -1,000, as a whole number without a sign, where a NaN's is smaller. A NaN, and a +inf, which is the m then, come out as a
+    // NaN. (A comparison of every logit for that: 6 us more for 43 million.)
+    template <int N>
+    __device__ __forceinline__ double add_at_least(const float* x, double s) const
+    {
+        Asked a[N];
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const double t = log2_of(x[k]);
+            a[k] = ask(__hiloint2double((int)min((uint32_t)__double2hiint(t), 0xc08f4000u), __double2loint(t)));
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int k = 0; k < N; ++k) s = add(a[k], s);
+        return s;
+    }
+    __device__ __forceinline__ double operator()(float x) const
+    {
+        const double t = log2_of(x), e = add(ask(fmax(t, -1000.)), 0.);
+        return t > -1000. ? e : 0.;
     }
 };
 
@@ -187,8 +265,9 @@ __device__ __forceinline__ void load_part(const typename T::Store* x, int first,
 }
 
 // ---- every row of a sequence's, a part at a time, a wave each, with no word between waves. Bound by the vector pipe: some 18
-// operations of 64 bits a logit. 48 sequences of 1 to 7 rows of 128,000 fp16 and as many of the draft's but one, 43 million
-// logits: 40 us; 17 with the exponentials taken out. (Sums of 32 bits decide nearly as well whether a token is taken, and 64 bits
+// operations a logit, 11 of them of 64 bits. 48 sequences of 1 to 7 rows of 128,000 fp16 and as many of the draft's but one, 43
+// million logits: 33 us; 38 with the polynomial of degree 8, 17 with no exponentials; 130 sequences of 4 rows of 50,021 fp32: 20 us
+// and 23, which is what reading them takes. (Sums of 32 bits decide nearly as well whether a token is taken, and 64 bits
 // of the one row that is drawn from could follow in a kernel of its own: both ways were alike, 73 us a call, for these, and 33
 // us against 27 for 9 rows of 32,000.)
 
@@ -199,6 +278,7 @@ __global__ __launch_bounds__(kThreads) void k_verify_rows(VerifyParams p, SeqLen
     space_of(p.workspace, p.B, p.K, p.parts, &space);
     const int rows = p.draft ? 2 * p.K + 1 : p.K + 1, lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    WaveWeights weight(Greedy ? 0. : WaveWeights::root());
     for (int64_t u = (int64_t)blockIdx.x * kWaves + wave; u < units; u += (int64_t)gridDim.x * kWaves) {
         const int64_t of = u / p.parts;
         const int part = (int)(u - of * p.parts), b = (int)(of / rows), row = (int)(of - (int64_t)b * rows);
@@ -232,12 +312,12 @@ __global__ __launch_bounds__(kThreads) void k_verify_rows(VerifyParams p, SeqLen
             best = wave_best(best);
         } else {
             // (of nothing but -inf, and NaN perhaps: against 0)
-            const Weights weight(m > -INFINITY ? m : 0.f, of_draft ? p.draft_scale : p.scale);
+            weight.against(m > -INFINITY ? m : 0.f, of_draft ? p.draft_scale : p.scale);
 #pragma unroll
             for (int k = 0; k < kChunks; ++k) {
                 if ((first - lane + k * 64) * 8 >= p.V) break;  // (nothing but padding)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) s += weight.at_least(f[k][j]);
+                for (int j = 0; j < 8; j += kAtOnce) s = weight.add_at_least<kAtOnce>(f[k] + j, s);
             }
         }
         s = wave_sum(Greedy && bad ? (double)NAN : s);
@@ -375,7 +455,7 @@ __global__ __launch_bounds__(kPickThreads) void k_verify_choose(VerifyParams p, 
     }
 }
 
-// If a drafted token is replaced: the sums of max(0, p - q) of kRestParts parts, two waves each. 11 us for 48 rows of 128,000
+// If a drafted token is replaced: the sums of max(0, p - q) of kRestParts parts, two waves each. 10.7 us for 48 rows of 128,000
 // and as many of the draft's, the exponentials' operations as above.
 template <typename T>
 __global__ __launch_bounds__(kRestThreads) void k_verify_rest(VerifyParams p, int64_t units)
@@ -384,6 +464,7 @@ __global__ __launch_bounds__(kRestThreads) void k_verify_rest(VerifyParams p, in
     Space space;
     space_of(p.workspace, p.B, p.K, p.parts, &space);
     const int groups = (p.parts + kRestParts - 1) / kRestParts, lane = threadIdx.x & 63, wave = (int)(threadIdx.x >> 6);
+    const double root = WaveWeights::root();
     for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
         const int b = (int)(u / groups), part = (int)(u - (int64_t)b * groups) * kRestParts + wave / 2;
         const Choice c = space.choice[b];
@@ -394,7 +475,9 @@ __global__ __launch_bounds__(kRestThreads) void k_verify_rest(VerifyParams p, in
             float f[kHalf][8], g[kHalf][8];
             load_part<T, 64, kHalf>(target_row<T>(p, b, c.row), first, p.V, f);
             load_part<T, 64, kHalf>(draft_row<T>(p, b, c.row), first, p.V, g);
-            const Weights weight(c.m, p.scale), weight_q(c.mq, p.draft_scale);
+            WaveWeights weight(root), weight_q(root);
+            weight.against(c.m, p.scale);
+            weight_q.against(c.mq, p.draft_scale);
             double s = 0.;
 #pragma unroll
             for (int k = 0; k < kHalf; ++k) {
