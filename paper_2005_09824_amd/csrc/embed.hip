@@ -73,7 +73,7 @@ int grid_of(int64_t units) { return (int)std::min<int64_t>(units, 1 << 20); }
 
 // ---- forward
 
-// Rows that a lane has on their way: a token, then its row, are two waits. Bound by HBM: 32,768 rows of 2,048 bf16 of a table of
+// Rows of 16 bits that a lane has on their way: a token, then its row, are two waits. Bound by HBM: 32,768 rows of 2,048 bf16 of a table of
 // 65,536, a third of them padding, 32 us (134 MB written, 65 MB of the table read; 55 us with one row a lane, 39 with rows in vector registers).
 constexpr int kEmbedRows = 4;
 
@@ -517,9 +517,11 @@ U* place(const EmbedGradParams& p, size_t at)
 hipError_t launch_embed(const EmbedParams& p, const SeqLengths& lens, int dtype, hipStream_t stream)
 {
     const int64_t rows = (int64_t)p.B * p.T;
-    // Few rows: one a lane, all at once (us, replayed, its own rows in the caches: 1,000 of 1,024 bf16 3.6, four a lane 4.0; 2,000 of
-    // 2,048 5.0 and 5.1; 8,000 of 1,024 7.4 and 7.2; 30,000 of 2,048, which the caches do not hold, 50 and 44).
-    const bool few = rows * ((p.D + 2047) / 2048) < 4096;
+    // One row a lane, or four (us of bf16, replayed, its own rows in the caches / others each time): 1,000 of 1,024 2.5 / 3.3 one,
+    // 3.3 / 4.0 four; 4,000 of 2,048 6.5 / 10.1 and 6.5 / 10.3; 8,000 of 1,024 6.5 / 9.8 and 6.5 / 9.6; 32,000 of 640 16.1 / 21.9 and
+    // 13.8 / 17.8; 30,000 of 2,048 35 / 46 and 36 / 41. Rows of 32 bits have twice as much on its way: 1,000 of 1,024 3.1 / 4.1 and
+    // 3.8 / 4.8; 32,000 of 640 24.6 / 32.4 and 25.3 / 32.4; 30,000 of 2,048 70 / 77 and 72 / 83.
+    const bool few = dtype == LFMMI_F32 || rows * ((p.D + 2047) / 2048) < 4096;
     const Tiles t = tiles_of(few ? rows : (rows + kEmbedRows - 1) / kEmbedRows, p.D);
     by_type(dtype, [&](auto type) {
         by_width<true>(p.D, [&](auto whole) {
@@ -527,8 +529,9 @@ hipError_t launch_embed(const EmbedParams& p, const SeqLengths& lens, int dtype,
             constexpr Width kWidth = decltype(whole)::value;
             by_wave(t, [&](auto wave) {
                 constexpr bool kWave = decltype(wave)::value;
+                constexpr int kMany = Type::kVec == 8 ? kEmbedRows : 1;
                 if (few) k_embed<Type, kWidth, 1, kWave><<<grid_of(t.units), kThreads, 0, stream>>>(p, lens, t);
-                else k_embed<Type, kWidth, kEmbedRows, kWave><<<grid_of(t.units), kThreads, 0, stream>>>(p, lens, t);
+                else k_embed<Type, kWidth, kMany, kWave><<<grid_of(t.units), kThreads, 0, stream>>>(p, lens, t);
             });
         });
     });
