@@ -401,7 +401,7 @@ lfmmi_status lfmmi_add_rms_norm(const void *x, int64_t stride_b, int64_t stride_
  * n = sum * rstd and g = weight * grad_y:
  *   d             = grad_sum + rstd * (g - n * mean_c(g_c n_c))
  *   grad_residual = d,  grad_x = dropout(d) with the forward call's p, seed, offset and step
- *   grad_weight   = sum over the rows of grad_y * n, in fp32, in an order that the sizes decide
+ *   grad_weight   = sum over the rows of grad_y * n, in fp32, in an order that sizes and type decide
  * sum (or x, where that is it; rows at their strides) and rstd: what the forward call read and
  * gave. grad_x, grad_residual [B, T, D] of `dtype` and grad_weight [D] of weight_dtype may be
  * NULL; either of the first two may be grad_y or grad_sum. Rows t >= lengths[b] become 0 and add

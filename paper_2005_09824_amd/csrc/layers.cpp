@@ -285,7 +285,8 @@ lfmmi_status lfmmi_add_rms_norm_workspace(int32_t B, int32_t T, int32_t D, int64
     lfmmi_status st = check_width(D);
     if (st == LFMMI_OK) st = check_batch(B, T, nullptr);
     if (st != LFMMI_OK) return st;
-    *bytes = (int64_t)norm_blocks((int64_t)B * T, D) * D * 4;
+    const int64_t N = (int64_t)B * T;
+    *bytes = (int64_t)std::max(norm_blocks(N, D, LFMMI_F32), norm_blocks(N, D, LFMMI_BF16)) * D * 4;
     return LFMMI_OK;
 }
 
@@ -313,7 +314,7 @@ try {
         !aligned(grad_sum, size) || !aligned(grad_x, size) || !aligned(grad_residual, size) ||
         !aligned(grad_weight, wsize))
         return fail_aligned();
-    a.blocks = norm_blocks(N, D);
+    a.blocks = norm_blocks(N, D, dtype);
     const int64_t need = grad_weight ? (int64_t)a.blocks * D * 4 : 0;
     if (need > 0 && (!workspace || !aligned(workspace, 16) || workspace_bytes < need)) return fail_workspace();
     const int64_t all = N * D * size;

@@ -45,7 +45,7 @@ struct NormParams {
 };
 hipError_t launch_norm(const NormParams& p, const SeqLengths& lens, int dtype, hipStream_t stream);
 
-int norm_blocks(int64_t rows, int D);  // workgroups of a backward launch, each with a row of partial sums
+int norm_blocks(int64_t rows, int D, int dtype);  // workgroups of a backward launch, each with a row of partial sums
 struct NormGradParams {
     const void* h;
     int64_t stride_b, stride_t;

@@ -332,7 +332,7 @@ __global__ __launch_bounds__(threads_of(G)) void k_norm_grad(NormGradParams p, S
     const auto dy_of = [&](uint32_t row) { return static_cast<const Store*>(p.grad_y) + (int64_t)row * p.D; };
     // What a row begins with is asked for while the row before is dealt with, and the weight is held; two chunks a lane
     // of 1,024 have no registers for that (16,384 columns of bf16, 8,000 rows: 448 us so, 340 without).
-    constexpr bool kAhead = N > 0 && G * N < 2048;
+    constexpr bool kAhead = N > 0 && G * N < 2048 && !(T::kVec == 4 && W == kAny && G * N >= 1536);
     Raw<T> h_next[kHeld], y_next[kHeld];
     float rstd_next = 0.f;
     const auto ask = [&](uint32_t row) {
@@ -519,18 +519,25 @@ struct Shape {
 // 256 x 4 7.1; 1,024 rows of 640: 5.4 and 4.7, of 4,096: 8.9 and 8.7.
 constexpr int kFewRows = 512;
 template <typename F>
-void by_shape(int64_t rows, int D, F&& f)
+void by_shape(int64_t rows, int D, int dtype, F&& f)
 {
     const int chunks = (D + 7) / 8;
+    const bool half = dtype != LFMMI_F32, odd = D % 8 != 0;
     if (chunks <= 64) f(Shape<64, 1>{});
     else if (rows <= kFewRows && chunks <= 256) f(Shape<256, 1>{});
     else if (rows <= kFewRows && chunks <= 512) f(Shape<512, 1>{});
     else if (rows <= kFewRows && chunks <= 1024) f(Shape<512, 2>{});
     else if (chunks <= 128) f(Shape<64, 2>{});
+    else if (chunks <= 192) f(Shape<64, 3>{});
+    else if (chunks <= 256 && (!half || odd)) f(Shape<64, 4>{});
     else if (chunks <= 256) f(Shape<128, 2>{});
+    else if (chunks <= 320 && half && odd) f(Shape<64, 5>{});
     else if (chunks <= 384) f(Shape<192, 2>{});
     else if (chunks <= 512) f(Shape<256, 2>{});
+    else if (chunks <= 640 && half) f(Shape<128, 5>{});
+    else if (chunks <= 768 && half) f(Shape<256, 3>{});
     else if (chunks <= 1024) f(Shape<256, 4>{});
+    else if (chunks <= 1536) f(Shape<512, 3>{});
     else if (chunks <= 2048) f(Shape<1024, 2>{});
     else f(Shape<1024, 0>{});
 }
@@ -545,16 +552,21 @@ struct Rounds : Shape<G_, N_> {
     static constexpr int kBlocks = Blocks_;
 };
 template <typename F>
-void by_rounds(int D, F&& f)
+void by_rounds(int D, int dtype, F&& f)
 {
     const int chunks = (D + 7) / 8;
+    const bool half = dtype != LFMMI_F32, odd = D % 8 != 0;
     if (chunks <= 64) f(Rounds<64, 1, 1024>{});
     else if (chunks <= 128) f(Rounds<64, 2, 768>{});
     else if (chunks <= 256) f(Rounds<256, 1, 1024>{});
+    else if (chunks <= 384 && half) f(Rounds<192, 2, 768>{});
     else if (chunks <= 512) f(Rounds<512, 1, 512>{});
     else if (chunks <= 640) f(Rounds<640, 1, 256>{});
+    else if (chunks <= 768 && half && odd) f(Rounds<256, 3, 512>{});
+    else if (chunks > 768 && chunks <= 1024 && half && odd) f(Rounds<1024, 1, 256>{});
     else if (chunks <= 1024) f(Rounds<512, 2, 256>{});
-    else if (chunks <= 2048) f(Rounds<1024, 2, 256>{});
+    else if (chunks <= 1536) f(Rounds<768, 2, 256>{});
+    else if (chunks <= 2048) f(Rounds<512, 4, 256>{});
     else f(Rounds<1024, 0, 256>{});
 }
 
@@ -583,7 +595,7 @@ hipError_t launch_norm(const NormParams& p, const SeqLengths& lens, int dtype, h
 {
     const int64_t rows = (int64_t)p.B * p.T;
     by_type(dtype, [&](auto t) {
-        by_shape(rows, p.D, [&](auto s) {
+        by_shape(rows, p.D, dtype, [&](auto s) {
             constexpr int G = decltype(s)::G, N = decltype(s)::N, kRows = threads_of(G) / G;
             const int grid = (int)std::min<int64_t>((rows + kRows - 1) / kRows, 1 << 20);
             by_width<G == 64 && N == 1>(p.D, [&](auto whole) {
@@ -594,10 +606,10 @@ hipError_t launch_norm(const NormParams& p, const SeqLengths& lens, int dtype, h
     return hipGetLastError();
 }
 
-int norm_blocks(int64_t rows, int D)
+int norm_blocks(int64_t rows, int D, int dtype)
 {
     int blocks = 0;
-    by_rounds(D, [&](auto s) {
+    by_rounds(D, dtype, [&](auto s) {
         constexpr int G = decltype(s)::G, kRows = threads_of(G) / G;
         blocks = (int)std::min<int64_t>((rows + kRows - 1) / kRows, decltype(s)::kBlocks);
     });
@@ -607,7 +619,7 @@ int norm_blocks(int64_t rows, int D)
 hipError_t launch_norm_grad(const NormGradParams& p, const SeqLengths& lens, int dtype, hipStream_t stream)
 {
     by_type(dtype, [&](auto t) {
-        by_rounds(p.D, [&](auto s) {
+        by_rounds(p.D, dtype, [&](auto s) {
             constexpr int G = decltype(s)::G, N = decltype(s)::N;
             by_width<G == 64 && N == 1>(p.D, [&](auto whole) {
                 k_norm_grad<decltype(t), decltype(whole)::value, G, N><<<p.blocks, threads_of(G), 0, stream>>>(p, lens);

@@ -270,6 +270,23 @@ def test_norm_of_many_rows(D, dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("N,D", [(1100, 1201), (520, 1536), (1100, 2001), (1600, 2501), (1600, 3072), (520, 5113), (520, 6000), (1040, 6001),
+                                 (520, 6145), (520, 7001), (520, 9001), (520, 12288), (520, 12289), (520, 16000)])
+def test_norm_and_gradients_of_more_rows_than_workgroups(N, D, dtype):
+    torch = _torch()
+    rng = np.random.default_rng(D)
+    x, x64 = _values(rng, (N, D), dtype)
+    res, r64 = _values(rng, (N, D), dtype, 3.0)
+    dy, dy64 = _values(rng, (N, D), dtype)
+    weight = torch.from_numpy(rng.normal(1, 0.3, D).astype(np.float32)).cuda()
+    kw = dict(p=0.2, seed=3, offset=4)
+    r = binding.lfmmi_add_rms_norm(x, res, weight, **kw)
+    total, w = check_norm(x64, r64, weight, 1e-6, None, 0.2, 3, 4, r, dtype, (N, D))
+    g = binding.lfmmi_add_rms_norm_backward(r.sum, r.rstd, weight, dy, x, **kw)
+    check_grads(total, w, r.rstd, dy64, x64, None, 0.2, 3, 4, g, dtype, "float32", (N, D))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("B,T,D", [(1, 1, 16), (5, 7, 40), (300, 3, 24), (600, 1, 640), (4, 700, 72), (3, 40, 2100), (2, 9, 16400),
                                    (1, 3000, 16), (280, 2, 20000)])
 def test_sequences(B, T, D, dtype):
