@@ -380,7 +380,7 @@ lfmmi_status lfmmi_dropout(const void *x, int32_t dtype, int32_t R, int32_t D, i
  *   x, residual [B, T, D] of `dtype`, rows at their strides (>= 0); residual may be NULL (0).
  *   weight   [D] of `dtype` or float32 (weight_dtype), or NULL (1)
  *   lengths  HOST int32 [B], or NULL: rows t >= lengths[b] are never read, their outputs are 0
- *   eps      1e-30 <= eps <= 1e30
+ *   eps      1e-30 <= eps <= 1e20
  *   p, seed, offset, step  as for lfmmi_dropout
  *   sum      [B, T, D]; may be NULL where it would be x itself (no residual, nothing dropped).
  *            It may be x or residual, where the rows of that one follow each other.

@@ -221,7 +221,7 @@ try {
     NormParams a{};
     if (st == LFMMI_OK) st = make_draw(p, seed, offset, step, &a.draw);
     if (st != LFMMI_OK) return st;
-    if (!(eps >= 1e-30f && eps <= 1e30f)) return fail(LFMMI_ERR_INVALID_ARG, "eps outside [1e-30, 1e30]");
+    if (!(eps >= 1e-30f && eps <= 1e20f)) return fail(LFMMI_ERR_INVALID_ARG, "eps outside [1e-30, 1e20]");
     if (B == 0 || T == 0) return LFMMI_OK;
     if (!x) return fail(LFMMI_ERR_INVALID_ARG, "x is null");
     if (!sum && (residual || a.draw.threshold > 0))

@@ -231,7 +231,7 @@ __global__ __launch_bounds__(threads_of(G)) void k_norm(NormParams p, SeqLengths
                 }
             }
             s = over_row<G, false>(s, parts[1]);
-            rstd = kSmaller / sqrtf(s / (float)p.D + p.eps * kSmaller * kSmaller);
+            rstd = kSmaller / sqrtf(s / (float)p.D);  // (eps of 1e20 at most is nothing beside a mean of 2e31)
             if (G > 64) __syncthreads();
         }
         if (p.rstd && lane == 0) p.rstd[row] = rstd;
@@ -330,8 +330,9 @@ __global__ __launch_bounds__(threads_of(G)) void k_norm_grad(NormGradParams p, S
         return static_cast<const Store*>(p.h) + offset_of(row, p.T, p.stride_b, p.stride_t);
     };
     const auto dy_of = [&](uint32_t row) { return static_cast<const Store*>(p.grad_y) + (int64_t)row * p.D; };
-    // What a row begins with is asked for while the row before is dealt with, and the weight is held; two chunks a lane
-    // of 1,024 have no registers for that (16,384 columns of bf16, 8,000 rows: 448 us so, 340 without).
+    // What a row begins with is asked for while the row before is dealt with, and the weight is held; four chunks a lane
+    // of 512 have no registers for that (16,384 columns, 6,000 rows of fp32: 476 us so, 407 without; of bf16 223 and 225), nor two
+    // of 768 in 32 bits and odd widths (9,001 columns, 9,000 rows: 577 and 365; of bf16 184 and 228).
     constexpr bool kAhead = N > 0 && G * N < 2048 && !(T::kVec == 4 && W == kAny && G * N >= 1536);
     Raw<T> h_next[kHeld], y_next[kHeld];
     float rstd_next = 0.f;
@@ -510,13 +511,26 @@ struct Shape {
     static constexpr int G = G_, N = N_;
 };
 
-// Lanes and chunks of a row, forward (us of fp32 / bf16, dropout 0.1, replayed; 32,000 rows of 640, 20,000 of 1,500, 8,000 of
-// 8,192, 6,000 of 16,384, 16,000 of the others): 640: 64 x 2 65 / 32, 128 x 1 69 / 42. 1,500: 128 x 2 100 / 53, 256 x 1 95 / 58.
-// 2,048: 128 x 2 102 / 43, 256 x 1 99 / 45. 2,500: 192 x 2 129 / 68, 256 x 2 130 / 94. 4,096: 256 x 2 192 / 103, 512 x 1 185 /
-// 105. 5,003: 256 x 4 242 / 170, 512 x 2 263 / 201. 8,192: 256 x 4 193 / 106, 512 x 2 190 / 104, 1024 x 1 192 / 126. 16,384: 1024
-// x 2 290 / 155, chunks read again 319 / 202. Few rows leave most of the chip idle, and each is spread over more lanes (256 rows
-// of bf16): 640: 256 x 1 3.8, 64 x 2 4.5. 2,048: 256 x 1 4.0, 128 x 2 4.6. 4,096: 512 x 1 4.6, 256 x 2 5.0. 8,192: 512 x 2 6.3,
-// 256 x 4 7.1; 1,024 rows of 640: 5.4 and 4.7, of 4,096: 8.9 and 8.7.
+// Lanes and chunks of a row, forward: us of fp32 / bf16, dropout 0.1, replayed, first what is taken (a width of both for one type
+// alone where the other keeps what follows it). Rows of 640 32,000; 1,101 40,000; 1,500, 2,000 and 2,001 32,000; 2,500 16,000; 2,501
+// and 3,001 24,000; 4,096, 5,000 and 5,003 16,000; 6,000 and 6,001 14,000; 7,001 12,000; 8,192 8,000; 9,001 9,000; 12,000 8,000; 16,384
+// 6,000.
+//    640:    64 x 2 65 / 32, 128 x 1 69 / 42
+//    1,101:  64 x 3 138 / 81, 64 x 4 137 / 89, 128 x 2 142 / 99
+//    1,500:  64 x 3 153 / 75, 128 x 2 153 / 81
+//    2,000:  64 x 4 194 / 99, 128 x 2 204 / 96 (bf16: this); 2,001: 195 / 105 and 205 / 114
+//    2,500:  192 x 2 129 / 68, 256 x 2 130 / 94; 2,501: 185 / 108, 64 x 5 195 / 101 (bf16: this), 128 x 3 189 / 112
+//    3,001:  192 x 2 223 / 120, 128 x 3 227 / 124, 64 x 6 232 / 137
+//    4,096:  256 x 2 192 / 103, 512 x 1 185 / 105; 20,000 of 4,001: 245 / 136, 128 x 4 249 / 144
+//    5,000:  256 x 4 233 / 117, 128 x 5 256 / 117, 320 x 2 243 / 117, 640 x 1 228 / 156; 5,003: 233 / 153, 240 / 146 (bf16: this), 233 / 168, 233 / 188
+//    6,000:  256 x 4 249 / 119, 256 x 3 263 / 119; 6,001: 245 / 152, 257 / 145 (bf16: this)
+//    7,001:  256 x 4 249 / 150, 192 x 6 259 / 219, 128 x 8 260 / 167
+//    8,192:  256 x 4 193 / 106, 512 x 2 190 / 104, 1024 x 1 192 / 126
+//    9,001:  512 x 3 245 / 169, 768 x 2 248 / 208, 1024 x 2 259 / 218, 384 x 4 287 / 190; 12,000: 283 / 139, 278 / 160, 301 / 167, 304 / 148
+//    16,384: 1024 x 2 288 / 150, 512 x 4 305 / 137, chunks read again 319 / 202; 13,001: 254 / 181 and 272 / 197
+// Few rows leave most of the chip idle, and each is spread over more lanes (256 rows of bf16): 640: 256 x 1 3.8, 64 x 2 4.5. 2,048: 256
+// x 1 4.0, 128 x 2 4.6. 4,096: 512 x 1 4.6, 256 x 2 5.0. 8,192: 512 x 2 6.3, 256 x 4 7.1; 1,024 rows of 640: 5.4 and 4.7, of 4,096: 8.9
+// and 8.7.
 constexpr int kFewRows = 512;
 template <typename F>
 void by_shape(int64_t rows, int D, int dtype, F&& f)
@@ -542,11 +556,20 @@ void by_shape(int64_t rows, int D, int dtype, F&& f)
     else f(Shape<1024, 0>{});
 }
 
-// ... and backward, with the workgroups that go round the rows, as many as the registers leave place for (the same rows, 60,000 of
-// 500): 500: 64 x 1 1,024 127 / 63, 2,048 130 / 74. 640: 64 x 2 768 84 / 38, 1,024 88 / 44, 128 x 1 2,048 87 / 41. 2,048: 256 x 1
-// 1,024 128 / 65, 128 x 2 1,024 128 / 67. 2,500: 512 x 1 512 156 / 109, 256 x 2 512 157 / 129, 192 x 2 768 188 / 100. 4,096: 512 x
-// 1 512 243 / 128, 256 x 2 512 240 / 124. 4,100: 640 x 1 256 248 / 198, 512 x 2 256 261 / 224; 5,003: 298 / 230 and 295 / 240.
-// 8,192: 512 x 2 256 256 / 126, 512 254 / 134, 1024 x 1 250 / 126. 16,384: 1024 x 2 420 / 282, chunks read again 536 / 344.
+// ... and backward, with the workgroups that go round the rows, as many as the registers leave place for (the same rows; 500 60,000, 2,048
+// 16,000, 2,496 and 3,072 24,000, 4,100 16,000, 8,190 9,000).
+//    500:    64 x 1 1,024 127 / 63, 2,048 130 / 74
+//    640:    64 x 2 768 84 / 38, 1,024 88 / 44, 128 x 1 2,048 87 / 41
+//    1,101:  256 x 1 1,024 181 / 129, 192 x 1 1,024 181 / 130, 128 x 2 1,024 179 / 158
+//    2,048:  256 x 1 1,024 128 / 65, 128 x 2 1,024 128 / 67; 2,001: 259 / 146, 255 / 150, 64 x 4 512 253 / 176
+//    2,496:  512 x 1 512 222 / 125, 192 x 2 768 224 / 120 (bf16: this), 320 x 1 768 229 / 116; 2,501: 232 / 165, 279 / 144, 267 / 207
+//    3,001:  512 x 1 512 277 / 171, 192 x 2 768 319 / 162, 384 x 1 512 278 / 170, 128 x 3 512 273 / 221
+//    4,096:  512 x 1 512 243 / 128, 256 x 2 512 240 / 124; 20,000 of 4,001: 308 / 177 and 308 / 181
+//    4,100:  640 x 1 256 248 / 198, 512 x 2 256 261 / 224; 5,003: 298 / 230 and 295 / 240
+//    6,000:  512 x 2 256 316 / 156, 256 x 3 512 323 / 160, 384 x 2 256 314 / 190; 6,001: 318 / 209, 323 / 192 (bf16: this), 310 / 246
+//    8,192:  512 x 2 256 256 / 126, 512 254 / 134, 1024 x 1 250 / 126; 8,190: 285 / 159, 1024 x 1 282 / 138; 7,001: 323 / 217, 319 / 200 (bf16: this)
+//    9,001:  768 x 2 256 365 / 184, 512 x 3 256 327 / 199, 512 x 4 256 567 / 320, 1024 x 2 624 / 388; 12,000: 376 / 174, 376 / 173, 409 / 224, 403 / 292
+//    16,384: 512 x 4 256 412 / 215, 512 blocks 411 / 233, 768 x 3 546 / 307, 1024 x 2 419 / 283, chunks read again 536 / 344
 template <int G_, int N_, int Blocks_>
 struct Rounds : Shape<G_, N_> {
     static constexpr int kBlocks = Blocks_;

@@ -133,7 +133,7 @@ def test_refused_norms(kw, code, text):
     _refused(_norm(**kw), code, text)
 
 
-@pytest.mark.parametrize("eps", [0.9e-30, 1.1e30, 3e38])
+@pytest.mark.parametrize("eps", [0.9e-30, 1.1e20, 1e30, 3e38])
 def test_eps_beyond_what_sums_of_squares_leave_room_for_is_refused(eps):
     _refused(_norm(eps=eps), INVALID, "eps")
 
