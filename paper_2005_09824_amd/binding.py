@@ -11,6 +11,7 @@ import array
 import collections
 import contextlib
 import ctypes
+import functools
 import os
 
 import numpy as np
@@ -666,6 +667,14 @@ def _token_bytes(tokens, what="tokens"):
     raise ValueError(what + " must be int32 or int64")
 
 
+@functools.lru_cache(maxsize=1024)
+def _workspace_bytes(entry, *sizes):
+    """What the call of that name gives for these sizes."""
+    need = ctypes.c_int64(0)
+    _check(getattr(load_library(), entry)(*sizes, ctypes.byref(need)))
+    return need.value
+
+
 def _like(x, dtype=None):
     """A contiguous tensor like x, its values not set."""
     import torch
@@ -714,11 +723,11 @@ def lfmmi_embed_tokens(table, tokens, lengths=None, scale=1.0, out=None, status=
     written = [t for t in (out, status) if t is not None]
     with context:
         if out is None:
-            out = torch.empty(shape + (D,), dtype=table.dtype, device=dev)
+            out = table.new_empty(shape + (D,))
         else:
             _check_out(out, shape + (D,), table.dtype, dev)
         if status is None:
-            status = torch.empty(shape, dtype=torch.int32, device=dev)
+            status = table.new_empty(shape, dtype=torch.int32)
         else:
             _check_out(status, shape, torch.int32, dev)
         _check(load_library().lfmmi_embed_tokens(
@@ -751,16 +760,15 @@ def lfmmi_embed_tokens_backward(grad_out, tokens, V, lengths=None, scale=1.0, gr
     mine = grad is None
     with context:
         if mine:
-            grad = torch.empty((V, D), dtype=grad_out.dtype, device=dev)
+            grad = grad_out.new_empty((V, D))
         else:
             _check_out(grad, (V, D), grad_out.dtype, dev)
-        need = ctypes.c_int64(0)
-        _check(lib.lfmmi_embed_tokens_workspace(V, D, B, T, ctypes.byref(need)))
-        ws = torch.empty(need.value, dtype=torch.uint8, device=dev)
+        need = _workspace_bytes("lfmmi_embed_tokens_workspace", V, D, B, T)
+        ws = grad_out.new_empty((need,), dtype=torch.uint8)
         _check(lib.lfmmi_embed_tokens_backward(
             grad_out.data_ptr(), code, V, D, stride_b, stride_t, tokens.data_ptr(), token_bytes, B, T,
             None if lens is None else _hp(lens), scale, 1 if accumulate else 0, grad.data_ptr(),
-            ws.data_ptr(), need.value, raw))
+            ws.data_ptr(), need, raw))
     if not mine:
         _written(grad)
     return grad
@@ -872,9 +880,9 @@ def lfmmi_add_rms_norm(x, residual=None, weight=None, eps=1e-6, lengths=None, p=
             f32 = torch.float32
             out = AddRmsNorm(
                 _like(x) if wants_sum else None, _like(x) if wants_y else None,
-                torch.empty(rows, dtype=f32, device=dev),
+                x.new_empty(rows, dtype=f32),
                 _like(x, torch.float8_e4m3fn) if quantized else None,
-                torch.empty(rows, dtype=f32, device=dev) if quantized else None)
+                x.new_empty(rows, dtype=f32) if quantized else None)
         else:
             for t, wanted, shape, dt in (
                     (out.sum, wants_sum, x.shape, dtype), (out.y, wants_y, x.shape, dtype),
@@ -924,7 +932,7 @@ def lfmmi_add_rms_norm_backward(sum, rstd, weight, grad_y, grad_sum=None, length
             dx = _like(sum)
             out = AddRmsNormGrads(
                 dx, None if not residual else dx if one else _like(sum),
-                torch.empty(D, dtype=weight.dtype, device=dev) if weight_grad else None)
+                weight.new_empty((D,)) if weight_grad else None)
         else:
             for t, wanted, shape, dt in ((out.x, True, sum.shape, dtype), (out.residual, residual, sum.shape, dtype),
                                          (out.weight, weight_grad, (D,), weight.dtype if weight_grad else None)):
@@ -932,16 +940,15 @@ def lfmmi_add_rms_norm_backward(sum, rstd, weight, grad_y, grad_sum=None, length
                     raise ValueError(_WRONG_OUT)
                 if t is not None:
                     _check_out(t, shape, dt, dev)
-        need = ctypes.c_int64(0)
-        ws = None
+        need, ws = 0, None
         if weight_grad:
-            _check(lib.lfmmi_add_rms_norm_workspace(B, T, D, ctypes.byref(need)))
-            ws = torch.empty(need.value, dtype=torch.uint8, device=dev)
+            need = _workspace_bytes("lfmmi_add_rms_norm_workspace", B, T, D)
+            ws = sum.new_empty((need,), dtype=torch.uint8)
         dres = None if out.residual is None or out.residual is out.x else out.residual
         _check(lib.lfmmi_add_rms_norm_backward(
             sum.data_ptr(), stride_b, stride_t, code, B, T, D, None if lens is None else _hp(lens), _ptr(weight),
             w_code, _ptr(rstd), _ptr(grad_y), _ptr(grad_sum), p, seed, offset, at, _ptr(out.x), _ptr(dres),
-            _ptr(out.weight), _ptr(ws), need.value, raw))
+            _ptr(out.weight), _ptr(ws), need, raw))
     if not mine:
         _written([t for t in out if t is not None])
     return out
@@ -987,19 +994,19 @@ def lfmmi_verify_tokens(logits, drafted=None, uniforms=None, draft_logits=None, 
     mine = out is None
     with context:
         if mine:
-            out = VerifiedTokens(*(torch.empty(shape, dtype=torch.int32, device=dev)
-                                   for shape in ((B,), (B, rows), (B,))))
+            i32 = torch.int32
+            out = VerifiedTokens(logits.new_empty((B,), dtype=i32), logits.new_empty((B, rows), dtype=i32),
+                                 logits.new_empty((B,), dtype=i32))
         else:
             for t, shape in zip(out, ((B,), (B, rows), (B,))):
                 _check_out(t, shape, torch.int32, dev)
-        need = ctypes.c_int64(0)
-        _check(lib.lfmmi_verify_tokens_workspace(B, K, V, ctypes.byref(need)))
-        ws = torch.empty(need.value, dtype=torch.uint8, device=dev)
+        need = _workspace_bytes("lfmmi_verify_tokens_workspace", B, K, V)
+        ws = logits.new_empty((need,), dtype=torch.uint8)
         _check(lib.lfmmi_verify_tokens(
             logits.data_ptr(), code, B, K, V, stride_b, stride_t, _ptr(draft_logits) if K > 0 else None, *draft_strides,
             _ptr(drafted) if K > 0 else None, token_bytes, None if lens is None else _hp(lens), scale, draft_scale,
             _ptr(uniforms), out.accepted.data_ptr(), out.tokens.data_ptr(), out.status.data_ptr(), ws.data_ptr(),
-            need.value, raw))
+            need, raw))
     if not mine:
         _written(list(out))
     return out
