@@ -557,7 +557,7 @@ void by_shape(int64_t rows, int D, int dtype, F&& f)
 }
 
 // ... and backward, with the workgroups that go round the rows, as many as the registers leave place for (the same rows; 500 60,000, 2,048
-// 16,000, 2,496 and 3,072 24,000, 4,100 16,000, 8,190 9,000).
+// 16,000, 2,496 24,000, 4,100 16,000, 8,190 9,000).
 //    500:    64 x 1 1,024 127 / 63, 2,048 130 / 74
 //    640:    64 x 2 768 84 / 38, 1,024 88 / 44, 128 x 1 2,048 87 / 41
 //    1,101:  256 x 1 1,024 181 / 129, 192 x 1 1,024 181 / 130, 128 x 2 1,024 179 / 158
