@@ -17,8 +17,8 @@ namespace {
 constexpr int32_t kMostWidth = 1 << 24;  // of a row; eight values make a chunk, whose number times eight has 32 bits
 
 // Whether an array of so many bytes is written past the caches: it would drive out what is read, and be gone before it is
-// read itself. (Past them and otherwise: dropout of 82 MB 31.9 and 29.2 us, of 268 MB 102 and 106; rows of a table of 134 MB 43
-// and 45; the gradient of a table of 268 MB with its sorting 117 and 131.)
+// read itself. (Past them and otherwise, replayed: dropout of 268 MB of bf16 80 and 101 us; rows of a table of 134 MB 28 and 31; the
+// gradient of a table of 268 MB with its sorting 108 and 124; dropout of 82 MB, which the caches hold, 31.9 and 29.2 called in turn.)
 bool past_caches(int64_t bytes) { return bytes > kCacheBytes / 2; }
 
 lfmmi_status fail_aligned() { return fail(LFMMI_ERR_INVALID_ARG, "an array is not aligned to its elements"); }
