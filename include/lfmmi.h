@@ -425,7 +425,9 @@ lfmmi_status lfmmi_add_rms_norm_workspace(int32_t B, int32_t T, int32_t D, int64
  * scale * logits[b,i,:], q_i that of draft_scale * draft_logits[b,i,:] (NULL: q_i is 1 at d_i, 0
  * elsewhere) and u = uniforms[b,:], float32 [B, K + 1] in [0, 1):
  *   d_i is taken if all before it are and u_i q_i(d_i) < p_i(d_i);
- *   the first that is not, d_r, is replaced by a token drawn from max(0, p_r - q_r), normalised;
+ *   the first that is not, d_r, is replaced by a token drawn from max(0, p_r - q_r), normalised
+ *   (from p_r where that is 0 everywhere; where p_r and q_r agree but for rounding it is what
+ *   rounding leaves);
  *   if all are taken (r = n), a token drawn from p_n follows.
  * Drawn means: the first token at which the running sum of what it is drawn from, in the order of
  * the tokens, passes u_K times the whole (a number of 1 or more: the last token of any

@@ -421,13 +421,24 @@ __global__ __launch_bounds__(kPickThreads) void k_verify_greedy(VerifyParams p, 
     }
 }
 
-// What is left of p - q. (Equal products have to leave nothing: no product goes unrounded into the difference.)
-__device__ __forceinline__ double left_over(double p, double per, double q, double per_q)
-{
+// What is left of p - q, for all 64 lanes of a wave. The sums of the parts and the token in one of them both go by this: where
+// p and q are the same but for rounding, another exponential leaves nothing of a part that has been chosen for what this one
+// leaves. (Equal products have to leave nothing: no product goes unrounded into the difference.)
+struct LeftOver {
+    WaveWeights p, q;
+    double per, per_q;
+    __device__ __forceinline__ LeftOver(double root, const VerifyParams& v, const Choice& c) : p(root), q(root), per(c.per), per_q(c.per_q)
+    {
+        p.against(c.m, v.scale);
+        q.against(c.mq, v.draft_scale);
+    }
+    __device__ __forceinline__ double operator()(float x, float y) const
+    {
 #pragma clang fp contract(off)
-    const double a = p * per, b = q * per_q;
-    return fmax(0., a - b);
-}
+        const double a = p(x) * per, b = q(y) * per_q;
+        return fmax(0., a - b);
+    }
+};
 
 // The sum over a workgroup, the same bits in every thread. `parts`: a place for each wave.
 __device__ __forceinline__ double block_sum(double v, double* parts)
@@ -475,15 +486,13 @@ __global__ __launch_bounds__(kRestThreads) void k_verify_rest(VerifyParams p, in
             float f[kHalf][8], g[kHalf][8];
             load_part<T, 64, kHalf>(target_row<T>(p, b, c.row), first, p.V, f);
             load_part<T, 64, kHalf>(draft_row<T>(p, b, c.row), first, p.V, g);
-            WaveWeights weight(root), weight_q(root);
-            weight.against(c.m, p.scale);
-            weight_q.against(c.mq, p.draft_scale);
+            const LeftOver left_over(root, p, c);
             double s = 0.;
 #pragma unroll
             for (int k = 0; k < kHalf; ++k) {
                 if ((first - lane + k * 64) * 8 >= p.V) break;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) s += left_over(weight(f[k][j]), c.per, weight_q(g[k][j]), c.per_q);
+                for (int j = 0; j < 8; ++j) s += left_over(f[k][j], g[k][j]);
             }
             s = wave_sum(s);
             if (lane == 0) halves[wave] = s;
@@ -507,6 +516,7 @@ __global__ __launch_bounds__(kPickThreads) void k_verify_pick(VerifyParams p, Se
     Space space;
     space_of(p.workspace, p.B, p.K, p.parts, &space);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const double root = Chosen ? WaveWeights::root() : 0.;
     for (int b = blockIdx.x; b < p.B; b += gridDim.x) {
         const float u = p.uniforms[(int64_t)b * (p.K + 1) + p.K];
         Choice c = Chosen ? space.choice[b] : choose<T, false>(p, space, b, drafts_of(p, lens, b), &ends, &shared);
@@ -518,10 +528,11 @@ __global__ __launch_bounds__(kPickThreads) void k_verify_pick(VerifyParams p, Se
             write_tokens(p, b, c, -1);
             continue;
         }
-        const Weights weight(c.m, p.scale), weight_q(c.mq, p.draft_scale);
+        const Weights weight(c.m, p.scale);
+        const LeftOver left_over(root, p, c);
         const Part* parts = space.parts + ((int64_t)b * (2 * p.K + 1) + c.row) * p.parts;
         const double* rest = space.rest + (int64_t)b * p.parts;
-        // a lane's weights of eight tokens of a part
+        // a lane's weights of eight tokens of a part (by whole waves)
         const auto weights_of = [&](int part, double* w) {
             double s = 0.;
 #pragma unroll
@@ -530,11 +541,10 @@ __global__ __launch_bounds__(kPickThreads) void k_verify_pick(VerifyParams p, Se
             const int chunk = part * (kVerifyPart / 8) + (int)threadIdx.x;
             float f[1][8], g[1][8];
             load_part<T, 1, 1>(target_row<T>(p, b, c.row), chunk, p.V, f);
-            if (c.kind == kDrafted) load_part<T, 1, 1>(draft_row<T>(p, b, c.row), chunk, p.V, g);
+            if (Chosen && c.kind == kDrafted) load_part<T, 1, 1>(draft_row<T>(p, b, c.row), chunk, p.V, g);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                w[j] = weight(f[0][j]);
-                if (c.kind == kDrafted) w[j] = left_over(w[j], c.per, weight_q(g[0][j]), c.per_q);
+                w[j] = Chosen && c.kind == kDrafted ? left_over(f[0][j], g[0][j]) : weight(f[0][j]);
                 if (c.kind == kGiven && chunk * 8 + j == c.token) w[j] = 0.;
                 s += w[j];
             }
@@ -548,7 +558,7 @@ __global__ __launch_bounds__(kPickThreads) void k_verify_pick(VerifyParams p, Se
             __syncthreads();
         }
         const auto weight_of = [&](int k) {
-            return k >= p.parts ? 0. : c.kind == kDrafted ? rest[k] : k == given ? without : parts[k].s * weight(parts[k].m);
+            return k >= p.parts ? 0. : Chosen && c.kind == kDrafted ? rest[k] : k == given ? without : parts[k].s * weight(parts[k].m);
         };
         // every wave: running sums of the parts, 64 at a time, and the part that passes
         double whole = 0.;

@@ -116,6 +116,48 @@ def test_equal_probabilities():
     assert r.accepted.tolist() == [0] * 4 and r.tokens[:, 0].tolist() == [49] * 4 and not r.status.any()
 
 
+def test_what_rounding_leaves_of_equal_probabilities():
+    # p and q are the same but for rounding, and the drafted token is masked out of both: whatever is left of
+    # p - q, and whatever the random number is, the token drawn is one that p gives something to
+    torch = _torch()
+    rng = np.random.default_rng(8)
+    B, V = 20000, 8
+    x = np.round(rng.normal(0, 4, (B, 2, V)) * 64).astype(np.float32) / 64   # (three times that is exact)
+    x[rng.random((B, 2, V)) < 0.2] = -np.inf
+    x[:, :, 1] = 0.25
+    x[:, :, 0] = -np.inf
+    logits = torch.from_numpy(x).cuda()
+    u = torch.from_numpy(rng.choice([0.0, 0.3, 0.9, 1.0 - 2.0 ** -24, 1.0], (B, 2)).astype(np.float32)).cuda()
+    t = torch.zeros((B, 1), dtype=torch.int64, device="cuda")
+    r = binding.lfmmi_verify_tokens(logits, t, u, logits[:, :1] * 3, scale=0.75, draft_scale=0.25)
+    assert not r.status.any() and not r.accepted.any() and bool((r.tokens[:, 1] == -1).all())
+    assert int(r.tokens[:, 0].min()) > 0
+    assert bool(torch.isfinite(logits[:, 0].gather(1, r.tokens[:, :1].long())).all())
+
+
+@pytest.mark.parametrize("dtype", ["float32", "float16"])
+@pytest.mark.parametrize("V", [2100, 4096, 150000])
+def test_a_part_that_rounding_alone_leaves(V, dtype):
+    # two tokens, the second alone in a part of the row's (a wave takes 2,048 logits); the draft also gives 1e-16
+    # and more to a drafted token that the target masks. Every sequence draws a token that the target knows
+    torch = _torch()
+    rng = np.random.default_rng(V)
+    B, far = 400 if V > 10000 else 4000, V - 7
+    x = torch.full((B, 2, V), -np.inf, dtype=getattr(torch, dtype), device="cuda")
+    x[:, :, 0] = 0.0
+    x[:, 0, far] = torch.from_numpy(rng.uniform(-3, 0, B).astype(np.float32)).cuda().to(x.dtype)
+    x[0, 0, far] = -0.916799545
+    d = x[:, :1].clone()
+    d[:, 0, 5] = torch.from_numpy(rng.uniform(-37, -33, B).astype(np.float32)).cuda().to(x.dtype)
+    d[0, 0, 5] = -35.7673492
+    t = torch.full((B, 1), 5, dtype=torch.int64, device="cuda")
+    for last in (0.0, 0.5, 0.9, 1.0):
+        u = torch.tensor([0.5, last], device="cuda").expand(B, 2).contiguous()
+        r = binding.lfmmi_verify_tokens(x, t, u, d)
+        assert not r.status.any() and not r.accepted.any()
+        assert bool(((r.tokens[:, 0] == 0) | (r.tokens[:, 0] == far)).all())
+
+
 def test_tokens_that_cannot_be_drawn():
     torch = _torch()
     V = 10000
