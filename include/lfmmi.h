@@ -405,7 +405,8 @@ lfmmi_status lfmmi_add_rms_norm(const void *x, int64_t stride_b, int64_t stride_
  * sum (or x, where that is it; rows at their strides) and rstd: what the forward call read and
  * gave. grad_x, grad_residual [B, T, D] of `dtype` and grad_weight [D] of weight_dtype may be
  * NULL; either of the first two may be grad_y or grad_sum. Rows t >= lengths[b] become 0 and add
- * nothing. workspace: needed with grad_weight.
+ * nothing (where x stands for sum, grad_sum is x's gradient there too, and the caller's to add).
+ * workspace: needed with grad_weight.
  */
 lfmmi_status lfmmi_add_rms_norm_backward(const void *sum, int64_t stride_b, int64_t stride_t,
                                          int32_t dtype, int32_t B, int32_t T, int32_t D,

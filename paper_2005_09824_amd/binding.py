@@ -905,10 +905,11 @@ def lfmmi_add_rms_norm_backward(sum, rstd, weight, grad_y, grad_sum=None, length
                                 offset=0, step=None, residual=True, weight_grad=True, out=None, stream=None):
     """Gradients of lfmmi_add_rms_norm for those of y and sum (contiguous tensors like sum; either
     may be None). sum, rstd: what that call returned; lengths, p, seed, offset, step: what it was
-    given. Returns AddRmsNormGrads (x, residual, weight): residual is None where `residual` is false,
-    and x's where nothing was dropped (one tensor); weight's is None without a weight, or where
-    `weight_grad` is false. `out`: an
-    AddRmsNormGrads to write into; x and residual of it may be grad_y or grad_sum."""
+    given. Rows behind the lengths get 0 (where sum is x itself, what grad_sum holds for them is
+    the caller's to add). Returns AddRmsNormGrads (x, residual, weight): residual is None where
+    `residual` is false, and x's where nothing was dropped (one tensor); weight's is None without a
+    weight, or where `weight_grad` is false. `out`: an AddRmsNormGrads to write into; x and residual of
+    it may be grad_y or grad_sum."""
     import torch
     code, B, T, D, stride_b, stride_t = _batch_rows(sum, "sum")
     dev, dtype = sum.device, sum.dtype

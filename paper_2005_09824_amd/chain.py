@@ -202,6 +202,17 @@ def dropout(x, p, seed, offset=0, step=None):
     return _dropout_cls.apply(x, float(p), int(seed), int(offset), step)
 
 
+def _copy_behind(out, rows, lengths):
+    """The rows behind the lengths of a contiguous tensor [B, T, D] or [B, D], into their places in `out`."""
+    import torch
+    if rows.dim() == 2:
+        out, rows = out[:, None], rows[:, None]
+    T = rows.shape[1]
+    places = [(out[b, n:], rows[b, n:]) for b, n in enumerate(lengths.tolist()) if n < T]
+    if places:
+        torch._foreach_copy_(*map(list, zip(*places)))   # (a launch for some hundred sequences)
+
+
 def _norm_class():
     import torch
     from torch.autograd.function import once_differentiable
@@ -212,6 +223,7 @@ def _norm_class():
             ctx.set_materialize_grads(False)  # what the loss does not use costs nothing
             r = binding.lfmmi_add_rms_norm(x, residual, weight, eps, lengths, p, seed, offset, step)
             ctx.draw, ctx.lengths, ctx.residual = (p, seed, offset), lengths, residual is not None
+            ctx.sum_is_x = r.sum is x
             ctx.save_for_backward(r.sum, r.rstd, weight, step)
             return r.y, (r.sum.view_as(r.sum) if r.sum is x else r.sum)
 
@@ -222,10 +234,12 @@ def _norm_class():
             if grad_y is None and grad_sum is None:
                 return none
             total, rstd, weight, step = ctx.saved_tensors
-            as_rows = lambda g: None if g is None else g.contiguous()
-            g = binding.lfmmi_add_rms_norm_backward(total, rstd, weight, as_rows(grad_y), as_rows(grad_sum),
+            grad_y, grad_sum = (None if g is None else g.contiguous() for g in (grad_y, grad_sum))
+            g = binding.lfmmi_add_rms_norm_backward(total, rstd, weight, grad_y, grad_sum,
                                                     ctx.lengths, *ctx.draw, step, residual=ctx.residual,
                                                     weight_grad=ctx.needs_input_grad[2])
+            if ctx.sum_is_x and ctx.lengths is not None and grad_sum is not None:
+                _copy_behind(g.x, grad_sum, ctx.lengths)   # (x's own rows, which the forward call passes on)
             return (g.x, g.residual, g.weight) + none[3:]
 
     return _AddRmsNorm
@@ -238,8 +252,8 @@ def add_rms_norm(x, residual=None, weight=None, eps=1e-6, lengths=None, p=0.0, s
     """The end of a residual block: sum = residual + dropout(x) and y = sum / sqrt(mean(sum^2) + eps)
     * weight, rows [B, T, D] or [B, D], differentiable in x, residual and weight. Rows behind
     `lengths` (host ints [B] or None) give 0 and no gradient; p, seed, offset, step: as for
-    dropout. Returns (y, sum): sum is what the next block adds to (x itself, rows behind its
-    lengths too, where nothing is added or dropped)."""
+    dropout. Returns (y, sum): sum is what the next block adds to. Where nothing is added or dropped that
+    is x itself, rows behind its lengths too, whose gradient is then x's."""
     global _norm_cls
     if _norm_cls is None:
         _norm_cls = _norm_class()

@@ -453,6 +453,62 @@ def test_norm_through_autograd(p, dtype):
                 binding.AddRmsNormGrads(got[0], None, got[1]), dtype, "float32", (B, T, D))
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("two", [False, True])
+def test_gradient_behind_the_lengths_where_sum_is_x(two, dtype):
+    # nothing added, nothing dropped: sum is x, rows behind the lengths too, and so is its gradient
+    torch = _torch()
+    rng = np.random.default_rng(22)
+    lengths, T, D = ([1, 0, 1, 1, 0], 1, 50) if two else ([6, 0, 4], 6, 50)
+    B = len(lengths)
+    shape = (B, D) if two else (B, T, D)
+    x, x64 = _values(rng, shape, dtype)
+    dy, dy64 = _values(rng, shape, dtype)
+    ds, ds64 = _values(rng, shape, dtype)
+    weight = torch.from_numpy(rng.normal(1, 0.3, D).astype(np.float32)).cuda().requires_grad_()
+    x.requires_grad_()
+    behind = torch.from_numpy(np.arange(T)[None] >= np.array(lengths)[:, None]).cuda().reshape(shape[:-1])
+    y, total = chain.add_rms_norm(x, None, weight, 1e-5, lengths)
+    assert torch.equal(total, x) and not y[behind].any()
+    rstd = binding.lfmmi_add_rms_norm(x.detach(), None, weight.detach(), 1e-5, lengths).rstd
+    x64 = np.where(behind.cpu().numpy()[..., None], 0.0, x64)
+    for grads, dsum in (((y, total), ds64), ((total,), ds64), ((y,), None)):
+        got = torch.autograd.grad(grads, (x, weight), [dy if v is y else ds for v in grads], retain_graph=True, allow_unused=True)
+        want = ds[behind] if dsum is not None else torch.zeros_like(ds[behind])
+        assert torch.equal(got[0][behind], want)
+        inside = got[0].clone()
+        inside[behind] = 0
+        check_grads(x64.reshape(-1, D), _host(weight.detach()), rstd, dy64 if len(grads) > 1 or dsum is None else None, dsum, lengths, 0.0, 0, 0,
+                    binding.AddRmsNormGrads(inside, None, got[1]), dtype, "float32", shape)
+
+
+def test_gradient_behind_the_lengths_captured():
+    torch = _torch()
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    x = torch.randn((3, 6, 50), generator=gen, device="cuda").requires_grad_()
+    weight = torch.ones(50, device="cuda").requires_grad_()
+    dy, ds = (torch.randn((3, 6, 50), generator=gen, device="cuda") for _ in range(2))
+
+    def step():
+        return torch.autograd.grad(chain.add_rms_norm(x, None, weight, 1e-5, [6, 0, 4]), (x, weight), (dy, ds))
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    for _ in range(4):
+        dy.copy_(torch.randn_like(dy))
+        ds.mul_(-1.5)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, step()))
+        assert torch.equal(out[0][1], ds[1]) and torch.equal(out[0][2, 4:], ds[2, 4:])
+
+
 def test_gradients_against_differences():
     # of the kernels' own loss: fp32, a step of 2^-6 and values near 1, so that the difference of two
     # losses of some 100 terms errs by 2 * 100 * 2^-24 * 8 / 2^-5 = 3e-3 at most, and its curvature by 2^-12
