@@ -909,7 +909,7 @@ def lfmmi_add_rms_norm_backward(sum, rstd, weight, grad_y, grad_sum=None, length
     the caller's to add). Returns AddRmsNormGrads (x, residual, weight): residual is None where
     `residual` is false, and x's where nothing was dropped (one tensor); weight's is None without a
     weight, or where `weight_grad` is false. `out`: an AddRmsNormGrads to write into; x and residual of
-    it may be grad_y or grad_sum."""
+    it may be grad_y or grad_sum, and one tensor where nothing was dropped."""
     import torch
     code, B, T, D, stride_b, stride_t = _batch_rows(sum, "sum")
     dev, dtype = sum.device, sum.dtype
@@ -941,6 +941,8 @@ def lfmmi_add_rms_norm_backward(sum, rstd, weight, grad_y, grad_sum=None, length
                     raise ValueError(_WRONG_OUT)
                 if t is not None:
                     _check_out(t, shape, dt, dev)
+            if out.residual is out.x and not one:
+                raise ValueError("one tensor for the gradients of x and residual, which dropout makes differ")
         need, ws = 0, None
         if weight_grad:
             need = _workspace_bytes("lfmmi_add_rms_norm_workspace", B, T, D)

@@ -372,6 +372,24 @@ def test_views_and_places(D, dtype):
         binding.lfmmi_add_rms_norm(xc, res, weight[:-1])
 
 
+def test_one_tensor_for_both_gradients():
+    # without dropout they are the same; with it, one tensor cannot hold both
+    torch = _torch()
+    x, dy = torch.randn((4, 30), device="cuda"), torch.randn((4, 30), device="cuda")
+    r = binding.lfmmi_add_rms_norm(x, x)
+    pair = binding.lfmmi_add_rms_norm_backward(r.sum, r.rstd, None, dy)
+    assert pair.x is pair.residual
+    assert binding.lfmmi_add_rms_norm_backward(r.sum, r.rstd, None, dy, out=pair) is pair
+    dropped = dict(p=0.5, seed=1)
+    r = binding.lfmmi_add_rms_norm(x, x, **dropped)
+    before = pair.x.clone()
+    with pytest.raises(ValueError, match="one tensor"):
+        binding.lfmmi_add_rms_norm_backward(r.sum, r.rstd, None, dy, out=pair, **dropped)
+    with pytest.raises(binding.LfmmiError):
+        binding.lfmmi_add_rms_norm_backward(r.sum, r.rstd, None, dy, out=pair._replace(residual=pair.x.view(4, 30)), **dropped)
+    assert torch.equal(pair.x, before)
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("D", [40, 3000, 20000])
 def test_rows_of_zeros_and_values_that_are_none(D, dtype):
