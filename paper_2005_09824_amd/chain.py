@@ -253,7 +253,8 @@ def add_rms_norm(x, residual=None, weight=None, eps=1e-6, lengths=None, p=0.0, s
     * weight, rows [B, T, D] or [B, D], differentiable in x, residual and weight. Rows behind
     `lengths` (host ints [B] or None) give 0 and no gradient; p, seed, offset, step: as for
     dropout. Returns (y, sum): sum is what the next block adds to. Where nothing is added or dropped that
-    is x itself, rows behind its lengths too, whose gradient is then x's."""
+    is x itself, rows behind its lengths too, whose gradient is then x's. x and residual of two types
+    are added in float32, as torch adds them, and y and sum are float32."""
     global _norm_cls
     if _norm_cls is None:
         _norm_cls = _norm_class()
@@ -261,7 +262,11 @@ def add_rms_norm(x, residual=None, weight=None, eps=1e-6, lengths=None, p=0.0, s
         lengths = np.array(lengths, dtype=np.int32)  # (a copy: backward reads it)
     x = _rows_in_order(x)
     if residual is not None:
-        residual = _rows_in_order(residual.to(x.dtype))
+        residual = _rows_in_order(residual)
+        if residual.dtype != x.dtype:   # (two of the three types: float32 holds every value of the others)
+            if weight is not None and weight.dtype == x.dtype:
+                weight = weight.float()
+            x, residual = x.float(), residual.float()
     if weight is not None:
         weight = weight.contiguous()
     return _norm_cls.apply(x, residual, weight, float(eps), lengths, float(p), int(seed), int(offset), step)

@@ -527,6 +527,29 @@ def test_gradient_behind_the_lengths_captured():
         assert torch.equal(out[0][1], ds[1]) and torch.equal(out[0][2, 4:], ds[2, 4:])
 
 
+@pytest.mark.parametrize("of_x,of_residual", [("bfloat16", "float32"), ("float16", "float32"), ("float32", "bfloat16"), ("bfloat16", "float16")])
+def test_a_residual_of_another_type(of_x, of_residual):
+    # as torch adds them: in float32, no bit of either is lost
+    torch = _torch()
+    rng = np.random.default_rng(23)
+    B, T, D = 3, 6, 50
+    lengths = [6, 0, 4]
+    x, x64 = _values(rng, (B, T, D), of_x)
+    res, r64 = _values(rng, (B, T, D), of_residual, 3.0)
+    for w_dtype in (of_x, "float32"):
+        weight = torch.from_numpy(rng.normal(1, 0.3, D).astype(np.float32)).to(getattr(torch, w_dtype)).cuda()
+        leaves = [v.detach().requires_grad_() for v in (x, res, weight)]
+        for p in (0.0, 0.3):
+            y, total = chain.add_rms_norm(*leaves, 1e-5, lengths, p, 3, 4)
+            assert y.dtype == total.dtype == torch.float32
+            r = binding.lfmmi_add_rms_norm(x.float(), res.float(), weight.float(), 1e-5, lengths, p, 3, 4)
+            assert torch.equal(y, r.y) and torch.equal(total, r.sum)
+            dy, ds = torch.randn_like(y), torch.randn_like(y)
+            got = torch.autograd.grad((y, total), leaves, (dy, ds))
+            want = binding.lfmmi_add_rms_norm_backward(r.sum, r.rstd, weight.float(), dy, ds, lengths, p, 3, 4)
+            assert all(a.dtype == b.dtype and torch.equal(a, c.to(a.dtype)) for a, b, c in zip(got, leaves, want))
+
+
 def test_gradients_against_differences():
     # of the kernels' own loss: fp32, a step of 2^-6 and values near 1, so that the difference of two
     # losses of some 100 terms errs by 2 * 100 * 2^-24 * 8 / 2^-5 = 3e-3 at most, and its curvature by 2^-12
