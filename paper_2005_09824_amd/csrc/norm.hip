@@ -16,7 +16,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr float kE4m3Max = 448.f;
 constexpr float kSmaller = 0x1p-80f;            // the square of the largest float times that has an exponent of 96
-constexpr float kLeastScale = 1.17549435e-38f;  // 2^-126: its inverse is finite
+constexpr float kLeastScale = 1.17549435e-38f;  // 2^-126
 
 // Waves of one workgroup take a row each, or all of them one together.
 constexpr int threads_of(int lanes) { return lanes == 64 ? kThreads : lanes; }
@@ -119,6 +119,31 @@ __device__ __forceinline__ void store_bytes(uint8_t* q, int left, const float* f
     if (left & 2) __builtin_memcpy(q + (left & 4), &two, 2);
     if (left & 1) q[left - 1] = (uint8_t)(left & 2 ? rest >> 16 : rest);
 }
+
+// y / scale for the values of a row: times the inverse, less what that is off, so that a quotient halfway between two values of
+// e4m3 comes out as that. (16,384 rows of 8,192 bf16: 114 us, 108 without what it is off, 138 with a division a value.) Small
+// scales are taken times 2^64, their values too, which loses nothing; over an infinite one finite values are 0.
+struct Quotient {
+    bool small;
+    float by, inverse;
+    __device__ __forceinline__ explicit Quotient(float scale) : small(scale < 0x1p-60f)
+    {
+        const float s = small ? scale * 0x1p64f : scale;
+        by = s < INFINITY ? s : 0.f;
+        inverse = 1.f / s;
+    }
+    __device__ __forceinline__ void operator()(float* y) const  // eight of them
+    {
+        if (__builtin_expect(small, 0))
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] *= 0x1p64f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float q = y[i] * inverse;
+            y[i] = fmaf(-fmaf(q, by, -y[i]), inverse, q);
+        }
+    }
+};
 
 // A value as it is kept in the type.
 template <typename T>
@@ -273,23 +298,21 @@ __global__ __launch_bounds__(threads_of(G)) void k_norm(NormParams p, SeqLengths
         const float best = over_row<G, true>(bad ? INFINITY : __uint_as_float(top), parts[1]);
         const float none = over_row<G, true>(bad ? 1.f : 0.f, parts[0]);
         const float scale = none > 0.f ? NAN : fmaxf(best / kE4m3Max, kLeastScale);
-        const float inverse = 1.f / scale;
+        const Quotient over(scale);
         if (p.q_scale && lane == 0) p.q_scale[row] = scale;
         if (N > 0) {
 #pragma unroll
             for (int k = 0; k < kHeld; ++k) {
                 const int c = lane + k * G;
                 if (c >= chunks) continue;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) h[k][i] *= inverse;
+                over(h[k]);
                 store_bytes(q + c * 8, p.D - c * 8, h[k]);
             }
         } else {
             for (int c = lane; c < chunks; c += G) {
                 float f[8];
                 scaled(c, 0, f);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) f[i] *= inverse;
+                over(f);
                 store_bytes(q + c * 8, p.D - c * 8, f);
             }
         }

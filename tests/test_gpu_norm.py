@@ -409,6 +409,26 @@ def test_rows_of_zeros_and_values_that_are_none(D, dtype):
         assert torch.isfinite(y[i]).all() and float(q[i].abs().max()) == 448.0
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("D", [128, 700, 5003, 20000])
+def test_bytes_next_to_a_tie(D, dtype):
+    # rows of 1: y is the weight, to the bit. Weights that are halfway between two e4m3 values times a scale of 17
+    # bits: the quotient is that halfway value, which goes to the even one of the two
+    torch = _torch()
+    ties = np.array([m * 2.0 ** e for m in range(17, 32, 2) for e in range(-6, 4)] + [448.0])
+    want = torch.from_numpy(np.tile(ties, D // len(ties) + 1)[:D] * np.where(np.arange(D) % 3 == 0, -1.0, 1.0))
+    want[0] = 448.0
+    x = torch.ones((1, D), dtype=getattr(torch, dtype), device="cuda")
+    rng = np.random.default_rng(D)
+    for exponent in (-142, -141, -100, -77, -76, -75, 100, *range(-30, -10)):   # (2^-126 is the least scale)
+        scale = float(rng.integers(1 << 16, 1 << 17)) * 2.0 ** exponent
+        weight = (want * scale).float().cuda()
+        assert torch.equal(weight.double().cpu(), want * scale)
+        r = binding.lfmmi_add_rms_norm(x, None, weight, eps=1e-30, quantized=True)
+        assert float(r.rstd) == 1.0 and float(r.q_scale) == scale
+        assert torch.equal(r.q[0].float().cpu(), want.float().to(torch.float8_e4m3fn).float())
+
+
 def test_eps_beside_squares_that_overflow():
     # 2^20 squares of 4e32 are beyond fp32 together; the largest eps is nothing beside their mean
     torch = _torch()
