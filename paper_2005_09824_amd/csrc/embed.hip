@@ -476,20 +476,31 @@ __global__ __launch_bounds__(kJoinWaves * 64) void k_embed_join(EmbedGradParams 
             if (c < chunks) {
                 const uint32_t head = g.from + wave * kEnds, tail = g.last * kEmbedPiece + wave * kEnds;
                 add_rows<T, W, kEnds, true>(p, order, head, min(head + kEnds, g.first * kEmbedPiece), c, s);
+                // A token of many positions has a long sum here: eight pieces are added up by themselves, and what is rounded away
+                // where their sum is added is added up beside it. (Half a million positions of one value:
+                // up to 110 millionths off with a plain sum, and 1,363 us for 640 columns against 1,051.)
+                float lost[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
                 for (uint32_t i = wave * each; i < to; i += 8) {
                     Raw<F32> f[8];
 #pragma unroll
                     for (int j = 0; j < 8; ++j)
                         f[j] = raw_at<F32, W>(part + (int64_t)min(i + j, to - 1) * p.D, c, p.D);
+                    float e[8][8];
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
-                        if (i + j >= to) continue;
-                        float e[8];
-                        unpack_at<F32, W>(f[j], c, p.D, e);
+                        if (i + j >= to) f[j] = no_values<F32>();
+                        unpack_at<F32, W>(f[j], c, p.D, e[j]);
+                    }
 #pragma unroll
-                        for (int x = 0; x < 8; ++x) s[x] += e[x];
+                    for (int x = 0; x < 8; ++x) {
+                        const float sum = ((e[0][x] + e[1][x]) + (e[2][x] + e[3][x])) + ((e[4][x] + e[5][x]) + (e[6][x] + e[7][x]));
+                        const float upto = s[x] + sum, added = upto - s[x];
+                        lost[x] += (s[x] - (upto - added)) + (sum - added);
+                        s[x] = upto;
                     }
                 }
+#pragma unroll
+                for (int x = 0; x < 8; ++x) s[x] += fabsf(lost[x]) < INFINITY ? lost[x] : 0.f;  // (s is no number either then)
                 add_rows<T, W, kEnds, true>(p, order, tail, min(tail + kEnds, g.to), c, s);
             }
 #pragma unroll

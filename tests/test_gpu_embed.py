@@ -104,6 +104,27 @@ def test_frequent_tokens(V, dtype):
         assert torch.equal(binding.lfmmi_embed_tokens_backward(g, tokens, V), grad)
 
 
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_one_token_of_most_positions(dtype):
+    # half a million positions of one token, all of one gradient, so that the roundings of a running sum add up. A value goes
+    # through 15 additions of its piece of 16 and 3 of eight pieces; the sum of a wave's 1,025 eights, which keeps what it loses,
+    # errs by one step and (1,025 U)^2 < 1 of them; 4 additions of positions behind the pieces, 3 of the waves' sums, the
+    # scale: 28, and 2 for these steps' own products
+    torch = _torch()
+    N, V, D = (1 << 19) + 37, 3, 24
+    tokens = torch.ones(N, dtype=torch.int64, device="cuda")
+    tokens[[5, 4000, N - 1]] = torch.tensor([0, 2, 0], device="cuda")
+    row = torch.linspace(-0.3, 0.3, D, device="cuda").to(getattr(torch, dtype))
+    grad = binding.lfmmi_embed_tokens_backward(row.expand(N, D), tokens, V)
+    want = row.double().cpu().numpy()[None] * np.array([[2.0], [N - 3.0], [1.0]])
+    tol = np.abs(want) * (30 * oracle.U + oracle.rounding(dtype)) + oracle.TINY[dtype]
+    assert np.all(np.abs(grad.double().cpu().numpy() - want) <= tol), (np.abs(grad.double().cpu().numpy() - want) / tol).max()
+    # a sum beyond the type is the infinity it would be in any order, and a NaN stays one
+    row = torch.tensor([1e38, -1e38, float("inf"), float("nan")], device="cuda")
+    grad = binding.lfmmi_embed_tokens_backward(row.expand(N, 4), tokens, V)[1].tolist()
+    assert grad[:3] == [np.inf, -np.inf, np.inf] and np.isnan(grad[3])
+
+
 @pytest.mark.parametrize("count", [15, 16, 17, 31, 32, 33, 63, 64, 65, 95, 96, 97, 2047, 2048, 2049, 4097])
 def test_counts_next_to_a_piece(count):
     torch = _torch()
