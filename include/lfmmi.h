@@ -432,9 +432,9 @@ lfmmi_status lfmmi_add_rms_norm_workspace(int32_t B, int32_t T, int32_t D, int64
  *   if all are taken (r = n), a token drawn from p_n follows.
  * Drawn means: the first token at which the running sum of what it is drawn from, in the order of
  * the tokens, passes u_K times the whole (a number of 1 or more: the last token of any
- * weight). All of it is in fp64; a probability below 2^-1000 times the largest of its row counts as
- * 0. The tokens that come out are distributed as p says. With K = 0 the call draws one token a
- * sequence.
+ * weight). All of it is in fp64, with exponentials that are off by 7e-12 of themselves at most; a
+ * probability below 2^-1000 times the largest of its row counts as 0. The tokens that come out are
+ * distributed as p says. With K = 0 the call draws one token a sequence.
  * uniforms NULL: greedy. d_i is taken if it is the first largest logit of row i, which replaces
  * or follows the others too; draft_logits must be NULL.
  *

@@ -238,7 +238,7 @@ def _norm_class():
             g = binding.lfmmi_add_rms_norm_backward(total, rstd, weight, grad_y, grad_sum,
                                                     ctx.lengths, *ctx.draw, step, residual=ctx.residual,
                                                     weight_grad=ctx.needs_input_grad[2])
-            if ctx.sum_is_x and ctx.lengths is not None and grad_sum is not None:
+            if ctx.sum_is_x and ctx.lengths is not None and grad_sum is not None and ctx.needs_input_grad[0]:
                 _copy_behind(g.x, grad_sum, ctx.lengths)   # (x's own rows, which the forward call passes on)
             return (g.x, g.residual, g.weight) + none[3:]
 

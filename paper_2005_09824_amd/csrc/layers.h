@@ -1,4 +1,4 @@
-// Plain-struct interface between the C ABI (layers.cpp, verify.cpp) and the kernels around an output
+// Plain-struct interface between the C ABI (layers.cpp) and the kernels around an output
 // layer: embeddings (embed.hip), dropout and norms (norm.hip), drafted tokens (verify.hip).
 #pragma once
 #include <hip/hip_runtime.h>

@@ -61,10 +61,6 @@ __global__ __launch_bounds__(kThreads) void k_dropout(DropoutParams p, int lanes
 // ---- norms
 
 // The sum, or the largest, over the G lanes that take a row.
-template <int G>
-struct Join {
-    float parts[2][G / 64];
-};
 template <int G, bool Max>
 __device__ __forceinline__ float over_row(float v, float* parts)
 {

@@ -264,12 +264,12 @@ __device__ __forceinline__ void load_part(const typename T::Store* x, int first,
     }
 }
 
-// ---- every row of a sequence's, a part at a time, a wave each, with no word between waves. Bound by the vector pipe: some 18
-// operations a logit, 11 of them of 64 bits. 48 sequences of 1 to 7 rows of 128,000 fp16 and as many of the draft's but one, 43
-// million logits: 33 us; 38 with the polynomial of degree 8, 17 with no exponentials; 130 sequences of 4 rows of 50,021 fp32: 20 us
-// and 23, which is what reading them takes. (Sums of 32 bits decide nearly as well whether a token is taken, and 64 bits
-// of the one row that is drawn from could follow in a kernel of its own: both ways were alike, 73 us a call, for these, and 33
-// us against 27 for 9 rows of 32,000.)
+// ---- every row of a sequence's, a part at a time, a wave each, with no word between waves. Bound by the vector pipe, for the most
+// part: 19 instructions a logit, 11 of them of 64 bits. 48 sequences of 1 to 7 rows of 128,000 fp16 and as many of the draft's but
+// one, 43 million logits: 33 us, of which the instructions fill 20; 38 with the polynomial of degree 8, 17 with no exponentials.
+// By counters they fill 81% of the cycles in which a compute unit has a wave, and those are 70% of the kernel's: the rest is its
+// beginning and end, and waves of rows that a sequence does not have, nearly half of those that start. 130 sequences of 4
+// rows of 50,021 fp32: 20 us and 23, which is what reading them takes.
 
 template <typename T, bool Greedy>
 __global__ __launch_bounds__(kThreads) void k_verify_rows(VerifyParams p, SeqLengths lens, int64_t units)
@@ -466,7 +466,7 @@ __global__ __launch_bounds__(kPickThreads) void k_verify_choose(VerifyParams p, 
     }
 }
 
-// If a drafted token is replaced: the sums of max(0, p - q) of kRestParts parts, two waves each. 10.7 us for 48 rows of 128,000
+// If a drafted token is replaced: the sums of max(0, p - q) of kRestParts parts, two waves each. 11 us for 48 rows of 128,000
 // and as many of the draft's, the exponentials' operations as above.
 template <typename T>
 __global__ __launch_bounds__(kRestThreads) void k_verify_rest(VerifyParams p, int64_t units)
@@ -505,8 +505,8 @@ __global__ __launch_bounds__(kRestThreads) void k_verify_rest(VerifyParams p, in
 }
 
 // The last token of every sequence: the first whose running sum passes the random number times the whole. Chosen: k_verify_choose
-// has said which row ends the sequence. Running sums of the parts, then of the tokens of one; 8 us of waits one after the other
-// (10 for 48 sequences; 13 where it also says which row).
+// has said which row ends the sequence. Running sums of the parts, then of the tokens of one; 9 us of waits one after the other
+// (10 for 48 sequences; 12 where it also says which row).
 template <typename T, bool Chosen>
 __global__ __launch_bounds__(kPickThreads) void k_verify_pick(VerifyParams p, SeqLengths lens)
 {

@@ -429,6 +429,21 @@ def test_bytes_next_to_a_tie(D, dtype):
         assert torch.equal(r.q[0].float().cpu(), want.float().to(torch.float8_e4m3fn).float())
 
 
+@pytest.mark.parametrize("D", [40, 3000, 20000])
+def test_bytes_of_values_beyond_the_type(D):
+    # a weight that takes a value to infinity: the scale is that, what is finite over it 0, infinity over it NaN
+    torch = _torch()
+    x = torch.ones((2, D), device="cuda")
+    weight = torch.full((D,), -3.0, device="cuda")
+    weight[D // 3] = 3e38
+    x[0, D // 3] = 4.0
+    r = binding.lfmmi_add_rms_norm(x, None, weight, quantized=True, y="both")
+    q = r.q.float()
+    assert torch.isinf(r.y[0, D // 3]) and torch.isinf(r.q_scale[0]) and torch.isnan(q[0, D // 3])
+    q[0, D // 3] = 0
+    assert not q[0].any() and float(q[1, D // 3]) == 448.0
+
+
 def test_eps_beside_squares_that_overflow():
     # 2^20 squares of 4e32 are beyond fp32 together; the largest eps is nothing beside their mean
     torch = _torch()
